@@ -1,0 +1,478 @@
+// C ABI of the layer operators: argument checks, choice of the kernels, work memory, launch order.
+#include "../../include/alpa_layers.h"
+#include "layers.hpp"
+
+#include <cmath>
+
+using namespace alpa;
+
+extern "C" __attribute__((visibility("hidden"))) int alpa_dp_set_error_(int code, const char *msg);   // alpa_dp_abi.hip
+
+namespace {
+
+int fail(int code, const char *msg) { return alpa_dp_set_error_(code, msg); }
+
+#define HIPCHK(expr)                                                            \
+    do {                                                                        \
+        const hipError_t e_ = (expr);                                           \
+        if (e_ != hipSuccess) return fail(ALPA_DP_EHIP, hipGetErrorString(e_)); \
+    } while (0)
+#define TRY(expr)                          \
+    do {                                   \
+        const int rc_ = (expr);            \
+        if (rc_ != ALPA_DP_OK) return rc_; \
+    } while (0)
+
+constexpr int64_t MAX_STRIDE = 1 << 22;      // bytes: a tile's offsets stay in 32 bits
+
+int64_t element(int dtype) { return dtype == ALPA_F32 ? 4 : 2; }
+int64_t round_up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
+int64_t block(int64_t bytes) { return round_up(bytes, 256); }
+bool by16(const void *p) { return ((uintptr_t)p & 15) == 0; }
+
+bool type_ok(int dtype) { return dtype == ALPA_F32 || dtype == ALPA_F16 || dtype == ALPA_BF16; }
+bool sizes_ok(int64_t rows, int64_t n_in, int64_t n_out, int64_t most_out)
+{
+    return rows >= 0 && rows <= ALPA_LAYER_MAX_ROWS && n_in >= 1 && n_in <= ALPA_LAYER_MAX_WIDTH && n_out >= 1 && n_out <= most_out;
+}
+int check_sizes(int dtype, int64_t rows, int64_t n_in, int64_t n_out, int64_t most_out)
+{
+    if (!type_ok(dtype)) return fail(ALPA_DP_EINVAL, "unknown type");
+    if (rows < 0 || rows > ALPA_LAYER_MAX_ROWS) return fail(ALPA_DP_EINVAL, "rows out of range");
+    if (n_in < 1 || n_in > ALPA_LAYER_MAX_WIDTH) return fail(ALPA_DP_EINVAL, "n_in out of range");
+    if (n_out < 1 || n_out > most_out) return fail(ALPA_DP_EINVAL, "n_out or words out of range");
+    return ALPA_DP_OK;
+}
+int check_mat(const alpa_mat_t &m, int64_t rows, int64_t len, int dtype, bool optional, const char *what)
+{
+    if (rows == 0 || (optional && !m.p)) return ALPA_DP_OK;
+    const int64_t es = element(dtype);
+    if (!m.p) return fail(ALPA_DP_EINVAL, what);
+    if ((uintptr_t)m.p % es) return fail(ALPA_DP_EINVAL, "a tensor is not aligned to its elements");
+    if (m.ld < len || m.ld > MAX_STRIDE / es) return fail(ALPA_DP_EINVAL, "a stride is shorter than a row or above 2^22 bytes");
+    return ALPA_DP_OK;
+}
+int check_vector(const void *p, int64_t es)
+{
+    return (uintptr_t)p % es ? fail(ALPA_DP_EINVAL, "a vector is not aligned to its elements") : ALPA_DP_OK;
+}
+int check_work(const void *work, int64_t have, int64_t need)
+{
+    if (need > 0 && (!work || have < need)) return fail(ALPA_DP_EINVAL, "work memory is null or too small");
+    if (need > 0 && ((uintptr_t)work & 255)) return fail(ALPA_DP_EINVAL, "work memory is not aligned to 256 bytes");
+    return ALPA_DP_OK;
+}
+
+// An activation as the product's epilogue takes it.
+Epilogue epilogue_of(int act, ProductArgs &g)
+{
+    g.low = act == ALPA_ACT_RELU ? 0.0f : -INFINITY;
+    g.c1 = act == ALPA_ACT_GELU_TANH ? 1.5957691216057308f : 1.0f;             // 2 sqrt(2 / pi), and 0.044715 of it
+    g.c3 = act == ALPA_ACT_GELU_TANH ? 0.071354816272600257f : 0.0f;
+    return act == ALPA_ACT_GELU ? EPI_ERF : act >= ALPA_ACT_GELU_TANH ? EPI_SIGMOID : EPI_LINE;
+}
+
+// A product of `m` x `n` results over `k`; `groups`: matrices of results (GROUP_STEPS), or groups of rows.
+struct Shape {
+    int64_t m, n, k;
+    Grouping grouping;
+    int groups;
+};
+
+int64_t tiles_of(const Shape &s, int tile)
+{
+    const int64_t cols = (s.n + tile - 1) / tile;
+    if (s.grouping == GROUP_ROWS) return slots_at_most(s.m, s.groups, tile) * cols;
+    return (s.m + tile - 1) / tile * cols * (s.grouping == GROUP_STEPS ? s.groups : 1);
+}
+
+// The contraction is split where its tiles leave most of the 256 compute units without work and each part still has eight steps; the parts' sums
+// go through memory in 32 bits and are joined in their order.
+int splits_of(const Shape &s, int dtype)
+{
+    if (s.grouping != GROUP_NONE) return 1;
+    const int64_t tiles = tiles_of(s, TILE), steps = (s.k * element(dtype) + STEP_BYTES - 1) / STEP_BYTES;
+    if (tiles == 0 || tiles > 128) return 1;
+    return (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(512 / tiles, steps / 8), 64));
+}
+int64_t split_bytes(const Shape &s, int dtype)
+{
+    const int n = splits_of(s, dtype);
+    return n > 1 ? block((int64_t)n * s.m * s.n * 4) : 0;
+}
+
+// Queues the product that `g` describes (operands, strides in bytes, epilogue), and the join if it is split.
+int run_product(hipStream_t st, int dtype, Forms forms, Epilogue epi, const Shape &s, ProductArgs g, void *split_work)
+{
+    if (s.m == 0 || (s.grouping == GROUP_STEPS && s.groups == 0)) return ALPA_DP_OK;
+    const int64_t es = element(dtype);
+    g.M = (int)s.m;
+    g.N = (int)s.n;
+    g.K = (int)s.k;
+    g.grouping = s.grouping;
+    g.experts = s.groups;
+    // 16-byte accesses: every chunk of a row lies in the tensor or behind it
+    const int64_t a_row = (forms == FORM_CC ? s.m : s.k) * es, b_row = (forms == FORM_RR ? s.k : s.n) * es;
+    const bool direct = by16(g.a) && by16(g.b) && g.lda % 16 == 0 && g.ldb % 16 == 0 && a_row % 16 == 0 && b_row % 16 == 0 &&
+                        (s.grouping != GROUP_ROWS || g.b_expert % 16 == 0);
+    g.wide = by16(g.out) && by16(g.z) && by16(g.residual) && by16(g.bias) && g.ldo * es % 16 == 0 && g.ldz * es % 16 == 0 &&
+             g.ldr * es % 16 == 0 && (s.grouping == GROUP_NONE || s.n * es % 16 == 0) &&
+             (s.grouping != GROUP_STEPS || g.b_expert * es % 16 == 0);
+    // The larger tile reads half as much of the operands per result, the smaller one fills the compute units with less.
+    const bool long_groups = s.grouping != GROUP_ROWS || s.m >= (int64_t)s.groups * 192;
+    const int tile = direct && long_groups && tiles_of(s, BIG_TILE) >= 256 ? BIG_TILE : TILE;
+    const int64_t tiles = tiles_of(s, tile);
+    if (tiles > (1 << 30)) return fail(ALPA_DP_EINVAL, "result too large");
+    g.row_tiles = (int)(s.grouping == GROUP_ROWS ? slots_at_most(s.m, s.groups, tile) : (s.m + tile - 1) / tile);
+    g.col_tiles = (int)((s.n + tile - 1) / tile);
+    g.splits = epi == EPI_LOSS || epi == EPI_GRAD || epi == EPI_SUM ? 1 : splits_of(s, dtype);
+    if (g.splits > 1) {
+        const int64_t steps = (s.k * es + STEP_BYTES - 1) / STEP_BYTES;
+        g.split_steps = (int)((steps + g.splits - 1) / g.splits);
+        g.splits = (int)((steps + g.split_steps - 1) / g.split_steps);
+        g.sum = (float *)split_work;
+        ProductArgs part = g;
+        part.first = 1;
+        part.last = 0;
+        part.scale = nullptr;
+        HIPCHK(launch_product(st, dtype, forms, EPI_SUM, tile, direct, part));
+        HIPCHK(launch_join(st, dtype, epi, g));
+        return ALPA_DP_OK;
+    }
+    HIPCHK(launch_product(st, dtype, forms, epi, tile, direct, g));
+    return ALPA_DP_OK;
+}
+
+ProductArgs operands(const alpa_mat_t &a, const alpa_mat_t &b, int dtype)
+{
+    ProductArgs g{};
+    g.a = (const char *)a.p;
+    g.b = (const char *)b.p;
+    g.lda = a.ld * element(dtype);
+    g.ldb = b.ld * element(dtype);
+    g.splits = 1;
+    g.first = g.last = 1;
+    return g;
+}
+void result(ProductArgs &g, const alpa_mat_t &out)
+{
+    g.out = (char *)out.p;
+    g.ldo = out.ld;
+}
+
+// ---------------------------------------------------------------- products of dense and expert layers
+
+// experts < 0: one weight for all rows
+int64_t forward_work(int dtype, int64_t rows, int experts, int64_t n_in, int64_t n_out)
+{
+    return experts < 0 ? split_bytes(Shape{rows, n_out, n_in, GROUP_NONE, 0}, dtype) : 0;
+}
+
+int forward(int dtype, int act, int64_t rows, int experts, int64_t n_in, int64_t n_out, const int32_t *offsets, const alpa_mat_t &x,
+            const alpa_mat_t &w, const void *bias, const alpa_mat_t &residual, const alpa_mat_t &y, const alpa_mat_t &z, void *work,
+            int64_t work_bytes, hipStream_t st)
+{
+    TRY(check_sizes(dtype, rows, n_in, n_out, ALPA_LAYER_MAX_WIDTH));
+    if (act < ALPA_ACT_NONE || act > ALPA_ACT_SILU) return fail(ALPA_DP_EINVAL, "unknown activation");
+    if (rows == 0) return ALPA_DP_OK;
+    TRY(check_mat(x, rows, n_in, dtype, false, "x is null"));
+    TRY(check_mat(w, n_out, n_in, dtype, false, "w is null"));
+    TRY(check_mat(y, rows, n_out, dtype, false, "y is null"));
+    TRY(check_mat(z, rows, n_out, dtype, true, ""));
+    TRY(check_mat(residual, rows, n_out, dtype, true, ""));
+    TRY(check_vector(bias, element(dtype)));
+    TRY(check_work(work, work_bytes, forward_work(dtype, rows, experts, n_in, n_out)));
+    ProductArgs g = operands(x, w, dtype);
+    const Epilogue epi = epilogue_of(act, g);
+    result(g, y);
+    g.bias = (const char *)bias;
+    g.residual = (const char *)residual.p;
+    g.ldr = residual.p ? residual.ld : 0;
+    g.z = (char *)z.p;
+    g.ldz = z.p ? z.ld : 0;
+    g.offsets = offsets;
+    g.b_expert = n_out * g.ldb;
+    return run_product(st, dtype, FORM_RR, epi, Shape{rows, n_out, n_in, experts < 0 ? GROUP_NONE : GROUP_ROWS, std::max(experts, 0)}, g,
+                       work);
+}
+
+// Parts of the backward pass's work memory.
+struct BackwardWork {
+    int64_t dz, part, split, total;     // offsets
+    int64_t ldd;
+    int slots;
+    BackwardWork(int dtype, int act, int64_t rows, int experts, int64_t n_in, int64_t n_out)
+    {
+        ldd = round_up(n_out, 16 / element(dtype));
+        slots = (int)(experts < 0 ? (rows + SLOPE_ROWS - 1) / SLOPE_ROWS : slots_at_most(rows, experts, SLOPE_ROWS));
+        dz = 0;
+        part = dz + (act == ALPA_ACT_NONE ? 0 : block(rows * ldd * element(dtype)));
+        split = part + block((int64_t)slots * n_out * 4);
+        int64_t most = 0;
+        if (experts < 0)
+            most = std::max(split_bytes(Shape{rows, n_in, n_out, GROUP_NONE, 0}, dtype),
+                            split_bytes(Shape{n_out, n_in, rows, GROUP_NONE, 0}, dtype));
+        total = split + most;
+    }
+};
+
+int backward(int dtype, int act, int64_t rows, int experts, int64_t n_in, int64_t n_out, const int32_t *offsets, const alpa_mat_t &dy,
+             const alpa_mat_t &z, const alpa_mat_t &x, const alpa_mat_t &w, const alpa_mat_t &dx, const alpa_mat_t &dw, void *dbias,
+             char *work, int64_t work_bytes, hipStream_t st)
+{
+    TRY(check_sizes(dtype, rows, n_in, n_out, ALPA_LAYER_MAX_WIDTH));
+    if (act < ALPA_ACT_NONE || act > ALPA_ACT_SILU) return fail(ALPA_DP_EINVAL, "unknown activation");
+    TRY(check_mat(dy, rows, n_out, dtype, false, "dy is null"));
+    TRY(check_mat(z, rows, n_out, dtype, act == ALPA_ACT_NONE, "z is null, and the activation has a slope"));
+    TRY(check_mat(x, rows, n_in, dtype, !dw.p, "x is null, and dw is wanted"));
+    TRY(check_mat(w, rows ? n_out : 0, n_in, dtype, !dx.p, "w is null, and dx is wanted"));
+    TRY(check_mat(dx, rows, n_in, dtype, true, ""));
+    TRY(check_mat(dw, n_out, n_in, dtype, true, ""));
+    TRY(check_vector(dbias, element(dtype)));
+    const BackwardWork at(dtype, act, rows, experts, n_in, n_out);
+    TRY(check_work(work, work_bytes, at.total));
+
+    const bool grouped = experts >= 0, has_z = act != ALPA_ACT_NONE;
+    alpa_mat_t dz = dy;
+    if (rows > 0 && (dbias || (has_z && (dx.p || dw.p)))) {
+        SlopeArgs s{};
+        const int64_t es = element(dtype);
+        s.dy = (const char *)dy.p;
+        s.lddy = dy.ld;
+        s.z = has_z ? (const char *)z.p : nullptr;
+        s.ldz = has_z ? z.ld : 0;
+        if (has_z) {
+            dz.p = work + at.dz;
+            dz.ld = at.ldd;
+            s.dz = (char *)dz.p;
+            s.ldd = dz.ld;
+        }
+        s.part = dbias ? (float *)(work + at.part) : nullptr;
+        s.rows = (int)rows;
+        s.N = (int)n_out;
+        s.slots = at.slots;
+        s.experts = grouped ? experts : 0;
+        s.offsets = offsets;
+        s.act = act;
+        s.wide = by16(s.dy) && by16(s.z) && s.lddy * es % 16 == 0 && s.ldz * es % 16 == 0;
+        HIPCHK(launch_slope(st, dtype, s));
+    }
+    if (dx.p && rows > 0) {
+        ProductArgs g = operands(dz, w, dtype);
+        g.low = -INFINITY;
+        result(g, dx);
+        g.offsets = offsets;
+        g.b_expert = n_out * g.ldb;
+        TRY(run_product(st, dtype, FORM_RC, EPI_LINE, Shape{rows, n_in, n_out, grouped ? GROUP_ROWS : GROUP_NONE, std::max(experts, 0)}, g,
+                        work + at.split));
+    }
+    if (dw.p) {
+        ProductArgs g = operands(dz, x, dtype);
+        g.low = -INFINITY;
+        result(g, dw);
+        g.offsets = offsets;
+        g.b_expert = n_out * dw.ld;
+        TRY(run_product(st, dtype, FORM_CC, EPI_LINE, Shape{n_out, n_in, rows, grouped ? GROUP_STEPS : GROUP_NONE, std::max(experts, 0)}, g,
+                        work + at.split));
+    }
+    if (dbias)
+        HIPCHK(launch_bias_sum(st, dtype, (const float *)(work + at.part), (char *)dbias, (int)rows, (int)n_out, rows ? at.slots : 0,
+                               grouped ? experts : 0, offsets));
+    return ALPA_DP_OK;
+}
+
+int check_experts(int experts, const int32_t *offsets)
+{
+    if (experts < 1 || experts > ALPA_LAYER_MAX_EXPERTS) return fail(ALPA_DP_EINVAL, "experts out of range");
+    if (!offsets) return fail(ALPA_DP_EINVAL, "offsets is null");
+    return check_vector(offsets, 4);
+}
+
+// ---------------------------------------------------------------- loss over a vocabulary
+
+int64_t stripes_of(int64_t words) { return (words + STRIPE - 1) / STRIPE; }
+
+// A piece's gradient of the logits is kept to 256 MiB, what the last-level cache holds, in pieces of one size (multiples of the larger tile).
+struct LossWork {
+    int64_t pieces, piece;              // number, words in each
+    int64_t coef, scale, grad, sum, split, total;
+    LossWork(int dtype, int64_t rows, int64_t n_in, int64_t words)
+    {
+        const int64_t es = element(dtype), r = std::max<int64_t>(rows, 1);
+        const int64_t most = std::min<int64_t>(std::max<int64_t>((256ll << 20) / (r * es) / BIG_TILE * BIG_TILE, 4 * BIG_TILE),
+                                               MAX_STRIDE / es);
+        pieces = (words + most - 1) / most;
+        piece = round_up((words + pieces - 1) / pieces, BIG_TILE);
+        pieces = (words + piece - 1) / piece;
+        coef = 0;
+        scale = coef + block(r * 4);
+        grad = scale + 256;
+        sum = grad + block(r * piece * es);
+        split = sum + (pieces > 1 ? block(r * n_in * 4) : 0);
+        const int64_t last = words - (pieces - 1) * piece;
+        total = split + std::max(std::max(split_bytes(Shape{rows, n_in, last, GROUP_NONE, 0}, dtype),
+                                          split_bytes(Shape{last, n_in, rows, GROUP_NONE, 0}, dtype)),
+                                 split_bytes(Shape{piece, n_in, rows, GROUP_NONE, 0}, dtype));
+    }
+};
+
+}  // namespace
+
+extern "C" {
+
+int64_t alpa_linear_forward_work(int dtype, int64_t rows, int64_t n_in, int64_t n_out)
+{
+    if (!type_ok(dtype) || !sizes_ok(rows, n_in, n_out, ALPA_LAYER_MAX_WIDTH)) return 0;
+    return forward_work(dtype, rows, -1, n_in, n_out);
+}
+
+int alpa_linear_forward(int dtype, int act, int64_t rows, int64_t n_in, int64_t n_out, alpa_mat_t x, alpa_mat_t w, const void *bias,
+                        alpa_mat_t residual, alpa_mat_t y, alpa_mat_t z, void *work, int64_t work_bytes, void *hip_stream)
+{
+    return forward(dtype, act, rows, -1, n_in, n_out, nullptr, x, w, bias, residual, y, z, work, work_bytes, (hipStream_t)hip_stream);
+}
+
+int64_t alpa_linear_backward_work(int dtype, int act, int64_t rows, int64_t n_in, int64_t n_out)
+{
+    if (!type_ok(dtype) || !sizes_ok(rows, n_in, n_out, ALPA_LAYER_MAX_WIDTH)) return 0;
+    return BackwardWork(dtype, act, rows, -1, n_in, n_out).total;
+}
+
+int alpa_linear_backward(int dtype, int act, int64_t rows, int64_t n_in, int64_t n_out, alpa_mat_t dy, alpa_mat_t z, alpa_mat_t x,
+                         alpa_mat_t w, alpa_mat_t dx, alpa_mat_t dw, void *dbias, void *work, int64_t work_bytes, void *hip_stream)
+{
+    return backward(dtype, act, rows, -1, n_in, n_out, nullptr, dy, z, x, w, dx, dw, dbias, (char *)work, work_bytes,
+                    (hipStream_t)hip_stream);
+}
+
+int64_t alpa_experts_forward_work(int dtype, int64_t rows, int experts, int64_t n_in, int64_t n_out)
+{
+    if (!type_ok(dtype) || !sizes_ok(rows, n_in, n_out, ALPA_LAYER_MAX_WIDTH) || experts < 1) return 0;
+    return forward_work(dtype, rows, experts, n_in, n_out);
+}
+
+int alpa_experts_forward(int dtype, int act, int64_t rows, int experts, int64_t n_in, int64_t n_out, const int32_t *offsets, alpa_mat_t x,
+                         alpa_mat_t w, const void *bias, alpa_mat_t residual, alpa_mat_t y, alpa_mat_t z, void *work, int64_t work_bytes,
+                         void *hip_stream)
+{
+    TRY(check_experts(experts, offsets));
+    return forward(dtype, act, rows, experts, n_in, n_out, offsets, x, w, bias, residual, y, z, work, work_bytes, (hipStream_t)hip_stream);
+}
+
+int64_t alpa_experts_backward_work(int dtype, int act, int64_t rows, int experts, int64_t n_in, int64_t n_out)
+{
+    if (!type_ok(dtype) || !sizes_ok(rows, n_in, n_out, ALPA_LAYER_MAX_WIDTH) || experts < 1 || experts > ALPA_LAYER_MAX_EXPERTS) return 0;
+    return BackwardWork(dtype, act, rows, experts, n_in, n_out).total;
+}
+
+int alpa_experts_backward(int dtype, int act, int64_t rows, int experts, int64_t n_in, int64_t n_out, const int32_t *offsets,
+                          alpa_mat_t dy, alpa_mat_t z, alpa_mat_t x, alpa_mat_t w, alpa_mat_t dx, alpa_mat_t dw, void *dbias, void *work,
+                          int64_t work_bytes, void *hip_stream)
+{
+    TRY(check_experts(experts, offsets));
+    return backward(dtype, act, rows, experts, n_in, n_out, offsets, dy, z, x, w, dx, dw, dbias, (char *)work, work_bytes,
+                    (hipStream_t)hip_stream);
+}
+
+int64_t alpa_vocab_loss_forward_work(int dtype, int64_t rows, int64_t n_in, int64_t words)
+{
+    if (!type_ok(dtype) || !sizes_ok(rows, n_in, words, ALPA_LAYER_MAX_WORDS)) return 0;
+    return block(stripes_of(words) * rows * 8) + block(rows * 4);
+}
+
+int alpa_vocab_loss_forward(int dtype, int64_t rows, int64_t n_in, int64_t words, alpa_mat_t x, alpa_mat_t w, const int64_t *target,
+                            float *loss, float *lse, void *work, int64_t work_bytes, void *hip_stream)
+{
+    TRY(check_sizes(dtype, rows, n_in, words, ALPA_LAYER_MAX_WORDS));
+    if (rows == 0) return ALPA_DP_OK;
+    TRY(check_mat(x, rows, n_in, dtype, false, "x is null"));
+    TRY(check_mat(w, words, n_in, dtype, false, "w is null"));
+    if (!target || !loss || !lse) return fail(ALPA_DP_EINVAL, "target, loss or lse is null");
+    TRY(check_vector(target, 8));
+    TRY(check_vector(loss, 4));
+    TRY(check_vector(lse, 4));
+    TRY(check_work(work, work_bytes, alpa_vocab_loss_forward_work(dtype, rows, n_in, words)));
+    const hipStream_t st = (hipStream_t)hip_stream;
+    ProductArgs g = operands(x, w, dtype);
+    g.target = target;
+    g.words = words;
+    g.stat = (float2 *)work;
+    g.at_target = (float *)((char *)work + block(stripes_of(words) * rows * 8));
+    TRY(run_product(st, dtype, FORM_RR, EPI_LOSS, Shape{rows, words, n_in, GROUP_NONE, 0}, g, nullptr));
+    HIPCHK(launch_loss(st, g.stat, (int)stripes_of(words), (int)rows, g.at_target, target, words, loss, lse));
+    return ALPA_DP_OK;
+}
+
+int64_t alpa_vocab_loss_backward_work(int dtype, int64_t rows, int64_t n_in, int64_t words)
+{
+    if (!type_ok(dtype) || !sizes_ok(rows, n_in, words, ALPA_LAYER_MAX_WORDS)) return 0;
+    return LossWork(dtype, rows, n_in, words).total;
+}
+
+int alpa_vocab_loss_backward(int dtype, int64_t rows, int64_t n_in, int64_t words, const float *dloss, alpa_mat_t x, alpa_mat_t w,
+                             const int64_t *target, const float *lse, alpa_mat_t dx, alpa_mat_t dw, void *work, int64_t work_bytes,
+                             void *hip_stream)
+{
+    TRY(check_sizes(dtype, rows, n_in, words, ALPA_LAYER_MAX_WORDS));
+    TRY(check_mat(x, rows, n_in, dtype, false, "x is null"));
+    TRY(check_mat(w, rows ? words : 0, n_in, dtype, false, "w is null"));
+    TRY(check_mat(dx, rows, n_in, dtype, true, ""));
+    TRY(check_mat(dw, words, n_in, dtype, true, ""));
+    if (rows > 0 && (!target || !dloss || !lse)) return fail(ALPA_DP_EINVAL, "target, dloss or lse is null");
+    TRY(check_vector(target, 8));
+    TRY(check_vector(dloss, 4));
+    TRY(check_vector(lse, 4));
+    const LossWork at(dtype, rows, n_in, words);
+    TRY(check_work(work, work_bytes, at.total));
+    if (!dx.p && !dw.p) return ALPA_DP_OK;
+    const hipStream_t st = (hipStream_t)hip_stream;
+    char *base = (char *)work;
+    float *coef = (float *)(base + at.coef), *scale = (float *)(base + at.scale);
+    HIPCHK(launch_coef(st, dloss, target, words, (int)rows, coef, scale));
+    const int64_t es = element(dtype);
+    for (int64_t p = 0; p < at.pieces; ++p) {
+        const int64_t word0 = p * at.piece, n = std::min(at.piece, words - word0);
+        const alpa_mat_t w_here{w.p ? (char *)w.p + word0 * w.ld * es : nullptr, w.ld}, grad{base + at.grad, at.piece};
+        if (rows > 0) {
+            ProductArgs g = operands(x, w_here, dtype);
+            result(g, grad);
+            g.target = target;
+            g.word0 = word0;
+            g.lse = lse;
+            g.coef = coef;
+            TRY(run_product(st, dtype, FORM_RR, EPI_GRAD, Shape{rows, n, n_in, GROUP_NONE, 0}, g, nullptr));
+        }
+        if (dx.p && rows > 0) {
+            ProductArgs g = operands(grad, w_here, dtype);
+            result(g, dx);
+            g.low = -INFINITY;
+            g.scale = scale;
+            g.sum = (float *)(base + at.sum);
+            g.first = p == 0;
+            g.last = p + 1 == at.pieces;
+            TRY(run_product(st, dtype, FORM_RC, at.pieces > 1 ? EPI_SUM : EPI_LINE, Shape{rows, n_in, n, GROUP_NONE, 0}, g,
+                            base + at.split));
+        }
+        if (dw.p) {
+            ProductArgs g = operands(grad, x, dtype);
+            result(g, alpa_mat_t{(char *)dw.p + word0 * dw.ld * es, dw.ld});
+            g.low = -INFINITY;
+            g.scale = scale;
+            TRY(run_product(st, dtype, FORM_CC, EPI_LINE, Shape{n, n_in, rows, GROUP_NONE, 0}, g, base + at.split));
+        }
+    }
+    return ALPA_DP_OK;
+}
+
+}  // extern "C"
+
+namespace alpa {
+
+hipError_t launch_product(hipStream_t st, int dtype, Forms forms, Epilogue epi, int tile, bool direct, const ProductArgs &g)
+{
+    return dtype == ALPA_F32   ? launch_product_f32(st, forms, epi, tile, direct, g)
+           : dtype == ALPA_F16 ? launch_product_f16(st, forms, epi, tile, direct, g)
+                               : launch_product_bf16(st, forms, epi, tile, direct, g);
+}
+
+}  // namespace alpa

@@ -1,0 +1,94 @@
+// Elements, activations, and what becomes of a product's results (device code).
+#pragma once
+#include "layers.hpp"
+#include "product.hpp"
+
+namespace alpa {
+
+// N consecutive elements as floats; `wide`: they may be loaded at once (N * sizeof(T) is 8 or 16 bytes, aligned so); `n`: how many exist
+template <class T, int N>
+__device__ __forceinline__ void load_row(const char *base, int64_t at, int n, int wide, float (&v)[N])
+{
+    const T *p = (const T *)base + at;
+    if (wide && n >= N) {
+        struct __align__(sizeof(T) * N) Pack { T e[N]; };
+        const Pack k = *(const Pack *)p;
+#pragma unroll
+        for (int j = 0; j < N; ++j) v[j] = (float)k.e[j];
+    } else {
+#pragma unroll
+        for (int j = 0; j < N; ++j) v[j] = j < n ? (float)p[j] : 0.0f;
+    }
+}
+
+// the one rounding of a result to its type (to nearest, ties to even)
+template <class T, int N>
+__device__ __forceinline__ void store_row(char *base, int64_t at, int n, int wide, const float (&v)[N])
+{
+    T *p = (T *)base + at;
+    if (wide && n >= N) {
+        struct __align__(sizeof(T) * N) Pack { T e[N]; };
+        Pack k;
+#pragma unroll
+        for (int j = 0; j < N; ++j) k.e[j] = (T)v[j];
+        *(Pack *)p = k;
+    } else {
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+            if (j < n) p[j] = (T)v[j];
+    }
+}
+
+// exp for values that end in 32 bits, and the faster one (its error grows with the exponent: 2^-24 |x|) for those rounded to 16
+template <class T>
+__device__ __forceinline__ float exp_for(float x)
+{
+    return sizeof(T) == 4 ? expf(x) : __expf(x);
+}
+
+// z * logistic(z (c1 + c3 z^2)).  An infinite z is given the limit: the formula would have inf / inf or 0 * inf there.
+template <class T>
+__device__ __forceinline__ float gated(float z, float c1, float c3)
+{
+    const float y = z / (1.0f + exp_for<T>(-z * (c1 + c3 * z * z)));
+    return fabsf(z) == INFINITY ? (z > 0.0f ? z : -0.0f) : y;
+}
+
+__device__ __forceinline__ float gelu(float z)
+{
+    const float y = 0.5f * z * erfcf(-0.70710678118654752f * z);      // erfc keeps its bits for very negative z
+    return z == -INFINITY ? -0.0f : y;
+}
+
+template <class T, int EPI>
+__device__ __forceinline__ float activate(float z, const ProductArgs &g)
+{
+    if (EPI == EPI_SIGMOID) return gated<T>(z, g.c1, g.c3);
+    if (EPI == EPI_ERF) return gelu(z);
+    return z < g.low ? g.low : z;              // (a NaN stays)
+}
+
+// Columns n .. n + N - 1 of row m, `cnt` of them real: z = v (+ bias), result act(z) (+ residual).  `skip`: a row of no expert, zeros.
+template <class T, int EPI, int N>
+__device__ __forceinline__ void put_row(const ProductArgs &g, int64_t out_base, int64_t bias_base, int64_t m, int n, int cnt, bool skip,
+                                        float (&v)[N])
+{
+    if (g.bias && !skip) {
+        float b[N];
+        load_row<T>(g.bias, bias_base + n, cnt, g.wide, b);
+#pragma unroll
+        for (int j = 0; j < N; ++j) v[j] += b[j];
+    }
+    if (g.z) store_row<T>(g.z, m * g.ldz + n, cnt, g.wide, v);
+#pragma unroll
+    for (int j = 0; j < N; ++j) v[j] = activate<T, EPI>(v[j], g);
+    if (g.residual && !skip) {
+        float r[N];
+        load_row<T>(g.residual, m * g.ldr + n, cnt, g.wide, r);
+#pragma unroll
+        for (int j = 0; j < N; ++j) v[j] += r[j];
+    }
+    store_row<T>(g.out, out_base + m * g.ldo + n, cnt, g.wide, v);
+}
+
+}  // namespace alpa

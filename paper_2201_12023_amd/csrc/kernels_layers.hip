@@ -1,0 +1,235 @@
+// The small kernels around the products of the layer operators: the activation's slope with the bias gradient's sums, the join of a
+// product that was split over its contraction, and the statistics of the loss.
+#include "epilogue.hpp"
+#include "slots.hpp"
+
+namespace alpa {
+
+// ---------------------------------------------------------------- dz = dy * act'(z), sums of its columns
+
+// act'(z); at infinities the limits
+template <class T>
+__device__ __forceinline__ float slope_of(float z, int act)
+{
+    if (act == 1) return z > 0.0f ? 1.0f : (z == z ? 0.0f : z);
+    if (act == 2) {
+        if (fabsf(z) == INFINITY) return z > 0.0f ? 1.0f : 0.0f;
+        return 0.5f * erfcf(-0.70710678118654752f * z) + z * 0.39894228040143268f * exp_for<T>(-0.5f * z * z);
+    }
+    // z s(u) with u = c1 z + c3 z^3:  s + z s (1 - s) u'
+    const float c1 = act == 3 ? 1.5957691216057308f : 1.0f, c3 = act == 3 ? 0.071354816272600257f : 0.0f;
+    if (fabsf(z) > 1e4f) return z > 0.0f ? 1.0f : 0.0f;          // (there 1 - s or s is 0 in 32 bits, and z^3 may not be finite)
+    const float zz = z * z, e = exp_for<T>(-z * (c1 + c3 * zz)), s = 1.0f / (1.0f + e);
+    return s + z * s * (1.0f - s) * (c1 + 3.0f * c3 * zz);
+}
+
+// A workgroup takes a slot of SLOPE_ROWS rows and 64 * V columns; a wave every fourth row, a lane V consecutive columns.  One pass: dy
+// and z are read once, dz written once, and the sums of a slot go to `part`, to be added in the order of the slots.
+template <class T, int V, bool HAS_Z>
+__global__ __launch_bounds__(256) void slope_kernel(const SlopeArgs g)
+{
+    __shared__ float sums[4][64 * V];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int n = (blockIdx.y * 64 + lane) * V, cnt = g.N - n;
+    int first = blockIdx.x * SLOPE_ROWS, end = min(first + SLOPE_ROWS, g.rows);
+    bool skip = false;
+    if (g.experts) {
+        const Slot s = find_slot(g.offsets, g.experts, g.rows, SLOPE_ROWS, blockIdx.x);
+        first = s.first;
+        end = s.end;
+        skip = s.expert < 0 || s.expert >= g.experts;      // rows of no expert: their dz is read by nobody
+    }
+    float sum[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) sum[j] = 0.0f;
+    if (!skip && cnt > 0) {
+#pragma unroll 4
+        for (int m = first + wave; m < end; m += 4) {
+            float d[V];
+            load_row<T>(g.dy, (int64_t)m * g.lddy + n, cnt, g.wide, d);
+            if (HAS_Z) {
+                float z[V];
+                load_row<T>(g.z, (int64_t)m * g.ldz + n, cnt, g.wide, z);
+#pragma unroll
+                for (int j = 0; j < V; ++j) d[j] *= slope_of<T>(z[j], g.act);
+                if (g.dz) store_row<T>(g.dz, (int64_t)m * g.ldd + n, cnt, g.wide, d);
+            }
+#pragma unroll
+            for (int j = 0; j < V; ++j) sum[j] += d[j];
+        }
+    }
+    if (!g.part) return;
+#pragma unroll
+    for (int j = 0; j < V; ++j) sums[wave][j * 64 + lane] = sum[j];
+    __syncthreads();
+    for (int c = threadIdx.x; c < 64 * V; c += 256) {
+        const int col = blockIdx.y * 64 * V + c;
+        if (col >= g.N) continue;
+        const int at = (c % V) * 64 + c / V;
+        g.part[(int64_t)blockIdx.x * g.N + col] = (sums[0][at] + sums[1][at]) + (sums[2][at] + sums[3][at]);
+    }
+}
+
+template <class T>
+hipError_t slope_typed(hipStream_t st, const SlopeArgs &g)
+{
+    constexpr int V = 16 / sizeof(T);
+    const int per = 64 * (g.wide ? V : 1);
+    const dim3 grid((unsigned)g.slots, (unsigned)((g.N + per - 1) / per));
+    if (g.wide) {
+        if (g.act) slope_kernel<T, V, true><<<grid, 256, 0, st>>>(g);
+        else slope_kernel<T, V, false><<<grid, 256, 0, st>>>(g);
+    } else {
+        if (g.act) slope_kernel<T, 1, true><<<grid, 256, 0, st>>>(g);
+        else slope_kernel<T, 1, false><<<grid, 256, 0, st>>>(g);
+    }
+    return hipGetLastError();
+}
+
+hipError_t launch_slope(hipStream_t st, int dtype, const SlopeArgs &g)
+{
+    return dtype == 0 ? slope_typed<float>(st, g) : dtype == 1 ? slope_typed<f16>(st, g) : slope_typed<bf16>(st, g);
+}
+
+// Sixty-four columns a workgroup, four waves each adding a quarter of the expert's slots; the quarters are joined in their order.
+template <class T>
+__global__ __launch_bounds__(256) void bias_sum_kernel(const float *part, T *dbias, int rows, int N, int slots, int experts,
+                                                       const int32_t *offsets)
+{
+    __shared__ float sums[4][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, e = blockIdx.y;
+    int first = 0, count = slots;
+    if (experts) {
+        int a, b;
+        group_rows(offsets, experts, rows, e, a, b);
+        first = slots_before(offsets, experts, rows, SLOPE_ROWS, e);
+        count = min((b - a + SLOPE_ROWS - 1) / SLOPE_ROWS, max(slots - first, 0));
+    }
+    const int n = blockIdx.x * 64 + lane, quarter = (count + 3) / 4;
+    float sum = 0.0f;
+    if (n < N)
+        for (int s = wave * quarter; s < min((wave + 1) * quarter, count); ++s) sum += part[(int64_t)(first + s) * N + n];
+    sums[wave][lane] = sum;
+    __syncthreads();
+    if (wave == 0 && n < N) dbias[(int64_t)e * N + n] = (T)((sums[0][lane] + sums[1][lane]) + (sums[2][lane] + sums[3][lane]));
+}
+
+hipError_t launch_bias_sum(hipStream_t st, int dtype, const float *part, char *dbias, int rows, int N, int slots, int experts,
+                           const int32_t *offsets)
+{
+    const dim3 grid((unsigned)((N + 63) / 64), (unsigned)(experts ? experts : 1));
+    if (dtype == 0) bias_sum_kernel<float><<<grid, 256, 0, st>>>(part, (float *)dbias, rows, N, slots, experts, offsets);
+    else if (dtype == 1) bias_sum_kernel<f16><<<grid, 256, 0, st>>>(part, (f16 *)dbias, rows, N, slots, experts, offsets);
+    else bias_sum_kernel<bf16><<<grid, 256, 0, st>>>(part, (bf16 *)dbias, rows, N, slots, experts, offsets);
+    return hipGetLastError();
+}
+
+// ---------------------------------------------------------------- join of a split product
+
+// Four columns a thread; the splits are added in their order.
+template <class T, int EPI>
+__global__ __launch_bounds__(256) void join_kernel(const ProductArgs g)
+{
+    const int per_row = (g.N + 3) / 4;
+    const int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int64_t m = t / per_row;
+    if (m >= g.M) return;
+    const int n = (int)(t - m * per_row) * 4, cnt = g.N - n, aligned = (g.N & 3) == 0;
+    float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int s = 0; s < g.splits; ++s) {
+        float part[4];
+        load_row<float>((const char *)g.sum, ((int64_t)s * g.M + m) * g.N + n, cnt, aligned, part);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] += part[j];
+    }
+    const float scale = g.scale ? *g.scale : 1.0f;
+    if (EPI == EPI_LINE) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] *= scale;
+    }
+    put_row<T, EPI>(g, 0, 0, m, n, cnt, false, v);
+}
+
+template <class T>
+hipError_t join_typed(hipStream_t st, Epilogue epi, const ProductArgs &g)
+{
+    const int64_t threads = (int64_t)g.M * ((g.N + 3) / 4);
+    const unsigned blocks = (unsigned)((threads + 255) / 256);
+    if (epi == EPI_SIGMOID) join_kernel<T, EPI_SIGMOID><<<blocks, 256, 0, st>>>(g);
+    else if (epi == EPI_ERF) join_kernel<T, EPI_ERF><<<blocks, 256, 0, st>>>(g);
+    else join_kernel<T, EPI_LINE><<<blocks, 256, 0, st>>>(g);
+    return hipGetLastError();
+}
+
+hipError_t launch_join(hipStream_t st, int dtype, Epilogue epi, const ProductArgs &g)
+{
+    return dtype == 0 ? join_typed<float>(st, epi, g) : dtype == 1 ? join_typed<f16>(st, epi, g) : join_typed<bf16>(st, epi, g);
+}
+
+// ---------------------------------------------------------------- the loss's statistics
+
+// (top, sum of exp(l - top)) of two sets of logits; of none: (-inf, 0)
+__device__ __forceinline__ float2 join_stat(float2 a, float2 b)
+{
+    const float top = fmaxf(a.x, b.x), ref = top == -INFINITY ? 0.0f : top;
+    return make_float2(top, a.y * expf(a.x - ref) + b.y * expf(b.x - ref));
+}
+
+// Sixteen rows a workgroup; sixteen threads a row take every sixteenth stripe, in order, and are joined in order.
+__global__ __launch_bounds__(256) void loss_kernel(const float2 *stat, int stripes, int rows, const float *at_target,
+                                                   const int64_t *target, int64_t words, float *loss, float *lse)
+{
+    __shared__ float2 share[16][17];
+    const int r = threadIdx.x & 15, part = threadIdx.x >> 4, m = blockIdx.x * 16 + r;
+    float2 s = make_float2(-INFINITY, 0.0f);
+    if (m < rows)
+        for (int j = part; j < stripes; j += 16) s = join_stat(s, stat[(int64_t)j * rows + m]);
+    share[part][r] = s;
+    __syncthreads();
+    if (part != 0 || m >= rows) return;
+    for (int j = 1; j < 16; ++j) s = join_stat(s, share[j][r]);
+    const float l = s.x + logf(s.y);
+    const int64_t word = target[m];
+    lse[m] = l;
+    loss[m] = word < 0 ? 0.0f : word >= words ? NAN : l - at_target[m];
+}
+
+hipError_t launch_loss(hipStream_t st, const float2 *stat, int stripes, int rows, const float *at_target, const int64_t *target,
+                       int64_t words, float *loss, float *lse)
+{
+    loss_kernel<<<(unsigned)((rows + 15) / 16), 256, 0, st>>>(stat, stripes, rows, at_target, target, words, loss, lse);
+    return hipGetLastError();
+}
+
+// One workgroup.  The largest |dloss| of a counted row becomes 2^14: |g| is no larger, so it fits in a 16-bit float, and a probability of
+// 2^-28 beside it is still a normal one.  The divisor is that largest value itself and no power of two near it: rows mostly have one weight,
+// the mean's, and what they add at their target, (1 - p) times it with small p, would be rounded the same way in all of them (measured
+// with 8192 rows: errors of the gradients 0.0035 relative with a power of two, 0.0017 being the least a 16-bit result can have).
+__global__ __launch_bounds__(1024) void coef_kernel(const float *dloss, const int64_t *target, int64_t words, int rows, float *coef,
+                                                    float *scale)
+{
+    __shared__ float tops[16];
+    float top = 0.0f;
+    for (int m = threadIdx.x; m < rows; m += 1024) {
+        const float d = fabsf(dloss[m]);
+        if (target[m] >= 0 && d < INFINITY) top = fmaxf(top, d);
+    }
+#pragma unroll
+    for (int off = 32; off; off >>= 1) top = fmaxf(top, __shfl_xor(top, off, 64));
+    if ((threadIdx.x & 63) == 0) tops[threadIdx.x >> 6] = top;
+    __syncthreads();
+    top = tops[0];
+    for (int j = 1; j < 16; ++j) top = fmaxf(top, tops[j]);
+    const float most = top > 0.0f ? fmaxf(top, 0x1p-100f) : 16384.0f, by = 16384.0f / most;
+    if (threadIdx.x == 0) *scale = most * 0x1p-14f;
+    for (int m = threadIdx.x; m < rows; m += 1024)
+        coef[m] = target[m] < 0 ? 0.0f : target[m] >= words ? NAN : dloss[m] * by;
+}
+
+hipError_t launch_coef(hipStream_t st, const float *dloss, const int64_t *target, int64_t words, int rows, float *coef, float *scale)
+{
+    coef_kernel<<<1, 1024, 0, st>>>(dloss, target, words, rows, coef, scale);
+    return hipGetLastError();
+}
+
+}  // namespace alpa

@@ -1,0 +1,11 @@
+// The tiled product for one element type (one file each, to build them side by side).
+#include "product_kernel.hpp"
+
+namespace alpa {
+
+hipError_t launch_product_f32(hipStream_t st, Forms forms, Epilogue epi, int tile, bool direct, const ProductArgs &g)
+{
+    return launch_forms<float>(st, forms, epi, tile, direct, g);
+}
+
+}  // namespace alpa

@@ -1,0 +1,93 @@
+// What the layer operators' kernels take, and how they are launched (device code: product_kernel.hpp, kernels_layers.hip).
+#pragma once
+#include "internal.hpp"
+
+namespace alpa {
+
+// What becomes of a tile of the product.
+enum Epilogue : int {
+    EPI_LINE,       // act(v) + residual with act none or relu:  v < low ? low : v
+    EPI_SIGMOID,    // v / (1 + exp(-v (c1 + c3 v^2))): silu, and gelu in its tanh form
+    EPI_ERF,        // gelu
+    EPI_SUM,        // 32-bit sums, added to what is there or put down, and rounded into the result by the last of several
+    EPI_LOSS,       // logits: per row and stripe of columns a maximum, a sum of exponentials, and the target's logit
+    EPI_GRAD,       // logits: (softmax - onehot) * coef
+};
+
+// How rows are dealt to weights.
+enum Grouping : int { GROUP_NONE, GROUP_ROWS, GROUP_STEPS };     // ragged in the result's rows, or in the contraction
+
+struct ProductArgs {
+    const char *a, *b;              // operands; strides in bytes
+    int64_t lda, ldb;
+    int M, N, K;                    // result rows (all groups together), columns, contraction (all groups together)
+    int grouping, experts;
+    const int32_t *offsets;
+    int64_t b_expert;               // GROUP_ROWS: bytes from an expert's b to the next one's; GROUP_STEPS: result elements
+    int row_tiles, col_tiles;       // grid: row tiles (GROUP_ROWS: slots), column tiles; GROUP_STEPS: times experts
+    int splits, split_steps;        // of the contraction, 128 bytes a step (GROUP_NONE only)
+    // epilogue
+    char *out;                      // result, strides in elements
+    int64_t ldo;
+    const char *bias, *residual;
+    int64_t ldr;
+    char *z;
+    int64_t ldz;
+    int wide;                       // pointers, strides and row length allow 16-byte accesses in the epilogue
+    float low, c1, c3;
+    float *sum;                     // EPI_SUM: [split][M][N]
+    int first, last;
+    const float *scale;             // EPI_SUM, EPI_LINE: result times *scale (NULL: 1)
+    const int64_t *target;          // EPI_LOSS, EPI_GRAD
+    int64_t words;                  // columns of the whole vocabulary; this product's are word0 ..
+    int64_t word0;
+    float2 *stat;                   // EPI_LOSS: [stripe][M]
+    float *at_target;
+    const float *lse, *coef;        // EPI_GRAD: [M]
+};
+
+constexpr int TILE = 128, BIG_TILE = 256;         // rows and columns of a workgroup's tile
+constexpr int STEP_BYTES = 128;
+constexpr int STRIPE = 64;                        // columns of a stripe of EPI_LOSS, in all tiles
+
+// Form of the two operands: both with their contraction contiguous (x wT), the second one's rows contiguous (dz w), or both (dzT x).
+enum Forms : int { FORM_RR, FORM_RC, FORM_CC };
+
+// tile: TILE or BIG_TILE; direct: operands allow 16-byte accesses throughout (BIG_TILE needs it)
+hipError_t launch_product(hipStream_t st, int dtype, Forms forms, Epilogue epi, int tile, bool direct, const ProductArgs &a);
+hipError_t launch_product_f32(hipStream_t, Forms, Epilogue, int, bool, const ProductArgs &);
+hipError_t launch_product_f16(hipStream_t, Forms, Epilogue, int, bool, const ProductArgs &);
+hipError_t launch_product_bf16(hipStream_t, Forms, Epilogue, int, bool, const ProductArgs &);
+
+// dz = dy * act'(z), and sums of dz over the rows of each slot of SLOPE_ROWS rows
+constexpr int SLOPE_ROWS = 64;
+struct SlopeArgs {
+    const char *dy, *z;             // strides in elements
+    int64_t lddy, ldz;
+    char *dz;                       // [rows][ldd], or NULL
+    int64_t ldd;
+    float *part;                    // [slots][N], or NULL
+    int rows, N, slots, experts;    // experts 0: no groups
+    const int32_t *offsets;
+    int act, wide;
+};
+hipError_t launch_slope(hipStream_t st, int dtype, const SlopeArgs &a);
+// dbias[e][n] = sum over the expert's slots
+hipError_t launch_bias_sum(hipStream_t st, int dtype, const float *part, char *dbias, int rows, int N, int slots, int experts,
+                           const int32_t *offsets);
+// result = act(sum over splits + bias) + residual, and z (epi: EPI_LINE, EPI_SIGMOID or EPI_ERF)
+hipError_t launch_join(hipStream_t st, int dtype, Epilogue epi, const ProductArgs &a);
+// loss and lse of each row from its stripes
+hipError_t launch_loss(hipStream_t st, const float2 *stat, int stripes, int rows, const float *at_target, const int64_t *target,
+                       int64_t words, float *loss, float *lse);
+// coef = dloss / *scale for counted rows, 0 for others; *scale = largest |dloss| / 2^14
+hipError_t launch_coef(hipStream_t st, const float *dloss, const int64_t *target, int64_t words, int rows, float *coef, float *scale);
+
+// slots of `tile` rows that the groups of `rows` rows can make at most, rows of no group among them
+inline int64_t slots_at_most(int64_t rows, int experts, int tile)
+{
+    const int64_t groups = (int64_t)experts + 2;
+    return rows / tile + (groups < rows ? groups : rows);
+}
+
+}  // namespace alpa

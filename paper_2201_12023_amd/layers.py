@@ -1,0 +1,241 @@
+"""Thin ctypes binding over the C ABI in ``include/alpa_layers.h`` (argument marshalling only): the products of
+dense and expert layers and the loss over a vocabulary, forward and backward.
+
+Same names as the C entry points.  Arguments and results are torch tensors on one GPU; results and work memory come from
+torch's allocator, every step runs in the HIP kernels of ``libalpa_dp.so``.  Work is queued on ``stream`` (a
+torch.cuda.Stream; the current one if None) and not waited for.  The last dimension of a tensor must be contiguous, rows may be
+any distance apart.
+"""
+from __future__ import annotations
+
+import ctypes
+
+import torch
+
+from . import binding
+
+ALPA_F32, ALPA_F16, ALPA_BF16 = 0, 1, 2
+ALPA_ACT_NONE, ALPA_ACT_RELU, ALPA_ACT_GELU, ALPA_ACT_GELU_TANH, ALPA_ACT_SILU = range(5)
+MAX_WIDTH = 1 << 20
+MAX_ROWS = 1 << 28
+MAX_EXPERTS = 4096
+MAX_WORDS = 1 << 24
+_TYPES = {torch.float32: ALPA_F32, torch.float16: ALPA_F16, torch.bfloat16: ALPA_BF16}
+
+SYMBOLS = ["alpa_linear_forward", "alpa_linear_forward_work", "alpa_linear_backward", "alpa_linear_backward_work",
+           "alpa_experts_forward", "alpa_experts_forward_work", "alpa_experts_backward", "alpa_experts_backward_work",
+           "alpa_vocab_loss_forward", "alpa_vocab_loss_forward_work", "alpa_vocab_loss_backward",
+           "alpa_vocab_loss_backward_work"]
+
+
+class alpa_mat_t(ctypes.Structure):
+    _fields_ = [("p", ctypes.c_void_p), ("ld", ctypes.c_int64)]
+
+
+_ready = None
+
+
+def load():
+    """The library with the argument types of the layer operators set (raises if it is not built)."""
+    global _ready
+    if _ready is not None:
+        return _ready
+    L = binding.load()
+    i, n, vp, mat = ctypes.c_int, ctypes.c_int64, ctypes.c_void_p, alpa_mat_t
+    L.alpa_linear_forward.argtypes = [i, i, n, n, n, mat, mat, vp, mat, mat, mat, vp, n, vp]
+    L.alpa_linear_backward.argtypes = [i, i, n, n, n, mat, mat, mat, mat, mat, mat, vp, vp, n, vp]
+    L.alpa_experts_forward.argtypes = [i, i, n, i, n, n, vp, mat, mat, vp, mat, mat, mat, vp, n, vp]
+    L.alpa_experts_backward.argtypes = [i, i, n, i, n, n, vp, mat, mat, mat, mat, mat, mat, vp, vp, n, vp]
+    L.alpa_vocab_loss_forward.argtypes = [i, n, n, n, mat, mat, vp, vp, vp, vp, n, vp]
+    L.alpa_vocab_loss_backward.argtypes = [i, n, n, n, vp, mat, mat, vp, vp, mat, mat, vp, n, vp]
+    L.alpa_linear_forward_work.argtypes = [i, n, n, n]
+    L.alpa_linear_backward_work.argtypes = [i, i, n, n, n]
+    L.alpa_experts_forward_work.argtypes = [i, n, i, n, n]
+    L.alpa_experts_backward_work.argtypes = [i, i, n, i, n, n]
+    L.alpa_vocab_loss_forward_work.argtypes = [i, n, n, n]
+    L.alpa_vocab_loss_backward_work.argtypes = [i, n, n, n]
+    for s in SYMBOLS:
+        getattr(L, s).restype = ctypes.c_int64 if s.endswith("_work") else ctypes.c_int
+    _ready = L
+    return L
+
+
+def _type(x):
+    if x.dtype not in _TYPES:
+        raise ValueError(f"type {x.dtype} is not one of float32, float16, bfloat16")
+    return _TYPES[x.dtype]
+
+
+def _check(name, t, shape, dtype, device):
+    if t.dtype != dtype or t.device != device:
+        raise ValueError(f"{name} is {t.dtype} on {t.device}; {dtype} on {device} expected")
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, {tuple(shape)} expected")
+
+
+def _mat(name, t, shape, like):
+    """A matrix, or matrices one behind the other, as the library takes it: its rows `ld` apart."""
+    if t is None:
+        return alpa_mat_t(None, 0)
+    _check(name, t, shape, like.dtype, like.device)
+    rows, n = shape[-2], shape[-1]
+    ld = t.stride(-2) if rows > 1 else n
+    if len(shape) == 3 and rows == 1 and shape[0] > 1:
+        ld = t.stride(0)
+    if t.numel() and ((n > 1 and t.stride(-1) != 1) or ld < n or
+                      (len(shape) == 3 and shape[0] > 1 and t.stride(0) != rows * ld)):
+        raise ValueError(f"{name} must have contiguous rows that do not overlap, experts one behind the other; "
+                         f"strides are {tuple(t.stride())}")
+    return alpa_mat_t(t.data_ptr(), ld)
+
+
+def _vec(name, t, shape, dtype, device):
+    if t is None:
+        return None
+    _check(name, t, shape, dtype, device)
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    return t.data_ptr()
+
+
+class _On:
+    """The tensors' device and the stream of the call, as torch's current ones, so that results and work memory
+    belong to that stream."""
+
+    def __init__(self, x, stream):
+        if not x.is_cuda:
+            raise ValueError("tensors must be on a GPU")
+        self.device = x.device
+        self.stream = torch.cuda.current_stream(x.device) if stream is None else stream
+        if self.stream.device != x.device:
+            raise ValueError(f"the stream is on {self.stream.device}, the tensors on {x.device}")
+        self.context = torch.cuda.stream(self.stream)
+
+    def __enter__(self):
+        self.context.__enter__()
+        return ctypes.c_void_p(self.stream.cuda_stream)
+
+    def __exit__(self, *a):
+        return self.context.__exit__(*a)
+
+
+def _work(need, device):
+    """(tensor that keeps the memory, pointer, bytes)"""
+    if need == 0:
+        return None, None, 0
+    t = torch.empty(need, dtype=torch.uint8, device=device)
+    return t, t.data_ptr(), need
+
+
+def _two(name, x):
+    if x.dim() != 2:
+        raise ValueError(f"{name} must have two dimensions, not {x.dim()}")
+    return x.shape
+
+
+def _forward(x, w, offsets, bias, residual, act, keep_z, stream):
+    L, d = load(), _type(x)
+    rows, n_in = _two("x", x)
+    n_out = w.shape[-2] if w.dim() >= 2 else 0
+    lead = () if offsets is None else (offsets.numel() - 1,)
+    with _On(x, stream) as s:
+        y = torch.empty(rows, n_out, dtype=x.dtype, device=x.device)
+        z = torch.empty_like(y) if keep_z else None
+        mats = (_mat("x", x, (rows, n_in), x), _mat("w", w, (*lead, n_out, n_in), x),
+                _vec("bias", bias, (*lead, n_out), x.dtype, x.device), _mat("residual", residual, (rows, n_out), x),
+                _mat("y", y, y.shape, x), _mat("z", z, y.shape, x))
+        if offsets is None:
+            keep, p, n = _work(L.alpa_linear_forward_work(d, rows, n_in, n_out), x.device)
+            rc = L.alpa_linear_forward(d, int(act), rows, n_in, n_out, *mats, p, n, s)
+        else:
+            off = _vec("offsets", offsets, (lead[0] + 1,), torch.int32, x.device)
+            keep, p, n = _work(L.alpa_experts_forward_work(d, rows, lead[0], n_in, n_out), x.device)
+            rc = L.alpa_experts_forward(d, int(act), rows, lead[0], n_in, n_out, off, *mats, p, n, s)
+        binding._check(rc)
+    return (y, z) if keep_z else y
+
+
+def _backward(dy, x, w, offsets, z, act, need, stream):
+    L, d = load(), _type(dy)
+    if not set(need) <= {"x", "w", "bias"}:
+        raise ValueError(f"need is {need!r}: names out of 'x', 'w', 'bias' expected")
+    rows, n_out = _two("dy", dy)
+    if x is None and w is None:
+        raise ValueError("one of x and w has to be given")
+    n_in = (w if x is None else x).shape[-1]
+    lead = () if offsets is None else (offsets.numel() - 1,)
+    with _On(dy, stream) as s:
+        new = lambda *size: torch.empty(*size, dtype=dy.dtype, device=dy.device)
+        dx = new(rows, n_in) if "x" in need else None
+        dw = new(*lead, n_out, n_in) if "w" in need else None
+        db = new(*lead, n_out) if "bias" in need else None
+        mats = (_mat("dy", dy, (rows, n_out), dy), _mat("z", z, (rows, n_out), dy), _mat("x", x, (rows, n_in), dy),
+                _mat("w", w, (*lead, n_out, n_in), dy), _mat("dx", dx, (rows, n_in), dy),
+                _mat("dw", dw, (*lead, n_out, n_in), dy))
+        bias = None if db is None else db.data_ptr()
+        if offsets is None:
+            keep, p, n = _work(L.alpa_linear_backward_work(d, int(act), rows, n_in, n_out), dy.device)
+            rc = L.alpa_linear_backward(d, int(act), rows, n_in, n_out, *mats, bias, p, n, s)
+        else:
+            off = _vec("offsets", offsets, (lead[0] + 1,), torch.int32, dy.device)
+            keep, p, n = _work(L.alpa_experts_backward_work(d, int(act), rows, lead[0], n_in, n_out), dy.device)
+            rc = L.alpa_experts_backward(d, int(act), rows, lead[0], n_in, n_out, off, *mats, bias, p, n, s)
+        binding._check(rc)
+    return dx, dw, db
+
+
+def alpa_linear_forward(x, w, bias=None, residual=None, act=ALPA_ACT_NONE, keep_z=False, stream=None):
+    """act(x w^T + bias) + residual for x [rows, in], w [out, in]; with ``keep_z`` also what stands in front of the
+    activation, which the backward pass takes: (y, z)."""
+    return _forward(x, w, None, bias, residual, act, keep_z, stream)
+
+
+def alpa_linear_backward(dy, x, w, z=None, act=ALPA_ACT_NONE, need=("x", "w", "bias"), stream=None):
+    """(dx, dw, dbias), None for those not in ``need``; x is only read for dw, w for dx, z for an activation."""
+    return _backward(dy, x, w, None, z, act, need, stream)
+
+
+def alpa_experts_forward(x, w, offsets, bias=None, residual=None, act=ALPA_ACT_NONE, keep_z=False, stream=None):
+    """The same for rows sorted by expert: rows offsets[e] .. offsets[e + 1] - 1 (int32 tensor [experts + 1] on the GPU)
+    through w[e] of [experts, out, in] and bias[e]; rows of no expert give zeros."""
+    return _forward(x, w, offsets, bias, residual, act, keep_z, stream)
+
+
+def alpa_experts_backward(dy, x, w, offsets, z=None, act=ALPA_ACT_NONE, need=("x", "w", "bias"), stream=None):
+    """(dx, dw, dbias) of alpa_experts_forward; an expert without rows gets zeros."""
+    return _backward(dy, x, w, offsets, z, act, need, stream)
+
+
+def alpa_vocab_loss_forward(x, w, target, stream=None):
+    """(loss, lse), float32 [rows]: cross entropy of softmax(x w^T) for x [rows, in], w [words, in], target int64 [rows];
+    a negative target leaves the row out (loss 0).  ``lse`` is what the backward pass takes."""
+    L, d = load(), _type(x)
+    rows, n_in = _two("x", x)
+    words = _two("w", w)[0]
+    with _On(x, stream) as s:
+        loss = torch.empty(rows, dtype=torch.float32, device=x.device)
+        lse = torch.empty_like(loss)
+        args = (_mat("x", x, (rows, n_in), x), _mat("w", w, (words, n_in), x),
+                _vec("target", target, (rows,), torch.int64, x.device))
+        keep, p, n = _work(L.alpa_vocab_loss_forward_work(d, rows, n_in, words), x.device)
+        binding._check(L.alpa_vocab_loss_forward(d, rows, n_in, words, *args, loss.data_ptr(), lse.data_ptr(), p, n, s))
+    return loss, lse
+
+
+def alpa_vocab_loss_backward(dloss, x, w, target, lse, need=("x", "w"), stream=None):
+    """(dx, dw) for the rows' loss gradients (float32 [rows]), None for those not in ``need``."""
+    L, d = load(), _type(x)
+    if not set(need) <= {"x", "w"}:
+        raise ValueError(f"need is {need!r}: names out of 'x', 'w' expected")
+    rows, n_in = _two("x", x)
+    words = _two("w", w)[0]
+    with _On(x, stream) as s:
+        dx = torch.empty(rows, n_in, dtype=x.dtype, device=x.device) if "x" in need else None
+        dw = torch.empty(words, n_in, dtype=x.dtype, device=x.device) if "w" in need else None
+        f32 = lambda name, t: _vec(name, t, (rows,), torch.float32, x.device)
+        args = (f32("dloss", dloss), _mat("x", x, (rows, n_in), x), _mat("w", w, (words, n_in), x),
+                _vec("target", target, (rows,), torch.int64, x.device), f32("lse", lse),
+                _mat("dx", dx, (rows, n_in), x), _mat("dw", dw, (words, n_in), x))
+        keep, p, n = _work(L.alpa_vocab_loss_backward_work(d, rows, n_in, words), x.device)
+        binding._check(L.alpa_vocab_loss_backward(d, rows, n_in, words, *args, p, n, s))
+    return dx, dw
