@@ -46,11 +46,18 @@ __device__ __forceinline__ float exp_for(float x)
     return sizeof(T) == 4 ? expf(x) : __expf(x);
 }
 
+// n / d: correctly rounded for values that end in 32 bits, within two units in the last place for those rounded to 16
+template <class T>
+__device__ __forceinline__ float divide_for(float n, float d)
+{
+    return sizeof(T) == 4 ? n / d : n * __builtin_amdgcn_rcpf(d);
+}
+
 // z * logistic(z (c1 + c3 z^2)).  An infinite z is given the limit: the formula would have inf / inf or 0 * inf there.
 template <class T>
 __device__ __forceinline__ float gated(float z, float c1, float c3)
 {
-    const float y = z / (1.0f + exp_for<T>(-z * (c1 + c3 * z * z)));
+    const float y = divide_for<T>(z, 1.0f + exp_for<T>(-z * (c1 + c3 * z * z)));
     return fabsf(z) == INFINITY ? (z > 0.0f ? z : -0.0f) : y;
 }
 

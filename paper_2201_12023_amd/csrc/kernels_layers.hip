@@ -19,7 +19,7 @@ __device__ __forceinline__ float slope_of(float z, int act)
     // z s(u) with u = c1 z + c3 z^3:  s + z s (1 - s) u'
     const float c1 = act == 3 ? 1.5957691216057308f : 1.0f, c3 = act == 3 ? 0.071354816272600257f : 0.0f;
     if (fabsf(z) > 1e4f) return z > 0.0f ? 1.0f : 0.0f;          // (there 1 - s or s is 0 in 32 bits, and z^3 may not be finite)
-    const float zz = z * z, e = exp_for<T>(-z * (c1 + c3 * zz)), s = 1.0f / (1.0f + e);
+    const float zz = z * z, e = exp_for<T>(-z * (c1 + c3 * zz)), s = divide_for<T>(1.0f, 1.0f + e);
     return s + z * s * (1.0f - s) * (c1 + 3.0f * c3 * zz);
 }
 

@@ -122,77 +122,95 @@ __device__ __forceinline__ u32x4 load_some(const char *p, int n)
     return r;
 }
 
-// Brings an operand's tiles to LDS.  DIRECT: the load unit writes LDS itself (addresses, strides and the contiguous extent are
-// multiples of 16 bytes, so every chunk exists or does not); otherwise through registers, element by element at the edges.
-template <class T, int FORM, int R, int NT, bool DIRECT>
-struct Loader {
+// Brings an operand's tiles to LDS with the load unit writing there itself.  Addresses, strides and the contiguous extent are multiples of 16
+// bytes, so every chunk exists or does not; those that do not are out of the buffer's range and arrive as zeros.  The loads are written as
+// assembly without a result register because the compiler, for the load's builtin, waits for all loads before the next transposing LDS
+// read (measured at 8192 x 16384 x 4096 in 16 bits, operands in COLS: 1340 us, and 1060 without those waits); what has arrived is
+// known here by counting (arrived()).
+template <class T, int FORM, int R, int NT>
+struct DirectLoader {
     using TL = Tile<T, FORM, R, NT>;
     static constexpr int N = TL::CHUNKS, ES = TL::ES, BK = TL::BK;
-    Operand o;
-    int K;                                  // extent of the contraction
-    uint32_t off[DIRECT ? N : 1];
-    u32x4 held[DIRECT ? 1 : N];
+    const char *p;                          // the next step
+    int64_t advance;
+    int rows, ld, left, chunk0;             // left: of the contraction
+    uint32_t off[N], cut;
+    u32x4 range;
 
-    __device__ __forceinline__ void init(const Operand &op, int k_extent, int tid)
+    __device__ __forceinline__ void init(const Operand &o, int k, int tid)
     {
-        o = op;
-        K = k_extent;
-        if constexpr (DIRECT) {
+        p = o.p;
+        rows = o.rows;
+        ld = (int)o.ld;
+        left = k;
+        advance = FORM == ROWS ? BK * ES : BK * o.ld;
 #pragma unroll
-            for (int j = 0; j < N; ++j) {
-                int major, chunk;
-                TL::place(j * NT + tid, major, chunk);
-                const bool in = FORM == ROWS ? major < o.rows : chunk * (16 / ES) < o.rows;
-                off[j] = in ? (uint32_t)(major * (int)o.ld + chunk * 16) : OUT_OF_RANGE;
-            }
+        for (int j = 0; j < N; ++j) {
+            int major, chunk;
+            TL::place(j * NT + tid, major, chunk);
+            const bool in = FORM == ROWS ? major < rows : chunk * (16 / ES) < rows;
+            off[j] = in ? (uint32_t)(major * ld + chunk * 16) : OUT_OF_RANGE;
+            if (j == 0) chunk0 = chunk;     // (ROWS: the same for all j, as rows NT / 8 apart are permuted alike)
         }
     }
-    // starts the loads of step kt (into LDS at `lds` if DIRECT)
-    __device__ __forceinline__ void start(int kt, char *lds, int tid)
+    // goes to the next step; behind the last one nothing is in range
+    __device__ __forceinline__ void step()
     {
-        const int k0 = kt * BK, left = K - k0;
-        const char *base = o.p + (FORM == ROWS ? (int64_t)k0 * ES : (int64_t)k0 * o.ld);
-        if constexpr (DIRECT) {
-            // what of the operand lies behind `base`; more than a tile can reach is cut to what a range holds
-            const int64_t span = FORM == ROWS ? (int64_t)(o.rows - 1) * o.ld + (int64_t)left * ES
-                                              : (int64_t)(left - 1) * o.ld + (int64_t)o.rows * ES;
-            const int range = o.rows > 0 ? (int)(span < 0x7fffffffll ? span : 0x7fffffffll) : 0;
-            const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc((void *)base, 0, range, 0x00020000);
-            const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-#pragma unroll
-            for (int j = 0; j < N; ++j) {
-                uint32_t v = off[j];
-                if (FORM == ROWS) {
-                    int major, chunk;
-                    TL::place(j * NT + tid, major, chunk);
-                    if (left < BK && chunk * (16 / ES) >= left) v = OUT_OF_RANGE;
-                }
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (ALPA_LDS void *)(lds + (j * NT + wave * 64) * 16), 16, v, 0, 0, 0);
-            }
-        } else {
-#pragma unroll
-            for (int j = 0; j < N; ++j) {
-                int major, chunk;
-                TL::place(j * NT + tid, major, chunk);
-                int n = FORM == ROWS ? left - chunk * (16 / ES) : o.rows - chunk * (16 / ES);
-                if (FORM == ROWS ? major >= o.rows : major >= left) n = 0;
-                held[j] = load_some<T>(base + (int64_t)major * o.ld + chunk * 16, n);
-            }
-        }
+        const int n = min(left, BK);
+        const int span = FORM == ROWS ? (rows - 1) * ld + n * ES : (n - 1) * ld + rows * ES;
+        const uint64_t at = (uint64_t)p;
+        range = u32x4{(uint32_t)at, (uint32_t)(at >> 32) & 0xffffu, (uint32_t)(rows > 0 && n > 0 ? span : 0), 0x00020000u};
+        cut = FORM == ROWS && chunk0 * (16 / ES) >= n ? OUT_OF_RANGE : 0;
+        p += advance;
+        left -= BK;
     }
-    __device__ __forceinline__ void finish(char *lds, int tid)
+    __device__ __forceinline__ void load(int j, char *lds, int wave) const
     {
-        if constexpr (!DIRECT) {
-#pragma unroll
-            for (int j = 0; j < N; ++j) *(u32x4 *)(lds + (j * NT + tid) * 16) = held[j];
-        }
+        const uint32_t to = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(ALPA_LDS char *)lds + (j * NT + wave * 64) * 16);
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"         // (m0 is reserved, and said to be overwritten all the same)
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+                     :
+                     : "s"(to), "v"(FORM == ROWS ? off[j] | cut : off[j]), "s"(range)
+                     : "m0");
+#pragma clang diagnostic pop
     }
 };
 
-// Every load to LDS of this wave has arrived, and every wave is here.
-__device__ __forceinline__ void loads_and_barrier()
+// The same through registers, from any address, element by element at the edges.
+template <class T, int FORM, int R, int NT>
+struct AnyLoader {
+    using TL = Tile<T, FORM, R, NT>;
+    static constexpr int N = TL::CHUNKS, ES = TL::ES, BK = TL::BK;
+    Operand o;
+    int K;
+    u32x4 held[N];
+
+    __device__ __forceinline__ void fetch(int kt, int tid)
+    {
+        const int k0 = kt * BK, left = K - k0;
+        const char *base = o.p + (FORM == ROWS ? (int64_t)k0 * ES : (int64_t)k0 * o.ld);
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            int major, chunk;
+            TL::place(j * NT + tid, major, chunk);
+            int n = FORM == ROWS ? left - chunk * (16 / ES) : o.rows - chunk * (16 / ES);
+            if (FORM == ROWS ? major >= o.rows : major >= left) n = 0;
+            held[j] = load_some<T>(base + (int64_t)major * o.ld + chunk * 16, n);
+        }
+    }
+    __device__ __forceinline__ void store(char *lds, int tid) const
+    {
+#pragma unroll
+        for (int j = 0; j < N; ++j) *(u32x4 *)(lds + (j * NT + tid) * 16) = held[j];
+    }
+};
+
+// All but the last N loads to LDS of this wave have arrived, its LDS reads are done, and every wave is here.
+template <int N>
+__device__ __forceinline__ void arrived()
 {
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(N) : "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
 }
@@ -204,51 +222,183 @@ struct Product {
     static constexpr int NT = WM * WN * 64, MT = BM / WM / 16, NTL = BN / WN / 16, ES = sizeof(T);
     using TA = Tile<T, FA, BM, NT>;
     using TB = Tile<T, FB, BN, NT>;
-    static constexpr int STAGE = TA::BYTES + TB::BYTES, LDS_BYTES = 2 * STAGE;
+    // The large tile: three stages of A and two of B, all the LDS there is.  The small one: two of each, two workgroups in a compute unit.
+    static constexpr bool DEEP = DIRECT && BM == 256;
+    static constexpr int A_STAGES = DEEP ? 3 : 2, LDS_BYTES = A_STAGES * TA::BYTES + 2 * TB::BYTES;
+    using Acc = f32x4[MT][NTL];
+    struct Fragments { u32x4 a[MT], b[NTL]; };
 
-    static __device__ __forceinline__ void run(const Operand &A, const Operand &B, int K, char *lds, f32x4 (&acc)[MT][NTL])
+    static __device__ __forceinline__ void clear(Acc &acc)
     {
-        const int tid = threadIdx.x, lane = tid & 63, i = lane & 15, q = lane >> 4;
-        const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-        const int m0 = wave / WN * (BM / WM), n0 = wave % WN * (BN / WN);
 #pragma unroll
         for (int a = 0; a < MT; ++a)
 #pragma unroll
             for (int b = 0; b < NTL; ++b) acc[a][b] = f32x4{0, 0, 0, 0};
-        Loader<T, FA, BM, NT, DIRECT> la;
-        Loader<T, FB, BN, NT, DIRECT> lb;
-        la.init(A, K, tid);
-        lb.init(B, K, tid);
+    }
+
+    static __device__ __forceinline__ void run(const Operand &A, const Operand &B, int K, char *lds, Acc &acc)
+    {
+        clear(acc);
         const int steps = (K + TA::BK - 1) / TA::BK;
         if (steps == 0) return;
-        la.start(0, lds, tid);
-        lb.start(0, lds + TA::BYTES, tid);
-        la.finish(lds, tid);
-        lb.finish(lds + TA::BYTES, tid);
+        const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        const int m0 = wave / WN * (BM / WM), n0 = wave % WN * (BN / WN);
+        if constexpr (DEEP) run_deep(A, B, K, steps, lds, acc, wave, m0, n0, lane & 15, lane >> 4);
+        else if constexpr (DIRECT) run_direct(A, B, K, steps, lds, acc, wave, m0, n0, lane & 15, lane >> 4);
+        else run_any(A, B, K, steps, lds, acc, m0, n0, lane & 15, lane >> 4);
+    }
+
+private:
+    static __device__ __forceinline__ void half_step(const char *a_lds, const char *b_lds, int ks, Acc &acc, int m0, int n0, int i, int q)
+    {
+        Fragments f;
+#pragma unroll
+        for (int b = 0; b < NTL; ++b) f.b[b] = TB::fragment(b_lds, n0, b, ks, i, q);
+#pragma unroll
+        for (int a = 0; a < MT; ++a) f.a[a] = TA::fragment(a_lds, m0, a, ks, i, q);
+#pragma unroll
+        for (int a = 0; a < MT; ++a)
+#pragma unroll
+            for (int b = 0; b < NTL; ++b) acc[a][b] = mma(f.b[b], f.a[a], acc[a][b], T{});
+    }
+
+    // The next step's loads are under way while this one is multiplied; the other workgroup of the compute unit fills what is left.
+    static __device__ __forceinline__ void run_direct(const Operand &A, const Operand &B, int K, int steps, char *lds, Acc &acc, int wave,
+                                                      int m0, int n0, int i, int q)
+    {
+        DirectLoader<T, FA, BM, NT> la;
+        DirectLoader<T, FB, BN, NT> lb;
+        la.init(A, K, threadIdx.x);
+        lb.init(B, K, threadIdx.x);
+        char *here = lds, *next = lds + TA::BYTES + TB::BYTES;
+        auto fetch = [&](char *to) {
+            la.step();
+            lb.step();
+#pragma unroll
+            for (int j = 0; j < la.N; ++j) la.load(j, to, wave);
+#pragma unroll
+            for (int j = 0; j < lb.N; ++j) lb.load(j, to + TA::BYTES, wave);
+        };
+        fetch(here);
         for (int kt = 0; kt < steps; ++kt) {
-            char *here = lds + (kt & 1) * STAGE, *next = lds + (~kt & 1) * STAGE;
-            loads_and_barrier();
-            if (kt + 1 < steps) {
-                la.start(kt + 1, next, tid);
-                lb.start(kt + 1, next + TA::BYTES, tid);
-            }
-#pragma unroll
-            for (int ks = 0; ks < 2; ++ks) {
-                u32x4 fa[MT], fb[NTL];
-#pragma unroll
-                for (int b = 0; b < NTL; ++b) fb[b] = TB::fragment(here + TA::BYTES, n0, b, ks, i, q);
-#pragma unroll
-                for (int a = 0; a < MT; ++a) fa[a] = TA::fragment(here, m0, a, ks, i, q);
-#pragma unroll
-                for (int a = 0; a < MT; ++a)
-#pragma unroll
-                    for (int b = 0; b < NTL; ++b) acc[a][b] = mma(fb[b], fa[a], acc[a][b], T{});
-            }
-            if (kt + 1 < steps) {
-                la.finish(next, tid);
-                lb.finish(next + TA::BYTES, tid);
-            }
+            arrived<0>();
+            fetch(next);
+            half_step(here, here + TA::BYTES, 0, acc, m0, n0, i, q);
+            half_step(here, here + TA::BYTES, 1, acc, m0, n0, i, q);
+            char *t = here;
+            here = next;
+            next = t;
         }
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // (the loads of nothing behind the last step)
+    }
+
+    static __device__ __forceinline__ void run_any(const Operand &A, const Operand &B, int K, int steps, char *lds, Acc &acc, int m0, int n0,
+                                                   int i, int q)
+    {
+        AnyLoader<T, FA, BM, NT> la{A, K};
+        AnyLoader<T, FB, BN, NT> lb{B, K};
+        char *here = lds, *next = lds + TA::BYTES + TB::BYTES;
+        la.fetch(0, threadIdx.x);
+        lb.fetch(0, threadIdx.x);
+        la.store(here, threadIdx.x);
+        lb.store(here + TA::BYTES, threadIdx.x);
+        for (int kt = 0; kt < steps; ++kt) {
+            arrived<0>();
+            if (kt + 1 < steps) {
+                la.fetch(kt + 1, threadIdx.x);
+                lb.fetch(kt + 1, threadIdx.x);
+            }
+            half_step(here, here + TA::BYTES, 0, acc, m0, n0, i, q);
+            half_step(here, here + TA::BYTES, 1, acc, m0, n0, i, q);
+            if (kt + 1 < steps) {
+                la.store(next, threadIdx.x);
+                lb.store(next + TA::BYTES, threadIdx.x);
+            }
+            char *t = here;
+            here = next;
+            next = t;
+        }
+    }
+
+    // A step is sixteen groups of four products, eight for each half of its contraction; a group also issues a share of the LDS reads of the
+    // next half and every second one a load, so that matrix unit, LDS and load unit have work all the time (eight loads together take the load
+    // unit as long as half a step's products).  A's and B's stages of step kt are read by group 3 (barrier) and then hold loads of
+    // A's step kt + 3 and B's step kt + 2, which gives A nearly two steps to arrive and B one; the last six loads may be under way when step
+    // kt + 1 is looked at (group 8).  At 8192 x 4096 x 16384 in 16 bits a step takes 2490 to 2650 cycles of the 2048 its products need, against
+    // 2810 with loads one step ahead, and the clock that the power limit leaves is 1.65 GHz.
+    static __device__ __forceinline__ void run_deep(const Operand &A, const Operand &B, int K, int steps, char *lds, Acc &acc, int wave,
+                                                    int m0, int n0, int i, int q)
+    {
+        DirectLoader<T, FA, BM, NT> la;
+        DirectLoader<T, FB, BN, NT> lb;
+        static_assert(la.N == 4 && lb.N == 4 && MT == 8 && NTL == 4, "loads and reads are dealt to groups for these");
+        la.init(A, K, threadIdx.x);
+        lb.init(B, K, threadIdx.x);
+        char *a0 = lds, *a1 = lds + TA::BYTES, *a2 = lds + 2 * TA::BYTES, *b0 = lds + 3 * TA::BYTES, *b1 = b0 + TB::BYTES;
+        la.step();
+        lb.step();
+#pragma unroll
+        for (int j = 0; j < 4; ++j) la.load(j, a0, wave);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) lb.load(j, b0, wave);
+        la.step();
+        lb.step();
+#pragma unroll
+        for (int j = 0; j < 4; ++j) la.load(j, a1, wave);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) lb.load(j, b1, wave);
+        la.step();
+        la.load(0, a2, wave);
+        la.load(1, a2, wave);
+        arrived<10>();
+        Fragments f[2];
+        auto read = [&](int half, int a, const char *a_lds, const char *b_lds) {
+            if (a & 1) f[half].b[a >> 1] = TB::fragment(b_lds, n0, a >> 1, half, i, q);
+            f[half].a[a] = TA::fragment(a_lds, m0, a, half, i, q);
+        };
+#pragma unroll
+        for (int a = 0; a < 8; ++a) read(0, a, a0, b0);
+        for (int kt = 0; kt < steps; ++kt) {
+#pragma unroll
+            for (int g = 0; g < 16; ++g) {
+                const int half = g >> 3, a = g & 7;
+                if (g == 0) la.load(2, a2, wave);
+                if (g == 2) la.load(3, a2, wave);
+                if (g < 4) {
+                    read(1, 2 * g, a0, b0);
+                    read(1, 2 * g + 1, a0, b0);
+                }
+                if (g == 4) {
+                    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                    __builtin_amdgcn_s_barrier();
+                    asm volatile("" ::: "memory");
+                    lb.step();
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                if (g == 8) {
+                    arrived<6>();
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                if (g >= 4 && g <= 10 && g % 2 == 0) lb.load((g - 4) / 2, b0, wave);
+                if (g == 12) {
+                    la.step();
+                    la.load(0, a0, wave);
+                }
+                if (g == 14) la.load(1, a0, wave);
+                if (g >= 8) read(0, a, a1, b1);
+#pragma unroll
+                for (int b = 0; b < 4; ++b) acc[a][b] = mma(f[half].b[b], f[half].a[a], acc[a][b], T{});
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            char *t = a0;
+            a0 = a1;
+            a1 = a2;
+            a2 = t;
+            t = b0;
+            b0 = b1;
+            b1 = t;
+        }
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");       // (the loads and reads of nothing behind the last step)
     }
 };
 
