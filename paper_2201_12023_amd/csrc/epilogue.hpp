@@ -5,13 +5,13 @@
 
 namespace alpa {
 
-// N consecutive elements as floats; `wide`: they may be loaded at once (N * sizeof(T) is 8 or 16 bytes, aligned so); `n`: how many exist
+// N consecutive elements as floats; `wide`: they are aligned to 16 bytes, or to their size if that is less; `n`: how many exist
 template <class T, int N>
 __device__ __forceinline__ void load_row(const char *base, int64_t at, int n, int wide, float (&v)[N])
 {
     const T *p = (const T *)base + at;
     if (wide && n >= N) {
-        struct __align__(sizeof(T) * N) Pack { T e[N]; };
+        struct __align__(sizeof(T) * N < 16 ? sizeof(T) * N : 16) Pack { T e[N]; };
         const Pack k = *(const Pack *)p;
 #pragma unroll
         for (int j = 0; j < N; ++j) v[j] = (float)k.e[j];
@@ -27,7 +27,7 @@ __device__ __forceinline__ void store_row(char *base, int64_t at, int n, int wid
 {
     T *p = (T *)base + at;
     if (wide && n >= N) {
-        struct __align__(sizeof(T) * N) Pack { T e[N]; };
+        struct __align__(sizeof(T) * N < 16 ? sizeof(T) * N : 16) Pack { T e[N]; };
         Pack k;
 #pragma unroll
         for (int j = 0; j < N; ++j) k.e[j] = (T)v[j];
@@ -75,17 +75,13 @@ __device__ __forceinline__ float activate(float z, const ProductArgs &g)
     return z < g.low ? g.low : z;              // (a NaN stays)
 }
 
-// Columns n .. n + N - 1 of row m, `cnt` of them real: z = v (+ bias), result act(z) (+ residual).  `skip`: a row of no expert, zeros.
+// Columns n .. n + N - 1 of row m, `cnt` of them real: z = v + bias, result act(z) (+ residual).  `skip`: a row of no expert, zeros.
 template <class T, int EPI, int N>
-__device__ __forceinline__ void put_row(const ProductArgs &g, int64_t out_base, int64_t bias_base, int64_t m, int n, int cnt, bool skip,
+__device__ __forceinline__ void put_row(const ProductArgs &g, int64_t out_base, const float (&bias)[N], int64_t m, int n, int cnt, bool skip,
                                         float (&v)[N])
 {
-    if (g.bias && !skip) {
-        float b[N];
-        load_row<T>(g.bias, bias_base + n, cnt, g.wide, b);
 #pragma unroll
-        for (int j = 0; j < N; ++j) v[j] += b[j];
-    }
+    for (int j = 0; j < N; ++j) v[j] += bias[j];
     if (g.z) store_row<T>(g.z, m * g.ldz + n, cnt, g.wide, v);
 #pragma unroll
     for (int j = 0; j < N; ++j) v[j] = activate<T, EPI>(v[j], g);

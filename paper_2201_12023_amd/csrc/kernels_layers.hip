@@ -147,7 +147,9 @@ __global__ __launch_bounds__(256) void join_kernel(const ProductArgs g)
 #pragma unroll
         for (int j = 0; j < 4; ++j) v[j] *= scale;
     }
-    put_row<T, EPI>(g, 0, 0, m, n, cnt, false, v);
+    float bias[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (g.bias) load_row<T>(g.bias, n, cnt, g.wide, bias);
+    put_row<T, EPI>(g, 0, bias, m, n, cnt, false, v);
 }
 
 template <class T>

@@ -79,27 +79,34 @@ struct Tile {
         if (FORM == ROWS) { major = c >> 3; chunk = (c & 7) ^ swz(major); }
         else { major = c / CPS; chunk = (c % CPS) ^ swz_step(major); }
     }
-    // the rows of block t as lane (i, q) holds them, elements of step ks (of two)
-    static __device__ __forceinline__ u32x4 fragment(const char *lds, int row0, int t, int ks, int i, int q)
+    static __device__ __forceinline__ int first_major(int c) { return FORM == ROWS ? c >> 3 : c / CPS; }
+
+    // Where lane (i, q) reads, in the tile: from there, blocks and halves of the step are an exclusive or and a constant away, so that one
+    // register serves all of a wave's reads.
+    static __device__ __forceinline__ uint32_t lane_at(int row0, int i, int q)
+    {
+        if (FORM == ROWS) return (row0 + row_of(i, 0)) * 128 + (q ^ swz(row_of(i, 0))) * 16;
+        if (ES == 2) {
+            const int k = q * 8 + (i >> 2);
+            return k * (R * 2) + (((row0 >> 3) ^ swz_step(k)) << 4) + (i & 3) * 8;
+        }
+        return q * 4 * (R * 4) + (((row0 >> 2) ^ swz_step(q * 4)) + (i >> 2)) * 16 + (i & 3) * 4;
+    }
+    // the rows of block t as lane (i, q) holds them, elements of half ks of the step; `at`: lane_at() behind the stage's first byte
+    static __device__ __forceinline__ u32x4 fragment(uint32_t at, int t, int ks)
     {
         if (FORM == ROWS) {
-            const int row = row_of(i, t);
-            return *(const u32x4 *)(lds + (row0 + row) * 128 + ((ks * 4 + q) ^ swz(row)) * 16);
+            return *(const ALPA_LDS u32x4 *)(uintptr_t)((at ^ (ks * 64)) + row_of(0, t) * 128);
         } else if (ES == 2) {
-            const int k = ks * 32 + q * 8 + (i >> 2), col = (row0 >> 4) + t;
-            const int at = k * (R * 2) + ((col ^ (swz_step(k) >> 1)) * 32) + (i & 3) * 8;
-            const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((ALPA_LDS i16x4 *)(lds + at));
-            const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((ALPA_LDS i16x4 *)(lds + at + 4 * (R * 2)));
+            const uint32_t from = (at ^ (t * 32)) + ks * 32 * (R * 2);
+            const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((ALPA_LDS i16x4 *)(uintptr_t)from);
+            const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((ALPA_LDS i16x4 *)(uintptr_t)(from + 4 * (R * 2)));
             const u32x2 l = __builtin_bit_cast(u32x2, lo), h = __builtin_bit_cast(u32x2, hi);
             return u32x4{l.x, l.y, h.x, h.y};
         } else {
             u32x4 r;
-            const int col = row0 + t * 16 + i;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int k = ks * 16 + q * 4 + j;
-                r[j] = *(const uint32_t *)(lds + k * (R * 4) + (((col >> 2) ^ swz_step(k)) << 4) + (col & 3) * 4);
-            }
+            for (int j = 0; j < 4; ++j) r[j] = *(const ALPA_LDS uint32_t *)(uintptr_t)((at ^ (t * 64)) + (ks * 16 + j) * (R * 4));
             return r;
         }
     }
@@ -133,8 +140,11 @@ struct DirectLoader {
     static constexpr int N = TL::CHUNKS, ES = TL::ES, BK = TL::BK;
     const char *p;                          // the next step
     int64_t advance;
-    int rows, ld, left, chunk0;             // left: of the contraction
-    uint32_t off[N], cut;
+    int rows, ld, left, chunk;              // left: of the contraction
+    // A thread's chunks lie at the same place of rows or steps that are NT / 8 or NT / CPS apart, which are permuted alike; steps of 32-bit
+    // elements, eight apart, are so every second time.
+    static constexpr int KINDS = FORM == COLS && ES == 4 ? 2 : 1;
+    uint32_t first[KINDS], off[KINDS], apart;      // this thread's first chunks, as they are in this step, and how far chunks are apart
     u32x4 range;
 
     __device__ __forceinline__ void init(const Operand &o, int k, int tid)
@@ -145,33 +155,35 @@ struct DirectLoader {
         left = k;
         advance = FORM == ROWS ? BK * ES : BK * o.ld;
 #pragma unroll
-        for (int j = 0; j < N; ++j) {
-            int major, chunk;
-            TL::place(j * NT + tid, major, chunk);
-            const bool in = FORM == ROWS ? major < rows : chunk * (16 / ES) < rows;
-            off[j] = in ? (uint32_t)(major * ld + chunk * 16) : OUT_OF_RANGE;
-            if (j == 0) chunk0 = chunk;     // (ROWS: the same for all j, as rows NT / 8 apart are permuted alike)
+        for (int j = 0; j < KINDS; ++j) {
+            int major, c;
+            TL::place(j * NT + tid, major, c);
+            if (j == 0) chunk = c;
+            first[j] = FORM == COLS && c * (16 / ES) >= rows ? OUT_OF_RANGE : (uint32_t)(TL::first_major(tid) * ld + c * 16);
         }
+        apart = (uint32_t)(ld * (FORM == ROWS ? NT / 8 : NT / TL::CPS));
     }
-    // goes to the next step; behind the last one nothing is in range
+    // Goes to the next step; behind the last one nothing is in range.  The range ends with the last row's (or step's) last byte, so rows and steps
+    // that do not exist are behind it; chunks behind a row's end but in front of the next row are cut.
     __device__ __forceinline__ void step()
     {
         const int n = min(left, BK);
         const int span = FORM == ROWS ? (rows - 1) * ld + n * ES : (n - 1) * ld + rows * ES;
         const uint64_t at = (uint64_t)p;
         range = u32x4{(uint32_t)at, (uint32_t)(at >> 32) & 0xffffu, (uint32_t)(rows > 0 && n > 0 ? span : 0), 0x00020000u};
-        cut = FORM == ROWS && chunk0 * (16 / ES) >= n ? OUT_OF_RANGE : 0;
+#pragma unroll
+        for (int j = 0; j < KINDS; ++j) off[j] = FORM == ROWS && chunk * (16 / ES) >= n ? first[j] | OUT_OF_RANGE : first[j];
         p += advance;
         left -= BK;
     }
-    __device__ __forceinline__ void load(int j, char *lds, int wave) const
+    __device__ __forceinline__ void load(int j, uint32_t lds, int wave) const
     {
-        const uint32_t to = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(ALPA_LDS char *)lds + (j * NT + wave * 64) * 16);
+        const uint32_t to = __builtin_amdgcn_readfirstlane(lds + (j * NT + wave * 64) * 16);
 #pragma clang diagnostic push
 #pragma clang diagnostic ignored "-Winline-asm"         // (m0 is reserved, and said to be overwritten all the same)
         asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
                      :
-                     : "s"(to), "v"(FORM == ROWS ? off[j] | cut : off[j]), "s"(range)
+                     : "s"(to), "v"(off[j % KINDS] + j * apart), "s"(range)
                      : "m0");
 #pragma clang diagnostic pop
     }
@@ -199,10 +211,10 @@ struct AnyLoader {
             held[j] = load_some<T>(base + (int64_t)major * o.ld + chunk * 16, n);
         }
     }
-    __device__ __forceinline__ void store(char *lds, int tid) const
+    __device__ __forceinline__ void store(uint32_t lds, int tid) const
     {
 #pragma unroll
-        for (int j = 0; j < N; ++j) *(u32x4 *)(lds + (j * NT + tid) * 16) = held[j];
+        for (int j = 0; j < N; ++j) *(ALPA_LDS u32x4 *)(uintptr_t)(lds + (j * NT + tid) * 16) = held[j];
     }
 };
 
@@ -236,26 +248,30 @@ struct Product {
             for (int b = 0; b < NTL; ++b) acc[a][b] = f32x4{0, 0, 0, 0};
     }
 
-    static __device__ __forceinline__ void run(const Operand &A, const Operand &B, int K, char *lds, Acc &acc)
+    // a wave's place: its rows and columns in the tile, where its lanes read
+    struct Wave { int id; uint32_t a_at, b_at; };
+
+    static __device__ __forceinline__ void run(const Operand &A, const Operand &B, int K, char *lds_memory, Acc &acc)
     {
         clear(acc);
         const int steps = (K + TA::BK - 1) / TA::BK;
         if (steps == 0) return;
         const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-        const int m0 = wave / WN * (BM / WM), n0 = wave % WN * (BN / WN);
-        if constexpr (DEEP) run_deep(A, B, K, steps, lds, acc, wave, m0, n0, lane & 15, lane >> 4);
-        else if constexpr (DIRECT) run_direct(A, B, K, steps, lds, acc, wave, m0, n0, lane & 15, lane >> 4);
-        else run_any(A, B, K, steps, lds, acc, m0, n0, lane & 15, lane >> 4);
+        const Wave w{wave, TA::lane_at(wave / WN * (BM / WM), lane & 15, lane >> 4), TB::lane_at(wave % WN * (BN / WN), lane & 15, lane >> 4)};
+        const uint32_t lds = (uint32_t)(uintptr_t)(ALPA_LDS char *)lds_memory;
+        if constexpr (DEEP) run_deep(A, B, K, steps, lds, acc, w);
+        else if constexpr (DIRECT) run_direct(A, B, K, steps, lds, acc, w);
+        else run_any(A, B, K, steps, lds, acc, w);
     }
 
 private:
-    static __device__ __forceinline__ void half_step(const char *a_lds, const char *b_lds, int ks, Acc &acc, int m0, int n0, int i, int q)
+    static __device__ __forceinline__ void half_step(uint32_t a_at, uint32_t b_at, int ks, Acc &acc)
     {
         Fragments f;
 #pragma unroll
-        for (int b = 0; b < NTL; ++b) f.b[b] = TB::fragment(b_lds, n0, b, ks, i, q);
+        for (int b = 0; b < NTL; ++b) f.b[b] = TB::fragment(b_at, b, ks);
 #pragma unroll
-        for (int a = 0; a < MT; ++a) f.a[a] = TA::fragment(a_lds, m0, a, ks, i, q);
+        for (int a = 0; a < MT; ++a) f.a[a] = TA::fragment(a_at, a, ks);
 #pragma unroll
         for (int a = 0; a < MT; ++a)
 #pragma unroll
@@ -263,41 +279,40 @@ private:
     }
 
     // The next step's loads are under way while this one is multiplied; the other workgroup of the compute unit fills what is left.
-    static __device__ __forceinline__ void run_direct(const Operand &A, const Operand &B, int K, int steps, char *lds, Acc &acc, int wave,
-                                                      int m0, int n0, int i, int q)
+    static __device__ __forceinline__ void run_direct(const Operand &A, const Operand &B, int K, int steps, uint32_t lds, Acc &acc,
+                                                      const Wave &w)
     {
         DirectLoader<T, FA, BM, NT> la;
         DirectLoader<T, FB, BN, NT> lb;
         la.init(A, K, threadIdx.x);
         lb.init(B, K, threadIdx.x);
-        char *here = lds, *next = lds + TA::BYTES + TB::BYTES;
-        auto fetch = [&](char *to) {
+        uint32_t here = lds, next = lds + TA::BYTES + TB::BYTES;
+        auto fetch = [&](uint32_t to) {
             la.step();
             lb.step();
 #pragma unroll
-            for (int j = 0; j < la.N; ++j) la.load(j, to, wave);
+            for (int j = 0; j < la.N; ++j) la.load(j, to, w.id);
 #pragma unroll
-            for (int j = 0; j < lb.N; ++j) lb.load(j, to + TA::BYTES, wave);
+            for (int j = 0; j < lb.N; ++j) lb.load(j, to + TA::BYTES, w.id);
         };
         fetch(here);
         for (int kt = 0; kt < steps; ++kt) {
             arrived<0>();
             fetch(next);
-            half_step(here, here + TA::BYTES, 0, acc, m0, n0, i, q);
-            half_step(here, here + TA::BYTES, 1, acc, m0, n0, i, q);
-            char *t = here;
+            half_step(here + w.a_at, here + TA::BYTES + w.b_at, 0, acc);
+            half_step(here + w.a_at, here + TA::BYTES + w.b_at, 1, acc);
+            const uint32_t t = here;
             here = next;
             next = t;
         }
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // (the loads of nothing behind the last step)
     }
 
-    static __device__ __forceinline__ void run_any(const Operand &A, const Operand &B, int K, int steps, char *lds, Acc &acc, int m0, int n0,
-                                                   int i, int q)
+    static __device__ __forceinline__ void run_any(const Operand &A, const Operand &B, int K, int steps, uint32_t lds, Acc &acc, const Wave &w)
     {
         AnyLoader<T, FA, BM, NT> la{A, K};
         AnyLoader<T, FB, BN, NT> lb{B, K};
-        char *here = lds, *next = lds + TA::BYTES + TB::BYTES;
+        uint32_t here = lds, next = lds + TA::BYTES + TB::BYTES;
         la.fetch(0, threadIdx.x);
         lb.fetch(0, threadIdx.x);
         la.store(here, threadIdx.x);
@@ -308,13 +323,13 @@ private:
                 la.fetch(kt + 1, threadIdx.x);
                 lb.fetch(kt + 1, threadIdx.x);
             }
-            half_step(here, here + TA::BYTES, 0, acc, m0, n0, i, q);
-            half_step(here, here + TA::BYTES, 1, acc, m0, n0, i, q);
+            half_step(here + w.a_at, here + TA::BYTES + w.b_at, 0, acc);
+            half_step(here + w.a_at, here + TA::BYTES + w.b_at, 1, acc);
             if (kt + 1 < steps) {
                 la.store(next, threadIdx.x);
                 lb.store(next + TA::BYTES, threadIdx.x);
             }
-            char *t = here;
+            const uint32_t t = here;
             here = next;
             next = t;
         }
@@ -326,47 +341,47 @@ private:
     // A's step kt + 3 and B's step kt + 2, which gives A nearly two steps to arrive and B one; the last six loads may be under way when step
     // kt + 1 is looked at (group 8).  At 8192 x 4096 x 16384 in 16 bits a step takes 2490 to 2650 cycles of the 2048 its products need, against
     // 2810 with loads one step ahead, and the clock that the power limit leaves is 1.65 GHz.
-    static __device__ __forceinline__ void run_deep(const Operand &A, const Operand &B, int K, int steps, char *lds, Acc &acc, int wave,
-                                                    int m0, int n0, int i, int q)
+    static __device__ __forceinline__ void run_deep(const Operand &A, const Operand &B, int K, int steps, uint32_t lds, Acc &acc,
+                                                    const Wave &w)
     {
         DirectLoader<T, FA, BM, NT> la;
         DirectLoader<T, FB, BN, NT> lb;
         static_assert(la.N == 4 && lb.N == 4 && MT == 8 && NTL == 4, "loads and reads are dealt to groups for these");
         la.init(A, K, threadIdx.x);
         lb.init(B, K, threadIdx.x);
-        char *a0 = lds, *a1 = lds + TA::BYTES, *a2 = lds + 2 * TA::BYTES, *b0 = lds + 3 * TA::BYTES, *b1 = b0 + TB::BYTES;
+        uint32_t a0 = lds, a1 = lds + TA::BYTES, a2 = lds + 2 * TA::BYTES, b0 = lds + 3 * TA::BYTES, b1 = b0 + TB::BYTES;
         la.step();
         lb.step();
 #pragma unroll
-        for (int j = 0; j < 4; ++j) la.load(j, a0, wave);
+        for (int j = 0; j < 4; ++j) la.load(j, a0, w.id);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) lb.load(j, b0, wave);
+        for (int j = 0; j < 4; ++j) lb.load(j, b0, w.id);
         la.step();
         lb.step();
 #pragma unroll
-        for (int j = 0; j < 4; ++j) la.load(j, a1, wave);
+        for (int j = 0; j < 4; ++j) la.load(j, a1, w.id);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) lb.load(j, b1, wave);
+        for (int j = 0; j < 4; ++j) lb.load(j, b1, w.id);
         la.step();
-        la.load(0, a2, wave);
-        la.load(1, a2, wave);
+        la.load(0, a2, w.id);
+        la.load(1, a2, w.id);
         arrived<10>();
         Fragments f[2];
-        auto read = [&](int half, int a, const char *a_lds, const char *b_lds) {
-            if (a & 1) f[half].b[a >> 1] = TB::fragment(b_lds, n0, a >> 1, half, i, q);
-            f[half].a[a] = TA::fragment(a_lds, m0, a, half, i, q);
+        auto read = [&](int half, int a, uint32_t a_at, uint32_t b_at) {
+            if (a & 1) f[half].b[a >> 1] = TB::fragment(b_at, a >> 1, half);
+            f[half].a[a] = TA::fragment(a_at, a, half);
         };
 #pragma unroll
-        for (int a = 0; a < 8; ++a) read(0, a, a0, b0);
+        for (int a = 0; a < 8; ++a) read(0, a, a0 + w.a_at, b0 + w.b_at);
         for (int kt = 0; kt < steps; ++kt) {
 #pragma unroll
             for (int g = 0; g < 16; ++g) {
                 const int half = g >> 3, a = g & 7;
-                if (g == 0) la.load(2, a2, wave);
-                if (g == 2) la.load(3, a2, wave);
+                if (g == 0) la.load(2, a2, w.id);
+                if (g == 2) la.load(3, a2, w.id);
                 if (g < 4) {
-                    read(1, 2 * g, a0, b0);
-                    read(1, 2 * g + 1, a0, b0);
+                    read(1, 2 * g, a0 + w.a_at, b0 + w.b_at);
+                    read(1, 2 * g + 1, a0 + w.a_at, b0 + w.b_at);
                 }
                 if (g == 4) {
                     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
@@ -379,18 +394,18 @@ private:
                     arrived<6>();
                     __builtin_amdgcn_sched_barrier(0);
                 }
-                if (g >= 4 && g <= 10 && g % 2 == 0) lb.load((g - 4) / 2, b0, wave);
+                if (g >= 4 && g <= 10 && g % 2 == 0) lb.load((g - 4) / 2, b0, w.id);
                 if (g == 12) {
                     la.step();
-                    la.load(0, a0, wave);
+                    la.load(0, a0, w.id);
                 }
-                if (g == 14) la.load(1, a0, wave);
-                if (g >= 8) read(0, a, a1, b1);
+                if (g == 14) la.load(1, a0, w.id);
+                if (g >= 8) read(0, a, a1 + w.a_at, b1 + w.b_at);
 #pragma unroll
                 for (int b = 0; b < 4; ++b) acc[a][b] = mma(f[half].b[b], f[half].a[a], acc[a][b], T{});
                 __builtin_amdgcn_sched_barrier(0);
             }
-            char *t = a0;
+            uint32_t t = a0;
             a0 = a1;
             a1 = a2;
             a2 = t;

@@ -21,6 +21,119 @@ __device__ __forceinline__ void tile_at(int place, int row_tiles, int col_tiles,
     tn = in / rows;
 }
 
+// Statistics of a wave's columns, by stripes: a lane has four rows' worth of blocks of one row, the four lanes of a row are joined.
+template <class T, class P, int SPAN>
+__device__ __forceinline__ void loss_stripes(const ProductArgs &g, const typename P::Acc &acc, int m_first, int m_end, int n_first, int i, int q)
+{
+    constexpr int CW = P::TB::PAIRED ? 8 : 4, PER = SPAN / STRIPE, IN = P::NTL * 4 / CW / PER;
+    static_assert(SPAN % STRIPE == 0, "stripes do not lie in waves");
+#pragma unroll
+    for (int a = 0; a < P::MT; ++a) {
+        // every lane of the wave takes part; rows behind the last one are not written
+        const int m = m_first + P::TA::row_of(i, a);
+        const int64_t word = m < m_end ? g.target[m] : -1;
+#pragma unroll
+        for (int s = 0; s < PER; ++s) {
+            float top = -INFINITY, sum = 0.0f;
+#pragma unroll
+            for (int c = s * IN; c < (s + 1) * IN; ++c)
+#pragma unroll
+                for (int j = 0; j < CW; ++j) {
+                    const int n = n_first + c * CW * 4 + q * CW + j;
+                    const float v = acc[a][c * CW / 4 + j / 4][j & 3];
+                    if (n < g.N) top = fmaxf(top, v);
+                    if (n < g.N && word == n) g.at_target[m] = v;
+                }
+            top = fmaxf(top, __shfl_xor(top, 16, 64));
+            top = fmaxf(top, __shfl_xor(top, 32, 64));
+            const float ref = top == -INFINITY ? 0.0f : top;
+#pragma unroll
+            for (int c = s * IN; c < (s + 1) * IN; ++c)
+#pragma unroll
+                for (int j = 0; j < CW; ++j) {
+                    const int n = n_first + c * CW * 4 + q * CW + j;
+                    const float v = acc[a][c * CW / 4 + j / 4][j & 3];
+                    if (n < g.N) sum += exp_for<T>(v - ref);
+                }
+            sum += __shfl_xor(sum, 16, 64);
+            sum += __shfl_xor(sum, 32, 64);
+            const int stripe = n_first / STRIPE + s;
+            if (q == 0 && m < m_end && stripe * STRIPE < g.N) g.stat[(int64_t)stripe * g.M + m] = make_float2(top, sum);
+        }
+    }
+}
+
+// The other epilogues: half of each wave's rows at a time go through LDS, from where a thread takes eight consecutive columns of a row, row after
+// row.  So the code is a short loop (unrolled over the accumulators it was 60 KB, fetched anew for every tile: at 512 rows an expert a
+// tile of the weights' gradient took 41 us, with this NN), and a row's columns are written as one piece whatever the operands' form was.
+template <class T, class P, int BM, int BN, int WM, int WN, int EPI>
+__device__ __forceinline__ void through_lds(const ProductArgs &g, const typename P::Acc &acc, char *lds, int m0, int m_end, int n0, int wm, int wn,
+                                            int i, int q, int64_t out_base, int64_t bias_base, bool skip)
+{
+    constexpr int LDT = BN + 4, PART = BM / WM / 2, CW = 8, THREADS = BN / CW, AT_ONCE = WM * WN * 64 / THREADS;      // (four columns more: no bank twice)
+    static_assert(BM / 2 * LDT * 4 <= P::LDS_BYTES, "half a tile does not fit in LDS");
+    float *const tile = (float *)lds;
+    const int col = threadIdx.x % THREADS * CW, n = n0 + col, cnt = g.N - n;
+    const float scale = (EPI == EPI_LINE || EPI == EPI_SUM) && g.scale ? *g.scale : 1.0f;
+    float bias[CW];
+#pragma unroll
+    for (int j = 0; j < CW; ++j) bias[j] = 0.0f;
+    if (g.bias && !skip && cnt > 0) load_row<T>(g.bias, bias_base + n, cnt, g.wide, bias);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        lds_barrier();
+#pragma unroll
+        for (int a = h * P::MT / 2; a < (h + 1) * P::MT / 2; ++a)
+#pragma unroll
+            for (int b = 0; b < P::NTL; ++b) {
+                const int row = wm / 2 + P::TA::row_of(i, a) - h * PART;
+                *(f32x4 *)(tile + row * LDT + wn + P::TB::row_of(q * 4, b)) = acc[a][b];
+            }
+        lds_barrier();
+        if (cnt <= 0) continue;
+#pragma unroll 2
+        for (int row = threadIdx.x / THREADS; row < BM / 2; row += AT_ONCE) {
+            const int m = m0 + row / PART * (2 * PART) + h * PART + row % PART;
+            if (m >= m_end) continue;
+            float v[CW];
+            *(f32x4 *)v = *(const f32x4 *)(tile + row * LDT + col);
+            *(f32x4 *)(v + 4) = *(const f32x4 *)(tile + row * LDT + col + 4);
+            if constexpr (EPI == EPI_GRAD) {
+                const float lse = g.lse[m], coef = g.coef[m];
+                const int64_t word = g.target[m] - g.word0;
+#pragma unroll
+                for (int j = 0; j < CW; ++j)
+                    v[j] = coef == 0.0f ? 0.0f : (exp_for<T>(v[j] - lse) - (word == n + j ? 1.0f : 0.0f)) * coef;
+                store_row<T>(g.out, (int64_t)m * g.ldo + n, cnt, g.wide, v);
+            } else if constexpr (EPI == EPI_SUM) {
+                char *sum = (char *)g.sum;
+                const int64_t at = ((int64_t)blockIdx.y * g.M + m) * g.N + n;
+                const int aligned = (g.N & 3) == 0;
+#pragma unroll
+                for (int k = 0; k < CW; k += 4) {
+                    float part[4] = {v[k], v[k + 1], v[k + 2], v[k + 3]};
+                    if (!g.first) {
+                        float old[4];
+                        load_row<float>(sum, at + k, cnt - k, aligned, old);
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) part[j] += old[j];
+                    }
+                    if (!g.last) store_row<float>(sum, at + k, cnt - k, aligned, part);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) v[k + j] = part[j] * scale;
+                }
+                if (g.last) store_row<T>(g.out, (int64_t)m * g.ldo + n, cnt, g.wide, v);
+            } else {
+                if (EPI == EPI_LINE) {
+#pragma unroll
+                    for (int j = 0; j < CW; ++j) v[j] *= scale;
+                }
+                put_row<T, EPI>(g, out_base, bias, m, n, cnt, skip, v);
+            }
+        }
+    }
+}
+
 template <class T, int FA, int FB, int BM, int BN, int WM, int WN, bool DIRECT, int EPI>
 __global__ __launch_bounds__(WM *WN * 64, 2) void product_kernel(const ProductArgs g)
 {
@@ -64,101 +177,14 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void product_kernel(const ProductAr
                     m_end - m0};
     const Operand B{b + (FB == ROWS ? (int64_t)n0 * g.ldb + (int64_t)k0 * ES : (int64_t)k0 * g.ldb + (int64_t)n0 * ES), g.ldb,
                     min(BN, g.N - n0)};
-    f32x4 acc[P::MT][P::NTL];
+    typename P::Acc acc;
     P::run(A, B, k_end - k0, lds, acc);
 
     const int lane = threadIdx.x & 63, i = lane & 15, q = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave / WN * (BM / WM), wn = wave % WN * (BN / WN);
-    // a lane's consecutive columns: eight over two blocks of the product, or four of one
-    constexpr int CW = P::TB::PAIRED ? 8 : 4, GROUPS = P::NTL * 4 / CW;
-    const float scale = (EPI == EPI_LINE || EPI == EPI_SUM) && g.scale ? *g.scale : 1.0f;
-
-#pragma unroll
-    for (int a = 0; a < P::MT; ++a) {
-        const int m = m0 + wm + P::TA::row_of(i, a);
-        if constexpr (EPI == EPI_LOSS) {
-            // every lane of the wave takes part; rows behind the last one are not written
-            constexpr int SPAN = BN / WN, PER = SPAN / STRIPE, IN = GROUPS / PER;
-            static_assert(SPAN % STRIPE == 0, "stripes do not lie in waves");
-            const int64_t word = m < m_end ? g.target[m] : -1;
-#pragma unroll
-            for (int s = 0; s < PER; ++s) {
-                float top = -INFINITY, sum = 0.0f;
-#pragma unroll
-                for (int c = s * IN; c < (s + 1) * IN; ++c)
-#pragma unroll
-                    for (int j = 0; j < CW; ++j) {
-                        const int n = n0 + wn + c * CW * 4 + q * CW + j;
-                        const float v = acc[a][c * CW / 4 + j / 4][j & 3];
-                        if (n < g.N) top = fmaxf(top, v);
-                        if (n < g.N && word == n) g.at_target[m] = v;
-                    }
-                top = fmaxf(top, __shfl_xor(top, 16, 64));
-                top = fmaxf(top, __shfl_xor(top, 32, 64));
-                const float ref = top == -INFINITY ? 0.0f : top;
-#pragma unroll
-                for (int c = s * IN; c < (s + 1) * IN; ++c)
-#pragma unroll
-                    for (int j = 0; j < CW; ++j) {
-                        const int n = n0 + wn + c * CW * 4 + q * CW + j;
-                        const float v = acc[a][c * CW / 4 + j / 4][j & 3];
-                        if (n < g.N) sum += exp_for<T>(v - ref);
-                    }
-                sum += __shfl_xor(sum, 16, 64);
-                sum += __shfl_xor(sum, 32, 64);
-                const int stripe = (n0 + wn) / STRIPE + s;
-                if (q == 0 && m < m_end && stripe * STRIPE < g.N) g.stat[(int64_t)stripe * g.M + m] = make_float2(top, sum);
-            }
-        } else {
-            if (m >= m_end) continue;
-            float lse = 0.0f, coef = 0.0f;
-            int64_t word = -1;
-            if constexpr (EPI == EPI_GRAD) {
-                lse = g.lse[m];
-                coef = g.coef[m];
-                word = g.target[m] - g.word0;
-            }
-#pragma unroll
-            for (int c = 0; c < GROUPS; ++c) {
-                const int n = n0 + wn + c * CW * 4 + q * CW, cnt = g.N - n;
-                if (cnt <= 0) continue;
-                float v[CW];
-#pragma unroll
-                for (int j = 0; j < CW; ++j) v[j] = acc[a][c * CW / 4 + j / 4][j & 3];
-                if constexpr (EPI == EPI_GRAD) {
-#pragma unroll
-                    for (int j = 0; j < CW; ++j)
-                        v[j] = coef == 0.0f ? 0.0f : (exp_for<T>(v[j] - lse) - (word == n + j ? 1.0f : 0.0f)) * coef;
-                    store_row<T>(g.out, (int64_t)m * g.ldo + n, cnt, g.wide, v);
-                } else if constexpr (EPI == EPI_SUM) {
-                    char *sum = (char *)g.sum;
-                    const int64_t at = ((int64_t)blockIdx.y * g.M + m) * g.N + n;
-                    const int aligned = (g.N & 3) == 0;
-#pragma unroll
-                    for (int h = 0; h < CW; h += 4) {
-                        float part[4] = {v[h], v[h + 1], v[h + 2], v[h + 3]};
-                        if (!g.first) {
-                            float old[4];
-                            load_row<float>(sum, at + h, cnt - h, aligned, old);
-#pragma unroll
-                            for (int j = 0; j < 4; ++j) part[j] += old[j];
-                        }
-                        if (!g.last) store_row<float>(sum, at + h, cnt - h, aligned, part);
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) v[h + j] = part[j] * scale;
-                    }
-                    if (g.last) store_row<T>(g.out, (int64_t)m * g.ldo + n, cnt, g.wide, v);
-                } else {
-                    if (EPI == EPI_LINE) {
-#pragma unroll
-                        for (int j = 0; j < CW; ++j) v[j] *= scale;
-                    }
-                    put_row<T, EPI>(g, out_base, bias_base, m, n, cnt, skip, v);
-                }
-            }
-        }
-    }
+    if constexpr (EPI == EPI_LOSS) loss_stripes<T, P, BN / WN>(g, acc, m0 + wm, m_end, n0 + wn, i, q);
+    else through_lds<T, P, BM, BN, WM, WN, EPI>(g, acc, lds, m0, m_end, n0, wm, wn, i, q, out_base, bias_base, skip);
 }
 
 template <class T, int FA, int FB, int EPI>
