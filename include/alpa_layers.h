@@ -13,14 +13,14 @@
  *   - a call only queues kernels on `hip_stream` (a hipStream_t, NULL = the null stream) and returns: it allocates nothing, copies
  *     nothing to or from the host and does not synchronise, so that it may be recorded into a HIP graph.  It must be made with the tensors'
  *     device current.  Calls that may overlap need work memory of their own each;
- *   - work memory: `work` of at least the bytes that the `_work` call of the same arguments returns, aligned to 256 bytes (NULL if that is 0).
- *     Nothing in it needs to be kept or cleared between calls;
+ *   - work memory: `work` of at least the bytes that the `_work` call of the same arguments returns (0 for arguments that are
+ *     refused), aligned to 256 bytes; NULL if that is 0.  Nothing in it needs to be kept or cleared between calls;
  *   - an output must not overlap any other tensor of the call;
  *   - results do not depend on the launch: two calls on the same arguments give the same bits.
  *
  * Limits: sizes of a row up to ALPA_LAYER_MAX_WIDTH, strides up to 2^22 bytes, rows up to ALPA_LAYER_MAX_ROWS (0 is allowed),
- * words and experts as below.  Pointers, strides and row lengths that are multiples of 16 bytes are served by the faster kernels; others need
- * no more than the alignment of one element.
+ * words and experts as below.  Tensors need no more than the alignment of one element; operands whose address, stride or row length is no
+ * multiple of 16 bytes are first copied to work memory.
  *
  * All functions return ALPA_DP_OK or a negative code of alpa_dp.h and never throw or abort; alpa_dp_last_error() has the message.
  */
@@ -58,7 +58,7 @@ typedef struct { void *p; int64_t ld; } alpa_mat_t;    /* first element; element
  * Errors: EINVAL (null pointer, size, type, activation or stride out of range, pointer not aligned to an element, work memory too small),
  * EHIP.
  */
-int64_t alpa_linear_forward_work(int dtype, int64_t rows, int64_t n_in, int64_t n_out);
+int64_t alpa_linear_forward_work(int dtype, int64_t rows, int64_t n_in, int64_t n_out, alpa_mat_t x, alpa_mat_t w);
 int alpa_linear_forward(int dtype, int act, int64_t rows, int64_t n_in, int64_t n_out, alpa_mat_t x, alpa_mat_t w,
                         const void *bias, alpa_mat_t residual, alpa_mat_t y, alpa_mat_t z, void *work,
                         int64_t work_bytes, void *hip_stream);
@@ -69,7 +69,8 @@ int alpa_linear_forward(int dtype, int act, int64_t rows, int64_t n_in, int64_t 
  *   `dtype` as an operand of the two products; dbias is summed from the 32-bit values.  The slope of ALPA_ACT_RELU at 0 is 0.  (The residual's gradient is dy.)
  * With rows == 0, dw and dbias are zero.
  */
-int64_t alpa_linear_backward_work(int dtype, int act, int64_t rows, int64_t n_in, int64_t n_out);
+int64_t alpa_linear_backward_work(int dtype, int act, int64_t rows, int64_t n_in, int64_t n_out, alpa_mat_t dy,
+                                  alpa_mat_t x, alpa_mat_t w);
 int alpa_linear_backward(int dtype, int act, int64_t rows, int64_t n_in, int64_t n_out, alpa_mat_t dy, alpa_mat_t z,
                          alpa_mat_t x, alpa_mat_t w, alpa_mat_t dx, alpa_mat_t dw, void *dbias, void *work,
                          int64_t work_bytes, void *hip_stream);
@@ -82,11 +83,13 @@ int alpa_linear_backward(int dtype, int act, int64_t rows, int64_t n_in, int64_t
  *   bias, dbias  [experts][n_out].
  * dw and dbias of an empty group are zero.
  */
-int64_t alpa_experts_forward_work(int dtype, int64_t rows, int experts, int64_t n_in, int64_t n_out);
+int64_t alpa_experts_forward_work(int dtype, int64_t rows, int experts, int64_t n_in, int64_t n_out, alpa_mat_t x,
+                                  alpa_mat_t w);
 int alpa_experts_forward(int dtype, int act, int64_t rows, int experts, int64_t n_in, int64_t n_out,
                          const int32_t *offsets, alpa_mat_t x, alpa_mat_t w, const void *bias, alpa_mat_t residual,
                          alpa_mat_t y, alpa_mat_t z, void *work, int64_t work_bytes, void *hip_stream);
-int64_t alpa_experts_backward_work(int dtype, int act, int64_t rows, int experts, int64_t n_in, int64_t n_out);
+int64_t alpa_experts_backward_work(int dtype, int act, int64_t rows, int experts, int64_t n_in, int64_t n_out,
+                                   alpa_mat_t dy, alpa_mat_t x, alpa_mat_t w);
 int alpa_experts_backward(int dtype, int act, int64_t rows, int experts, int64_t n_in, int64_t n_out,
                           const int32_t *offsets, alpa_mat_t dy, alpa_mat_t z, alpa_mat_t x, alpa_mat_t w,
                           alpa_mat_t dx, alpa_mat_t dw, void *dbias, void *work, int64_t work_bytes,
@@ -99,7 +102,7 @@ int alpa_experts_backward(int dtype, int act, int64_t rows, int experts, int64_t
  *   loss    DEVICE float [rows]: log(sum_v exp(l_v)) - l_target.
  *   lse     DEVICE float [rows]: the logarithm, which the backward pass takes back.
  */
-int64_t alpa_vocab_loss_forward_work(int dtype, int64_t rows, int64_t n_in, int64_t words);
+int64_t alpa_vocab_loss_forward_work(int dtype, int64_t rows, int64_t n_in, int64_t words, alpa_mat_t x, alpa_mat_t w);
 int alpa_vocab_loss_forward(int dtype, int64_t rows, int64_t n_in, int64_t words, alpa_mat_t x, alpa_mat_t w,
                             const int64_t *target, float *loss, float *lse, void *work, int64_t work_bytes,
                             void *hip_stream);
@@ -110,7 +113,8 @@ int alpa_vocab_loss_forward(int dtype, int64_t rows, int64_t n_in, int64_t words
  *   largest |dloss| (found on the device) so that small probabilities keep their bits in 16-bit floats.  dx or dw may be NULL.  A row without a
  *   loss is not read into dx; in dw it counts as 0 times its x.
  */
-int64_t alpa_vocab_loss_backward_work(int dtype, int64_t rows, int64_t n_in, int64_t words);
+int64_t alpa_vocab_loss_backward_work(int dtype, int64_t rows, int64_t n_in, int64_t words, alpa_mat_t x,
+                                      alpa_mat_t w);
 int alpa_vocab_loss_backward(int dtype, int64_t rows, int64_t n_in, int64_t words, const float *dloss, alpa_mat_t x,
                              alpa_mat_t w, const int64_t *target, const float *lse, alpa_mat_t dx, alpa_mat_t dw,
                              void *work, int64_t work_bytes, void *hip_stream);

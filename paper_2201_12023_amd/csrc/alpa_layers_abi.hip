@@ -72,6 +72,31 @@ Epilogue epilogue_of(int act, ProductArgs &g)
     return act == ALPA_ACT_GELU ? EPI_ERF : act >= ALPA_ACT_GELU_TANH ? EPI_SIGMOID : EPI_LINE;
 }
 
+// An operand as the tiled product takes it: address, stride and row length are multiples of 16 bytes.
+struct Source {
+    const char *p;
+    int64_t ld, len;        // elements; len with its padding, which holds zeros
+};
+
+// Work memory for the copy of a matrix that is not so (0: it is taken as it is).
+int64_t pack_bytes(const alpa_mat_t &m, int64_t rows, int64_t len, int dtype)
+{
+    const int64_t es = element(dtype);
+    if (!m.p || rows == 0 || (by16(m.p) && (m.ld * es) % 16 == 0 && (len * es) % 16 == 0)) return 0;
+    return block(rows * round_up(len, 16 / es) * es);
+}
+int pack(hipStream_t st, const alpa_mat_t &m, int64_t rows, int64_t len, int dtype, char *work, Source &out)
+{
+    if (pack_bytes(m, rows, len, dtype) == 0) {
+        out = Source{(const char *)m.p, m.ld, len};
+        return ALPA_DP_OK;
+    }
+    const int64_t to = round_up(len, 16 / element(dtype));
+    HIPCHK(launch_pack(st, dtype, (const char *)m.p, m.ld, rows, (int)len, work, (int)to));
+    out = Source{work, to, to};
+    return ALPA_DP_OK;
+}
+
 // A product of `m` x `n` results over `k`; `groups`: matrices of results (GROUP_STEPS), or groups of rows.
 struct Shape {
     int64_t m, n, k;
@@ -101,33 +126,30 @@ int64_t split_bytes(const Shape &s, int dtype)
     return n > 1 ? block((int64_t)n * s.m * s.n * 4) : 0;
 }
 
-// Queues the product that `g` describes (operands, strides in bytes, epilogue), and the join if it is split.
+// Queues the product that `g` describes (operands, epilogue), and the join if it is split.
 int run_product(hipStream_t st, int dtype, Forms forms, Epilogue epi, const Shape &s, ProductArgs g, void *split_work)
 {
     if (s.m == 0 || (s.grouping == GROUP_STEPS && s.groups == 0)) return ALPA_DP_OK;
     const int64_t es = element(dtype);
     g.M = (int)s.m;
     g.N = (int)s.n;
-    g.K = (int)s.k;
+    // the longer of the two operands' contractions: one may be padded with zeros
+    g.K = s.grouping == GROUP_STEPS ? (int)s.k : std::max(g.a_k, g.b_k);
     g.grouping = s.grouping;
     g.experts = s.groups;
-    // 16-byte accesses: every chunk of a row lies in the tensor or behind it
-    const int64_t a_row = (forms == FORM_CC ? s.m : s.k) * es, b_row = (forms == FORM_RR ? s.k : s.n) * es;
-    const bool direct = by16(g.a) && by16(g.b) && g.lda % 16 == 0 && g.ldb % 16 == 0 && a_row % 16 == 0 && b_row % 16 == 0 &&
-                        (s.grouping != GROUP_ROWS || g.b_expert % 16 == 0);
     g.wide = by16(g.out) && by16(g.z) && by16(g.residual) && by16(g.bias) && g.ldo * es % 16 == 0 && g.ldz * es % 16 == 0 &&
              g.ldr * es % 16 == 0 && (s.grouping == GROUP_NONE || s.n * es % 16 == 0) &&
              (s.grouping != GROUP_STEPS || g.b_expert * es % 16 == 0);
     // The larger tile reads half as much of the operands per result, the smaller one fills the compute units with less.
     const bool long_groups = s.grouping != GROUP_ROWS || s.m >= (int64_t)s.groups * 192;
-    const int tile = direct && long_groups && tiles_of(s, BIG_TILE) >= 256 ? BIG_TILE : TILE;
+    const int tile = long_groups && tiles_of(s, BIG_TILE) >= 256 ? BIG_TILE : TILE;
     const int64_t tiles = tiles_of(s, tile);
     if (tiles > (1 << 30)) return fail(ALPA_DP_EINVAL, "result too large");
     g.row_tiles = (int)(s.grouping == GROUP_ROWS ? slots_at_most(s.m, s.groups, tile) : (s.m + tile - 1) / tile);
     g.col_tiles = (int)((s.n + tile - 1) / tile);
     g.splits = epi == EPI_LOSS || epi == EPI_GRAD || epi == EPI_SUM ? 1 : splits_of(s, dtype);
     if (g.splits > 1) {
-        const int64_t steps = (s.k * es + STEP_BYTES - 1) / STEP_BYTES;
+        const int64_t steps = (g.K * es + STEP_BYTES - 1) / STEP_BYTES;
         g.split_steps = (int)((steps + g.splits - 1) / g.splits);
         g.splits = (int)((steps + g.split_steps - 1) / g.split_steps);
         g.sum = (float *)split_work;
@@ -135,23 +157,30 @@ int run_product(hipStream_t st, int dtype, Forms forms, Epilogue epi, const Shap
         part.first = 1;
         part.last = 0;
         part.scale = nullptr;
-        HIPCHK(launch_product(st, dtype, forms, EPI_SUM, tile, direct, part));
+        part.bias = nullptr;
+        HIPCHK(launch_product(st, dtype, forms, EPI_SUM, tile, part));
         HIPCHK(launch_join(st, dtype, epi, g));
         return ALPA_DP_OK;
     }
-    HIPCHK(launch_product(st, dtype, forms, epi, tile, direct, g));
+    HIPCHK(launch_product(st, dtype, forms, epi, tile, g));
     return ALPA_DP_OK;
 }
 
-ProductArgs operands(const alpa_mat_t &a, const alpa_mat_t &b, int dtype)
+// Operands of a product over `k`: an operand whose contraction is contiguous (its row) has it with its padding.
+ProductArgs operands(Forms forms, const Source &a, const Source &b, int64_t k, int dtype)
 {
     ProductArgs g{};
-    g.a = (const char *)a.p;
-    g.b = (const char *)b.p;
+    g.a = a.p;
+    g.b = b.p;
     g.lda = a.ld * element(dtype);
     g.ldb = b.ld * element(dtype);
+    g.a_k = (int)(forms == FORM_CC ? k : a.len);
+    g.b_k = (int)(forms == FORM_RR ? b.len : k);
+    g.a_len = (int)a.len;
+    g.b_len = (int)b.len;
     g.splits = 1;
     g.first = g.last = 1;
+    g.low = -INFINITY;
     return g;
 }
 void result(ProductArgs &g, const alpa_mat_t &out)
@@ -162,14 +191,20 @@ void result(ProductArgs &g, const alpa_mat_t &out)
 
 // ---------------------------------------------------------------- products of dense and expert layers
 
-// experts < 0: one weight for all rows
-int64_t forward_work(int dtype, int64_t rows, int experts, int64_t n_in, int64_t n_out)
-{
-    return experts < 0 ? split_bytes(Shape{rows, n_out, n_in, GROUP_NONE, 0}, dtype) : 0;
-}
+// Parts of the work memory, experts < 0: one weight for all rows.
+struct ForwardWork {
+    int64_t x, w, split, total;         // offsets
+    ForwardWork(int dtype, int64_t rows, int experts, int64_t n_in, int64_t n_out, const alpa_mat_t &xm, const alpa_mat_t &wm)
+    {
+        x = 0;
+        w = x + pack_bytes(xm, rows, n_in, dtype);
+        split = w + (rows ? pack_bytes(wm, n_out * std::max(experts, 1), n_in, dtype) : 0);
+        total = split + (experts < 0 ? split_bytes(Shape{rows, n_out, n_in, GROUP_NONE, 0}, dtype) : 0);
+    }
+};
 
 int forward(int dtype, int act, int64_t rows, int experts, int64_t n_in, int64_t n_out, const int32_t *offsets, const alpa_mat_t &x,
-            const alpa_mat_t &w, const void *bias, const alpa_mat_t &residual, const alpa_mat_t &y, const alpa_mat_t &z, void *work,
+            const alpa_mat_t &w, const void *bias, const alpa_mat_t &residual, const alpa_mat_t &y, const alpa_mat_t &z, char *work,
             int64_t work_bytes, hipStream_t st)
 {
     TRY(check_sizes(dtype, rows, n_in, n_out, ALPA_LAYER_MAX_WIDTH));
@@ -181,8 +216,12 @@ int forward(int dtype, int act, int64_t rows, int experts, int64_t n_in, int64_t
     TRY(check_mat(z, rows, n_out, dtype, true, ""));
     TRY(check_mat(residual, rows, n_out, dtype, true, ""));
     TRY(check_vector(bias, element(dtype)));
-    TRY(check_work(work, work_bytes, forward_work(dtype, rows, experts, n_in, n_out)));
-    ProductArgs g = operands(x, w, dtype);
+    const ForwardWork at(dtype, rows, experts, n_in, n_out, x, w);
+    TRY(check_work(work, work_bytes, at.total));
+    Source xs, ws;
+    TRY(pack(st, x, rows, n_in, dtype, work + at.x, xs));
+    TRY(pack(st, w, n_out * std::max(experts, 1), n_in, dtype, work + at.w, ws));
+    ProductArgs g = operands(FORM_RR, xs, ws, n_in, dtype);
     const Epilogue epi = epilogue_of(act, g);
     result(g, y);
     g.bias = (const char *)bias;
@@ -193,21 +232,24 @@ int forward(int dtype, int act, int64_t rows, int experts, int64_t n_in, int64_t
     g.offsets = offsets;
     g.b_expert = n_out * g.ldb;
     return run_product(st, dtype, FORM_RR, epi, Shape{rows, n_out, n_in, experts < 0 ? GROUP_NONE : GROUP_ROWS, std::max(experts, 0)}, g,
-                       work);
+                       work + at.split);
 }
 
-// Parts of the backward pass's work memory.
 struct BackwardWork {
-    int64_t dz, part, split, total;     // offsets
+    int64_t dz, part, x, w, split, total;     // offsets
     int64_t ldd;
     int slots;
-    BackwardWork(int dtype, int act, int64_t rows, int experts, int64_t n_in, int64_t n_out)
+    // (dym, xm and wm with p NULL if they are not read)
+    BackwardWork(int dtype, int act, int64_t rows, int experts, int64_t n_in, int64_t n_out, const alpa_mat_t &dym, const alpa_mat_t &xm,
+                 const alpa_mat_t &wm)
     {
         ldd = round_up(n_out, 16 / element(dtype));
         slots = (int)(experts < 0 ? (rows + SLOPE_ROWS - 1) / SLOPE_ROWS : slots_at_most(rows, experts, SLOPE_ROWS));
         dz = 0;
-        part = dz + (act == ALPA_ACT_NONE ? 0 : block(rows * ldd * element(dtype)));
-        split = part + block((int64_t)slots * n_out * 4);
+        part = dz + (act == ALPA_ACT_NONE ? pack_bytes(dym, rows, n_out, dtype) : block(rows * ldd * element(dtype)));
+        x = part + block((int64_t)slots * n_out * 4);
+        w = x + pack_bytes(xm, rows, n_in, dtype);
+        split = w + (rows ? pack_bytes(wm, n_out * std::max(experts, 1), n_in, dtype) : 0);
         int64_t most = 0;
         if (experts < 0)
             most = std::max(split_bytes(Shape{rows, n_in, n_out, GROUP_NONE, 0}, dtype),
@@ -229,23 +271,23 @@ int backward(int dtype, int act, int64_t rows, int experts, int64_t n_in, int64_
     TRY(check_mat(dx, rows, n_in, dtype, true, ""));
     TRY(check_mat(dw, n_out, n_in, dtype, true, ""));
     TRY(check_vector(dbias, element(dtype)));
-    const BackwardWork at(dtype, act, rows, experts, n_in, n_out);
+    const alpa_mat_t none{nullptr, 0};
+    const BackwardWork at(dtype, act, rows, experts, n_in, n_out, dy, dw.p ? x : none, dx.p ? w : none);
     TRY(check_work(work, work_bytes, at.total));
 
-    const bool grouped = experts >= 0, has_z = act != ALPA_ACT_NONE;
-    alpa_mat_t dz = dy;
-    if (rows > 0 && (dbias || (has_z && (dx.p || dw.p)))) {
+    const bool grouped = experts >= 0, has_z = act != ALPA_ACT_NONE, products = dx.p || dw.p;
+    Source dz{(const char *)dy.p, dy.ld, n_out}, xs{}, ws{};
+    if (rows > 0 && (dbias || (has_z && products))) {
         SlopeArgs s{};
         const int64_t es = element(dtype);
         s.dy = (const char *)dy.p;
         s.lddy = dy.ld;
         s.z = has_z ? (const char *)z.p : nullptr;
         s.ldz = has_z ? z.ld : 0;
-        if (has_z) {
-            dz.p = work + at.dz;
-            dz.ld = at.ldd;
-            s.dz = (char *)dz.p;
-            s.ldd = dz.ld;
+        if (has_z && products) {
+            s.dz = work + at.dz;
+            s.ldd = at.ldd;
+            dz = Source{s.dz, at.ldd, at.ldd};
         }
         s.part = dbias ? (float *)(work + at.part) : nullptr;
         s.rows = (int)rows;
@@ -257,9 +299,10 @@ int backward(int dtype, int act, int64_t rows, int experts, int64_t n_in, int64_
         s.wide = by16(s.dy) && by16(s.z) && s.lddy * es % 16 == 0 && s.ldz * es % 16 == 0;
         HIPCHK(launch_slope(st, dtype, s));
     }
+    if (rows > 0 && !has_z && products) TRY(pack(st, dy, rows, n_out, dtype, work + at.dz, dz));
     if (dx.p && rows > 0) {
-        ProductArgs g = operands(dz, w, dtype);
-        g.low = -INFINITY;
+        TRY(pack(st, w, n_out * std::max(experts, 1), n_in, dtype, work + at.w, ws));
+        ProductArgs g = operands(FORM_RC, dz, ws, n_out, dtype);
         result(g, dx);
         g.offsets = offsets;
         g.b_expert = n_out * g.ldb;
@@ -267,8 +310,8 @@ int backward(int dtype, int act, int64_t rows, int experts, int64_t n_in, int64_
                         work + at.split));
     }
     if (dw.p) {
-        ProductArgs g = operands(dz, x, dtype);
-        g.low = -INFINITY;
+        TRY(pack(st, x, rows, n_in, dtype, work + at.x, xs));
+        ProductArgs g = operands(FORM_CC, dz, xs, rows, dtype);
         result(g, dw);
         g.offsets = offsets;
         g.b_expert = n_out * dw.ld;
@@ -292,27 +335,52 @@ int check_experts(int experts, const int32_t *offsets)
 
 int64_t stripes_of(int64_t words) { return (words + STRIPE - 1) / STRIPE; }
 
-// A piece's gradient of the logits is kept to 256 MiB, what the last-level cache holds, in pieces of one size (multiples of the larger tile).
+// A piece's gradient of the logits is kept to 256 MiB, what the last-level cache holds, in pieces of one size: a multiple of the columns that
+// give every compute unit the same number of the larger tiles.
 struct LossWork {
     int64_t pieces, piece;              // number, words in each
-    int64_t coef, scale, grad, sum, split, total;
-    LossWork(int dtype, int64_t rows, int64_t n_in, int64_t words)
+    int64_t coef, scale, x, w, grad, sum, split, total;
+    LossWork(int dtype, int64_t rows, int64_t n_in, int64_t words, const alpa_mat_t &xm, const alpa_mat_t &wm)
     {
-        const int64_t es = element(dtype), r = std::max<int64_t>(rows, 1);
+        const int64_t es = element(dtype), r = std::max<int64_t>(rows, 1), row_tiles = (r + BIG_TILE - 1) / BIG_TILE;
         const int64_t most = std::min<int64_t>(std::max<int64_t>((256ll << 20) / (r * es) / BIG_TILE * BIG_TILE, 4 * BIG_TILE),
                                                MAX_STRIDE / es);
+        int64_t even = BIG_TILE;
+        while (even * 2 <= most && even / BIG_TILE * row_tiles % 256 != 0) even *= 2;
         pieces = (words + most - 1) / most;
-        piece = round_up((words + pieces - 1) / pieces, BIG_TILE);
+        piece = std::min(round_up((words + pieces - 1) / pieces, even), most);
         pieces = (words + piece - 1) / piece;
+        piece = std::min(piece, round_up(words, BIG_TILE));
         coef = 0;
         scale = coef + block(r * 4);
-        grad = scale + 256;
+        x = scale + 256;
+        w = x + pack_bytes(xm, rows, n_in, dtype);
+        // (of the weights, a piece at a time; those behind the first piece lie as that does or not, so there may be room for nothing)
+        grad = w + piece_bytes(wm, rows, n_in, dtype);
         sum = grad + block(r * piece * es);
         split = sum + (pieces > 1 ? block(r * n_in * 4) : 0);
         const int64_t last = words - (pieces - 1) * piece;
         total = split + std::max(std::max(split_bytes(Shape{rows, n_in, last, GROUP_NONE, 0}, dtype),
                                           split_bytes(Shape{last, n_in, rows, GROUP_NONE, 0}, dtype)),
-                                 split_bytes(Shape{piece, n_in, rows, GROUP_NONE, 0}, dtype));
+                                 std::max(split_bytes(Shape{rows, n_in, piece, GROUP_NONE, 0}, dtype),
+                                          split_bytes(Shape{piece, n_in, rows, GROUP_NONE, 0}, dtype)));
+    }
+    int64_t piece_bytes(const alpa_mat_t &wm, int64_t rows, int64_t n_in, int dtype) const
+    {
+        return rows ? pack_bytes(wm, piece, n_in, dtype) : 0;
+    }
+};
+
+// Forward: statistics of stripes, logits of the targets, copies of operands.
+struct EvalWork {
+    int64_t stat, at_target, x, w, total;
+    EvalWork(int dtype, int64_t rows, int64_t n_in, int64_t words, const alpa_mat_t &xm, const alpa_mat_t &wm)
+    {
+        stat = 0;
+        at_target = stat + block(stripes_of(words) * rows * 8);
+        x = at_target + block(rows * 4);
+        w = x + pack_bytes(xm, rows, n_in, dtype);
+        total = w + (rows ? pack_bytes(wm, words, n_in, dtype) : 0);
     }
 };
 
@@ -320,22 +388,23 @@ struct LossWork {
 
 extern "C" {
 
-int64_t alpa_linear_forward_work(int dtype, int64_t rows, int64_t n_in, int64_t n_out)
+int64_t alpa_linear_forward_work(int dtype, int64_t rows, int64_t n_in, int64_t n_out, alpa_mat_t x, alpa_mat_t w)
 {
     if (!type_ok(dtype) || !sizes_ok(rows, n_in, n_out, ALPA_LAYER_MAX_WIDTH)) return 0;
-    return forward_work(dtype, rows, -1, n_in, n_out);
+    return ForwardWork(dtype, rows, -1, n_in, n_out, x, w).total;
 }
 
 int alpa_linear_forward(int dtype, int act, int64_t rows, int64_t n_in, int64_t n_out, alpa_mat_t x, alpa_mat_t w, const void *bias,
                         alpa_mat_t residual, alpa_mat_t y, alpa_mat_t z, void *work, int64_t work_bytes, void *hip_stream)
 {
-    return forward(dtype, act, rows, -1, n_in, n_out, nullptr, x, w, bias, residual, y, z, work, work_bytes, (hipStream_t)hip_stream);
+    return forward(dtype, act, rows, -1, n_in, n_out, nullptr, x, w, bias, residual, y, z, (char *)work, work_bytes,
+                   (hipStream_t)hip_stream);
 }
 
-int64_t alpa_linear_backward_work(int dtype, int act, int64_t rows, int64_t n_in, int64_t n_out)
+int64_t alpa_linear_backward_work(int dtype, int act, int64_t rows, int64_t n_in, int64_t n_out, alpa_mat_t dy, alpa_mat_t x, alpa_mat_t w)
 {
     if (!type_ok(dtype) || !sizes_ok(rows, n_in, n_out, ALPA_LAYER_MAX_WIDTH)) return 0;
-    return BackwardWork(dtype, act, rows, -1, n_in, n_out).total;
+    return BackwardWork(dtype, act, rows, -1, n_in, n_out, dy, x, w).total;
 }
 
 int alpa_linear_backward(int dtype, int act, int64_t rows, int64_t n_in, int64_t n_out, alpa_mat_t dy, alpa_mat_t z, alpa_mat_t x,
@@ -345,10 +414,10 @@ int alpa_linear_backward(int dtype, int act, int64_t rows, int64_t n_in, int64_t
                     (hipStream_t)hip_stream);
 }
 
-int64_t alpa_experts_forward_work(int dtype, int64_t rows, int experts, int64_t n_in, int64_t n_out)
+int64_t alpa_experts_forward_work(int dtype, int64_t rows, int experts, int64_t n_in, int64_t n_out, alpa_mat_t x, alpa_mat_t w)
 {
-    if (!type_ok(dtype) || !sizes_ok(rows, n_in, n_out, ALPA_LAYER_MAX_WIDTH) || experts < 1) return 0;
-    return forward_work(dtype, rows, experts, n_in, n_out);
+    if (!type_ok(dtype) || !sizes_ok(rows, n_in, n_out, ALPA_LAYER_MAX_WIDTH) || experts < 1 || experts > ALPA_LAYER_MAX_EXPERTS) return 0;
+    return ForwardWork(dtype, rows, experts, n_in, n_out, x, w).total;
 }
 
 int alpa_experts_forward(int dtype, int act, int64_t rows, int experts, int64_t n_in, int64_t n_out, const int32_t *offsets, alpa_mat_t x,
@@ -356,13 +425,15 @@ int alpa_experts_forward(int dtype, int act, int64_t rows, int experts, int64_t 
                          void *hip_stream)
 {
     TRY(check_experts(experts, offsets));
-    return forward(dtype, act, rows, experts, n_in, n_out, offsets, x, w, bias, residual, y, z, work, work_bytes, (hipStream_t)hip_stream);
+    return forward(dtype, act, rows, experts, n_in, n_out, offsets, x, w, bias, residual, y, z, (char *)work, work_bytes,
+                   (hipStream_t)hip_stream);
 }
 
-int64_t alpa_experts_backward_work(int dtype, int act, int64_t rows, int experts, int64_t n_in, int64_t n_out)
+int64_t alpa_experts_backward_work(int dtype, int act, int64_t rows, int experts, int64_t n_in, int64_t n_out, alpa_mat_t dy, alpa_mat_t x,
+                                   alpa_mat_t w)
 {
     if (!type_ok(dtype) || !sizes_ok(rows, n_in, n_out, ALPA_LAYER_MAX_WIDTH) || experts < 1 || experts > ALPA_LAYER_MAX_EXPERTS) return 0;
-    return BackwardWork(dtype, act, rows, experts, n_in, n_out).total;
+    return BackwardWork(dtype, act, rows, experts, n_in, n_out, dy, x, w).total;
 }
 
 int alpa_experts_backward(int dtype, int act, int64_t rows, int experts, int64_t n_in, int64_t n_out, const int32_t *offsets,
@@ -374,10 +445,10 @@ int alpa_experts_backward(int dtype, int act, int64_t rows, int experts, int64_t
                     (hipStream_t)hip_stream);
 }
 
-int64_t alpa_vocab_loss_forward_work(int dtype, int64_t rows, int64_t n_in, int64_t words)
+int64_t alpa_vocab_loss_forward_work(int dtype, int64_t rows, int64_t n_in, int64_t words, alpa_mat_t x, alpa_mat_t w)
 {
     if (!type_ok(dtype) || !sizes_ok(rows, n_in, words, ALPA_LAYER_MAX_WORDS)) return 0;
-    return block(stripes_of(words) * rows * 8) + block(rows * 4);
+    return EvalWork(dtype, rows, n_in, words, x, w).total;
 }
 
 int alpa_vocab_loss_forward(int dtype, int64_t rows, int64_t n_in, int64_t words, alpa_mat_t x, alpa_mat_t w, const int64_t *target,
@@ -391,22 +462,26 @@ int alpa_vocab_loss_forward(int dtype, int64_t rows, int64_t n_in, int64_t words
     TRY(check_vector(target, 8));
     TRY(check_vector(loss, 4));
     TRY(check_vector(lse, 4));
-    TRY(check_work(work, work_bytes, alpa_vocab_loss_forward_work(dtype, rows, n_in, words)));
+    const EvalWork at(dtype, rows, n_in, words, x, w);
+    TRY(check_work(work, work_bytes, at.total));
     const hipStream_t st = (hipStream_t)hip_stream;
-    ProductArgs g = operands(x, w, dtype);
+    char *base = (char *)work;
+    Source xs, ws;
+    TRY(pack(st, x, rows, n_in, dtype, base + at.x, xs));
+    TRY(pack(st, w, words, n_in, dtype, base + at.w, ws));
+    ProductArgs g = operands(FORM_RR, xs, ws, n_in, dtype);
     g.target = target;
-    g.words = words;
-    g.stat = (float2 *)work;
-    g.at_target = (float *)((char *)work + block(stripes_of(words) * rows * 8));
+    g.stat = (float2 *)(base + at.stat);
+    g.at_target = (float *)(base + at.at_target);
     TRY(run_product(st, dtype, FORM_RR, EPI_LOSS, Shape{rows, words, n_in, GROUP_NONE, 0}, g, nullptr));
     HIPCHK(launch_loss(st, g.stat, (int)stripes_of(words), (int)rows, g.at_target, target, words, loss, lse));
     return ALPA_DP_OK;
 }
 
-int64_t alpa_vocab_loss_backward_work(int dtype, int64_t rows, int64_t n_in, int64_t words)
+int64_t alpa_vocab_loss_backward_work(int dtype, int64_t rows, int64_t n_in, int64_t words, alpa_mat_t x, alpa_mat_t w)
 {
     if (!type_ok(dtype) || !sizes_ok(rows, n_in, words, ALPA_LAYER_MAX_WORDS)) return 0;
-    return LossWork(dtype, rows, n_in, words).total;
+    return LossWork(dtype, rows, n_in, words, x, w).total;
 }
 
 int alpa_vocab_loss_backward(int dtype, int64_t rows, int64_t n_in, int64_t words, const float *dloss, alpa_mat_t x, alpa_mat_t w,
@@ -422,7 +497,7 @@ int alpa_vocab_loss_backward(int dtype, int64_t rows, int64_t n_in, int64_t word
     TRY(check_vector(target, 8));
     TRY(check_vector(dloss, 4));
     TRY(check_vector(lse, 4));
-    const LossWork at(dtype, rows, n_in, words);
+    const LossWork at(dtype, rows, n_in, words, x, w);
     TRY(check_work(work, work_bytes, at.total));
     if (!dx.p && !dw.p) return ALPA_DP_OK;
     const hipStream_t st = (hipStream_t)hip_stream;
@@ -430,12 +505,16 @@ int alpa_vocab_loss_backward(int dtype, int64_t rows, int64_t n_in, int64_t word
     float *coef = (float *)(base + at.coef), *scale = (float *)(base + at.scale);
     HIPCHK(launch_coef(st, dloss, target, words, (int)rows, coef, scale));
     const int64_t es = element(dtype);
+    Source xs{}, ws{};
+    TRY(pack(st, x, rows, n_in, dtype, base + at.x, xs));
     for (int64_t p = 0; p < at.pieces; ++p) {
         const int64_t word0 = p * at.piece, n = std::min(at.piece, words - word0);
-        const alpa_mat_t w_here{w.p ? (char *)w.p + word0 * w.ld * es : nullptr, w.ld}, grad{base + at.grad, at.piece};
+        const Source grad{base + at.grad, at.piece, round_up(n, 16 / es)};
         if (rows > 0) {
-            ProductArgs g = operands(x, w_here, dtype);
-            result(g, grad);
+            // (pieces are multiples of 256 words, so a piece's rows are aligned as the first piece's are)
+            TRY(pack(st, alpa_mat_t{(char *)w.p + word0 * w.ld * es, w.ld}, n, n_in, dtype, base + at.w, ws));
+            ProductArgs g = operands(FORM_RR, xs, ws, n_in, dtype);
+            result(g, alpa_mat_t{base + at.grad, at.piece});
             g.target = target;
             g.word0 = word0;
             g.lse = lse;
@@ -443,9 +522,8 @@ int alpa_vocab_loss_backward(int dtype, int64_t rows, int64_t n_in, int64_t word
             TRY(run_product(st, dtype, FORM_RR, EPI_GRAD, Shape{rows, n, n_in, GROUP_NONE, 0}, g, nullptr));
         }
         if (dx.p && rows > 0) {
-            ProductArgs g = operands(grad, w_here, dtype);
+            ProductArgs g = operands(FORM_RC, grad, ws, n, dtype);
             result(g, dx);
-            g.low = -INFINITY;
             g.scale = scale;
             g.sum = (float *)(base + at.sum);
             g.first = p == 0;
@@ -454,9 +532,8 @@ int alpa_vocab_loss_backward(int dtype, int64_t rows, int64_t n_in, int64_t word
                             base + at.split));
         }
         if (dw.p) {
-            ProductArgs g = operands(grad, x, dtype);
+            ProductArgs g = operands(FORM_CC, grad, xs, rows, dtype);
             result(g, alpa_mat_t{(char *)dw.p + word0 * dw.ld * es, dw.ld});
-            g.low = -INFINITY;
             g.scale = scale;
             TRY(run_product(st, dtype, FORM_CC, EPI_LINE, Shape{n, n_in, rows, GROUP_NONE, 0}, g, base + at.split));
         }
@@ -468,11 +545,11 @@ int alpa_vocab_loss_backward(int dtype, int64_t rows, int64_t n_in, int64_t word
 
 namespace alpa {
 
-hipError_t launch_product(hipStream_t st, int dtype, Forms forms, Epilogue epi, int tile, bool direct, const ProductArgs &g)
+hipError_t launch_product(hipStream_t st, int dtype, Forms forms, Epilogue epi, int tile, const ProductArgs &g)
 {
-    return dtype == ALPA_F32   ? launch_product_f32(st, forms, epi, tile, direct, g)
-           : dtype == ALPA_F16 ? launch_product_f16(st, forms, epi, tile, direct, g)
-                               : launch_product_bf16(st, forms, epi, tile, direct, g);
+    return dtype == ALPA_F32   ? launch_product_f32(st, forms, epi, tile, g)
+           : dtype == ALPA_F16 ? launch_product_f16(st, forms, epi, tile, g)
+                               : launch_product_bf16(st, forms, epi, tile, g);
 }
 
 }  // namespace alpa

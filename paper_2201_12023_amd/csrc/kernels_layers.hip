@@ -5,6 +5,34 @@
 
 namespace alpa {
 
+// ---------------------------------------------------------------- rows in 16-byte units
+
+// A thread writes sixteen bytes; reads of one row are consecutive, so the lines they share come from the cache.
+template <class T>
+__global__ __launch_bounds__(256) void pack_kernel(const T *from, int64_t ld, int64_t rows, int len, T *to, int to_len)
+{
+    constexpr int V = 16 / sizeof(T);
+    const int per_row = to_len / V;
+    const int64_t total = rows * per_row;
+    for (int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x; c < total; c += (int64_t)gridDim.x * 256) {
+        const int64_t r = c / per_row;
+        const int n = (int)(c - r * per_row) * V;
+        float v[V];
+        load_row<T>((const char *)from, r * ld + n, len - n, 0, v);
+        store_row<T>((char *)to, r * to_len + n, V, 1, v);
+    }
+}
+
+hipError_t launch_pack(hipStream_t st, int dtype, const char *from, int64_t ld, int64_t rows, int len, char *to, int to_len)
+{
+    const int64_t chunks = rows * to_len * (dtype == 0 ? 4 : 2) / 16;
+    const unsigned blocks = (unsigned)std::min<int64_t>((chunks + 255) / 256, 8192);
+    if (dtype == 0) pack_kernel<float><<<blocks, 256, 0, st>>>((const float *)from, ld, rows, len, (float *)to, to_len);
+    else if (dtype == 1) pack_kernel<f16><<<blocks, 256, 0, st>>>((const f16 *)from, ld, rows, len, (f16 *)to, to_len);
+    else pack_kernel<bf16><<<blocks, 256, 0, st>>>((const bf16 *)from, ld, rows, len, (bf16 *)to, to_len);
+    return hipGetLastError();
+}
+
 // ---------------------------------------------------------------- dz = dy * act'(z), sums of its columns
 
 // act'(z); at infinities the limits
@@ -42,7 +70,7 @@ __global__ __launch_bounds__(256) void slope_kernel(const SlopeArgs g)
     float sum[V];
 #pragma unroll
     for (int j = 0; j < V; ++j) sum[j] = 0.0f;
-    if (!skip && cnt > 0) {
+    if (!skip && n < (g.dz ? (int)g.ldd : g.N)) {
 #pragma unroll 4
         for (int m = first + wave; m < end; m += 4) {
             float d[V];
@@ -52,7 +80,7 @@ __global__ __launch_bounds__(256) void slope_kernel(const SlopeArgs g)
                 load_row<T>(g.z, (int64_t)m * g.ldz + n, cnt, g.wide, z);
 #pragma unroll
                 for (int j = 0; j < V; ++j) d[j] *= slope_of<T>(z[j], g.act);
-                if (g.dz) store_row<T>(g.dz, (int64_t)m * g.ldd + n, cnt, g.wide, d);
+                if (g.dz) store_row<T>(g.dz, (int64_t)m * g.ldd + n, V, 1, d);       // (behind N: zeros)
             }
 #pragma unroll
             for (int j = 0; j < V; ++j) sum[j] += d[j];
@@ -74,8 +102,8 @@ template <class T>
 hipError_t slope_typed(hipStream_t st, const SlopeArgs &g)
 {
     constexpr int V = 16 / sizeof(T);
-    const int per = 64 * (g.wide ? V : 1);
-    const dim3 grid((unsigned)g.slots, (unsigned)((g.N + per - 1) / per));
+    const int per = 64 * (g.wide ? V : 1), columns = g.dz ? (int)g.ldd : g.N;
+    const dim3 grid((unsigned)g.slots, (unsigned)((columns + per - 1) / per));
     if (g.wide) {
         if (g.act) slope_kernel<T, V, true><<<grid, 256, 0, st>>>(g);
         else slope_kernel<T, V, false><<<grid, 256, 0, st>>>(g);
@@ -107,8 +135,10 @@ __global__ __launch_bounds__(256) void bias_sum_kernel(const float *part, T *dbi
     }
     const int n = blockIdx.x * 64 + lane, quarter = (count + 3) / 4;
     float sum = 0.0f;
-    if (n < N)
+    if (n < N) {
+#pragma unroll 8
         for (int s = wave * quarter; s < min((wave + 1) * quarter, count); ++s) sum += part[(int64_t)(first + s) * N + n];
+    }
     sums[wave][lane] = sum;
     __syncthreads();
     if (wave == 0 && n < N) dbias[(int64_t)e * N + n] = (T)((sums[0][lane] + sums[1][lane]) + (sums[2][lane] + sums[3][lane]));
@@ -177,19 +207,27 @@ __device__ __forceinline__ float2 join_stat(float2 a, float2 b)
     return make_float2(top, a.y * expf(a.x - ref) + b.y * expf(b.x - ref));
 }
 
-// Sixteen rows a workgroup; sixteen threads a row take every sixteenth stripe, in order, and are joined in order.
-__global__ __launch_bounds__(256) void loss_kernel(const float2 *stat, int stripes, int rows, const float *at_target,
-                                                   const int64_t *target, int64_t words, float *loss, float *lse)
+// Sixteen rows a workgroup; sixty-four threads a row take every sixty-fourth stripe, in order, and are joined in order by eights.
+__global__ __launch_bounds__(1024) void loss_kernel(const float2 *stat, int stripes, int rows, const float *at_target,
+                                                    const int64_t *target, int64_t words, float *loss, float *lse)
 {
-    __shared__ float2 share[16][17];
+    __shared__ float2 share[64][17], eights[8][17];
     const int r = threadIdx.x & 15, part = threadIdx.x >> 4, m = blockIdx.x * 16 + r;
     float2 s = make_float2(-INFINITY, 0.0f);
-    if (m < rows)
-        for (int j = part; j < stripes; j += 16) s = join_stat(s, stat[(int64_t)j * rows + m]);
+    if (m < rows) {
+#pragma unroll 4
+        for (int j = part; j < stripes; j += 64) s = join_stat(s, stat[(int64_t)j * rows + m]);
+    }
     share[part][r] = s;
     __syncthreads();
+    if (part < 8) {
+        s = share[part * 8][r];
+        for (int j = 1; j < 8; ++j) s = join_stat(s, share[part * 8 + j][r]);
+        eights[part][r] = s;
+    }
+    __syncthreads();
     if (part != 0 || m >= rows) return;
-    for (int j = 1; j < 16; ++j) s = join_stat(s, share[j][r]);
+    for (int j = 1; j < 8; ++j) s = join_stat(s, eights[j][r]);
     const float l = s.x + logf(s.y);
     const int64_t word = target[m];
     lse[m] = l;
@@ -199,7 +237,7 @@ __global__ __launch_bounds__(256) void loss_kernel(const float2 *stat, int strip
 hipError_t launch_loss(hipStream_t st, const float2 *stat, int stripes, int rows, const float *at_target, const int64_t *target,
                        int64_t words, float *loss, float *lse)
 {
-    loss_kernel<<<(unsigned)((rows + 15) / 16), 256, 0, st>>>(stat, stripes, rows, at_target, target, words, loss, lse);
+    loss_kernel<<<(unsigned)((rows + 15) / 16), 1024, 0, st>>>(stat, stripes, rows, at_target, target, words, loss, lse);
     return hipGetLastError();
 }
 

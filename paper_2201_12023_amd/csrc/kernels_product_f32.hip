@@ -3,9 +3,9 @@
 
 namespace alpa {
 
-hipError_t launch_product_f32(hipStream_t st, Forms forms, Epilogue epi, int tile, bool direct, const ProductArgs &g)
+hipError_t launch_product_f32(hipStream_t st, Forms forms, Epilogue epi, int tile, const ProductArgs &g)
 {
-    return launch_forms<float>(st, forms, epi, tile, direct, g);
+    return launch_forms<float>(st, forms, epi, tile, g);
 }
 
 }  // namespace alpa

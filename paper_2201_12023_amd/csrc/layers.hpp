@@ -21,6 +21,7 @@ struct ProductArgs {
     const char *a, *b;              // operands; strides in bytes
     int64_t lda, ldb;
     int M, N, K;                    // result rows (all groups together), columns, contraction (all groups together)
+    int a_k, b_k, a_len, b_len;     // extents of the contraction, and of rows where those are contiguous, with their padding to 16 bytes
     int grouping, experts;
     const int32_t *offsets;
     int64_t b_expert;               // GROUP_ROWS: bytes from an expert's b to the next one's; GROUP_STEPS: result elements
@@ -39,8 +40,7 @@ struct ProductArgs {
     int first, last;
     const float *scale;             // EPI_SUM, EPI_LINE: result times *scale (NULL: 1)
     const int64_t *target;          // EPI_LOSS, EPI_GRAD
-    int64_t words;                  // columns of the whole vocabulary; this product's are word0 ..
-    int64_t word0;
+    int64_t word0;                  // EPI_GRAD: the first column's word
     float2 *stat;                   // EPI_LOSS: [stripe][M]
     float *at_target;
     const float *lse, *coef;        // EPI_GRAD: [M]
@@ -53,18 +53,21 @@ constexpr int STRIPE = 64;                        // columns of a stripe of EPI_
 // Form of the two operands: both with their contraction contiguous (x wT), the second one's rows contiguous (dz w), or both (dzT x).
 enum Forms : int { FORM_RR, FORM_RC, FORM_CC };
 
-// tile: TILE or BIG_TILE; direct: operands allow 16-byte accesses throughout (BIG_TILE needs it)
-hipError_t launch_product(hipStream_t st, int dtype, Forms forms, Epilogue epi, int tile, bool direct, const ProductArgs &a);
-hipError_t launch_product_f32(hipStream_t, Forms, Epilogue, int, bool, const ProductArgs &);
-hipError_t launch_product_f16(hipStream_t, Forms, Epilogue, int, bool, const ProductArgs &);
-hipError_t launch_product_bf16(hipStream_t, Forms, Epilogue, int, bool, const ProductArgs &);
+// tile: TILE or BIG_TILE.  Addresses, strides and contiguous extents of the operands are multiples of 16 bytes.
+hipError_t launch_product(hipStream_t st, int dtype, Forms forms, Epilogue epi, int tile, const ProductArgs &a);
+hipError_t launch_product_f32(hipStream_t, Forms, Epilogue, int, const ProductArgs &);
+hipError_t launch_product_f16(hipStream_t, Forms, Epilogue, int, const ProductArgs &);
+hipError_t launch_product_bf16(hipStream_t, Forms, Epilogue, int, const ProductArgs &);
+
+// Copies [rows][len] to rows of `to_len` elements (a multiple of 16 bytes), zeros behind len: what an operand needs that is not aligned to 16 bytes.
+hipError_t launch_pack(hipStream_t st, int dtype, const char *from, int64_t ld, int64_t rows, int len, char *to, int to_len);
 
 // dz = dy * act'(z), and sums of dz over the rows of each slot of SLOPE_ROWS rows
 constexpr int SLOPE_ROWS = 64;
 struct SlopeArgs {
     const char *dy, *z;             // strides in elements
     int64_t lddy, ldz;
-    char *dz;                       // [rows][ldd], or NULL
+    char *dz;                       // [rows][ldd], zeros behind N, or NULL
     int64_t ldd;
     float *part;                    // [slots][N], or NULL
     int rows, N, slots, experts;    // experts 0: no groups

@@ -47,6 +47,7 @@ struct Operand {
     const char *p;          // bytes
     int64_t ld;             // bytes between rows (ROWS) or between steps of the contraction (COLS)
     int rows;               // rows of this tile that exist
+    int k;                  // extent of the contraction; a multiple of 16 bytes if it is the contiguous one, as is `rows` otherwise
 };
 
 constexpr uint32_t OUT_OF_RANGE = 0x80000000u;       // a buffer offset beyond every range used here: such loads give zero
@@ -112,23 +113,6 @@ struct Tile {
     }
 };
 
-// Sixteen bytes from an address of any alignment, of which the first `n` elements exist.
-template <class T>
-__device__ __forceinline__ u32x4 load_some(const char *p, int n)
-{
-    constexpr int V = 16 / sizeof(T);
-    u32x4 r = {0, 0, 0, 0};
-    if (n >= V) {
-        __builtin_memcpy(&r, p, 16);
-    } else if (n > 0) {
-        T e[V];
-#pragma unroll
-        for (int j = 0; j < V; ++j) e[j] = j < n ? ((const T *)p)[j] : (T)0.0f;
-        __builtin_memcpy(&r, e, 16);
-    }
-    return r;
-}
-
 // Brings an operand's tiles to LDS with the load unit writing there itself.  Addresses, strides and the contiguous extent are multiples of 16
 // bytes, so every chunk exists or does not; those that do not are out of the buffer's range and arrive as zeros.  The loads are written as
 // assembly without a result register because the compiler, for the load's builtin, waits for all loads before the next transposing LDS
@@ -147,12 +131,12 @@ struct DirectLoader {
     uint32_t first[KINDS], off[KINDS], apart;      // this thread's first chunks, as they are in this step, and how far chunks are apart
     u32x4 range;
 
-    __device__ __forceinline__ void init(const Operand &o, int k, int tid)
+    __device__ __forceinline__ void init(const Operand &o, int tid)
     {
         p = o.p;
         rows = o.rows;
         ld = (int)o.ld;
-        left = k;
+        left = o.k;
         advance = FORM == ROWS ? BK * ES : BK * o.ld;
 #pragma unroll
         for (int j = 0; j < KINDS; ++j) {
@@ -189,35 +173,6 @@ struct DirectLoader {
     }
 };
 
-// The same through registers, from any address, element by element at the edges.
-template <class T, int FORM, int R, int NT>
-struct AnyLoader {
-    using TL = Tile<T, FORM, R, NT>;
-    static constexpr int N = TL::CHUNKS, ES = TL::ES, BK = TL::BK;
-    Operand o;
-    int K;
-    u32x4 held[N];
-
-    __device__ __forceinline__ void fetch(int kt, int tid)
-    {
-        const int k0 = kt * BK, left = K - k0;
-        const char *base = o.p + (FORM == ROWS ? (int64_t)k0 * ES : (int64_t)k0 * o.ld);
-#pragma unroll
-        for (int j = 0; j < N; ++j) {
-            int major, chunk;
-            TL::place(j * NT + tid, major, chunk);
-            int n = FORM == ROWS ? left - chunk * (16 / ES) : o.rows - chunk * (16 / ES);
-            if (FORM == ROWS ? major >= o.rows : major >= left) n = 0;
-            held[j] = load_some<T>(base + (int64_t)major * o.ld + chunk * 16, n);
-        }
-    }
-    __device__ __forceinline__ void store(uint32_t lds, int tid) const
-    {
-#pragma unroll
-        for (int j = 0; j < N; ++j) *(ALPA_LDS u32x4 *)(uintptr_t)(lds + (j * NT + tid) * 16) = held[j];
-    }
-};
-
 // All but the last N loads to LDS of this wave have arrived, its LDS reads are done, and every wave is here.
 template <int N>
 __device__ __forceinline__ void arrived()
@@ -229,13 +184,13 @@ __device__ __forceinline__ void arrived()
 
 // A workgroup of WM x WN waves computes the BM x BN tile.  The product's first operand is B, so that a lane's four results of a
 // 16 x 16 block are consecutive columns n of one row m: acc[mt][nt][r] is row row_of(i, mt), column (of block nt) 4 q + r.
-template <class T, int FA, int FB, int BM, int BN, int WM, int WN, bool DIRECT>
+template <class T, int FA, int FB, int BM, int BN, int WM, int WN>
 struct Product {
     static constexpr int NT = WM * WN * 64, MT = BM / WM / 16, NTL = BN / WN / 16, ES = sizeof(T);
     using TA = Tile<T, FA, BM, NT>;
     using TB = Tile<T, FB, BN, NT>;
     // The large tile: three stages of A and two of B, all the LDS there is.  The small one: two of each, two workgroups in a compute unit.
-    static constexpr bool DEEP = DIRECT && BM == 256;
+    static constexpr bool DEEP = BM == 256;
     static constexpr int A_STAGES = DEEP ? 3 : 2, LDS_BYTES = A_STAGES * TA::BYTES + 2 * TB::BYTES;
     using Acc = f32x4[MT][NTL];
     struct Fragments { u32x4 a[MT], b[NTL]; };
@@ -251,17 +206,16 @@ struct Product {
     // a wave's place: its rows and columns in the tile, where its lanes read
     struct Wave { int id; uint32_t a_at, b_at; };
 
-    static __device__ __forceinline__ void run(const Operand &A, const Operand &B, int K, char *lds_memory, Acc &acc)
+    static __device__ __forceinline__ void run(const Operand &A, const Operand &B, char *lds_memory, Acc &acc)
     {
         clear(acc);
-        const int steps = (K + TA::BK - 1) / TA::BK;
+        const int steps = (max(A.k, B.k) + TA::BK - 1) / TA::BK;
         if (steps == 0) return;
         const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
         const Wave w{wave, TA::lane_at(wave / WN * (BM / WM), lane & 15, lane >> 4), TB::lane_at(wave % WN * (BN / WN), lane & 15, lane >> 4)};
         const uint32_t lds = (uint32_t)(uintptr_t)(ALPA_LDS char *)lds_memory;
-        if constexpr (DEEP) run_deep(A, B, K, steps, lds, acc, w);
-        else if constexpr (DIRECT) run_direct(A, B, K, steps, lds, acc, w);
-        else run_any(A, B, K, steps, lds, acc, w);
+        if constexpr (DEEP) run_deep(A, B, steps, lds, acc, w);
+        else run_shallow(A, B, steps, lds, acc, w);
     }
 
 private:
@@ -279,13 +233,12 @@ private:
     }
 
     // The next step's loads are under way while this one is multiplied; the other workgroup of the compute unit fills what is left.
-    static __device__ __forceinline__ void run_direct(const Operand &A, const Operand &B, int K, int steps, uint32_t lds, Acc &acc,
-                                                      const Wave &w)
+    static __device__ __forceinline__ void run_shallow(const Operand &A, const Operand &B, int steps, uint32_t lds, Acc &acc, const Wave &w)
     {
         DirectLoader<T, FA, BM, NT> la;
         DirectLoader<T, FB, BN, NT> lb;
-        la.init(A, K, threadIdx.x);
-        lb.init(B, K, threadIdx.x);
+        la.init(A, threadIdx.x);
+        lb.init(B, threadIdx.x);
         uint32_t here = lds, next = lds + TA::BYTES + TB::BYTES;
         auto fetch = [&](uint32_t to) {
             la.step();
@@ -308,47 +261,19 @@ private:
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // (the loads of nothing behind the last step)
     }
 
-    static __device__ __forceinline__ void run_any(const Operand &A, const Operand &B, int K, int steps, uint32_t lds, Acc &acc, const Wave &w)
-    {
-        AnyLoader<T, FA, BM, NT> la{A, K};
-        AnyLoader<T, FB, BN, NT> lb{B, K};
-        uint32_t here = lds, next = lds + TA::BYTES + TB::BYTES;
-        la.fetch(0, threadIdx.x);
-        lb.fetch(0, threadIdx.x);
-        la.store(here, threadIdx.x);
-        lb.store(here + TA::BYTES, threadIdx.x);
-        for (int kt = 0; kt < steps; ++kt) {
-            arrived<0>();
-            if (kt + 1 < steps) {
-                la.fetch(kt + 1, threadIdx.x);
-                lb.fetch(kt + 1, threadIdx.x);
-            }
-            half_step(here + w.a_at, here + TA::BYTES + w.b_at, 0, acc);
-            half_step(here + w.a_at, here + TA::BYTES + w.b_at, 1, acc);
-            if (kt + 1 < steps) {
-                la.store(next, threadIdx.x);
-                lb.store(next + TA::BYTES, threadIdx.x);
-            }
-            const uint32_t t = here;
-            here = next;
-            next = t;
-        }
-    }
-
     // A step is sixteen groups of four products, eight for each half of its contraction; a group also issues a share of the LDS reads of the
     // next half and every second one a load, so that matrix unit, LDS and load unit have work all the time (eight loads together take the load
     // unit as long as half a step's products).  A's and B's stages of step kt are read by group 3 (barrier) and then hold loads of
     // A's step kt + 3 and B's step kt + 2, which gives A nearly two steps to arrive and B one; the last six loads may be under way when step
     // kt + 1 is looked at (group 8).  At 8192 x 4096 x 16384 in 16 bits a step takes 2490 to 2650 cycles of the 2048 its products need, against
     // 2810 with loads one step ahead, and the clock that the power limit leaves is 1.65 GHz.
-    static __device__ __forceinline__ void run_deep(const Operand &A, const Operand &B, int K, int steps, uint32_t lds, Acc &acc,
-                                                    const Wave &w)
+    static __device__ __forceinline__ void run_deep(const Operand &A, const Operand &B, int steps, uint32_t lds, Acc &acc, const Wave &w)
     {
         DirectLoader<T, FA, BM, NT> la;
         DirectLoader<T, FB, BN, NT> lb;
         static_assert(la.N == 4 && lb.N == 4 && MT == 8 && NTL == 4, "loads and reads are dealt to groups for these");
-        la.init(A, K, threadIdx.x);
-        lb.init(B, K, threadIdx.x);
+        la.init(A, threadIdx.x);
+        lb.init(B, threadIdx.x);
         uint32_t a0 = lds, a1 = lds + TA::BYTES, a2 = lds + 2 * TA::BYTES, b0 = lds + 3 * TA::BYTES, b1 = b0 + TB::BYTES;
         la.step();
         lb.step();

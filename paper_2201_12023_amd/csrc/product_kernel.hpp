@@ -103,8 +103,8 @@ __device__ __forceinline__ void through_lds(const ProductArgs &g, const typename
                 const int64_t word = g.target[m] - g.word0;
 #pragma unroll
                 for (int j = 0; j < CW; ++j)
-                    v[j] = coef == 0.0f ? 0.0f : (exp_for<T>(v[j] - lse) - (word == n + j ? 1.0f : 0.0f)) * coef;
-                store_row<T>(g.out, (int64_t)m * g.ldo + n, cnt, g.wide, v);
+                    v[j] = coef == 0.0f || j >= cnt ? 0.0f : (exp_for<T>(v[j] - lse) - (word == n + j ? 1.0f : 0.0f)) * coef;
+                store_row<T>(g.out, (int64_t)m * g.ldo + n, CW, 1, v);         // (work memory, with zeros up to the next 16 bytes)
             } else if constexpr (EPI == EPI_SUM) {
                 char *sum = (char *)g.sum;
                 const int64_t at = ((int64_t)blockIdx.y * g.M + m) * g.N + n;
@@ -134,10 +134,10 @@ __device__ __forceinline__ void through_lds(const ProductArgs &g, const typename
     }
 }
 
-template <class T, int FA, int FB, int BM, int BN, int WM, int WN, bool DIRECT, int EPI>
+template <class T, int FA, int FB, int BM, int BN, int WM, int WN, int EPI>
 __global__ __launch_bounds__(WM *WN * 64, 2) void product_kernel(const ProductArgs g)
 {
-    using P = Product<T, FA, FB, BM, BN, WM, WN, DIRECT>;
+    using P = Product<T, FA, FB, BM, BN, WM, WN>;
     __shared__ __align__(1024) char lds[P::LDS_BYTES];
     constexpr int ES = sizeof(T), BK = STEP_BYTES / ES;
 
@@ -173,12 +173,13 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void product_kernel(const ProductAr
         k_end = min(k0 + g.split_steps * BK, g.K);
     }
     const int n0 = tn * BN;
-    const Operand A{g.a + (FA == ROWS ? (int64_t)m0 * g.lda + (int64_t)k0 * ES : (int64_t)k0 * g.lda + (int64_t)m0 * ES), g.lda,
-                    m_end - m0};
-    const Operand B{b + (FB == ROWS ? (int64_t)n0 * g.ldb + (int64_t)k0 * ES : (int64_t)k0 * g.ldb + (int64_t)n0 * ES), g.ldb,
-                    min(BN, g.N - n0)};
+    // (a contiguous contraction is padded with zeros to 16 bytes, the other operand's may end before)
+    const int a_rows = FA == ROWS ? m_end - m0 : min(BM, g.a_len - m0), a_k = min(k_end, g.a_k) - k0;
+    const int b_rows = min(BN, (FB == ROWS ? g.N : g.b_len) - n0), b_k = min(k_end, g.b_k) - k0;
+    const Operand A{g.a + (FA == ROWS ? (int64_t)m0 * g.lda + (int64_t)k0 * ES : (int64_t)k0 * g.lda + (int64_t)m0 * ES), g.lda, a_rows, a_k};
+    const Operand B{b + (FB == ROWS ? (int64_t)n0 * g.ldb + (int64_t)k0 * ES : (int64_t)k0 * g.ldb + (int64_t)n0 * ES), g.ldb, b_rows, b_k};
     typename P::Acc acc;
-    P::run(A, B, k_end - k0, lds, acc);
+    P::run(A, B, lds, acc);
 
     const int lane = threadIdx.x & 63, i = lane & 15, q = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -188,37 +189,33 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void product_kernel(const ProductAr
 }
 
 template <class T, int FA, int FB, int EPI>
-hipError_t launch_tiles(hipStream_t st, int tile, bool direct, const ProductArgs &g)
+hipError_t launch_tiles(hipStream_t st, int tile, const ProductArgs &g)
 {
     const int64_t tiles = (int64_t)g.row_tiles * g.col_tiles * (g.grouping == GROUP_STEPS ? g.experts : 1);
     const dim3 grid((unsigned)tiles, (unsigned)g.splits);
-    if (tile == BIG_TILE)
-        product_kernel<T, FA, FB, 256, 256, 2, 4, true, EPI><<<grid, 512, 0, st>>>(g);
-    else if (direct)
-        product_kernel<T, FA, FB, 128, 128, 2, 2, true, EPI><<<grid, 256, 0, st>>>(g);
-    else
-        product_kernel<T, FA, FB, 128, 128, 2, 2, false, EPI><<<grid, 256, 0, st>>>(g);
+    if (tile == BIG_TILE) product_kernel<T, FA, FB, 256, 256, 2, 4, EPI><<<grid, 512, 0, st>>>(g);
+    else product_kernel<T, FA, FB, 128, 128, 2, 2, EPI><<<grid, 256, 0, st>>>(g);
     return hipGetLastError();
 }
 
 template <class T>
-hipError_t launch_forms(hipStream_t st, Forms forms, Epilogue epi, int tile, bool direct, const ProductArgs &g)
+hipError_t launch_forms(hipStream_t st, Forms forms, Epilogue epi, int tile, const ProductArgs &g)
 {
     if (forms == FORM_RR) {
         switch (epi) {
-        case EPI_LINE: return launch_tiles<T, ROWS, ROWS, EPI_LINE>(st, tile, direct, g);
-        case EPI_SIGMOID: return launch_tiles<T, ROWS, ROWS, EPI_SIGMOID>(st, tile, direct, g);
-        case EPI_ERF: return launch_tiles<T, ROWS, ROWS, EPI_ERF>(st, tile, direct, g);
-        case EPI_SUM: return launch_tiles<T, ROWS, ROWS, EPI_SUM>(st, tile, direct, g);
-        case EPI_LOSS: return launch_tiles<T, ROWS, ROWS, EPI_LOSS>(st, tile, direct, g);
-        case EPI_GRAD: return launch_tiles<T, ROWS, ROWS, EPI_GRAD>(st, tile, direct, g);
+        case EPI_LINE: return launch_tiles<T, ROWS, ROWS, EPI_LINE>(st, tile, g);
+        case EPI_SIGMOID: return launch_tiles<T, ROWS, ROWS, EPI_SIGMOID>(st, tile, g);
+        case EPI_ERF: return launch_tiles<T, ROWS, ROWS, EPI_ERF>(st, tile, g);
+        case EPI_SUM: return launch_tiles<T, ROWS, ROWS, EPI_SUM>(st, tile, g);
+        case EPI_LOSS: return launch_tiles<T, ROWS, ROWS, EPI_LOSS>(st, tile, g);
+        case EPI_GRAD: return launch_tiles<T, ROWS, ROWS, EPI_GRAD>(st, tile, g);
         }
     } else if (forms == FORM_RC) {
-        if (epi == EPI_LINE) return launch_tiles<T, ROWS, COLS, EPI_LINE>(st, tile, direct, g);
-        if (epi == EPI_SUM) return launch_tiles<T, ROWS, COLS, EPI_SUM>(st, tile, direct, g);
+        if (epi == EPI_LINE) return launch_tiles<T, ROWS, COLS, EPI_LINE>(st, tile, g);
+        if (epi == EPI_SUM) return launch_tiles<T, ROWS, COLS, EPI_SUM>(st, tile, g);
     } else {
-        if (epi == EPI_LINE) return launch_tiles<T, COLS, COLS, EPI_LINE>(st, tile, direct, g);
-        if (epi == EPI_SUM) return launch_tiles<T, COLS, COLS, EPI_SUM>(st, tile, direct, g);
+        if (epi == EPI_LINE) return launch_tiles<T, COLS, COLS, EPI_LINE>(st, tile, g);
+        if (epi == EPI_SUM) return launch_tiles<T, COLS, COLS, EPI_SUM>(st, tile, g);
     }
     return hipErrorInvalidValue;
 }

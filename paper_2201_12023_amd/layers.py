@@ -48,12 +48,12 @@ def load():
     L.alpa_experts_backward.argtypes = [i, i, n, i, n, n, vp, mat, mat, mat, mat, mat, mat, vp, vp, n, vp]
     L.alpa_vocab_loss_forward.argtypes = [i, n, n, n, mat, mat, vp, vp, vp, vp, n, vp]
     L.alpa_vocab_loss_backward.argtypes = [i, n, n, n, vp, mat, mat, vp, vp, mat, mat, vp, n, vp]
-    L.alpa_linear_forward_work.argtypes = [i, n, n, n]
-    L.alpa_linear_backward_work.argtypes = [i, i, n, n, n]
-    L.alpa_experts_forward_work.argtypes = [i, n, i, n, n]
-    L.alpa_experts_backward_work.argtypes = [i, i, n, i, n, n]
-    L.alpa_vocab_loss_forward_work.argtypes = [i, n, n, n]
-    L.alpa_vocab_loss_backward_work.argtypes = [i, n, n, n]
+    L.alpa_linear_forward_work.argtypes = [i, n, n, n, mat, mat]
+    L.alpa_linear_backward_work.argtypes = [i, i, n, n, n, mat, mat, mat]
+    L.alpa_experts_forward_work.argtypes = [i, n, i, n, n, mat, mat]
+    L.alpa_experts_backward_work.argtypes = [i, i, n, i, n, n, mat, mat, mat]
+    L.alpa_vocab_loss_forward_work.argtypes = [i, n, n, n, mat, mat]
+    L.alpa_vocab_loss_backward_work.argtypes = [i, n, n, n, mat, mat]
     for s in SYMBOLS:
         getattr(L, s).restype = ctypes.c_int64 if s.endswith("_work") else ctypes.c_int
     _ready = L
@@ -145,11 +145,11 @@ def _forward(x, w, offsets, bias, residual, act, keep_z, stream):
                 _vec("bias", bias, (*lead, n_out), x.dtype, x.device), _mat("residual", residual, (rows, n_out), x),
                 _mat("y", y, y.shape, x), _mat("z", z, y.shape, x))
         if offsets is None:
-            keep, p, n = _work(L.alpa_linear_forward_work(d, rows, n_in, n_out), x.device)
+            keep, p, n = _work(L.alpa_linear_forward_work(d, rows, n_in, n_out, *mats[:2]), x.device)
             rc = L.alpa_linear_forward(d, int(act), rows, n_in, n_out, *mats, p, n, s)
         else:
             off = _vec("offsets", offsets, (lead[0] + 1,), torch.int32, x.device)
-            keep, p, n = _work(L.alpa_experts_forward_work(d, rows, lead[0], n_in, n_out), x.device)
+            keep, p, n = _work(L.alpa_experts_forward_work(d, rows, lead[0], n_in, n_out, *mats[:2]), x.device)
             rc = L.alpa_experts_forward(d, int(act), rows, lead[0], n_in, n_out, off, *mats, p, n, s)
         binding._check(rc)
     return (y, z) if keep_z else y
@@ -172,13 +172,14 @@ def _backward(dy, x, w, offsets, z, act, need, stream):
         mats = (_mat("dy", dy, (rows, n_out), dy), _mat("z", z, (rows, n_out), dy), _mat("x", x, (rows, n_in), dy),
                 _mat("w", w, (*lead, n_out, n_in), dy), _mat("dx", dx, (rows, n_in), dy),
                 _mat("dw", dw, (*lead, n_out, n_in), dy))
+        read = (mats[0], *mats[2:4])
         bias = None if db is None else db.data_ptr()
         if offsets is None:
-            keep, p, n = _work(L.alpa_linear_backward_work(d, int(act), rows, n_in, n_out), dy.device)
+            keep, p, n = _work(L.alpa_linear_backward_work(d, int(act), rows, n_in, n_out, *read), dy.device)
             rc = L.alpa_linear_backward(d, int(act), rows, n_in, n_out, *mats, bias, p, n, s)
         else:
             off = _vec("offsets", offsets, (lead[0] + 1,), torch.int32, dy.device)
-            keep, p, n = _work(L.alpa_experts_backward_work(d, int(act), rows, lead[0], n_in, n_out), dy.device)
+            keep, p, n = _work(L.alpa_experts_backward_work(d, int(act), rows, lead[0], n_in, n_out, *read), dy.device)
             rc = L.alpa_experts_backward(d, int(act), rows, lead[0], n_in, n_out, off, *mats, bias, p, n, s)
         binding._check(rc)
     return dx, dw, db
@@ -217,7 +218,7 @@ def alpa_vocab_loss_forward(x, w, target, stream=None):
         lse = torch.empty_like(loss)
         args = (_mat("x", x, (rows, n_in), x), _mat("w", w, (words, n_in), x),
                 _vec("target", target, (rows,), torch.int64, x.device))
-        keep, p, n = _work(L.alpa_vocab_loss_forward_work(d, rows, n_in, words), x.device)
+        keep, p, n = _work(L.alpa_vocab_loss_forward_work(d, rows, n_in, words, *args[:2]), x.device)
         binding._check(L.alpa_vocab_loss_forward(d, rows, n_in, words, *args, loss.data_ptr(), lse.data_ptr(), p, n, s))
     return loss, lse
 
@@ -236,6 +237,6 @@ def alpa_vocab_loss_backward(dloss, x, w, target, lse, need=("x", "w"), stream=N
         args = (f32("dloss", dloss), _mat("x", x, (rows, n_in), x), _mat("w", w, (words, n_in), x),
                 _vec("target", target, (rows,), torch.int64, x.device), f32("lse", lse),
                 _mat("dx", dx, (rows, n_in), x), _mat("dw", dw, (words, n_in), x))
-        keep, p, n = _work(L.alpa_vocab_loss_backward_work(d, rows, n_in, words), x.device)
+        keep, p, n = _work(L.alpa_vocab_loss_backward_work(d, rows, n_in, words, *args[1:3]), x.device)
         binding._check(L.alpa_vocab_loss_backward(d, rows, n_in, words, *args, p, n, s))
     return dx, dw

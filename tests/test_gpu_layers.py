@@ -200,7 +200,8 @@ def test_vocab_loss_in_several_pieces(dtype):
     g = C.gen(3)
     rows, n_in, words = 20000, 32, 14001
     x, w = C.normal(g, dtype, rows, n_in), C.normal(g, dtype, words, n_in, scale=0.3)
-    assert L.load().alpa_vocab_loss_backward_work(0 if dtype == F32 else 2, rows, n_in, words) < rows * words * x.element_size()
+    mats = [L.alpa_mat_t(t.data_ptr(), n_in) for t in (x, w)]
+    assert L.load().alpa_vocab_loss_backward_work(0 if dtype == F32 else 2, rows, n_in, words, *mats) < rows * words * x.element_size()
     t = torch.randint(0, words, (rows,), device="cuda", generator=g)
     dloss = torch.full((rows,), 1.0 / rows, device="cuda")
     loss, lse = L.alpa_vocab_loss_forward(x, w, t)

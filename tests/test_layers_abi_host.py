@@ -45,12 +45,12 @@ def test_products_refuse_bad_arguments():
     assert b"stride" in L.load().alpa_dp_last_error() or b"aligned" in L.load().alpa_dp_last_error()
     assert linear(rows=0, x=M(None, 0), y=M(None, 0)) == 0          # nothing to do
     # a product that is split needs work memory
-    need = L.load().alpa_linear_forward_work(2, 4, 8192, 64)
+    need = L.load().alpa_linear_forward_work(2, 4, 8192, 64, M(P, 8192), M(P, 8192))
     assert need > 0
     wide = dict(n_in=8192, n_out=64, x=M(P, 8192), w=M(P, 8192), y=M(P, 64))
     assert linear(**wide) == -1 and linear(**wide, work=P, n=need - 1) == -1 and linear(**wide, work=P + 64, n=need) == -1
     assert backward() == -1                                           # dz needs work memory
-    assert L.load().alpa_linear_backward_work(2, 3, 4, 8, 6) > 0
+    assert L.load().alpa_linear_backward_work(2, 3, 4, 8, 6, M(P, 6), M(P, 8), M(P, 8)) > 0
     big = dict(work=P, n=1 << 20)
     assert backward(z=M(None, 0), **big) == -1 and backward(x=M(None, 0), **big) == -1 and backward(w=M(None, 0), **big) == -1
     assert backward(dy=M(None, 0), **big) == -1 and backward(dw=M(P, 7), **big) == -1 and backward(db=P + 1, **big) == -1
@@ -64,7 +64,7 @@ def test_experts_and_loss_refuse_bad_arguments():
 
     assert experts(E=0) == -1 and experts(E=L.MAX_EXPERTS + 1) == -1 and experts(off=None) == -1 and experts(off=P + 2) == -1
     assert lib.alpa_experts_backward(2, 0, 4, 0, 8, 6, P, M(P, 6), M(None, 0), M(P, 8), M(P, 8), M(P, 8), M(P, 8), None, P, 1 << 20, None) == -1
-    need = lib.alpa_vocab_loss_forward_work(2, 4, 8, 100)
+    need = lib.alpa_vocab_loss_forward_work(2, 4, 8, 100, M(P, 8), M(P, 8))
     assert need > 0
 
     def loss(rows=4, words=100, t=P, out=P, work=P, n=need):
@@ -72,12 +72,22 @@ def test_experts_and_loss_refuse_bad_arguments():
 
     assert loss(words=0) == -1 and loss(words=L.MAX_WORDS + 1) == -1 and loss(t=None) == -1 and loss(out=None) == -1
     assert loss(t=P + 4) == -1 and loss(n=need - 1) == -1 and loss(work=None) == -1 and loss(rows=-3) == -1
-    need = lib.alpa_vocab_loss_backward_work(2, 4, 8, 100)
+    need = lib.alpa_vocab_loss_backward_work(2, 4, 8, 100, M(P, 8), M(P, 8))
     args = lambda dloss, n: (2, 4, 8, 100, dloss, M(P, 8), M(P, 8), P, P, M(P, 8), M(P, 8), P, n, None)
     assert lib.alpa_vocab_loss_backward(*args(None, need)) == -1 and lib.alpa_vocab_loss_backward(*args(P, need - 1)) == -1
 
 
 def test_work_of_refused_sizes_is_none():
+    lib, m = L.load(), M(P, 8)
+    assert lib.alpa_linear_forward_work(9, 4, 8, 8, m, m) == 0 and lib.alpa_linear_backward_work(2, 3, -1, 8, 8, m, m, m) == 0
+    assert lib.alpa_vocab_loss_backward_work(2, 4, 0, 8, m, m) == 0 and lib.alpa_experts_backward_work(2, 3, 4, 0, 8, 8, m, m, m) == 0
+
+
+def test_work_holds_copies_of_unaligned_operands():
     lib = L.load()
-    assert lib.alpa_linear_forward_work(9, 4, 8, 8) == 0 and lib.alpa_linear_backward_work(2, 3, -1, 8, 8) == 0
-    assert lib.alpa_vocab_loss_backward_work(2, 4, 0, 8) == 0 and lib.alpa_experts_backward_work(2, 3, 4, 0, 8, 8) == 0
+    work = lambda x, w, n_in=4096: lib.alpa_linear_forward_work(2, 4096, n_in, 8192, x, w)
+    assert work(M(P, 4096), M(P, 4096)) == 0
+    assert work(M(P + 2, 4096), M(P, 4096)) == work(M(P, 4097), M(P, 4096)) == 4096 * 4096 * 2
+    assert work(M(P, 4096), M(P, 4100)) == 8192 * 4096 * 2
+    assert work(M(P, 4104), M(P, 4096 + 8)) == 0
+    assert work(M(P, 4095), M(P, 4095), n_in=4095) == (4096 + 8192) * 4096 * 2
