@@ -111,18 +111,49 @@ int64_t tiles_of(const Shape &s, int tile)
     return (s.m + tile - 1) / tile * cols * (s.grouping == GROUP_STEPS ? s.groups : 1);
 }
 
-// The contraction is split where its tiles leave most of the 256 compute units without work and each part still has eight steps; the parts' sums
-// go through memory in 32 bits and are joined in their order.
-int splits_of(const Shape &s, int dtype)
+// How a product is cut: the tile, and into how many parts its contraction is split where the tiles alone leave compute units without work (the
+// parts' sums go through memory in 32 bits and are joined in their order).
+struct Cut {
+    int tile, splits, split_steps;
+};
+
+// Of the three tiles and a few numbers of parts the ones with the least time by a model of it.  A compute unit holds one workgroup of the large tile or
+// two of the others; a step of one takes `alone`, of two `both`, and a workgroup's beginning and end `ends` microseconds.  The figures are measured
+// (products of 1 to 8192 rows, 512 to 16384 deep, all three forms, one shape after the other with every tile and 1 to 32 parts), the choice was within
+// 12 % of the best of them everywhere.  Ragged groups are taken to be of one size with half a tile left over.
+Cut cut_of(const Shape &s, int dtype, bool may_split)
 {
-    if (s.grouping != GROUP_NONE) return 1;
-    const int64_t tiles = tiles_of(s, TILE), steps = (s.k * element(dtype) + STEP_BYTES - 1) / STEP_BYTES;
-    if (tiles == 0 || tiles > 128) return 1;
-    return (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(512 / tiles, steps / 8), 64));
+    struct Model { int tile; double alone, both, ends; };
+    static const Model half[] = {{SMALL_TILE, 0.28, 0.42, 2.5}, {TILE, 0.65, 1.0, 5.0}, {BIG_TILE, 1.45, 0.0, 12.0}};
+    static const Model full[] = {{SMALL_TILE, 0.68, 1.25, 2.5}, {TILE, 2.0, 3.9, 5.0}, {BIG_TILE, 7.3, 0.0, 12.0}};
+    static const int parts[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32};
+    const double units = 256.0;
+    int64_t depth = s.k;
+    if (s.grouping == GROUP_STEPS) depth = s.k / std::max(s.groups, 1) + 1;
+    const int64_t steps = std::max<int64_t>((depth * element(dtype) + STEP_BYTES - 1) / STEP_BYTES, 1);
+    Cut best{TILE, 1, 0};
+    double least = INFINITY;
+    for (const Model &m : dtype == ALPA_F32 ? full : half) {
+        double tiles = (double)tiles_of(s, m.tile);
+        if (s.grouping == GROUP_ROWS)
+            tiles = ((double)s.m / m.tile + 0.5 * (double)std::min<int64_t>(s.m, s.groups)) * (double)((s.n + m.tile - 1) / m.tile);
+        for (int p : parts) {
+            if (p > 1 && (!may_split || s.grouping != GROUP_NONE || steps / p < 4 || (double)s.m * (double)s.n * p > 1 << 26)) break;
+            const int64_t share = (steps + p - 1) / p;
+            const double each = std::ceil(tiles * p / units), pairs = m.both > 0.0 ? std::floor(each / 2.0) : 0.0, rest = each - 2.0 * pairs;
+            double t = (double)share * (pairs * m.both + rest * m.alone) + (pairs + rest) * m.ends;
+            if (p > 1) t += 6.0 + (double)(p + 1) * (double)s.m * (double)s.n * 4.0 / 3.5e6;
+            if (t < least) {
+                least = t;
+                best = Cut{m.tile, (int)((steps + share - 1) / share), (int)share};
+            }
+        }
+    }
+    return best;
 }
 int64_t split_bytes(const Shape &s, int dtype)
 {
-    const int n = splits_of(s, dtype);
+    const int n = cut_of(s, dtype, true).splits;
     return n > 1 ? block((int64_t)n * s.m * s.n * 4) : 0;
 }
 
@@ -140,29 +171,26 @@ int run_product(hipStream_t st, int dtype, Forms forms, Epilogue epi, const Shap
     g.wide = by16(g.out) && by16(g.z) && by16(g.residual) && by16(g.bias) && g.ldo * es % 16 == 0 && g.ldz * es % 16 == 0 &&
              g.ldr * es % 16 == 0 && (s.grouping == GROUP_NONE || s.n * es % 16 == 0) &&
              (s.grouping != GROUP_STEPS || g.b_expert * es % 16 == 0);
-    // The larger tile reads half as much of the operands per result, the smaller one fills the compute units with less.
-    const bool long_groups = s.grouping != GROUP_ROWS || s.m >= (int64_t)s.groups * 192;
-    const int tile = long_groups && tiles_of(s, BIG_TILE) >= 256 ? BIG_TILE : TILE;
-    const int64_t tiles = tiles_of(s, tile);
+    const bool may_split = epi != EPI_LOSS && epi != EPI_GRAD && epi != EPI_SUM;
+    const Cut cut = cut_of(s, dtype, may_split);
+    const int64_t tiles = tiles_of(s, cut.tile);
     if (tiles > (1 << 30)) return fail(ALPA_DP_EINVAL, "result too large");
-    g.row_tiles = (int)(s.grouping == GROUP_ROWS ? slots_at_most(s.m, s.groups, tile) : (s.m + tile - 1) / tile);
-    g.col_tiles = (int)((s.n + tile - 1) / tile);
-    g.splits = epi == EPI_LOSS || epi == EPI_GRAD || epi == EPI_SUM ? 1 : splits_of(s, dtype);
+    g.row_tiles = (int)(s.grouping == GROUP_ROWS ? slots_at_most(s.m, s.groups, cut.tile) : (s.m + cut.tile - 1) / cut.tile);
+    g.col_tiles = (int)((s.n + cut.tile - 1) / cut.tile);
+    g.splits = cut.splits;
+    g.split_steps = cut.split_steps;
     if (g.splits > 1) {
-        const int64_t steps = (g.K * es + STEP_BYTES - 1) / STEP_BYTES;
-        g.split_steps = (int)((steps + g.splits - 1) / g.splits);
-        g.splits = (int)((steps + g.split_steps - 1) / g.split_steps);
         g.sum = (float *)split_work;
         ProductArgs part = g;
         part.first = 1;
         part.last = 0;
         part.scale = nullptr;
         part.bias = nullptr;
-        HIPCHK(launch_product(st, dtype, forms, EPI_SUM, tile, part));
+        HIPCHK(launch_product(st, dtype, forms, EPI_SUM, cut.tile, part));
         HIPCHK(launch_join(st, dtype, epi, g));
         return ALPA_DP_OK;
     }
-    HIPCHK(launch_product(st, dtype, forms, epi, tile, g));
+    HIPCHK(launch_product(st, dtype, forms, epi, cut.tile, g));
     return ALPA_DP_OK;
 }
 

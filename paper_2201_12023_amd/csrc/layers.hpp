@@ -46,14 +46,14 @@ struct ProductArgs {
     const float *lse, *coef;        // EPI_GRAD: [M]
 };
 
-constexpr int TILE = 128, BIG_TILE = 256;         // rows and columns of a workgroup's tile
+constexpr int SMALL_TILE = 64, TILE = 128, BIG_TILE = 256;         // rows and columns of a workgroup's tile
 constexpr int STEP_BYTES = 128;
 constexpr int STRIPE = 64;                        // columns of a stripe of EPI_LOSS, in all tiles
 
 // Form of the two operands: both with their contraction contiguous (x wT), the second one's rows contiguous (dz w), or both (dzT x).
 enum Forms : int { FORM_RR, FORM_RC, FORM_CC };
 
-// tile: TILE or BIG_TILE.  Addresses, strides and contiguous extents of the operands are multiples of 16 bytes.
+// tile: one of the three.  Addresses, strides and contiguous extents of the operands are multiples of 16 bytes.
 hipError_t launch_product(hipStream_t st, int dtype, Forms forms, Epilogue epi, int tile, const ProductArgs &a);
 hipError_t launch_product_f32(hipStream_t, Forms, Epilogue, int, const ProductArgs &);
 hipError_t launch_product_f16(hipStream_t, Forms, Epilogue, int, const ProductArgs &);

@@ -56,11 +56,12 @@ constexpr uint32_t OUT_OF_RANGE = 0x80000000u;       // a buffer offset beyond e
 //   ROWS: 128 bytes a row; the 16-byte chunk c of row r is stored at place c ^ swz(r), so that the sixteen rows that a read takes
 //   at one chunk are spread over all banks.
 //   COLS: R * es bytes a step; chunks are permuted within a step, so that the steps that a read takes at one column are.
-template <class T, int FORM, int R, int NT>
+template <class T, int FORM, int R, int NT, bool COLUMNS>
 struct Tile {
     static constexpr int ES = sizeof(T), BK = 128 / ES, BYTES = R * 128, CHUNKS = R * 8 / NT, CPS = R * ES / 16;
-    // rows of two 16-row blocks are dealt to the product's rows so that a lane ends with eight consecutive columns of the result
-    static constexpr bool PAIRED = FORM == ROWS && ES == 2;
+    // COLUMNS: the tile's rows are the result's columns; those of two blocks of sixteen are dealt to the product's rows so that a lane
+    // ends with eight consecutive ones
+    static constexpr bool PAIRED = COLUMNS && FORM == ROWS && ES == 2;
 
     static __device__ __forceinline__ int row_of(int i, int t)
     {
@@ -72,7 +73,8 @@ struct Tile {
     }
     static __device__ __forceinline__ int swz_step(int k)        // in 16-byte chunks
     {
-        return ES == 2 ? ((k & 3) | (k >> 1 & 4)) << 1 : (k >> 2 & 3) << 2;
+        if (ES == 4) return (k >> 2 & 3) << 2;
+        return R == 64 ? ((k >> 1 & 1) | (k >> 2 & 2)) << 1 : ((k & 3) | (k >> 1 & 4)) << 1;      // (R == 64: two steps cover all banks)
     }
     // chunk `c` of the tile: its row (ROWS) or step (COLS), and which 16 bytes of that it holds
     static __device__ __forceinline__ void place(int c, int &major, int &chunk)
@@ -118,9 +120,8 @@ struct Tile {
 // assembly without a result register because the compiler, for the load's builtin, waits for all loads before the next transposing LDS
 // read (measured at 8192 x 16384 x 4096 in 16 bits, operands in COLS: 1340 us, and 1060 without those waits); what has arrived is
 // known here by counting (arrived()).
-template <class T, int FORM, int R, int NT>
+template <class T, class TL, int FORM, int NT>
 struct DirectLoader {
-    using TL = Tile<T, FORM, R, NT>;
     static constexpr int N = TL::CHUNKS, ES = TL::ES, BK = TL::BK;
     const char *p;                          // the next step
     int64_t advance;
@@ -187,11 +188,14 @@ __device__ __forceinline__ void arrived()
 template <class T, int FA, int FB, int BM, int BN, int WM, int WN>
 struct Product {
     static constexpr int NT = WM * WN * 64, MT = BM / WM / 16, NTL = BN / WN / 16, ES = sizeof(T);
-    using TA = Tile<T, FA, BM, NT>;
-    using TB = Tile<T, FB, BN, NT>;
-    // The large tile: three stages of A and two of B, all the LDS there is.  The small one: two of each, two workgroups in a compute unit.
+    using TA = Tile<T, FA, BM, NT, false>;
+    using TB = Tile<T, FB, BN, NT, true>;
+    using LoaderA = DirectLoader<T, TA, FA, NT>;
+    using LoaderB = DirectLoader<T, TB, FB, NT>;
+    // The large tile: three stages of A and two of B, all the LDS there is.  The others: as many stages as leave room for a second workgroup.
     static constexpr bool DEEP = BM == 256;
-    static constexpr int A_STAGES = DEEP ? 3 : 2, LDS_BYTES = A_STAGES * TA::BYTES + 2 * TB::BYTES;
+    static constexpr int STAGE = TA::BYTES + TB::BYTES, STAGES = BM == 128 ? 2 : 5;
+    static constexpr int LDS_BYTES = DEEP ? 3 * TA::BYTES + 2 * TB::BYTES : STAGES * STAGE;
     using Acc = f32x4[MT][NTL];
     struct Fragments { u32x4 a[MT], b[NTL]; };
 
@@ -215,7 +219,7 @@ struct Product {
         const Wave w{wave, TA::lane_at(wave / WN * (BM / WM), lane & 15, lane >> 4), TB::lane_at(wave % WN * (BN / WN), lane & 15, lane >> 4)};
         const uint32_t lds = (uint32_t)(uintptr_t)(ALPA_LDS char *)lds_memory;
         if constexpr (DEEP) run_deep(A, B, steps, lds, acc, w);
-        else run_shallow(A, B, steps, lds, acc, w);
+        else run_ring(A, B, steps, lds, acc, w);
     }
 
 private:
@@ -232,14 +236,14 @@ private:
             for (int b = 0; b < NTL; ++b) acc[a][b] = mma(f.b[b], f.a[a], acc[a][b], T{});
     }
 
-    // The next step's loads are under way while this one is multiplied; the other workgroup of the compute unit fills what is left.
-    static __device__ __forceinline__ void run_shallow(const Operand &A, const Operand &B, int steps, uint32_t lds, Acc &acc, const Wave &w)
+    // STAGES - 1 steps' loads are under way; a stage is loaded again when every wave has read it, one barrier later.  The other workgroup of
+    // the compute unit fills what is left.
+    static __device__ __forceinline__ void run_ring(const Operand &A, const Operand &B, int steps, uint32_t lds, Acc &acc, const Wave &w)
     {
-        DirectLoader<T, FA, BM, NT> la;
-        DirectLoader<T, FB, BN, NT> lb;
+        LoaderA la;
+        LoaderB lb;
         la.init(A, threadIdx.x);
         lb.init(B, threadIdx.x);
-        uint32_t here = lds, next = lds + TA::BYTES + TB::BYTES;
         auto fetch = [&](uint32_t to) {
             la.step();
             lb.step();
@@ -248,15 +252,17 @@ private:
 #pragma unroll
             for (int j = 0; j < lb.N; ++j) lb.load(j, to + TA::BYTES, w.id);
         };
-        fetch(here);
+        const uint32_t end = lds + STAGES * STAGE;
+        uint32_t here = lds, to = lds;
+#pragma unroll
+        for (int k = 0; k < STAGES - 1; ++k, to += STAGE) fetch(to);
         for (int kt = 0; kt < steps; ++kt) {
-            arrived<0>();
-            fetch(next);
+            arrived<(STAGES - 2) * (la.N + lb.N)>();
+            fetch(to);
             half_step(here + w.a_at, here + TA::BYTES + w.b_at, 0, acc);
             half_step(here + w.a_at, here + TA::BYTES + w.b_at, 1, acc);
-            const uint32_t t = here;
-            here = next;
-            next = t;
+            here = here + STAGE == end ? lds : here + STAGE;
+            to = to + STAGE == end ? lds : to + STAGE;
         }
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // (the loads of nothing behind the last step)
     }
@@ -269,8 +275,8 @@ private:
     // 2810 with loads one step ahead, and the clock that the power limit leaves is 1.65 GHz.
     static __device__ __forceinline__ void run_deep(const Operand &A, const Operand &B, int steps, uint32_t lds, Acc &acc, const Wave &w)
     {
-        DirectLoader<T, FA, BM, NT> la;
-        DirectLoader<T, FB, BN, NT> lb;
+        LoaderA la;
+        LoaderB lb;
         static_assert(la.N == 4 && lb.N == 4 && MT == 8 && NTL == 4, "loads and reads are dealt to groups for these");
         la.init(A, threadIdx.x);
         lb.init(B, threadIdx.x);

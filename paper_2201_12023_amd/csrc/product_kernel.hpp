@@ -63,15 +63,15 @@ __device__ __forceinline__ void loss_stripes(const ProductArgs &g, const typenam
     }
 }
 
-// The other epilogues: half of each wave's rows at a time go through LDS, from where a thread takes eight consecutive columns of a row, row after
+// The other epilogues: each wave's rows, half of them at a time where they are many, go through LDS, from where a thread takes eight consecutive columns of a row, row after
 // row.  So the code is a short loop (unrolled over the accumulators it was 60 KB, fetched anew for every tile: at 512 rows an expert a
 // tile of the weights' gradient took 41 us, with this NN), and a row's columns are written as one piece whatever the operands' form was.
 template <class T, class P, int BM, int BN, int WM, int WN, int EPI>
 __device__ __forceinline__ void through_lds(const ProductArgs &g, const typename P::Acc &acc, char *lds, int m0, int m_end, int n0, int wm, int wn,
                                             int i, int q, int64_t out_base, int64_t bias_base, bool skip)
 {
-    constexpr int LDT = BN + 4, PART = BM / WM / 2, CW = 8, THREADS = BN / CW, AT_ONCE = WM * WN * 64 / THREADS;      // (four columns more: no bank twice)
-    static_assert(BM / 2 * LDT * 4 <= P::LDS_BYTES, "half a tile does not fit in LDS");
+    constexpr int PARTS = P::MT > 1 ? 2 : 1, LDT = BN + 4, PART = BM / WM / PARTS, CW = 8, THREADS = BN / CW, AT_ONCE = WM * WN * 64 / THREADS;      // (four columns more: no bank twice)
+    static_assert(BM / PARTS * LDT * 4 <= P::LDS_BYTES, "the tile's part does not fit in LDS");
     float *const tile = (float *)lds;
     const int col = threadIdx.x % THREADS * CW, n = n0 + col, cnt = g.N - n;
     const float scale = (EPI == EPI_LINE || EPI == EPI_SUM) && g.scale ? *g.scale : 1.0f;
@@ -80,20 +80,20 @@ __device__ __forceinline__ void through_lds(const ProductArgs &g, const typename
     for (int j = 0; j < CW; ++j) bias[j] = 0.0f;
     if (g.bias && !skip && cnt > 0) load_row<T>(g.bias, bias_base + n, cnt, g.wide, bias);
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
+    for (int h = 0; h < PARTS; ++h) {
         lds_barrier();
 #pragma unroll
-        for (int a = h * P::MT / 2; a < (h + 1) * P::MT / 2; ++a)
+        for (int a = h * P::MT / PARTS; a < (h + 1) * P::MT / PARTS; ++a)
 #pragma unroll
             for (int b = 0; b < P::NTL; ++b) {
-                const int row = wm / 2 + P::TA::row_of(i, a) - h * PART;
+                const int row = wm / PARTS + P::TA::row_of(i, a) - h * PART;
                 *(f32x4 *)(tile + row * LDT + wn + P::TB::row_of(q * 4, b)) = acc[a][b];
             }
         lds_barrier();
         if (cnt <= 0) continue;
 #pragma unroll 2
-        for (int row = threadIdx.x / THREADS; row < BM / 2; row += AT_ONCE) {
-            const int m = m0 + row / PART * (2 * PART) + h * PART + row % PART;
+        for (int row = threadIdx.x / THREADS; row < BM / PARTS; row += AT_ONCE) {
+            const int m = m0 + row / PART * (PARTS * PART) + h * PART + row % PART;
             if (m >= m_end) continue;
             float v[CW];
             *(f32x4 *)v = *(const f32x4 *)(tile + row * LDT + col);
@@ -194,7 +194,8 @@ hipError_t launch_tiles(hipStream_t st, int tile, const ProductArgs &g)
     const int64_t tiles = (int64_t)g.row_tiles * g.col_tiles * (g.grouping == GROUP_STEPS ? g.experts : 1);
     const dim3 grid((unsigned)tiles, (unsigned)g.splits);
     if (tile == BIG_TILE) product_kernel<T, FA, FB, 256, 256, 2, 4, EPI><<<grid, 512, 0, st>>>(g);
-    else product_kernel<T, FA, FB, 128, 128, 2, 2, EPI><<<grid, 256, 0, st>>>(g);
+    else if (tile == TILE) product_kernel<T, FA, FB, 128, 128, 2, 2, EPI><<<grid, 256, 0, st>>>(g);
+    else product_kernel<T, FA, FB, 64, 64, 4, 1, EPI><<<grid, 256, 0, st>>>(g);
     return hipGetLastError();
 }
 

@@ -69,24 +69,33 @@ def _type(x):
 def _check(name, t, shape, dtype, device):
     if t.dtype != dtype or t.device != device:
         raise ValueError(f"{name} is {t.dtype} on {t.device}; {dtype} on {device} expected")
-    if tuple(t.shape) != tuple(shape):
+    if t.shape != shape:
         raise ValueError(f"{name} has shape {tuple(t.shape)}, {tuple(shape)} expected")
 
 
-def _mat(name, t, shape, like):
+_NONE = alpa_mat_t(None, 0)
+
+
+def _mat(name, t, shape, dtype, device):
     """A matrix, or matrices one behind the other, as the library takes it: its rows `ld` apart."""
     if t is None:
-        return alpa_mat_t(None, 0)
-    _check(name, t, shape, like.dtype, like.device)
+        return _NONE
+    _check(name, t, shape, dtype, device)
     rows, n = shape[-2], shape[-1]
+    if t.is_contiguous():
+        return alpa_mat_t(t.data_ptr(), n)
     ld = t.stride(-2) if rows > 1 else n
     if len(shape) == 3 and rows == 1 and shape[0] > 1:
         ld = t.stride(0)
-    if t.numel() and ((n > 1 and t.stride(-1) != 1) or ld < n or
-                      (len(shape) == 3 and shape[0] > 1 and t.stride(0) != rows * ld)):
+    if (n > 1 and t.stride(-1) != 1) or ld < n or (len(shape) == 3 and shape[0] > 1 and t.stride(0) != rows * ld):
         raise ValueError(f"{name} must have contiguous rows that do not overlap, experts one behind the other; "
                          f"strides are {tuple(t.stride())}")
     return alpa_mat_t(t.data_ptr(), ld)
+
+
+def _new(t):
+    """A result, contiguous as it was allocated."""
+    return _NONE if t is None else alpa_mat_t(t.data_ptr(), t.shape[-1])
 
 
 def _vec(name, t, shape, dtype, device):
@@ -100,23 +109,31 @@ def _vec(name, t, shape, dtype, device):
 
 class _On:
     """The tensors' device and the stream of the call, as torch's current ones, so that results and work memory
-    belong to that stream."""
+    belong to that stream.  (Entering a context costs 6 us of the host's time: not done where nothing would change.)"""
 
     def __init__(self, x, stream):
-        if not x.is_cuda:
+        device = x.device
+        if device.type != "cuda":
             raise ValueError("tensors must be on a GPU")
-        self.device = x.device
-        self.stream = torch.cuda.current_stream(x.device) if stream is None else stream
-        if self.stream.device != x.device:
-            raise ValueError(f"the stream is on {self.stream.device}, the tensors on {x.device}")
-        self.context = torch.cuda.stream(self.stream)
+        self.context = None
+        if stream is None:
+            stream = torch.cuda.current_stream(device)
+            if device.index != torch.cuda.current_device():
+                self.context = torch.cuda.device(device)
+        else:
+            if stream.device != device:
+                raise ValueError(f"the stream is on {stream.device}, the tensors on {device}")
+            self.context = torch.cuda.stream(stream)
+        self.raw = stream.cuda_stream
 
     def __enter__(self):
-        self.context.__enter__()
-        return ctypes.c_void_p(self.stream.cuda_stream)
+        if self.context is not None:
+            self.context.__enter__()
+        return self.raw
 
     def __exit__(self, *a):
-        return self.context.__exit__(*a)
+        if self.context is not None:
+            self.context.__exit__(*a)
 
 
 def _work(need, device):
@@ -137,20 +154,20 @@ def _forward(x, w, offsets, bias, residual, act, keep_z, stream):
     L, d = load(), _type(x)
     rows, n_in = _two("x", x)
     n_out = w.shape[-2] if w.dim() >= 2 else 0
+    dtype, device = x.dtype, x.device
     lead = () if offsets is None else (offsets.numel() - 1,)
     with _On(x, stream) as s:
-        y = torch.empty(rows, n_out, dtype=x.dtype, device=x.device)
+        xm, wm = _mat("x", x, (rows, n_in), dtype, device), _mat("w", w, (*lead, n_out, n_in), dtype, device)
+        b, r = _vec("bias", bias, (*lead, n_out), dtype, device), _mat("residual", residual, (rows, n_out), dtype, device)
+        y = torch.empty((rows, n_out), dtype=dtype, device=device)
         z = torch.empty_like(y) if keep_z else None
-        mats = (_mat("x", x, (rows, n_in), x), _mat("w", w, (*lead, n_out, n_in), x),
-                _vec("bias", bias, (*lead, n_out), x.dtype, x.device), _mat("residual", residual, (rows, n_out), x),
-                _mat("y", y, y.shape, x), _mat("z", z, y.shape, x))
         if offsets is None:
-            keep, p, n = _work(L.alpa_linear_forward_work(d, rows, n_in, n_out, *mats[:2]), x.device)
-            rc = L.alpa_linear_forward(d, int(act), rows, n_in, n_out, *mats, p, n, s)
+            keep, p, n = _work(L.alpa_linear_forward_work(d, rows, n_in, n_out, xm, wm), device)
+            rc = L.alpa_linear_forward(d, act, rows, n_in, n_out, xm, wm, b, r, _new(y), _new(z), p, n, s)
         else:
-            off = _vec("offsets", offsets, (lead[0] + 1,), torch.int32, x.device)
-            keep, p, n = _work(L.alpa_experts_forward_work(d, rows, lead[0], n_in, n_out, *mats[:2]), x.device)
-            rc = L.alpa_experts_forward(d, int(act), rows, lead[0], n_in, n_out, off, *mats, p, n, s)
+            off = _vec("offsets", offsets, (lead[0] + 1,), torch.int32, device)
+            keep, p, n = _work(L.alpa_experts_forward_work(d, rows, lead[0], n_in, n_out, xm, wm), device)
+            rc = L.alpa_experts_forward(d, act, rows, lead[0], n_in, n_out, off, xm, wm, b, r, _new(y), _new(z), p, n, s)
         binding._check(rc)
     return (y, z) if keep_z else y
 
@@ -163,24 +180,24 @@ def _backward(dy, x, w, offsets, z, act, need, stream):
     if x is None and w is None:
         raise ValueError("one of x and w has to be given")
     n_in = (w if x is None else x).shape[-1]
+    dtype, device = dy.dtype, dy.device
     lead = () if offsets is None else (offsets.numel() - 1,)
     with _On(dy, stream) as s:
-        new = lambda *size: torch.empty(*size, dtype=dy.dtype, device=dy.device)
+        dym, zm = _mat("dy", dy, (rows, n_out), dtype, device), _mat("z", z, (rows, n_out), dtype, device)
+        xm, wm = _mat("x", x, (rows, n_in), dtype, device), _mat("w", w, (*lead, n_out, n_in), dtype, device)
+        new = lambda *size: torch.empty(size, dtype=dtype, device=device)
         dx = new(rows, n_in) if "x" in need else None
         dw = new(*lead, n_out, n_in) if "w" in need else None
         db = new(*lead, n_out) if "bias" in need else None
-        mats = (_mat("dy", dy, (rows, n_out), dy), _mat("z", z, (rows, n_out), dy), _mat("x", x, (rows, n_in), dy),
-                _mat("w", w, (*lead, n_out, n_in), dy), _mat("dx", dx, (rows, n_in), dy),
-                _mat("dw", dw, (*lead, n_out, n_in), dy))
-        read = (mats[0], *mats[2:4])
         bias = None if db is None else db.data_ptr()
         if offsets is None:
-            keep, p, n = _work(L.alpa_linear_backward_work(d, int(act), rows, n_in, n_out, *read), dy.device)
-            rc = L.alpa_linear_backward(d, int(act), rows, n_in, n_out, *mats, bias, p, n, s)
+            keep, p, n = _work(L.alpa_linear_backward_work(d, act, rows, n_in, n_out, dym, xm, wm), device)
+            rc = L.alpa_linear_backward(d, act, rows, n_in, n_out, dym, zm, xm, wm, _new(dx), _new(dw), bias, p, n, s)
         else:
-            off = _vec("offsets", offsets, (lead[0] + 1,), torch.int32, dy.device)
-            keep, p, n = _work(L.alpa_experts_backward_work(d, int(act), rows, lead[0], n_in, n_out, *read), dy.device)
-            rc = L.alpa_experts_backward(d, int(act), rows, lead[0], n_in, n_out, off, *mats, bias, p, n, s)
+            off = _vec("offsets", offsets, (lead[0] + 1,), torch.int32, device)
+            keep, p, n = _work(L.alpa_experts_backward_work(d, act, rows, lead[0], n_in, n_out, dym, xm, wm), device)
+            rc = L.alpa_experts_backward(d, act, rows, lead[0], n_in, n_out, off, dym, zm, xm, wm, _new(dx), _new(dw),
+                                         bias, p, n, s)
         binding._check(rc)
     return dx, dw, db
 
@@ -213,13 +230,14 @@ def alpa_vocab_loss_forward(x, w, target, stream=None):
     L, d = load(), _type(x)
     rows, n_in = _two("x", x)
     words = _two("w", w)[0]
+    dtype, device = x.dtype, x.device
     with _On(x, stream) as s:
-        loss = torch.empty(rows, dtype=torch.float32, device=x.device)
+        xm, wm = _mat("x", x, (rows, n_in), dtype, device), _mat("w", w, (words, n_in), dtype, device)
+        t = _vec("target", target, (rows,), torch.int64, device)
+        loss = torch.empty((rows,), dtype=torch.float32, device=device)
         lse = torch.empty_like(loss)
-        args = (_mat("x", x, (rows, n_in), x), _mat("w", w, (words, n_in), x),
-                _vec("target", target, (rows,), torch.int64, x.device))
-        keep, p, n = _work(L.alpa_vocab_loss_forward_work(d, rows, n_in, words, *args[:2]), x.device)
-        binding._check(L.alpa_vocab_loss_forward(d, rows, n_in, words, *args, loss.data_ptr(), lse.data_ptr(), p, n, s))
+        keep, p, n = _work(L.alpa_vocab_loss_forward_work(d, rows, n_in, words, xm, wm), device)
+        binding._check(L.alpa_vocab_loss_forward(d, rows, n_in, words, xm, wm, t, loss.data_ptr(), lse.data_ptr(), p, n, s))
     return loss, lse
 
 
@@ -230,13 +248,13 @@ def alpa_vocab_loss_backward(dloss, x, w, target, lse, need=("x", "w"), stream=N
         raise ValueError(f"need is {need!r}: names out of 'x', 'w' expected")
     rows, n_in = _two("x", x)
     words = _two("w", w)[0]
+    dtype, device = x.dtype, x.device
     with _On(x, stream) as s:
-        dx = torch.empty(rows, n_in, dtype=x.dtype, device=x.device) if "x" in need else None
-        dw = torch.empty(words, n_in, dtype=x.dtype, device=x.device) if "w" in need else None
-        f32 = lambda name, t: _vec(name, t, (rows,), torch.float32, x.device)
-        args = (f32("dloss", dloss), _mat("x", x, (rows, n_in), x), _mat("w", w, (words, n_in), x),
-                _vec("target", target, (rows,), torch.int64, x.device), f32("lse", lse),
-                _mat("dx", dx, (rows, n_in), x), _mat("dw", dw, (words, n_in), x))
-        keep, p, n = _work(L.alpa_vocab_loss_backward_work(d, rows, n_in, words, *args[1:3]), x.device)
-        binding._check(L.alpa_vocab_loss_backward(d, rows, n_in, words, *args, p, n, s))
+        xm, wm = _mat("x", x, (rows, n_in), dtype, device), _mat("w", w, (words, n_in), dtype, device)
+        t = _vec("target", target, (rows,), torch.int64, device)
+        g, l = (_vec(k, v, (rows,), torch.float32, device) for k, v in (("dloss", dloss), ("lse", lse)))
+        dx = torch.empty((rows, n_in), dtype=dtype, device=device) if "x" in need else None
+        dw = torch.empty((words, n_in), dtype=dtype, device=device) if "w" in need else None
+        keep, p, n = _work(L.alpa_vocab_loss_backward_work(d, rows, n_in, words, xm, wm), device)
+        binding._check(L.alpa_vocab_loss_backward(d, rows, n_in, words, g, xm, wm, t, l, _new(dx), _new(dw), p, n, s))
     return dx, dw
