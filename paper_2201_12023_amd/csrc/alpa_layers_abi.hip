@@ -121,19 +121,20 @@ struct Cut {
 // two of the others; a step of one takes `alone`, of two `both`, and a workgroup's beginning and end `ends` microseconds.  The figures are measured
 // (products of 1 to 8192 rows, 512 to 16384 deep, all three forms, one shape after the other with every tile and 1 to 32 parts), the choice was within
 // 12 % of the best of them everywhere.  Ragged groups are taken to be of one size with half a tile left over.
-Cut cut_of(const Shape &s, int dtype, bool may_split)
+Cut cut_of(const Shape &s, int dtype, bool may_split, bool may_be_big)
 {
     struct Model { int tile; double alone, both, ends; };
     static const Model half[] = {{SMALL_TILE, 0.28, 0.42, 2.5}, {TILE, 0.65, 1.0, 5.0}, {BIG_TILE, 1.45, 0.0, 12.0}};
     static const Model full[] = {{SMALL_TILE, 0.68, 1.25, 2.5}, {TILE, 2.0, 3.9, 5.0}, {BIG_TILE, 7.3, 0.0, 12.0}};
     static const int parts[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32};
-    const double units = 256.0;
+    const double units = COMPUTE_UNITS;
     int64_t depth = s.k;
     if (s.grouping == GROUP_STEPS) depth = s.k / std::max(s.groups, 1) + 1;
     const int64_t steps = std::max<int64_t>((depth * element(dtype) + STEP_BYTES - 1) / STEP_BYTES, 1);
     Cut best{TILE, 1, 0};
     double least = INFINITY;
     for (const Model &m : dtype == ALPA_F32 ? full : half) {
+        if (m.tile == BIG_TILE && !may_be_big) break;
         double tiles = (double)tiles_of(s, m.tile);
         if (s.grouping == GROUP_ROWS)
             tiles = ((double)s.m / m.tile + 0.5 * (double)std::min<int64_t>(s.m, s.groups)) * (double)((s.n + m.tile - 1) / m.tile);
@@ -153,7 +154,7 @@ Cut cut_of(const Shape &s, int dtype, bool may_split)
 }
 int64_t split_bytes(const Shape &s, int dtype)
 {
-    const int n = cut_of(s, dtype, true).splits;
+    const int n = cut_of(s, dtype, true, s.n % 8 == 0).splits;
     return n > 1 ? block((int64_t)n * s.m * s.n * 4) : 0;
 }
 
@@ -172,13 +173,15 @@ int run_product(hipStream_t st, int dtype, Forms forms, Epilogue epi, const Shap
              g.ldr * es % 16 == 0 && (s.grouping == GROUP_NONE || s.n * es % 16 == 0) &&
              (s.grouping != GROUP_STEPS || g.b_expert * es % 16 == 0);
     const bool may_split = epi != EPI_LOSS && epi != EPI_GRAD && epi != EPI_SUM;
-    const Cut cut = cut_of(s, dtype, may_split);
+    Cut cut = cut_of(s, dtype, may_split, s.n % 8 == 0 || epi == EPI_LOSS);
+    // (parts of a split product and statistics go to work memory, where everything is aligned)
+    if (cut.tile == BIG_TILE && cut.splits == 1 && epi != EPI_LOSS && !g.wide) cut = cut_of(s, dtype, false, false);
     const int64_t tiles = tiles_of(s, cut.tile);
     if (tiles > (1 << 30)) return fail(ALPA_DP_EINVAL, "result too large");
     g.row_tiles = (int)(s.grouping == GROUP_ROWS ? slots_at_most(s.m, s.groups, cut.tile) : (s.m + cut.tile - 1) / cut.tile);
     g.col_tiles = (int)((s.n + cut.tile - 1) / cut.tile);
     g.splits = cut.splits;
-    g.split_steps = cut.split_steps;
+    g.split_steps = cut.splits > 1 ? cut.split_steps : (int)((g.K * es + STEP_BYTES - 1) / STEP_BYTES);
     if (g.splits > 1) {
         g.sum = (float *)split_work;
         ProductArgs part = g;

@@ -77,21 +77,21 @@ __device__ __forceinline__ float activate(float z, const ProductArgs &g)
 
 // Columns n .. n + N - 1 of row m, `cnt` of them real: z = v + bias, result act(z) (+ residual).  `skip`: a row of no expert, zeros.
 template <class T, int EPI, int N>
-__device__ __forceinline__ void put_row(const ProductArgs &g, int64_t out_base, const float (&bias)[N], int64_t m, int n, int cnt, bool skip,
-                                        float (&v)[N])
+__device__ __forceinline__ void put_row(const ProductArgs &g, int64_t out_base, const float (&bias)[N], int64_t m, int n, int cnt, int wide,
+                                        bool skip, float (&v)[N])
 {
 #pragma unroll
     for (int j = 0; j < N; ++j) v[j] += bias[j];
-    if (g.z) store_row<T>(g.z, m * g.ldz + n, cnt, g.wide, v);
+    if (g.z) store_row<T>(g.z, m * g.ldz + n, cnt, wide, v);
 #pragma unroll
     for (int j = 0; j < N; ++j) v[j] = activate<T, EPI>(v[j], g);
     if (g.residual && !skip) {
         float r[N];
-        load_row<T>(g.residual, m * g.ldr + n, cnt, g.wide, r);
+        load_row<T>(g.residual, m * g.ldr + n, cnt, wide, r);
 #pragma unroll
         for (int j = 0; j < N; ++j) v[j] += r[j];
     }
-    store_row<T>(g.out, out_base + m * g.ldo + n, cnt, g.wide, v);
+    store_row<T>(g.out, out_base + m * g.ldo + n, cnt, wide, v);
 }
 
 }  // namespace alpa

@@ -26,7 +26,7 @@ struct ProductArgs {
     const int32_t *offsets;
     int64_t b_expert;               // GROUP_ROWS: bytes from an expert's b to the next one's; GROUP_STEPS: result elements
     int row_tiles, col_tiles;       // grid: row tiles (GROUP_ROWS: slots), column tiles; GROUP_STEPS: times experts
-    int splits, split_steps;        // of the contraction, 128 bytes a step (GROUP_NONE only)
+    int splits, split_steps;        // of the contraction, 128 bytes a step, all of them if it is not split (GROUP_NONE only)
     // epilogue
     char *out;                      // result, strides in elements
     int64_t ldo;
@@ -47,13 +47,14 @@ struct ProductArgs {
 };
 
 constexpr int SMALL_TILE = 64, TILE = 128, BIG_TILE = 256;         // rows and columns of a workgroup's tile
+constexpr int COMPUTE_UNITS = 256;
 constexpr int STEP_BYTES = 128;
 constexpr int STRIPE = 64;                        // columns of a stripe of EPI_LOSS, in all tiles
 
 // Form of the two operands: both with their contraction contiguous (x wT), the second one's rows contiguous (dz w), or both (dzT x).
 enum Forms : int { FORM_RR, FORM_RC, FORM_CC };
 
-// tile: one of the three.  Addresses, strides and contiguous extents of the operands are multiples of 16 bytes.
+// tile: one of the three; the large one only where results are aligned (`wide`) and their rows multiples of eight elements.  Addresses, strides and contiguous extents of the operands are multiples of 16 bytes.
 hipError_t launch_product(hipStream_t st, int dtype, Forms forms, Epilogue epi, int tile, const ProductArgs &a);
 hipError_t launch_product_f32(hipStream_t, Forms, Epilogue, int, const ProductArgs &);
 hipError_t launch_product_f16(hipStream_t, Forms, Epilogue, int, const ProductArgs &);

@@ -123,41 +123,54 @@ struct Tile {
 template <class T, class TL, int FORM, int NT>
 struct DirectLoader {
     static constexpr int N = TL::CHUNKS, ES = TL::ES, BK = TL::BK;
-    const char *p;                          // the next step
+    const char *p, *p_next;                 // the next step; the operand that follows
     int64_t advance;
-    int rows, ld, left, chunk;              // left: of the contraction
+    int ld, rows, left, steps;              // left, steps: of the contraction
+    int rows_next, left_next, steps_next;
     // A thread's chunks lie at the same place of rows or steps that are NT / 8 or NT / CPS apart, which are permuted alike; steps of 32-bit
     // elements, eight apart, are so every second time.
     static constexpr int KINDS = FORM == COLS && ES == 4 ? 2 : 1;
-    uint32_t first[KINDS], off[KINDS], apart;      // this thread's first chunks, as they are in this step, and how far chunks are apart
+    int chunk[KINDS];
+    uint32_t first, off[KINDS], apart;      // this thread's first row or step, its first chunks in this step, and how far chunks are apart
     u32x4 range;
 
-    __device__ __forceinline__ void init(const Operand &o, int tid)
+    __device__ __forceinline__ void init(int64_t ld_bytes, int tid)
     {
-        p = o.p;
-        rows = o.rows;
-        ld = (int)o.ld;
-        left = o.k;
-        advance = FORM == ROWS ? BK * ES : BK * o.ld;
+        ld = (int)ld_bytes;
+        advance = FORM == ROWS ? BK * ES : BK * ld_bytes;
 #pragma unroll
         for (int j = 0; j < KINDS; ++j) {
-            int major, c;
-            TL::place(j * NT + tid, major, c);
-            if (j == 0) chunk = c;
-            first[j] = FORM == COLS && c * (16 / ES) >= rows ? OUT_OF_RANGE : (uint32_t)(TL::first_major(tid) * ld + c * 16);
+            int major;
+            TL::place(j * NT + tid, major, chunk[j]);
         }
+        first = (uint32_t)(TL::first_major(tid) * ld);
         apart = (uint32_t)(ld * (FORM == ROWS ? NT / 8 : NT / TL::CPS));
+        steps = 0;
     }
-    // Goes to the next step; behind the last one nothing is in range.  The range ends with the last row's (or step's) last byte, so rows and steps
-    // that do not exist are behind it; chunks behind a row's end but in front of the next row are cut.
+    // The operand whose first step follows the present one's last: `n` steps, of which those behind its extent are empty.
+    __device__ __forceinline__ void follow(const Operand &o, int n)
+    {
+        p_next = o.p;
+        rows_next = o.rows;
+        left_next = o.k;
+        steps_next = n;
+    }
+    // Goes to the next step.  The range ends with the last row's (or step's) last byte, so rows and steps that do not exist are behind it; chunks
+    // behind a row's end but in front of the next row are cut.
     __device__ __forceinline__ void step()
     {
+        const bool over = steps == 0;
+        p = over ? p_next : p;
+        rows = over ? rows_next : rows;
+        left = over ? left_next : left;
+        steps = (over ? steps_next : steps) - 1;
         const int n = min(left, BK);
         const int span = FORM == ROWS ? (rows - 1) * ld + n * ES : (n - 1) * ld + rows * ES;
         const uint64_t at = (uint64_t)p;
         range = u32x4{(uint32_t)at, (uint32_t)(at >> 32) & 0xffffu, (uint32_t)(rows > 0 && n > 0 ? span : 0), 0x00020000u};
 #pragma unroll
-        for (int j = 0; j < KINDS; ++j) off[j] = FORM == ROWS && chunk * (16 / ES) >= n ? first[j] | OUT_OF_RANGE : first[j];
+        for (int j = 0; j < KINDS; ++j)
+            off[j] = chunk[j] * (16 / ES) >= (FORM == ROWS ? n : rows) ? OUT_OF_RANGE : first + chunk[j] * 16;
         p += advance;
         left -= BK;
     }
@@ -208,21 +221,18 @@ struct Product {
     }
 
     // a wave's place: its rows and columns in the tile, where its lanes read
-    struct Wave { int id; uint32_t a_at, b_at; };
+    struct Wave {
+        int id;
+        uint32_t a_at, b_at;
+        __device__ __forceinline__ Wave()
+        {
+            const int lane = threadIdx.x & 63;
+            id = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+            a_at = TA::lane_at(id / WN * (BM / WM), lane & 15, lane >> 4);
+            b_at = TB::lane_at(id % WN * (BN / WN), lane & 15, lane >> 4);
+        }
+    };
 
-    static __device__ __forceinline__ void run(const Operand &A, const Operand &B, char *lds_memory, Acc &acc)
-    {
-        clear(acc);
-        const int steps = (max(A.k, B.k) + TA::BK - 1) / TA::BK;
-        if (steps == 0) return;
-        const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-        const Wave w{wave, TA::lane_at(wave / WN * (BM / WM), lane & 15, lane >> 4), TB::lane_at(wave % WN * (BN / WN), lane & 15, lane >> 4)};
-        const uint32_t lds = (uint32_t)(uintptr_t)(ALPA_LDS char *)lds_memory;
-        if constexpr (DEEP) run_deep(A, B, steps, lds, acc, w);
-        else run_ring(A, B, steps, lds, acc, w);
-    }
-
-private:
     static __device__ __forceinline__ void half_step(uint32_t a_at, uint32_t b_at, int ks, Acc &acc)
     {
         Fragments f;
@@ -236,14 +246,21 @@ private:
             for (int b = 0; b < NTL; ++b) acc[a][b] = mma(f.b[b], f.a[a], acc[a][b], T{});
     }
 
-    // STAGES - 1 steps' loads are under way; a stage is loaded again when every wave has read it, one barrier later.  The other workgroup of
-    // the compute unit fills what is left.
-    static __device__ __forceinline__ void run_ring(const Operand &A, const Operand &B, int steps, uint32_t lds, Acc &acc, const Wave &w)
+    // The smaller tiles.  STAGES - 1 steps' loads are under way; a stage is loaded again when every wave has read it, one barrier later.  The other
+    // workgroup of the compute unit fills what is left.
+    static __device__ __forceinline__ void run(const Operand &A, const Operand &B, char *lds_memory, Acc &acc)
     {
+        clear(acc);
+        const int steps = (max(A.k, B.k) + TA::BK - 1) / TA::BK;
+        if (steps <= 0) return;
+        const Wave w;
+        const uint32_t lds = (uint32_t)(uintptr_t)(ALPA_LDS char *)lds_memory, end = lds + STAGES * STAGE;
         LoaderA la;
         LoaderB lb;
-        la.init(A, threadIdx.x);
-        lb.init(B, threadIdx.x);
+        la.init(A.ld, threadIdx.x);
+        lb.init(B.ld, threadIdx.x);
+        la.follow(A, 1 << 30);
+        lb.follow(B, 1 << 30);
         auto fetch = [&](uint32_t to) {
             la.step();
             lb.step();
@@ -252,7 +269,6 @@ private:
 #pragma unroll
             for (int j = 0; j < lb.N; ++j) lb.load(j, to + TA::BYTES, w.id);
         };
-        const uint32_t end = lds + STAGES * STAGE;
         uint32_t here = lds, to = lds;
 #pragma unroll
         for (int k = 0; k < STAGES - 1; ++k, to += STAGE) fetch(to);
@@ -267,85 +283,122 @@ private:
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // (the loads of nothing behind the last step)
     }
 
+    // The large tile: tile after tile as one row of steps, so that the loads of a tile's first steps are under way during the steps and the
+    // epilogue of the tile in front (8192 x 16384 x 4096, sixteen tiles a compute unit: see the kernel).
+    //
     // A step is sixteen groups of four products, eight for each half of its contraction; a group also issues a share of the LDS reads of the
     // next half and every second one a load, so that matrix unit, LDS and load unit have work all the time (eight loads together take the load
     // unit as long as half a step's products).  A's and B's stages of step kt are read by group 3 (barrier) and then hold loads of
     // A's step kt + 3 and B's step kt + 2, which gives A nearly two steps to arrive and B one; the last six loads may be under way when step
     // kt + 1 is looked at (group 8).  At 8192 x 4096 x 16384 in 16 bits a step takes 2490 to 2650 cycles of the 2048 its products need, against
     // 2810 with loads one step ahead, and the clock that the power limit leaves is 1.65 GHz.
-    static __device__ __forceinline__ void run_deep(const Operand &A, const Operand &B, int steps, uint32_t lds, Acc &acc, const Wave &w)
-    {
+    struct Deep {
+        static constexpr int LEAST = 3;        // steps of a tile at least: loads run into the next tile, but not past it
         LoaderA la;
         LoaderB lb;
-        static_assert(la.N == 4 && lb.N == 4 && MT == 8 && NTL == 4, "loads and reads are dealt to groups for these");
-        la.init(A, threadIdx.x);
-        lb.init(B, threadIdx.x);
-        uint32_t a0 = lds, a1 = lds + TA::BYTES, a2 = lds + 2 * TA::BYTES, b0 = lds + 3 * TA::BYTES, b1 = b0 + TB::BYTES;
-        la.step();
-        lb.step();
-#pragma unroll
-        for (int j = 0; j < 4; ++j) la.load(j, a0, w.id);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) lb.load(j, b0, w.id);
-        la.step();
-        lb.step();
-#pragma unroll
-        for (int j = 0; j < 4; ++j) la.load(j, a1, w.id);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) lb.load(j, b1, w.id);
-        la.step();
-        la.load(0, a2, w.id);
-        la.load(1, a2, w.id);
-        arrived<10>();
+        Wave w;
+        uint32_t a0, a1, a2, b0, b1;           // stages: of this step, the next one and the one after that
         Fragments f[2];
-        auto read = [&](int half, int a, uint32_t a_at, uint32_t b_at) {
+
+        // A stage's first byte plus a lane's place in it, as one opaque value: the reads' constants then go into the instructions and not, added to
+        // the lane's place in front of the loop, into registers of their own.
+        static __device__ __forceinline__ uint32_t place(uint32_t stage, uint32_t lane)
+        {
+            uint32_t at;
+            asm("v_add_u32 %0, %1, %2" : "=v"(at) : "s"(stage), "v"(lane));
+            return at;
+        }
+        // fragments of group a: a block of rows, and every second time one of columns
+        __device__ __forceinline__ void read(int half, int a, uint32_t a_at, uint32_t b_at)
+        {
             if (a & 1) f[half].b[a >> 1] = TB::fragment(b_at, a >> 1, half);
             f[half].a[a] = TA::fragment(a_at, a, half);
-        };
-#pragma unroll
-        for (int a = 0; a < 8; ++a) read(0, a, a0 + w.a_at, b0 + w.b_at);
-        for (int kt = 0; kt < steps; ++kt) {
-#pragma unroll
-            for (int g = 0; g < 16; ++g) {
-                const int half = g >> 3, a = g & 7;
-                if (g == 0) la.load(2, a2, w.id);
-                if (g == 2) la.load(3, a2, w.id);
-                if (g < 4) {
-                    read(1, 2 * g, a0 + w.a_at, b0 + w.b_at);
-                    read(1, 2 * g + 1, a0 + w.a_at, b0 + w.b_at);
-                }
-                if (g == 4) {
-                    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-                    __builtin_amdgcn_s_barrier();
-                    asm volatile("" ::: "memory");
-                    lb.step();
-                    __builtin_amdgcn_sched_barrier(0);
-                }
-                if (g == 8) {
-                    arrived<6>();
-                    __builtin_amdgcn_sched_barrier(0);
-                }
-                if (g >= 4 && g <= 10 && g % 2 == 0) lb.load((g - 4) / 2, b0, w.id);
-                if (g == 12) {
-                    la.step();
-                    la.load(0, a0, w.id);
-                }
-                if (g == 14) la.load(1, a0, w.id);
-                if (g >= 8) read(0, a, a1 + w.a_at, b1 + w.b_at);
-#pragma unroll
-                for (int b = 0; b < 4; ++b) acc[a][b] = mma(f[half].b[b], f[half].a[a], acc[a][b], T{});
-                __builtin_amdgcn_sched_barrier(0);
-            }
-            uint32_t t = a0;
-            a0 = a1;
-            a1 = a2;
-            a2 = t;
-            t = b0;
-            b0 = b1;
-            b1 = t;
         }
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");       // (the loads and reads of nothing behind the last step)
-    }
+        // the first tile's operands, `steps` steps
+        __device__ __forceinline__ void begin(const Operand &A, const Operand &B, int steps, char *lds_memory)
+        {
+            static_assert(LoaderA::N == 4 && LoaderB::N == 4 && MT == 8 && NTL == 4, "loads and reads are dealt to groups for these");
+            const uint32_t lds = (uint32_t)(uintptr_t)(ALPA_LDS char *)lds_memory;
+            a0 = lds;
+            a1 = a0 + TA::BYTES;
+            a2 = a1 + TA::BYTES;
+            b0 = a2 + TA::BYTES;
+            b1 = b0 + TB::BYTES;
+            la.init(A.ld, threadIdx.x);
+            lb.init(B.ld, threadIdx.x);
+            la.follow(A, steps);
+            lb.follow(B, steps);
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                la.step();
+                lb.step();
+#pragma unroll
+                for (int j = 0; j < 4; ++j) la.load(j, k ? a1 : a0, w.id);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) lb.load(j, k ? b1 : b0, w.id);
+            }
+            la.step();
+            la.load(0, a2, w.id);
+            la.load(1, a2, w.id);
+            arrived<10>();
+#pragma unroll
+            for (int a = 0; a < 8; ++a) read(0, a, place(a0, w.a_at), place(b0, w.b_at));
+        }
+        // One tile's steps; la and lb follow into the next tile's.  `first`: the tile that begin() was for.  Others begin with their first two steps
+        // arrived.
+        __device__ __forceinline__ void run(int steps, bool first, Acc &acc)
+        {
+            clear(acc);
+            for (int kt = 0; kt < steps; ++kt) {
+                const uint32_t a_here = place(a0, w.a_at), b_here = place(b0, w.b_at), a_next = place(a1, w.a_at), b_next = place(b1, w.b_at);
+#pragma unroll
+                for (int g = 0; g < 16; ++g) {
+                    const int half = g >> 3, a = g & 7;
+                    if (g == 0) la.load(2, a2, w.id);
+                    if (g == 2) la.load(3, a2, w.id);
+                    if (g < 4) {
+                        read(1, 2 * g, a_here, b_here);
+                        read(1, 2 * g + 1, a_here, b_here);
+                    }
+                    if (g == 4) {
+                        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                        __builtin_amdgcn_s_barrier();
+                        asm volatile("" ::: "memory");
+                        lb.step();
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+                    if (g == 8) {
+                        if (first || kt > 0) asm volatile("s_waitcnt vmcnt(6)" ::: "memory");
+                        __builtin_amdgcn_s_barrier();
+                        asm volatile("" ::: "memory");
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+                    if (g >= 4 && g <= 10 && g % 2 == 0) lb.load((g - 4) / 2, b0, w.id);
+                    if (g == 12) {
+                        la.step();
+                        la.load(0, a0, w.id);
+                    }
+                    if (g == 14) la.load(1, a0, w.id);
+                    if (g >= 8) read(0, a, a_next, b_next);
+#pragma unroll
+                    for (int b = 0; b < 4; ++b) acc[a][b] = mma(f[half].b[b], f[half].a[a], acc[a][b], T{});
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                uint32_t t = a0;
+                a0 = a1;
+                a1 = a2;
+                a2 = t;
+                t = b0;
+                b0 = b1;
+                b1 = t;
+            }
+            // The next tile's first two steps, all but the last two loads: waited for here, as the epilogue's stores are not to be waited for
+            // when that tile looks at its second step.
+            asm volatile("s_waitcnt vmcnt(2)" ::: "memory");
+        }
+        // (loads of nothing and reads behind the last tile)
+        __device__ __forceinline__ void end() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory"); }
+    };
 };
 
 }  // namespace alpa

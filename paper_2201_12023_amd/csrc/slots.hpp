@@ -31,7 +31,8 @@ struct Slot {
 // wave has to be here.
 __device__ __forceinline__ Slot find_slot(const int32_t *offsets, int experts, int rows, int tile, int slot)
 {
-    const int lane = threadIdx.x & 63;
+    int lane = threadIdx.x & 63;
+    asm volatile("" : "+v"(lane));         // (what follows from it is not kept in registers between two calls)
     int before = 0;
     for (int base = 0; base < experts + 2; base += 64) {
         int first, end;
@@ -67,7 +68,7 @@ __device__ __forceinline__ int slots_before(const int32_t *offsets, int experts,
         int n = base + lane < group ? (end - first + tile - 1) / tile : 0;
 #pragma unroll
         for (int off = 32; off; off >>= 1) n += __shfl_xor(n, off, 64);
-        sum += n;
+        sum += __builtin_amdgcn_readfirstlane(n);
     }
     return sum;
 }

@@ -160,6 +160,71 @@ def test_experts_in_large_tiles():
             C.within(name, got, *ref[name])
 
 
+# two or more of the largest tiles for each workgroup, edges of tiles in rows and columns, a contraction that ends inside a step
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=ids)
+def test_tile_after_tile(dtype):
+    g = C.gen(31)
+    many, few = (5000, 5128, 568), (5000, 568, 5128)
+    for rows, n_in, n_out in ((many[0], many[2], many[1]), few, (568, 5128, 5000)):       # y, dx and dw are the large results in turn
+        x, w = C.normal(g, dtype, rows, n_in), C.normal(g, dtype, n_out, n_in, scale=n_in ** -0.5)
+        z, dy, b = C.normal(g, dtype, rows, n_out), C.normal(g, dtype, rows, n_out), C.normal(g, dtype, n_out)
+        for kind in (0, 2, 4):
+            y, kept = L.alpa_linear_forward(x, w, bias=b, residual=dy, act=kind, keep_z=True)
+            ry, ey, rz, ez = C.forward(x, w, b, dy, kind)
+            C.within("y", y, ry, ey)
+            C.within("z", kept, rz, ez)
+        ref = C.backward(dy, z, x, w, 4)
+        for name, got in zip(("dx", "dw", "dbias"), L.alpa_linear_backward(dy, x, w, z=z, act=4)):
+            C.within(name, got, *ref[name])
+
+
+def test_experts_tile_after_tile():
+    g = C.gen(32)
+    counts = [1700, 0, 3, 2500, 900, 0, 260]
+    rows, E, n_in, n_out = sum(counts) + 70, len(counts), 1032, 4104
+    ends = [0]
+    for n in counts:
+        ends.append(ends[-1] + n)
+    off = torch.tensor(ends, dtype=torch.int32, device="cuda")
+    x, w, dy = C.normal(g, BF16, rows, n_in), C.normal(g, BF16, E, n_out, n_in, scale=0.03), C.normal(g, BF16, rows, n_out)
+    z, b = C.normal(g, BF16, rows, n_out), C.normal(g, BF16, E, n_out)
+    for t in (x, dy, z):
+        t[ends[-1]:] = float("nan")
+    wide = torch.randn(E, n_in, n_out, device="cuda", generator=g).mul_(0.03).to(BF16)     # the other way, so that dx is large too
+    for act, xx, dd, zz, ww, bb in ((3, x, dy, z, w, b), (0, dy, x, x, wide, None)):
+        y, kept = L.alpa_experts_forward(xx, ww, off, bias=bb, act=act, keep_z=True)
+        dx, dw, db = L.alpa_experts_backward(dd, xx, ww, off, z=zz if act else None, act=act)
+        for t in (y, kept, dx):
+            assert not bool(t[ends[-1]:].any())
+        for e in range(E):
+            p = slice(ends[e], ends[e + 1])
+            if counts[e] == 0:
+                assert not bool(dw[e].any()) and not bool(db[e].any())
+                continue
+            ry, ey, rz, ez = C.forward(xx[p], ww[e], None if bb is None else bb[e], None, act)
+            C.within("y", y[p], ry, ey)
+            C.within("z", kept[p], rz, ez)
+            ref = C.backward(dd[p], zz[p], xx[p], ww[e], act)
+            for name, got in (("dx", dx[p]), ("dw", dw[e]), ("dbias", db[e])):
+                C.within(name, got, *ref[name])
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16], ids=ids)
+def test_vocab_loss_tile_after_tile(dtype):
+    g = C.gen(33)
+    rows, n_in, words = 3000, 1032, 10504
+    x, w = C.normal(g, dtype, rows, n_in), C.normal(g, dtype, words, n_in, scale=0.05)
+    t = torch.randint(0, words, (rows,), device="cuda", generator=g)
+    t[::7] = -100
+    dloss = torch.rand(rows, device="cuda", generator=g)
+    ref = C.vocab(x, w, t, dloss)
+    loss, lse = L.alpa_vocab_loss_forward(x, w, t)
+    C.within("loss", loss, *ref["loss"])
+    dx, dw = L.alpa_vocab_loss_backward(dloss, x, w, t, lse)
+    C.within("dx", dx, *ref["dx"])
+    C.within("dw", dw, *ref["dw"])
+
+
 def test_offsets_that_make_no_sense_stay_inside():
     """Results are unspecified, but nothing outside the tensors is touched and the calls end."""
     x, w = torch.ones(50, 64, dtype=BF16, device="cuda"), torch.ones(3, 32, 64, dtype=BF16, device="cuda")
