@@ -344,9 +344,9 @@ struct Product {
 #pragma unroll
             for (int a = 0; a < 8; ++a) read(0, a, place(a0, w.a_at), place(b0, w.b_at));
         }
-        // One tile's steps; la and lb follow into the next tile's.  `first`: the tile that begin() was for.  Others begin with their first two steps
-        // arrived.
-        __device__ __forceinline__ void run(int steps, bool first, Acc &acc)
+        // One tile's steps; la and lb follow into the next tile's.  (Stores of the tile before may be under way: they only make vmcnt(6) wait
+        // for more.)
+        __device__ __forceinline__ void run(int steps, Acc &acc)
         {
             clear(acc);
             for (int kt = 0; kt < steps; ++kt) {
@@ -368,7 +368,7 @@ struct Product {
                         __builtin_amdgcn_sched_barrier(0);
                     }
                     if (g == 8) {
-                        if (first || kt > 0) asm volatile("s_waitcnt vmcnt(6)" ::: "memory");
+                        asm volatile("s_waitcnt vmcnt(6)" ::: "memory");
                         __builtin_amdgcn_s_barrier();
                         asm volatile("" ::: "memory");
                         __builtin_amdgcn_sched_barrier(0);
@@ -392,9 +392,6 @@ struct Product {
                 b0 = b1;
                 b1 = t;
             }
-            // The next tile's first two steps, all but the last two loads: waited for here, as the epilogue's stores are not to be waited for
-            // when that tile looks at its second step.
-            asm volatile("s_waitcnt vmcnt(2)" ::: "memory");
         }
         // (loads of nothing and reads behind the last tile)
         __device__ __forceinline__ void end() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory"); }

@@ -262,7 +262,7 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void product_kernel(const ProductAr
         int steps = max((max(job.A.k, job.B.k) + P::TA::BK - 1) / P::TA::BK, P::Deep::LEAST);
         typename P::Deep deep;
         deep.begin(job.A, job.B, steps, lds);
-        for (bool first = true;; first = false) {
+        for (;;) {
             i += apart;
             const bool more = i < walk.count;
             // (behind the last tile: that tile once more, with no rows)
@@ -272,7 +272,7 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void product_kernel(const ProductAr
             const int steps_next = max((max(next.A.k, next.B.k) + P::TA::BK - 1) / P::TA::BK, P::Deep::LEAST);
             deep.la.follow(next.A, steps_next);
             deep.lb.follow(next.B, steps_next);
-            deep.run(steps, first, acc);
+            deep.run(steps, acc);
             epilogue<T, P, BM, BN, WM, WN, EPI>(g, acc, lds, job);
             if (!more) break;
             job = next;
