@@ -26,20 +26,18 @@ using f16 = _Float16;
 // Sixteen bytes of one row's contraction in each lane: lane (i, q) = (lane & 15, lane >> 4) holds row i, elements
 // q * 8 .. q * 8 + 7 of 32 (16 bits), or q * 4 .. q * 4 + 3 of 16 (32 bits; four products of four elements each, the j-th taking
 // element j of every lane: the order of a sum's terms is free as long as both operands have the same one).
-__device__ __forceinline__ f32x4 mma(u32x4 a, u32x4 b, f32x4 c, bf16)
+__device__ __forceinline__ f32x4 mma(u32x4 a, u32x4 b, f32x4 c, int, bf16)
 {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
-__device__ __forceinline__ f32x4 mma(u32x4 a, u32x4 b, f32x4 c, f16)
+__device__ __forceinline__ f32x4 mma(u32x4 a, u32x4 b, f32x4 c, int, f16)
 {
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
 }
-__device__ __forceinline__ f32x4 mma(u32x4 a, u32x4 b, f32x4 c, float)
+// `parts` instructions make the product: the parts of several go in turn, so that none waits for the one in front.
+__device__ __forceinline__ f32x4 mma(u32x4 a, u32x4 b, f32x4 c, int j, float)
 {
-    const f32x4 x = __builtin_bit_cast(f32x4, a), y = __builtin_bit_cast(f32x4, b);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_16x16x4f32(x[j], y[j], c, 0, 0, 0);
-    return c;
+    return __builtin_amdgcn_mfma_f32_16x16x4f32(__builtin_bit_cast(f32x4, a)[j], __builtin_bit_cast(f32x4, b)[j], c, 0, 0, 0);
 }
 
 // One operand's place in memory, as a tile sees it: the tile's first row and step are at `p`.
@@ -120,7 +118,7 @@ struct Tile {
 // assembly without a result register because the compiler, for the load's builtin, waits for all loads before the next transposing LDS
 // read (measured at 8192 x 16384 x 4096 in 16 bits, operands in COLS: 1340 us, and 1060 without those waits); what has arrived is
 // known here by counting (arrived()).
-template <class T, class TL, int FORM, int NT>
+template <class T, class TL, int FORM, int NT, bool FOLLOWED>
 struct DirectLoader {
     static constexpr int N = TL::CHUNKS, ES = TL::ES, BK = TL::BK;
     const char *p, *p_next;                 // the next step; the operand that follows
@@ -147,6 +145,13 @@ struct DirectLoader {
         apart = (uint32_t)(ld * (FORM == ROWS ? NT / 8 : NT / TL::CPS));
         steps = 0;
     }
+    // The only operand (not FOLLOWED).
+    __device__ __forceinline__ void begin(const Operand &o)
+    {
+        p = o.p;
+        rows = o.rows;
+        left = o.k;
+    }
     // The operand whose first step follows the present one's last: `n` steps, of which those behind its extent are empty.
     __device__ __forceinline__ void follow(const Operand &o, int n)
     {
@@ -159,11 +164,13 @@ struct DirectLoader {
     // behind a row's end but in front of the next row are cut.
     __device__ __forceinline__ void step()
     {
-        const bool over = steps == 0;
-        p = over ? p_next : p;
-        rows = over ? rows_next : rows;
-        left = over ? left_next : left;
-        steps = (over ? steps_next : steps) - 1;
+        if constexpr (FOLLOWED) {
+            const bool over = steps == 0;
+            p = over ? p_next : p;
+            rows = over ? rows_next : rows;
+            left = over ? left_next : left;
+            steps = (over ? steps_next : steps) - 1;
+        }
         const int n = min(left, BK);
         const int span = FORM == ROWS ? (rows - 1) * ld + n * ES : (n - 1) * ld + rows * ES;
         const uint64_t at = (uint64_t)p;
@@ -200,13 +207,13 @@ __device__ __forceinline__ void arrived()
 // 16 x 16 block are consecutive columns n of one row m: acc[mt][nt][r] is row row_of(i, mt), column (of block nt) 4 q + r.
 template <class T, int FA, int FB, int BM, int BN, int WM, int WN>
 struct Product {
-    static constexpr int NT = WM * WN * 64, MT = BM / WM / 16, NTL = BN / WN / 16, ES = sizeof(T);
+    static constexpr int NT = WM * WN * 64, MT = BM / WM / 16, NTL = BN / WN / 16, ES = sizeof(T), MMA_PARTS = ES == 4 ? 4 : 1;
     using TA = Tile<T, FA, BM, NT, false>;
     using TB = Tile<T, FB, BN, NT, true>;
-    using LoaderA = DirectLoader<T, TA, FA, NT>;
-    using LoaderB = DirectLoader<T, TB, FB, NT>;
     // The large tile: three stages of A and two of B, all the LDS there is.  The others: as many stages as leave room for a second workgroup.
     static constexpr bool DEEP = BM == 256;
+    using LoaderA = DirectLoader<T, TA, FA, NT, DEEP>;
+    using LoaderB = DirectLoader<T, TB, FB, NT, DEEP>;
     static constexpr int STAGE = TA::BYTES + TB::BYTES, STAGES = BM == 128 ? 2 : 5;
     static constexpr int LDS_BYTES = DEEP ? 3 * TA::BYTES + 2 * TB::BYTES : STAGES * STAGE;
     using Acc = f32x4[MT][NTL];
@@ -233,23 +240,31 @@ struct Product {
         }
     };
 
-    static __device__ __forceinline__ void half_step(uint32_t a_at, uint32_t b_at, int ks, Acc &acc)
+    // The smaller tiles' share g of four: of the reads of a half step, and of its products.
+    static __device__ __forceinline__ void read(uint32_t stage, const Wave &w, int ks, int g, Fragments &f)
     {
-        Fragments f;
+        f.b[g] = TB::fragment(stage + TA::BYTES + w.b_at, g, ks);
+        if (g < MT) f.a[g] = TA::fragment(stage + w.a_at, g, ks);
+    }
+    static __device__ __forceinline__ void multiply(const Fragments &f, int g, Acc &acc)
+    {
 #pragma unroll
-        for (int b = 0; b < NTL; ++b) f.b[b] = TB::fragment(b_at, b, ks);
+        for (int j = 0; j < MMA_PARTS; ++j)
 #pragma unroll
-        for (int a = 0; a < MT; ++a) f.a[a] = TA::fragment(a_at, a, ks);
+            for (int a = 0; a < MT; ++a)
 #pragma unroll
-        for (int a = 0; a < MT; ++a)
-#pragma unroll
-            for (int b = 0; b < NTL; ++b) acc[a][b] = mma(f.b[b], f.a[a], acc[a][b], T{});
+                for (int b = 0; b < NTL; ++b)
+                    if (g == (MT > 1 ? a : MMA_PARTS > 1 ? j : b)) acc[a][b] = mma(f.b[b], f.a[a], acc[a][b], j, T{});
+        __builtin_amdgcn_sched_barrier(0);
     }
 
-    // The smaller tiles.  STAGES - 1 steps' loads are under way; a stage is loaded again when every wave has read it, one barrier later.  The other
-    // workgroup of the compute unit fills what is left.
+    // The smaller tiles.  The products of a step's first half run while its second half is read and the next loads are prepared; then the stage that
+    // all have read is loaded again and the next step's first half is read while the products of the second half run.  STAGES - 1 steps' loads
+    // are under way, and the other workgroup of the compute unit fills what is left.
     static __device__ __forceinline__ void run(const Operand &A, const Operand &B, char *lds_memory, Acc &acc)
     {
+        static_assert(NTL == 4 && (MT == 1 || MT == 4) && LoaderA::N == LoaderB::N, "reads, loads and products are dealt to four groups for these");
+        constexpr int LOADS = LoaderA::N;
         clear(acc);
         const int steps = (max(A.k, B.k) + TA::BK - 1) / TA::BK;
         if (steps <= 0) return;
@@ -259,28 +274,45 @@ struct Product {
         LoaderB lb;
         la.init(A.ld, threadIdx.x);
         lb.init(B.ld, threadIdx.x);
-        la.follow(A, 1 << 30);
-        lb.follow(B, 1 << 30);
-        auto fetch = [&](uint32_t to) {
+        la.begin(A);
+        lb.begin(B);
+        auto load = [&](int j, uint32_t to) {
+            if (j < LOADS) la.load(j, to, w.id);
+            else lb.load(j - LOADS, to + TA::BYTES, w.id);
+        };
+#pragma unroll
+        for (int k = 0; k < STAGES; ++k) {
             la.step();
             lb.step();
 #pragma unroll
-            for (int j = 0; j < la.N; ++j) la.load(j, to, w.id);
-#pragma unroll
-            for (int j = 0; j < lb.N; ++j) lb.load(j, to + TA::BYTES, w.id);
-        };
-        uint32_t here = lds, to = lds;
-#pragma unroll
-        for (int k = 0; k < STAGES - 1; ++k, to += STAGE) fetch(to);
-        for (int kt = 0; kt < steps; ++kt) {
-            arrived<(STAGES - 2) * (la.N + lb.N)>();
-            fetch(to);
-            half_step(here + w.a_at, here + TA::BYTES + w.b_at, 0, acc);
-            half_step(here + w.a_at, here + TA::BYTES + w.b_at, 1, acc);
-            here = here + STAGE == end ? lds : here + STAGE;
-            to = to + STAGE == end ? lds : to + STAGE;
+            for (int j = 0; j < 2 * LOADS; ++j) load(j, lds + k * STAGE);
         }
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // (the loads of nothing behind the last step)
+        arrived<(STAGES - 1) * 2 * LOADS>();
+        Fragments first, second;
+#pragma unroll
+        for (int g = 0; g < 4; ++g) read(lds, w, 0, g, first);
+        uint32_t here = lds;
+        for (int kt = 0; kt < steps; ++kt) {
+            const uint32_t next = here + STAGE == end ? lds : here + STAGE;
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                read(here, w, 1, g, second);
+                if (g == 1) la.step();
+                if (g == 2) lb.step();
+                multiply(first, g, acc);
+            }
+            arrived<(STAGES - 2) * 2 * LOADS>();
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+#pragma unroll
+                for (int j = g * LOADS / 2; j < (g + 1) * LOADS / 2; ++j) load(j, here);
+                read(next, w, 0, g, first);
+                multiply(second, g, acc);
+            }
+            here = next;
+        }
+        // (the loads of nothing and the reads behind the last step)
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
     }
 
     // The large tile: tile after tile as one row of steps, so that the loads of a tile's first steps are under way during the steps and the
@@ -381,7 +413,9 @@ struct Product {
                     if (g == 14) la.load(1, a0, w.id);
                     if (g >= 8) read(0, a, a_next, b_next);
 #pragma unroll
-                    for (int b = 0; b < 4; ++b) acc[a][b] = mma(f[half].b[b], f[half].a[a], acc[a][b], T{});
+                    for (int j = 0; j < MMA_PARTS; ++j)
+#pragma unroll
+                        for (int b = 0; b < 4; ++b) acc[a][b] = mma(f[half].b[b], f[half].a[a], acc[a][b], j, T{});
                     __builtin_amdgcn_sched_barrier(0);
                 }
                 uint32_t t = a0;
