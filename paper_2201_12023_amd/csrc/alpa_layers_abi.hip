@@ -85,17 +85,22 @@ int64_t pack_bytes(const alpa_mat_t &m, int64_t rows, int64_t len, int dtype)
     if (!m.p || rows == 0 || (by16(m.p) && (m.ld * es) % 16 == 0 && (len * es) % 16 == 0)) return 0;
     return block(rows * round_up(len, 16 / es) * es);
 }
-int pack(hipStream_t st, const alpa_mat_t &m, int64_t rows, int64_t len, int dtype, char *work, Source &out)
-{
-    if (pack_bytes(m, rows, len, dtype) == 0) {
-        out = Source{(const char *)m.p, m.ld, len};
+// The copies that a call needs, all queued at once.
+struct Packs {
+    PackArgs g{};
+    Source add(const alpa_mat_t &m, int64_t rows, int64_t len, int dtype, char *work)
+    {
+        if (pack_bytes(m, rows, len, dtype) == 0) return Source{(const char *)m.p, m.ld, len};
+        const int64_t to = round_up(len, 16 / element(dtype));
+        g.mats[g.count++] = {(const char *)m.p, work, m.ld, rows, (int)len, (int)to};
+        return Source{work, to, to};
+    }
+    int queue(hipStream_t st, int dtype)
+    {
+        if (g.count) HIPCHK(launch_pack(st, dtype, g));
         return ALPA_DP_OK;
     }
-    const int64_t to = round_up(len, 16 / element(dtype));
-    HIPCHK(launch_pack(st, dtype, (const char *)m.p, m.ld, rows, (int)len, work, (int)to));
-    out = Source{work, to, to};
-    return ALPA_DP_OK;
-}
+};
 
 // A product of `m` x `n` results over `k`; `groups`: matrices of results (GROUP_STEPS), or groups of rows.
 struct Shape {
@@ -249,9 +254,10 @@ int forward(int dtype, int act, int64_t rows, int experts, int64_t n_in, int64_t
     TRY(check_vector(bias, element(dtype)));
     const ForwardWork at(dtype, rows, experts, n_in, n_out, x, w);
     TRY(check_work(work, work_bytes, at.total));
-    Source xs, ws;
-    TRY(pack(st, x, rows, n_in, dtype, work + at.x, xs));
-    TRY(pack(st, w, n_out * std::max(experts, 1), n_in, dtype, work + at.w, ws));
+    Packs packs;
+    const Source xs = packs.add(x, rows, n_in, dtype, work + at.x);
+    const Source ws = packs.add(w, n_out * std::max(experts, 1), n_in, dtype, work + at.w);
+    TRY(packs.queue(st, dtype));
     ProductArgs g = operands(FORM_RR, xs, ws, n_in, dtype);
     const Epilogue epi = epilogue_of(act, g);
     result(g, y);
@@ -330,9 +336,12 @@ int backward(int dtype, int act, int64_t rows, int experts, int64_t n_in, int64_
         s.wide = by16(s.dy) && by16(s.z) && s.lddy * es % 16 == 0 && s.ldz * es % 16 == 0;
         HIPCHK(launch_slope(st, dtype, s));
     }
-    if (rows > 0 && !has_z && products) TRY(pack(st, dy, rows, n_out, dtype, work + at.dz, dz));
+    Packs packs;
+    if (rows > 0 && !has_z && products) dz = packs.add(dy, rows, n_out, dtype, work + at.dz);
+    if (dx.p && rows > 0) ws = packs.add(w, n_out * std::max(experts, 1), n_in, dtype, work + at.w);
+    if (dw.p) xs = packs.add(x, rows, n_in, dtype, work + at.x);
+    TRY(packs.queue(st, dtype));
     if (dx.p && rows > 0) {
-        TRY(pack(st, w, n_out * std::max(experts, 1), n_in, dtype, work + at.w, ws));
         ProductArgs g = operands(FORM_RC, dz, ws, n_out, dtype);
         result(g, dx);
         g.offsets = offsets;
@@ -341,7 +350,6 @@ int backward(int dtype, int act, int64_t rows, int experts, int64_t n_in, int64_
                         work + at.split));
     }
     if (dw.p) {
-        TRY(pack(st, x, rows, n_in, dtype, work + at.x, xs));
         ProductArgs g = operands(FORM_CC, dz, xs, rows, dtype);
         result(g, dw);
         g.offsets = offsets;
@@ -497,9 +505,9 @@ int alpa_vocab_loss_forward(int dtype, int64_t rows, int64_t n_in, int64_t words
     TRY(check_work(work, work_bytes, at.total));
     const hipStream_t st = (hipStream_t)hip_stream;
     char *base = (char *)work;
-    Source xs, ws;
-    TRY(pack(st, x, rows, n_in, dtype, base + at.x, xs));
-    TRY(pack(st, w, words, n_in, dtype, base + at.w, ws));
+    Packs packs;
+    const Source xs = packs.add(x, rows, n_in, dtype, base + at.x), ws = packs.add(w, words, n_in, dtype, base + at.w);
+    TRY(packs.queue(st, dtype));
     ProductArgs g = operands(FORM_RR, xs, ws, n_in, dtype);
     g.target = target;
     g.stat = (float2 *)(base + at.stat);
@@ -537,13 +545,15 @@ int alpa_vocab_loss_backward(int dtype, int64_t rows, int64_t n_in, int64_t word
     HIPCHK(launch_coef(st, dloss, target, words, (int)rows, coef, scale));
     const int64_t es = element(dtype);
     Source xs{}, ws{};
-    TRY(pack(st, x, rows, n_in, dtype, base + at.x, xs));
     for (int64_t p = 0; p < at.pieces; ++p) {
         const int64_t word0 = p * at.piece, n = std::min(at.piece, words - word0);
         const Source grad{base + at.grad, at.piece, round_up(n, 16 / es)};
         if (rows > 0) {
             // (pieces are multiples of 256 words, so a piece's rows are aligned as the first piece's are)
-            TRY(pack(st, alpa_mat_t{(char *)w.p + word0 * w.ld * es, w.ld}, n, n_in, dtype, base + at.w, ws));
+            Packs packs;
+            if (p == 0) xs = packs.add(x, rows, n_in, dtype, base + at.x);
+            ws = packs.add(alpa_mat_t{(char *)w.p + word0 * w.ld * es, w.ld}, n, n_in, dtype, base + at.w);
+            TRY(packs.queue(st, dtype));
             ProductArgs g = operands(FORM_RR, xs, ws, n_in, dtype);
             result(g, alpa_mat_t{base + at.grad, at.piece});
             g.target = target;

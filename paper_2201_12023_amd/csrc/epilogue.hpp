@@ -61,9 +61,30 @@ __device__ __forceinline__ float gated(float z, float c1, float c3)
     return fabsf(z) == INFINITY ? (z > 0.0f ? z : -0.0f) : y;
 }
 
+// The normal distribution's integral up to z; e = exp(-z^2 / 2).  For values rounded to 16 bits erfc(x) = exp(-x^2) t P(t), t = 1 / (1 + 0.46 x), x >= 0,
+// P of least relative error in its class (7e-7, fitted here): an eighth of erfcf's instructions and one exponential for it and the slope.  Either
+// way very negative z keep their relative error.
+template <class T>
+__device__ __forceinline__ float normal_integral(float z, float e)
+{
+    if (sizeof(T) == 4) return 0.5f * erfcf(-0.70710678118654752f * z);
+    const float t = __builtin_amdgcn_rcpf(fmaf(fabsf(z), 0.46f * 0.70710678118654752f, 1.0f));
+    float p = 0.06771395355463028f;
+    p = fmaf(p, t, -0.22664865851402283f);
+    p = fmaf(p, t, 0.16924932599067688f);
+    p = fmaf(p, t, 0.05254606902599335f);
+    p = fmaf(p, t, 0.18688102066516876f);
+    p = fmaf(p, t, 0.23117370903491974f);
+    p = fmaf(p, t, 0.25955814123153687f);
+    p = fmaf(p, t, 0.2595270276069641f);
+    const float below = 0.5f * e * t * p;
+    return z < 0.0f ? below : 1.0f - below;
+}
+
+template <class T>
 __device__ __forceinline__ float gelu(float z)
 {
-    const float y = 0.5f * z * erfcf(-0.70710678118654752f * z);      // erfc keeps its bits for very negative z
+    const float y = z * normal_integral<T>(z, exp_for<T>(-0.5f * z * z));
     return z == -INFINITY ? -0.0f : y;
 }
 
@@ -71,7 +92,7 @@ template <class T, int EPI>
 __device__ __forceinline__ float activate(float z, const ProductArgs &g)
 {
     if (EPI == EPI_SIGMOID) return gated<T>(z, g.c1, g.c3);
-    if (EPI == EPI_ERF) return gelu(z);
+    if (EPI == EPI_ERF) return gelu<T>(z);
     return z < g.low ? g.low : z;              // (a NaN stays)
 }
 

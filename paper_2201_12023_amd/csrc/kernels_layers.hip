@@ -7,29 +7,32 @@ namespace alpa {
 
 // ---------------------------------------------------------------- rows in 16-byte units
 
-// A thread writes sixteen bytes; reads of one row are consecutive, so the lines they share come from the cache.
+// A thread writes sixteen bytes; reads of one row are consecutive, so the lines they share come from the cache.  All of a call's matrices go in one
+// launch (two launches took 5 us more where both are small).
 template <class T>
-__global__ __launch_bounds__(256) void pack_kernel(const T *from, int64_t ld, int64_t rows, int len, T *to, int to_len)
+__global__ __launch_bounds__(256) void pack_kernel(const PackArgs g)
 {
     constexpr int V = 16 / sizeof(T);
-    const int per_row = to_len / V;
-    const int64_t total = rows * per_row;
+    const auto &mat = g.mats[blockIdx.y];
+    const int per_row = mat.to_len / V;
+    const int64_t total = mat.rows * per_row;
     for (int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x; c < total; c += (int64_t)gridDim.x * 256) {
         const int64_t r = c / per_row;
         const int n = (int)(c - r * per_row) * V;
         float v[V];
-        load_row<T>((const char *)from, r * ld + n, len - n, 0, v);
-        store_row<T>((char *)to, r * to_len + n, V, 1, v);
+        load_row<T>(mat.from, r * mat.ld + n, mat.len - n, 0, v);
+        store_row<T>(mat.to, r * mat.to_len + n, V, 1, v);
     }
 }
 
-hipError_t launch_pack(hipStream_t st, int dtype, const char *from, int64_t ld, int64_t rows, int len, char *to, int to_len)
+hipError_t launch_pack(hipStream_t st, int dtype, const PackArgs &g)
 {
-    const int64_t chunks = rows * to_len * (dtype == 0 ? 4 : 2) / 16;
-    const unsigned blocks = (unsigned)std::min<int64_t>((chunks + 255) / 256, 8192);
-    if (dtype == 0) pack_kernel<float><<<blocks, 256, 0, st>>>((const float *)from, ld, rows, len, (float *)to, to_len);
-    else if (dtype == 1) pack_kernel<f16><<<blocks, 256, 0, st>>>((const f16 *)from, ld, rows, len, (f16 *)to, to_len);
-    else pack_kernel<bf16><<<blocks, 256, 0, st>>>((const bf16 *)from, ld, rows, len, (bf16 *)to, to_len);
+    int64_t chunks = 0;
+    for (int k = 0; k < g.count; ++k) chunks = std::max(chunks, g.mats[k].rows * g.mats[k].to_len * (dtype == 0 ? 4 : 2) / 16);
+    const dim3 grid((unsigned)std::min<int64_t>((chunks + 255) / 256, 8192), (unsigned)g.count);
+    if (dtype == 0) pack_kernel<float><<<grid, 256, 0, st>>>(g);
+    else if (dtype == 1) pack_kernel<f16><<<grid, 256, 0, st>>>(g);
+    else pack_kernel<bf16><<<grid, 256, 0, st>>>(g);
     return hipGetLastError();
 }
 
@@ -42,7 +45,8 @@ __device__ __forceinline__ float slope_of(float z, int act)
     if (act == 1) return z > 0.0f ? 1.0f : (z == z ? 0.0f : z);
     if (act == 2) {
         if (fabsf(z) == INFINITY) return z > 0.0f ? 1.0f : 0.0f;
-        return 0.5f * erfcf(-0.70710678118654752f * z) + z * 0.39894228040143268f * exp_for<T>(-0.5f * z * z);
+        const float e = exp_for<T>(-0.5f * z * z);
+        return normal_integral<T>(z, e) + z * 0.39894228040143268f * e;
     }
     // z s(u) with u = c1 z + c3 z^3:  s + z s (1 - s) u'
     const float c1 = act == 3 ? 1.5957691216057308f : 1.0f, c3 = act == 3 ? 0.071354816272600257f : 0.0f;

@@ -60,8 +60,12 @@ hipError_t launch_product_f32(hipStream_t, Forms, Epilogue, int, const ProductAr
 hipError_t launch_product_f16(hipStream_t, Forms, Epilogue, int, const ProductArgs &);
 hipError_t launch_product_bf16(hipStream_t, Forms, Epilogue, int, const ProductArgs &);
 
-// Copies [rows][len] to rows of `to_len` elements (a multiple of 16 bytes), zeros behind len: what an operand needs that is not aligned to 16 bytes.
-hipError_t launch_pack(hipStream_t st, int dtype, const char *from, int64_t ld, int64_t rows, int len, char *to, int to_len);
+// Copies matrices, [rows][len], to rows of `to_len` elements (a multiple of 16 bytes), zeros behind len: what an operand needs that is not aligned to 16 bytes.
+struct PackArgs {
+    struct { const char *from; char *to; int64_t ld, rows; int len, to_len; } mats[3];
+    int count;
+};
+hipError_t launch_pack(hipStream_t st, int dtype, const PackArgs &g);
 
 // dz = dy * act'(z), and sums of dz over the rows of each slot of SLOPE_ROWS rows
 constexpr int SLOPE_ROWS = 64;
