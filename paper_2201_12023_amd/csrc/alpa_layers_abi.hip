@@ -123,19 +123,23 @@ struct Cut {
 };
 
 // Of the three tiles and a few numbers of parts the ones with the least time by a model of it.  A compute unit holds one workgroup of the large tile or
-// two of the others; a step of one takes `alone`, of two `both`, and a workgroup's beginning and end `ends` microseconds.  The figures are measured
-// (products of 1 to 8192 rows, 512 to 16384 deep, all three forms, one shape after the other with every tile and 1 to 32 parts), the choice was within
-// 12 % of the best of them everywhere.  Ragged groups are taken to be of one size with half a tile left over.
+// two of the others; a step of one takes `alone`, of two `both`, a workgroup's beginning and end `ends` microseconds, of the large
+// tile's, which goes on to its next one, 4 for all but the first, and all of it no less than the
+// operands take at 4.9 TB/s; a join adds a launch and its traffic.  The figures are measured (fifty products of 1 to 8192 rows and 296 to 16384 deep, all
+// three forms, each with every tile and 1 to 32 parts): the choice was the best of them in most and within 8 % of it everywhere.  Ragged groups are taken to
+// be of one size with half a tile left over; where they are contractions, one is taken to be twice as long.
 Cut cut_of(const Shape &s, int dtype, bool may_split, bool may_be_big)
 {
     struct Model { int tile; double alone, both, ends; };
-    static const Model half[] = {{SMALL_TILE, 0.28, 0.42, 2.5}, {TILE, 0.65, 1.0, 5.0}, {BIG_TILE, 1.45, 0.0, 12.0}};
-    static const Model full[] = {{SMALL_TILE, 0.68, 1.25, 2.5}, {TILE, 2.0, 3.9, 5.0}, {BIG_TILE, 7.3, 0.0, 12.0}};
+    static const Model half[] = {{SMALL_TILE, 0.26, 0.40, 2.5}, {TILE, 0.65, 1.0, 4.0}, {BIG_TILE, 1.4, 0.0, 9.0}};
+    static const Model full[] = {{SMALL_TILE, 0.60, 1.10, 2.5}, {TILE, 1.95, 3.8, 4.0}, {BIG_TILE, 7.2, 0.0, 9.0}};
     static const int parts[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32};
     const double units = COMPUTE_UNITS;
     int64_t depth = s.k;
     if (s.grouping == GROUP_STEPS) depth = s.k / std::max(s.groups, 1) + 1;
     const int64_t steps = std::max<int64_t>((depth * element(dtype) + STEP_BYTES - 1) / STEP_BYTES, 1);
+    const double weights = s.grouping == GROUP_ROWS ? (double)std::min<int64_t>(s.m, s.groups) : 1.0;
+    const double memory = 3.0 + ((double)s.m + weights * (double)s.n) * (double)(s.k * element(dtype)) / 4.9e6;
     Cut best{TILE, 1, 0};
     double least = INFINITY;
     for (const Model &m : dtype == ALPA_F32 ? full : half) {
@@ -147,7 +151,9 @@ Cut cut_of(const Shape &s, int dtype, bool may_split, bool may_be_big)
             if (p > 1 && (!may_split || s.grouping != GROUP_NONE || steps / p < 4 || (double)s.m * (double)s.n * p > 1 << 26)) break;
             const int64_t share = (steps + p - 1) / p;
             const double each = std::ceil(tiles * p / units), pairs = m.both > 0.0 ? std::floor(each / 2.0) : 0.0, rest = each - 2.0 * pairs;
-            double t = (double)share * (pairs * m.both + rest * m.alone) + (pairs + rest) * m.ends;
+            double t = (double)share * (pairs * m.both + rest * m.alone) + (m.tile == BIG_TILE ? m.ends + 4.0 * (rest - 1.0) : (pairs + rest) * m.ends);
+            if (s.grouping == GROUP_STEPS) t = std::max(t, 2.0 * (double)share * m.alone + m.ends);
+            t = std::max(t, memory);
             if (p > 1) t += 6.0 + (double)(p + 1) * (double)s.m * (double)s.n * 4.0 / 3.5e6;
             if (t < least) {
                 least = t;
