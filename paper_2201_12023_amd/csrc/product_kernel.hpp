@@ -202,12 +202,17 @@ __device__ __forceinline__ void through_lds(const ProductArgs &g, const typename
 template <class T, class P, int EPI>
 __device__ __forceinline__ void straight(const ProductArgs &g, const typename P::Acc &acc, const Job &job, int wm, int wn, int i, int q)
 {
-    constexpr int CW = P::TB::PAIRED ? 8 : 4, GROUPS = P::NTL * 4 / CW;
+    // With w in COLS a lane has four columns of each block: of two blocks lanes of even q take the first one's from their neighbour of odd q, whose
+    // share of the second they give, so that every lane has eight consecutive ones (stores of 8 bytes, 32 a row, instead: products by
+    // w in COLS 2 % slower, and with the contraction ragged 4 %).
+    constexpr bool TAKE = sizeof(T) == 2 && !P::TB::PAIRED;
+    constexpr int CW = 16 / sizeof(T), GROUPS = P::NTL * 4 / CW;
+    const int at = TAKE ? (q & 1) * 16 + (q >> 1) * 8 : q * CW;
     const float scale = (EPI == EPI_LINE || EPI == EPI_SUM) && g.scale ? *g.scale : 1.0f;
     float bias[GROUPS][CW];
 #pragma unroll
     for (int c = 0; c < GROUPS; ++c) {
-        const int n = job.n0 + wn + c * CW * 4 + q * CW;
+        const int n = job.n0 + wn + c * CW * 4 + at;
 #pragma unroll
         for (int j = 0; j < CW; ++j) bias[c][j] = 0.0f;
         if (g.bias && job.skip == 0 && n < g.N) load_row<T>(g.bias, job.bias_base + n, CW, 1, bias[c]);
@@ -222,14 +227,23 @@ __device__ __forceinline__ void straight(const ProductArgs &g, const typename P:
 #pragma unroll
     for (int a = 0; a < P::MT; ++a) {
         const int m = job.m0 + wm + P::TA::row_of(i, a);
-        if (m >= job.m_end) continue;
+        if (!TAKE && m >= job.m_end) continue;
 #pragma unroll
         for (int c = 0; c < GROUPS; ++c) {
-            const int n = job.n0 + wn + c * CW * 4 + q * CW;
-            if (n >= g.N) continue;
+            const int n = job.n0 + wn + c * CW * 4 + at;
+            if (!TAKE && n >= g.N) continue;
             float v[CW];
 #pragma unroll
             for (int j = 0; j < CW; ++j) v[j] = acc[a][c * CW / 4 + j / 4][j & 3];
+            if constexpr (TAKE) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const u32x2 both = __builtin_amdgcn_permlane16_swap(__float_as_uint(v[j]), __float_as_uint(v[j + 4]), false, false);
+                    v[j] = __uint_as_float(both.x);
+                    v[j + 4] = __uint_as_float(both.y);
+                }
+                if (m >= job.m_end || n >= g.N) continue;
+            }
             finish_row<T, EPI>(g, job, scale, bias[c], m, n, CW, 1, v);
         }
     }
