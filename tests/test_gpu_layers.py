@@ -178,6 +178,20 @@ def test_tile_after_tile(dtype):
             C.within(name, got, *ref[name])
 
 
+@pytest.mark.parametrize("dtype", TYPES, ids=ids)
+def test_results_larger_than_the_caches(dtype):
+    """A result of 256 MiB and more, alone and with z, rows and columns that end inside a tile."""
+    g = C.gen(35)
+    n_out = 8200 if dtype == F32 else 16392
+    x, w, b, r = C.normal(g, dtype, 8203, 72), C.normal(g, dtype, n_out, 72, scale=0.1), C.normal(g, dtype, n_out), C.normal(g, dtype, 8203, n_out)
+    for kind, keep in ((0, False), (3, True), (2, False)):
+        got = L.alpa_linear_forward(x, w, bias=b, residual=None if keep else r, act=kind, keep_z=keep)
+        ry, ey, rz, ez = C.forward(x, w, b, None if keep else r, kind)
+        C.within("y", got[0] if keep else got, ry, ey)
+        if keep:
+            C.within("z", got[1], rz, ez)
+
+
 def test_experts_tile_after_tile():
     g = C.gen(32)
     counts = [1700, 0, 3, 2500, 900, 0, 260]
