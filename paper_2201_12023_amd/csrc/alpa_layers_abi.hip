@@ -193,9 +193,6 @@ int run_product(hipStream_t st, int dtype, Forms forms, Epilogue epi, const Shap
     g.col_tiles = (int)((s.n + cut.tile - 1) / cut.tile);
     g.splits = cut.splits;
     g.split_steps = cut.splits > 1 ? cut.split_steps : (int)((g.K * es + STEP_BYTES - 1) / STEP_BYTES);
-    // Results of x wT that the 256 MiB of cache behind the L2s do not hold go past the caches, and the operands stay in them: 8192 x 16384 x 4096 with z
-    // 860 -> 830 us, without 815 -> 795; 8192 x 8192 x 2048, 128 MiB, 202 -> 206.  Ragged rows (660 -> 663) and products by w in COLS (1745 -> 1755) gain nothing.
-    g.stream = forms == FORM_RR && s.grouping == GROUP_NONE && s.m * s.n * es * (g.z ? 2 : 1) >= (int64_t)256 << 20;
     if (g.splits > 1) {
         g.sum = (float *)split_work;
         ProductArgs part = g;

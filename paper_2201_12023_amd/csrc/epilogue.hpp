@@ -39,22 +39,6 @@ __device__ __forceinline__ void store_row(char *base, int64_t at, int n, int wid
     }
 }
 
-// The same for a result that may be written past the caches (`stream`).
-template <class T, bool MAY, int N>
-__device__ __forceinline__ void store_result(char *base, int64_t at, int n, int wide, int stream, const float (&v)[N])
-{
-    if constexpr (MAY && sizeof(T) * N == 16) {
-        if (stream && wide && n >= N) {
-            struct { T e[N]; } k;
-#pragma unroll
-            for (int j = 0; j < N; ++j) k.e[j] = (T)v[j];
-            __builtin_nontemporal_store(__builtin_bit_cast(u32x4, k), (u32x4 *)((T *)base + at));
-            return;
-        }
-    }
-    store_row<T>(base, at, n, wide, v);
-}
-
 // exp for values that end in 32 bits, and the faster one (its error grows with the exponent: 2^-24 |x|) for those rounded to 16
 template <class T>
 __device__ __forceinline__ float exp_for(float x)
@@ -113,13 +97,13 @@ __device__ __forceinline__ float activate(float z, const ProductArgs &g)
 }
 
 // Columns n .. n + N - 1 of row m, `cnt` of them real: z = v + bias, result act(z) (+ residual).  `skip`: a row of no expert, zeros.
-template <class T, int EPI, bool STREAM, int N>
+template <class T, int EPI, int N>
 __device__ __forceinline__ void put_row(const ProductArgs &g, int64_t out_base, const float (&bias)[N], int64_t m, int n, int cnt, int wide,
                                         bool skip, float (&v)[N])
 {
 #pragma unroll
     for (int j = 0; j < N; ++j) v[j] += bias[j];
-    if (g.z) store_result<T, STREAM>(g.z, m * g.ldz + n, cnt, wide, g.stream, v);
+    if (g.z) store_row<T>(g.z, m * g.ldz + n, cnt, wide, v);
 #pragma unroll
     for (int j = 0; j < N; ++j) v[j] = activate<T, EPI>(v[j], g);
     if (g.residual && !skip) {
@@ -128,7 +112,7 @@ __device__ __forceinline__ void put_row(const ProductArgs &g, int64_t out_base, 
 #pragma unroll
         for (int j = 0; j < N; ++j) v[j] += r[j];
     }
-    store_result<T, STREAM>(g.out, out_base + m * g.ldo + n, cnt, wide, g.stream, v);
+    store_row<T>(g.out, out_base + m * g.ldo + n, cnt, wide, v);
 }
 
 }  // namespace alpa

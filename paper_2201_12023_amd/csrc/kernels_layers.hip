@@ -183,7 +183,7 @@ __global__ __launch_bounds__(256) void join_kernel(const ProductArgs g)
     }
     float bias[4] = {0.0f, 0.0f, 0.0f, 0.0f};
     if (g.bias) load_row<T>(g.bias, n, cnt, g.wide, bias);
-    put_row<T, EPI, false>(g, 0, bias, m, n, cnt, g.wide, false, v);
+    put_row<T, EPI>(g, 0, bias, m, n, cnt, g.wide, false, v);
 }
 
 template <class T>

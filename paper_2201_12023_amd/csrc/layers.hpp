@@ -35,7 +35,6 @@ struct ProductArgs {
     char *z;
     int64_t ldz;
     int wide;                       // pointers, strides and row length allow 16-byte accesses in the epilogue
-    int stream;                     // the result and z are written past the caches
     float low, c1, c3;
     float *sum;                     // EPI_SUM: [split][M][N]
     int first, last;

@@ -120,7 +120,7 @@ __device__ __forceinline__ void loss_stripes(const ProductArgs &g, const typenam
 }
 
 // What becomes of columns n .. n + CW - 1 of row m, `cnt` of them real, in the other epilogues.
-template <class T, int EPI, bool STREAM, int CW>
+template <class T, int EPI, int CW>
 __device__ __forceinline__ void finish_row(const ProductArgs &g, const Job &job, float scale, const float (&bias)[CW], int m, int n, int cnt,
                                            int wide, float (&v)[CW])
 {
@@ -154,7 +154,7 @@ __device__ __forceinline__ void finish_row(const ProductArgs &g, const Job &job,
 #pragma unroll
             for (int j = 0; j < CW; ++j) v[j] *= scale;
         }
-        put_row<T, EPI, STREAM>(g, job.out_base, bias, m, n, cnt, wide, job.skip, v);
+        put_row<T, EPI>(g, job.out_base, bias, m, n, cnt, wide, job.skip, v);
     }
 }
 
@@ -192,14 +192,14 @@ __device__ __forceinline__ void through_lds(const ProductArgs &g, const typename
             float v[CW];
             *(f32x4 *)v = *(const f32x4 *)(tile + row * LDT + col);
             *(f32x4 *)(v + 4) = *(const f32x4 *)(tile + row * LDT + col + 4);
-            finish_row<T, EPI, false>(g, job, scale, bias, m, n, cnt, g.wide, v);
+            finish_row<T, EPI>(g, job, scale, bias, m, n, cnt, g.wide, v);
         }
     }
 }
 
 // The large tile, whose LDS holds the next tile's operands: straight from the accumulators.  Everything is aligned and rows are multiples of eight
 // elements, so a lane's columns exist or do not and the code stays short.
-template <class T, class P, int EPI, bool STREAM>
+template <class T, class P, int EPI>
 __device__ __forceinline__ void straight(const ProductArgs &g, const typename P::Acc &acc, const Job &job, int wm, int wn, int i, int q)
 {
     // With w in COLS a lane has four columns of each block: of two blocks lanes of even q take the first one's from their neighbour of odd q, whose
@@ -244,19 +244,19 @@ __device__ __forceinline__ void straight(const ProductArgs &g, const typename P:
                 }
                 if (m >= job.m_end || n >= g.N) continue;
             }
-            finish_row<T, EPI, STREAM>(g, job, scale, bias[c], m, n, CW, 1, v);
+            finish_row<T, EPI>(g, job, scale, bias[c], m, n, CW, 1, v);
         }
     }
 }
 
-template <class T, class P, int BM, int BN, int WM, int WN, int EPI, bool STREAM>
+template <class T, class P, int BM, int BN, int WM, int WN, int EPI>
 __device__ __forceinline__ void epilogue(const ProductArgs &g, const typename P::Acc &acc, char *lds, const Job &job)
 {
     const int lane = threadIdx.x & 63, i = lane & 15, q = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave / WN * (BM / WM), wn = wave % WN * (BN / WN);
     if constexpr (EPI == EPI_LOSS) loss_stripes<T, P, BN / WN>(g, acc, job.m0 + wm, job.m_end, job.n0 + wn, i, q);
-    else if constexpr (P::DEEP) straight<T, P, EPI, STREAM>(g, acc, job, wm, wn, i, q);
+    else if constexpr (P::DEEP) straight<T, P, EPI>(g, acc, job, wm, wn, i, q);
     else through_lds<T, P, BM, BN, WM, WN, EPI>(g, acc, lds, job, wm, wn, i, q);
 }
 
@@ -287,7 +287,7 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void product_kernel(const ProductAr
             deep.la.follow(next.A, steps_next);
             deep.lb.follow(next.B, steps_next);
             deep.run(steps, acc);
-            epilogue<T, P, BM, BN, WM, WN, EPI, GROUPING == GROUP_NONE && FB == ROWS>(g, acc, lds, job);
+            epilogue<T, P, BM, BN, WM, WN, EPI>(g, acc, lds, job);
             if (!more) break;
             job = next;
             steps = steps_next;
@@ -295,7 +295,7 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void product_kernel(const ProductAr
         deep.end();
     } else {
         P::run(job.A, job.B, lds, acc);
-        epilogue<T, P, BM, BN, WM, WN, EPI, false>(g, acc, lds, job);
+        epilogue<T, P, BM, BN, WM, WN, EPI>(g, acc, lds, job);
     }
 }
 
