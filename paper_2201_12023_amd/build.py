@@ -37,7 +37,10 @@ _BAND_INSTANCE = re.compile(r"(recurrence_band|band_exact_bounds)_kernelI")
 # outside its loops.
 _OTHER_INSTANCES = [(re.compile(r"sparse_eval_kernelI"), 3, 0), (re.compile(r"sparse_graph_kernelILi1E"), 4, 0),
                     (re.compile(r"sparse_graph_kernelILi[24]E"), 4, 12), (re.compile(r"band_thresholds_kernelI"), 4, 0),
-                    (re.compile(r"cluster_rows_kernelI"), 2, 0)]
+                    (re.compile(r"cluster_rows_kernelI"), 2, 0),
+                    # products of the layer operators: two waves, whose accumulators and fragments fill the registers; a spill's reload
+                    # in the steps would make the compiler wait for all loads under way
+                    (re.compile(r"14product_kernelI"), 2, 0)]
 
 
 def parse_resource_remarks(text: str) -> dict:
