@@ -119,8 +119,9 @@ __device__ __forceinline__ void loss_stripes(const ProductArgs &g, const typenam
     }
 }
 
-// What becomes of columns n .. n + CW - 1 of row m, `cnt` of them real, in the other epilogues.
-template <class T, int EPI, int CW>
+// What becomes of columns n .. n + CW - 1 of row m, `cnt` of them real, in the other epilogues.  BARE: gradients, which have no bias, activation,
+// z or residual.
+template <class T, int EPI, bool BARE, int CW>
 __device__ __forceinline__ void finish_row(const ProductArgs &g, const Job &job, float scale, const float (&bias)[CW], int m, int n, int cnt,
                                            int wide, float (&v)[CW])
 {
@@ -154,14 +155,15 @@ __device__ __forceinline__ void finish_row(const ProductArgs &g, const Job &job,
 #pragma unroll
             for (int j = 0; j < CW; ++j) v[j] *= scale;
         }
-        put_row<T, EPI>(g, job.out_base, bias, m, n, cnt, wide, job.skip, v);
+        if (BARE) store_row<T>(g.out, job.out_base + (int64_t)m * g.ldo + n, cnt, wide, v);
+        else put_row<T, EPI>(g, job.out_base, bias, m, n, cnt, wide, job.skip, v);
     }
 }
 
 // The small tiles: each wave's rows, half of them at a time where they are many, go through LDS, from where a thread takes eight consecutive columns
 // of a row, row after row.  So the code is a short loop, whatever is aligned and whatever is not (unrolled over the accumulators it was 60 KB,
 // fetched anew for every tile), and a row's columns are written as one piece whatever the operands' form was.
-template <class T, class P, int BM, int BN, int WM, int WN, int EPI>
+template <class T, class P, int BM, int BN, int WM, int WN, int EPI, bool BARE>
 __device__ __forceinline__ void through_lds(const ProductArgs &g, const typename P::Acc &acc, char *lds, const Job &job, int wm, int wn, int i, int q)
 {
     constexpr int PARTS = P::MT > 1 ? 2 : 1, LDT = BN + 4, PART = BM / WM / PARTS, CW = 8, THREADS = BN / CW, AT_ONCE = WM * WN * 64 / THREADS;      // (four columns more: no bank twice)
@@ -172,7 +174,7 @@ __device__ __forceinline__ void through_lds(const ProductArgs &g, const typename
     float bias[CW];
 #pragma unroll
     for (int j = 0; j < CW; ++j) bias[j] = 0.0f;
-    if (g.bias && job.skip == 0 && cnt > 0) load_row<T>(g.bias, job.bias_base + n, cnt, g.wide, bias);
+    if (!BARE && g.bias && job.skip == 0 && cnt > 0) load_row<T>(g.bias, job.bias_base + n, cnt, g.wide, bias);
 #pragma unroll
     for (int h = 0; h < PARTS; ++h) {
         lds_barrier();
@@ -192,14 +194,14 @@ __device__ __forceinline__ void through_lds(const ProductArgs &g, const typename
             float v[CW];
             *(f32x4 *)v = *(const f32x4 *)(tile + row * LDT + col);
             *(f32x4 *)(v + 4) = *(const f32x4 *)(tile + row * LDT + col + 4);
-            finish_row<T, EPI>(g, job, scale, bias, m, n, cnt, g.wide, v);
+            finish_row<T, EPI, BARE>(g, job, scale, bias, m, n, cnt, g.wide, v);
         }
     }
 }
 
 // The large tile, whose LDS holds the next tile's operands: straight from the accumulators.  Everything is aligned and rows are multiples of eight
 // elements, so a lane's columns exist or do not and the code stays short.
-template <class T, class P, int EPI>
+template <class T, class P, int EPI, bool BARE>
 __device__ __forceinline__ void straight(const ProductArgs &g, const typename P::Acc &acc, const Job &job, int wm, int wn, int i, int q)
 {
     // With w in COLS a lane has four columns of each block: of two blocks lanes of even q take the first one's from their neighbour of odd q, whose
@@ -215,7 +217,7 @@ __device__ __forceinline__ void straight(const ProductArgs &g, const typename P:
         const int n = job.n0 + wn + c * CW * 4 + at;
 #pragma unroll
         for (int j = 0; j < CW; ++j) bias[c][j] = 0.0f;
-        if (g.bias && job.skip == 0 && n < g.N) load_row<T>(g.bias, job.bias_base + n, CW, 1, bias[c]);
+        if (!BARE && g.bias && job.skip == 0 && n < g.N) load_row<T>(g.bias, job.bias_base + n, CW, 1, bias[c]);
     }
     // Waited for here: to the compiler a load that no row may use is under way until its register is used again, which is in the steps of the next
     // tile, and there it would wait for all loads in every step.
@@ -244,20 +246,20 @@ __device__ __forceinline__ void straight(const ProductArgs &g, const typename P:
                 }
                 if (m >= job.m_end || n >= g.N) continue;
             }
-            finish_row<T, EPI>(g, job, scale, bias[c], m, n, CW, 1, v);
+            finish_row<T, EPI, BARE>(g, job, scale, bias[c], m, n, CW, 1, v);
         }
     }
 }
 
-template <class T, class P, int BM, int BN, int WM, int WN, int EPI>
+template <class T, class P, int BM, int BN, int WM, int WN, int EPI, bool BARE>
 __device__ __forceinline__ void epilogue(const ProductArgs &g, const typename P::Acc &acc, char *lds, const Job &job)
 {
     const int lane = threadIdx.x & 63, i = lane & 15, q = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave / WN * (BM / WM), wn = wave % WN * (BN / WN);
     if constexpr (EPI == EPI_LOSS) loss_stripes<T, P, BN / WN>(g, acc, job.m0 + wm, job.m_end, job.n0 + wn, i, q);
-    else if constexpr (P::DEEP) straight<T, P, EPI>(g, acc, job, wm, wn, i, q);
-    else through_lds<T, P, BM, BN, WM, WN, EPI>(g, acc, lds, job, wm, wn, i, q);
+    else if constexpr (P::DEEP) straight<T, P, EPI, BARE>(g, acc, job, wm, wn, i, q);
+    else through_lds<T, P, BM, BN, WM, WN, EPI, BARE>(g, acc, lds, job, wm, wn, i, q);
 }
 
 template <class T, int FA, int FB, int BM, int BN, int WM, int WN, int EPI, int GROUPING>
@@ -287,7 +289,7 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void product_kernel(const ProductAr
             deep.la.follow(next.A, steps_next);
             deep.lb.follow(next.B, steps_next);
             deep.run(steps, acc);
-            epilogue<T, P, BM, BN, WM, WN, EPI>(g, acc, lds, job);
+            epilogue<T, P, BM, BN, WM, WN, EPI, FB == COLS>(g, acc, lds, job);
             if (!more) break;
             job = next;
             steps = steps_next;
@@ -295,7 +297,7 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void product_kernel(const ProductAr
         deep.end();
     } else {
         P::run(job.A, job.B, lds, acc);
-        epilogue<T, P, BM, BN, WM, WN, EPI>(g, acc, lds, job);
+        epilogue<T, P, BM, BN, WM, WN, EPI, FB == COLS>(g, acc, lds, job);
     }
 }
 
