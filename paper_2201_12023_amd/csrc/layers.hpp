@@ -67,21 +67,20 @@ struct PackArgs {
 };
 hipError_t launch_pack(hipStream_t st, int dtype, const PackArgs &g);
 
-// dz = dy * act'(z), and sums of dz over the rows of each slot of SLOPE_ROWS rows
-constexpr int SLOPE_ROWS = 64;
+// dz = dy * act'(z), and sums of dz over the rows of each slot of `slot_rows` rows
 struct SlopeArgs {
     const char *dy, *z;             // strides in elements
     int64_t lddy, ldz;
     char *dz;                       // [rows][ldd], zeros behind N, or NULL
     int64_t ldd;
     float *part;                    // [slots][N], or NULL
-    int rows, N, slots, experts;    // experts 0: no groups
+    int rows, N, slots, slot_rows, experts;    // experts 0: no groups
     const int32_t *offsets;
-    int act, wide;
+    int act, bytes;                 // bytes: of dy and z that may be read at once, 16, 8 or 0 (one element)
 };
 hipError_t launch_slope(hipStream_t st, int dtype, const SlopeArgs &a);
 // dbias[e][n] = sum over the expert's slots
-hipError_t launch_bias_sum(hipStream_t st, int dtype, const float *part, char *dbias, int rows, int N, int slots, int experts,
+hipError_t launch_bias_sum(hipStream_t st, int dtype, const float *part, char *dbias, int rows, int N, int slots, int slot_rows, int experts,
                            const int32_t *offsets);
 // result = act(sum over splits + bias) + residual, and z (epi: EPI_LINE, EPI_SIGMOID or EPI_ERF)
 hipError_t launch_join(hipStream_t st, int dtype, Epilogue epi, const ProductArgs &a);

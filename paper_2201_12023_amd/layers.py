@@ -3,7 +3,8 @@ dense and expert layers and the loss over a vocabulary, forward and backward.
 
 Same names as the C entry points.  Arguments and results are torch tensors on one GPU; results and work memory come from
 torch's allocator, every step runs in the HIP kernels of ``libalpa_dp.so``.  Work is queued on ``stream`` (a
-torch.cuda.Stream; the current one if None) and not waited for.  The last dimension of a tensor must be contiguous, rows may be
+torch.cuda.Stream; the current one if None) and not waited for; tensors that belong to another stream are the caller's to
+order and to keep.  The last dimension of a tensor must be contiguous, rows may be
 any distance apart.
 """
 from __future__ import annotations

@@ -192,6 +192,33 @@ def test_results_larger_than_the_caches(dtype):
             C.within("z", got[1], rz, ez)
 
 
+@pytest.mark.parametrize("bytes_apart", [0, 8, 2])
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=ids)
+def test_slopes_of_few_and_of_many_rows(dtype, bytes_apart):
+    """dz with slots of 16 and of 64 rows, read by 16 bytes, by 8 and by elements, dense and ragged."""
+    g = C.gen(36)
+    pad = 0 if bytes_apart == 0 else max(bytes_apart // dtype.itemsize, 1)
+    for rows, n_out in ((331, 520), (8203, 4104)):
+        x, w = C.normal(g, dtype, rows, 24), C.normal(g, dtype, n_out, 24, scale=0.2)
+        dy, z = C.normal(g, dtype, rows, n_out), C.normal(g, dtype, rows, n_out)
+        dys, zs = (slice_of(t, pad, 0) for t in (dy, z))
+        ref = C.backward(dy, z, x, w, 2)
+        for name, got in zip(("dx", "dw", "dbias"), L.alpa_linear_backward(dys, x, w, z=zs, act=2)):
+            C.within(name, got, *ref[name])
+        ends = [0, 0, rows // 3, rows // 3 + 17, rows - 5]
+        off = torch.tensor(ends, dtype=torch.int32, device="cuda")
+        ws = torch.stack([w] * 4)
+        dx, dw, db = L.alpa_experts_backward(dys, x, ws, off, z=zs, act=2)
+        for e in range(4):
+            p = slice(ends[e], ends[e + 1])
+            if ends[e] == ends[e + 1]:
+                assert not bool(dw[e].any()) and not bool(db[e].any())
+                continue
+            ref = C.backward(dy[p], z[p], x[p], w, 2)
+            for name, got in (("dx", dx[p]), ("dw", dw[e]), ("dbias", db[e])):
+                C.within(name, got, *ref[name])
+
+
 def test_experts_tile_after_tile():
     g = C.gen(32)
     counts = [1700, 0, 3, 2500, 900, 0, 260]
