@@ -283,9 +283,10 @@ int forward(int dtype, int act, int64_t rows, int experts, int64_t n_in, int64_t
 constexpr int SMALL_SLOPE = 1 << 25;
 
 struct BackwardWork {
-    int64_t dz, part, x, w, split, total;     // offsets
+    int64_t dz, part, tops, x, w, split, total;     // offsets; tops: the scale of dz and what it is found from
     int64_t ldd;
     int slots, slot_rows;
+    bool scaled;
     // (dym, xm and wm with p NULL if they are not read)
     BackwardWork(int dtype, int act, int64_t rows, int experts, int64_t n_in, int64_t n_out, const alpa_mat_t &dym, const alpa_mat_t &xm,
                  const alpa_mat_t &wm)
@@ -295,7 +296,9 @@ struct BackwardWork {
         slots = (int)(experts < 0 ? (rows + slot_rows - 1) / slot_rows : slots_at_most(rows, experts, slot_rows));
         dz = 0;
         part = dz + (act == ALPA_ACT_NONE ? pack_bytes(dym, rows, n_out, dtype) : block(rows * ldd * element(dtype)));
-        x = part + block((int64_t)slots * n_out * 4);
+        scaled = dtype == ALPA_F16 && act >= ALPA_ACT_GELU && rows > 0;
+        tops = part + block((int64_t)slots * n_out * 4);
+        x = tops + (scaled ? block((1 + TOP_PARTS) * 4) : 0);
         w = x + pack_bytes(xm, rows, n_in, dtype);
         split = w + (rows ? pack_bytes(wm, n_out * std::max(experts, 1), n_in, dtype) : 0);
         int64_t most = 0;
@@ -325,6 +328,7 @@ int backward(int dtype, int act, int64_t rows, int experts, int64_t n_in, int64_
 
     const bool grouped = experts >= 0, has_z = act != ALPA_ACT_NONE, products = dx.p || dw.p;
     Source dz{(const char *)dy.p, dy.ld, n_out}, xs{}, ws{};
+    float *const scale = at.scaled ? (float *)(work + at.tops) : nullptr;
     if (rows > 0 && (dbias || (has_z && products))) {
         SlopeArgs s{};
         const int64_t es = element(dtype);
@@ -336,6 +340,8 @@ int backward(int dtype, int act, int64_t rows, int experts, int64_t n_in, int64_
             s.dz = work + at.dz;
             s.ldd = at.ldd;
             dz = Source{s.dz, at.ldd, at.ldd};
+            s.scale = scale;
+            s.tops = scale ? scale + 1 : nullptr;
         }
         s.part = dbias ? (float *)(work + at.part) : nullptr;
         s.rows = (int)rows;
@@ -357,6 +363,7 @@ int backward(int dtype, int act, int64_t rows, int experts, int64_t n_in, int64_
     if (dx.p && rows > 0) {
         ProductArgs g = operands(FORM_RC, dz, ws, n_out, dtype);
         result(g, dx);
+        g.scale = scale;
         g.offsets = offsets;
         g.b_expert = n_out * g.ldb;
         TRY(run_product(st, dtype, FORM_RC, EPI_LINE, Shape{rows, n_in, n_out, grouped ? GROUP_ROWS : GROUP_NONE, std::max(experts, 0)}, g,
@@ -365,6 +372,7 @@ int backward(int dtype, int act, int64_t rows, int experts, int64_t n_in, int64_
     if (dw.p) {
         ProductArgs g = operands(FORM_CC, dz, xs, rows, dtype);
         result(g, dw);
+        g.scale = scale;
         g.offsets = offsets;
         g.b_expert = n_out * dw.ld;
         TRY(run_product(st, dtype, FORM_CC, EPI_LINE, Shape{n_out, n_in, rows, grouped ? GROUP_STEPS : GROUP_NONE, std::max(experts, 0)}, g,

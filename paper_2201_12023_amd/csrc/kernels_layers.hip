@@ -3,6 +3,8 @@
 #include "epilogue.hpp"
 #include "slots.hpp"
 
+#include <type_traits>
+
 namespace alpa {
 
 // ---------------------------------------------------------------- rows in 16-byte units
@@ -55,6 +57,54 @@ __device__ __forceinline__ float slope_of(float z, int act)
     return s + z * s * (1.0f - s) * (c1 + 3.0f * c3 * zz);
 }
 
+// Float16 has room for neither end: a slope of 1.13 takes a dy of 6e4 past its largest value, and a dy of 1e-6 has four bits left, which dz would lose.
+// So dz is kept times a power of two that brings the largest |dy| to 2^13 .. 2^14, and the products' results are given the inverse: powers of two
+// are exact, so no other result changes.  (bfloat16 has the exponents of 32 bits; relu's slopes are 0 and 1, dz is a dy then.)  The largest value is
+// looked for in a pass of its own (3001 x 1500 in 16 bits: 7 us of a backward pass of 75; 8192 x 16384: 71 of 1930).  Here its parts: a wave takes every so-many-th row, a lane V consecutive columns; rows of no
+// expert and values that are not finite do not count.
+template <int V>
+__global__ __launch_bounds__(256) void top_kernel(const SlopeArgs g)
+{
+    __shared__ float tops[4];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    int first = 0, end = g.rows;
+    if (g.experts) {
+        first = min(max(g.offsets[0], 0), g.rows);
+        end = min(max(g.offsets[g.experts], 0), g.rows);
+    }
+    float top = 0.0f;
+    for (int n = (blockIdx.y * 64 + lane) * V; n < g.N; n += gridDim.y * 64 * V) {
+#pragma unroll 4
+        for (int m = first + blockIdx.x * 4 + wave; m < end; m += gridDim.x * 4) {
+            float d[V];
+            load_row<f16>(g.dy, (int64_t)m * g.lddy + n, g.N - n, V > 1, d);
+#pragma unroll
+            for (int j = 0; j < V; ++j) top = fabsf(d[j]) < INFINITY ? fmaxf(top, fabsf(d[j])) : top;
+        }
+    }
+#pragma unroll
+    for (int off = 32; off; off >>= 1) top = fmaxf(top, __shfl_xor(top, off, 64));
+    if (lane == 0) tops[wave] = top;
+    __syncthreads();
+    if (threadIdx.x == 0) g.tops[blockIdx.y * gridDim.x + blockIdx.x] = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
+}
+
+// The power of two that dz is multiplied with, found by a workgroup from the parts' largest values.
+__device__ __forceinline__ float factor_of(const float *parts, int count)
+{
+    __shared__ float tops[4];
+    float top = 0.0f;
+    for (int k = threadIdx.x; k < count; k += 256) top = fmaxf(top, parts[k]);
+#pragma unroll
+    for (int off = 32; off; off >>= 1) top = fmaxf(top, __shfl_xor(top, off, 64));
+    if ((threadIdx.x & 63) == 0) tops[threadIdx.x >> 6] = top;
+    __syncthreads();
+    top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
+    int e = 14;
+    if (top > 0.0f) (void)frexpf(top, &e);
+    return ldexpf(1.0f, 14 - e);
+}
+
 // A workgroup takes a slot of rows and 64 * V columns; a wave every fourth row, a lane V consecutive columns.  One pass: dy
 // and z are read once, dz written once, and the sums of a slot go to `part`, to be added in the order of the slots.
 template <class T, int V, bool HAS_Z>
@@ -71,6 +121,13 @@ __global__ __launch_bounds__(256) void slope_kernel(const SlopeArgs g)
         end = s.end;
         skip = s.expert < 0 || s.expert >= g.experts;      // rows of no expert: their dz is read by nobody
     }
+    float by = 1.0f;
+    if constexpr (std::is_same_v<T, f16> && HAS_Z) {
+        if (g.tops) {
+            by = factor_of(g.tops, g.top_count);
+            if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *g.scale = 1.0f / by;
+        }
+    }
     float sum[V];
 #pragma unroll
     for (int j = 0; j < V; ++j) sum[j] = 0.0f;
@@ -84,7 +141,12 @@ __global__ __launch_bounds__(256) void slope_kernel(const SlopeArgs g)
                 load_row<T>(g.z, (int64_t)m * g.ldz + n, cnt, V > 1, z);
 #pragma unroll
                 for (int j = 0; j < V; ++j) d[j] *= slope_of<T>(z[j], g.act);
-                if (g.dz) store_row<T>(g.dz, (int64_t)m * g.ldd + n, V, 1, d);       // (behind N: zeros)
+                if (g.dz) {                                                           // (behind N: zeros)
+                    float kept[V];
+#pragma unroll
+                    for (int j = 0; j < V; ++j) kept[j] = d[j] * by;
+                    store_row<T>(g.dz, (int64_t)m * g.ldd + n, V, 1, kept);
+                }
             }
 #pragma unroll
             for (int j = 0; j < V; ++j) sum[j] += d[j];
@@ -112,6 +174,22 @@ hipError_t slope_wide(hipStream_t st, const SlopeArgs &g)
     return hipGetLastError();
 }
 
+// TOP_PARTS workgroups at most, each with four rows and more
+dim3 top_grid(const SlopeArgs &g)
+{
+    const int per = 64 * (g.bytes ? g.bytes / 2 : 1), columns = std::min((g.N + per - 1) / per, TOP_PARTS);
+    return dim3((unsigned)std::min((g.rows + 15) / 16, TOP_PARTS / columns), (unsigned)columns);
+}
+
+hipError_t launch_top(hipStream_t st, const SlopeArgs &g)
+{
+    const dim3 grid = top_grid(g);
+    if (g.bytes == 16) top_kernel<8><<<grid, 256, 0, st>>>(g);
+    else if (g.bytes == 8) top_kernel<4><<<grid, 256, 0, st>>>(g);
+    else top_kernel<1><<<grid, 256, 0, st>>>(g);
+    return hipGetLastError();
+}
+
 // (3001 x 1500 in 16 bits, rows aligned to 8 bytes: 12.4 us by 8 bytes, 18 by elements)
 template <class T>
 hipError_t slope_typed(hipStream_t st, const SlopeArgs &g)
@@ -119,8 +197,15 @@ hipError_t slope_typed(hipStream_t st, const SlopeArgs &g)
     return g.bytes == 16 ? slope_wide<T, 16 / sizeof(T)>(st, g) : g.bytes == 8 ? slope_wide<T, 8 / sizeof(T)>(st, g) : slope_wide<T, 1>(st, g);
 }
 
-hipError_t launch_slope(hipStream_t st, int dtype, const SlopeArgs &g)
+hipError_t launch_slope(hipStream_t st, int dtype, const SlopeArgs &args)
 {
+    SlopeArgs g = args;
+    if (g.tops) {
+        const dim3 grid = top_grid(g);
+        g.top_count = (int)(grid.x * grid.y);
+        const hipError_t e = launch_top(st, g);
+        if (e != hipSuccess) return e;
+    }
     return dtype == 0 ? slope_typed<float>(st, g) : dtype == 1 ? slope_typed<f16>(st, g) : slope_typed<bf16>(st, g);
 }
 

@@ -77,7 +77,10 @@ struct SlopeArgs {
     int rows, N, slots, slot_rows, experts;    // experts 0: no groups
     const int32_t *offsets;
     int act, bytes;                 // bytes: of dy and z that may be read at once, 16, 8 or 0 (one element)
+    float *tops, *scale;            // float16: dz is kept divided by *scale, a power of two found here (tops, [TOP_PARTS]: room for that; NULL: as it is)
+    int top_count;
 };
+constexpr int TOP_PARTS = 1024;
 hipError_t launch_slope(hipStream_t st, int dtype, const SlopeArgs &a);
 // dbias[e][n] = sum over the expert's slots
 hipError_t launch_bias_sum(hipStream_t st, int dtype, const float *part, char *dbias, int rows, int N, int slots, int slot_rows, int experts,

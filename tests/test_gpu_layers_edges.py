@@ -1,0 +1,75 @@
+"""The layer operators on the device where types and sizes end (bounds: tests/layer_cases.py)."""
+import pytest
+import torch
+
+from paper_2201_12023_amd import layers as L
+from tests import layer_cases as C
+
+pytestmark = pytest.mark.gpu
+BF16, F16, F32 = torch.bfloat16, torch.float16, torch.float32
+
+
+def gradients(dy, z, x, w, kind):
+    """layer_cases.backward for a dz that keeps the bits of a float16 whatever dy's size: it is multiplied by a power of two that
+    brings the largest |dy| to 2^13 at least, so a dz is off by U relative and TINY 2^-13 of that largest |dy|."""
+    t, rows, n_out = dy.dtype, dy.shape[0], dy.shape[1]
+    dy, x, w = dy.to(C.D), x.to(C.D), w.to(C.D)
+    dz = dy * C.act(z.to(C.D), kind)[1]
+    exact_off = (C.ACT_ERR * 2 + 2 * C.STEP) * dy.abs()
+    off = exact_off + C.U[t] * (dz.abs() + exact_off) + C.TINY[t] * 2.0 ** -13 * dy.abs().max()
+    out = {}
+    for name, a, ao, b, n in (("dx", dz, off, w, n_out), ("dw", dz.t(), off.t(), x, rows)):
+        v = a @ b
+        e = (ao + (n + 1) * C.STEP * (a.abs() + ao)) @ b.abs()
+        out[name] = (v, e + C.U[t] * (v.abs() + e) + C.TINY[t])
+    return out
+
+
+# a dy of 6e4 times a slope of 1.13 is no float16, a dy of 1e-6 has four bits left as one
+@pytest.mark.parametrize("kind", [2, 3, 4])
+@pytest.mark.parametrize("size, other", [(6e4, 1e-3), (1e-6, 64.0)], ids=["large", "small"])
+@pytest.mark.parametrize("pad", [0, 4, 3])
+def test_float16_keeps_gradients_of_any_size(kind, size, other, pad):
+    g = C.gen(41 + pad)
+    rows, n_in, n_out = 517, 72, 264
+    x, w = C.normal(g, F16, rows, n_in, scale=other), C.normal(g, F16, n_out, n_in, scale=other)
+    wide = (torch.randint(0, 2, (rows, n_out + pad), device="cuda", generator=g) * 2 - 1) * (0.9 + 0.1 * torch.rand(rows, n_out + pad, device="cuda",
+                                                                                                               generator=g)) * size
+    dy = wide.to(F16)[:, :n_out]
+    z = torch.rand(rows, n_out, device="cuda", generator=g).mul_(2.0).add_(0.5).to(F16)
+    ref = gradients(dy, z, x, w, kind)
+    dx, dw, _ = L.alpa_linear_backward(dy, x, w, z=z, act=kind, need=("x", "w"))
+    C.within("dx", dx, *ref["dx"])
+    C.within("dw", dw, *ref["dw"])
+    # rows of no expert say nothing about the others' size
+    ends = [5, 200, 200, 500]
+    loud, quiet = torch.full_like(dy, 6e4), torch.zeros(rows, dtype=torch.bool, device="cuda")
+    quiet[ends[0]:ends[-1]] = True
+    mixed = torch.where(quiet[:, None], dy, loud)
+    mixed[-1] = float("nan")
+    off = torch.tensor(ends, dtype=torch.int32, device="cuda")
+    ws = torch.stack([w, w, -w])
+    dx, dw, _ = L.alpa_experts_backward(mixed, x, ws, off, z=z, act=kind, need=("x", "w"))
+    for e in (0, 2):
+        p = slice(ends[e], ends[e + 1])
+        ref = gradients(dy[p], z[p], x[p], ws[e], kind)
+        C.within("dx", dx[p], *ref["dx"])
+        C.within("dw", dw[e], *ref["dw"])
+
+
+def test_float16_gradients_of_zeros_and_of_infinities():
+    rows, n_in, n_out = 40, 16, 24
+    x, w = torch.ones(rows, n_in, dtype=F16, device="cuda"), torch.ones(n_out, n_in, dtype=F16, device="cuda")
+    z = torch.ones(rows, n_out, dtype=F16, device="cuda")
+    dy = torch.zeros(rows, n_out, dtype=F16, device="cuda")
+    dx, dw, db = L.alpa_linear_backward(dy, x, w, z=z, act=3)
+    assert not bool(dx.any()) and not bool(dw.any()) and not bool(db.any())
+    dy[3, 5] = float("inf")
+    dy[7] = 1e-6
+    dx, dw, _ = L.alpa_linear_backward(dy, x, w, z=z, act=4)
+    assert bool(torch.isinf(dx[3]).all()) and bool(torch.isinf(dw[5]).all())
+    ref = gradients(dy[7:8], z[7:8], x[7:8], w, 4)["dx"]
+    C.within("dx", dx[7:8], *ref)
+    dy[3, 5] = float("nan")
+    dx, dw, _ = L.alpa_linear_backward(dy, x, w, z=z, act=4)
+    assert bool(torch.isnan(dx[3]).all()) and bool(torch.isnan(dw[5]).all()) and not bool(torch.isnan(dw[4]).any())
