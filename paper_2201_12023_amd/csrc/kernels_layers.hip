@@ -297,37 +297,43 @@ __device__ __forceinline__ float2 join_stat(float2 a, float2 b)
     return make_float2(top, a.y * expf(a.x - ref) + b.y * expf(b.x - ref));
 }
 
-// Sixteen rows a workgroup; sixty-four threads a row take every sixty-fourth stripe, in order, and are joined in order by eights.
+// Sixteen rows at a time; sixty-four threads a row take every sixty-fourth stripe, in order, and are joined in order by eights.
+constexpr int LOSS_GROUPS = 1 << 21;               // (a grid's threads are counted in 32 bits)
+
 __global__ __launch_bounds__(1024) void loss_kernel(const float2 *stat, int stripes, int rows, const float *at_target,
                                                     const int64_t *target, int64_t words, float *loss, float *lse)
 {
     __shared__ float2 share[64][17], eights[8][17];
-    const int r = threadIdx.x & 15, part = threadIdx.x >> 4, m = blockIdx.x * 16 + r;
-    float2 s = make_float2(-INFINITY, 0.0f);
-    if (m < rows) {
+    const int r = threadIdx.x & 15, part = threadIdx.x >> 4;
+    for (int first = blockIdx.x * 16; first < rows; first += gridDim.x * 16) {
+        const int m = first + r;
+        float2 s = make_float2(-INFINITY, 0.0f);
+        if (m < rows) {
 #pragma unroll 4
-        for (int j = part; j < stripes; j += 64) s = join_stat(s, stat[(int64_t)j * rows + m]);
+            for (int j = part; j < stripes; j += 64) s = join_stat(s, stat[(int64_t)j * rows + m]);
+        }
+        __syncthreads();                           // (the rows before have been joined)
+        share[part][r] = s;
+        __syncthreads();
+        if (part < 8) {
+            s = share[part * 8][r];
+            for (int j = 1; j < 8; ++j) s = join_stat(s, share[part * 8 + j][r]);
+            eights[part][r] = s;
+        }
+        __syncthreads();
+        if (part != 0 || m >= rows) continue;
+        for (int j = 1; j < 8; ++j) s = join_stat(s, eights[j][r]);
+        const float l = s.x + logf(s.y);
+        const int64_t word = target[m];
+        lse[m] = l;
+        loss[m] = word < 0 ? 0.0f : word >= words ? NAN : l - at_target[m];
     }
-    share[part][r] = s;
-    __syncthreads();
-    if (part < 8) {
-        s = share[part * 8][r];
-        for (int j = 1; j < 8; ++j) s = join_stat(s, share[part * 8 + j][r]);
-        eights[part][r] = s;
-    }
-    __syncthreads();
-    if (part != 0 || m >= rows) return;
-    for (int j = 1; j < 8; ++j) s = join_stat(s, eights[j][r]);
-    const float l = s.x + logf(s.y);
-    const int64_t word = target[m];
-    lse[m] = l;
-    loss[m] = word < 0 ? 0.0f : word >= words ? NAN : l - at_target[m];
 }
 
 hipError_t launch_loss(hipStream_t st, const float2 *stat, int stripes, int rows, const float *at_target, const int64_t *target,
                        int64_t words, float *loss, float *lse)
 {
-    loss_kernel<<<(unsigned)((rows + 15) / 16), 1024, 0, st>>>(stat, stripes, rows, at_target, target, words, loss, lse);
+    loss_kernel<<<(unsigned)std::min((rows + 15) / 16, LOSS_GROUPS), 1024, 0, st>>>(stat, stripes, rows, at_target, target, words, loss, lse);
     return hipGetLastError();
 }
 

@@ -73,3 +73,19 @@ def test_float16_gradients_of_zeros_and_of_infinities():
     dy[3, 5] = float("nan")
     dx, dw, _ = L.alpa_linear_backward(dy, x, w, z=z, act=4)
     assert bool(torch.isnan(dx[3]).all()) and bool(torch.isnan(dw[5]).all()) and not bool(torch.isnan(dw[4]).any())
+
+
+def test_loss_of_more_rows_than_a_launch_has_room_for():
+    """2^26 rows and some, 64 threads a row: more threads than HIP counts in a grid."""
+    g = C.gen(42)
+    rows, n_in, words = (1 << 26) + 21, 8, 3
+    w = C.normal(g, BF16, words, n_in)
+    x = torch.empty(rows, n_in, dtype=BF16, device="cuda")
+    x.view(torch.int16).random_(0x3f80, 0x4000, generator=g)                   # (the bits of 1 to 2)
+    t = torch.arange(rows, device="cuda") % (words + 1) - 1
+    loss, lse = L.alpa_vocab_loss_forward(x, w, t)
+    for part in (slice(0, 50000), slice((1 << 25) - 20000, (1 << 25) + 20000), slice(rows - 50000, rows)):
+        ref = C.vocab(x[part], w, t[part], None)
+        C.within("loss", loss[part], *ref["loss"])
+        C.within("lse", lse[part], *ref["lse"])
+    assert bool(torch.isfinite(lse).all()) and not bool(loss[::words + 1].any()) and bool((loss >= 0).all())
