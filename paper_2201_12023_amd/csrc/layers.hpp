@@ -26,6 +26,7 @@ struct ProductArgs {
     const int32_t *offsets;
     int64_t b_expert;               // GROUP_ROWS: bytes from an expert's b to the next one's; GROUP_STEPS: result elements
     int row_tiles, col_tiles;       // grid: row tiles (GROUP_ROWS: slots), column tiles; GROUP_STEPS: times experts
+    int before;                     // of each XCD's tiles, those that earlier launches took
     int splits, split_steps;        // of the contraction, 128 bytes a step, all of them if it is not split (GROUP_NONE only)
     // epilogue
     char *out;                      // result, strides in elements

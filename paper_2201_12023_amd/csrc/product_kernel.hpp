@@ -268,7 +268,7 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void product_kernel(const ProductAr
     using P = Product<T, FA, FB, BM, BN, WM, WN>;
     __shared__ __align__(1024) char lds[P::LDS_BYTES];
     const Walk<T, FA, FB, BM, BN, GROUPING> walk(g);
-    int i = blockIdx.x >> 3;
+    int i = (P::DEEP ? 0 : g.before) + (blockIdx.x >> 3);
     if (i >= walk.count) return;
     Job job = walk.at(g, i);
     typename P::Acc acc;
@@ -306,11 +306,23 @@ hipError_t launch_tiles(hipStream_t st, int tile, const ProductArgs &g)
 {
     const int64_t tiles = (int64_t)g.row_tiles * g.col_tiles;
     const int64_t all = GROUPING == GROUP_STEPS ? (tiles + 7) / 8 * 8 * g.experts : tiles;
-    const dim3 grid((unsigned)(tile == BIG_TILE && all > COMPUTE_UNITS ? COMPUTE_UNITS : all), (unsigned)g.splits);
-    if (tile == BIG_TILE) product_kernel<T, FA, FB, 256, 256, 2, 4, EPI, GROUPING><<<grid, 512, 0, st>>>(g);
-    else if (tile == TILE) product_kernel<T, FA, FB, 128, 128, 2, 2, EPI, GROUPING><<<grid, 256, 0, st>>>(g);
-    else product_kernel<T, FA, FB, 64, 64, 4, 1, EPI, GROUPING><<<grid, 256, 0, st>>>(g);
-    return hipGetLastError();
+    if (tile == BIG_TILE) {
+        const dim3 grid((unsigned)std::min<int64_t>(all, COMPUTE_UNITS), (unsigned)g.splits);
+        product_kernel<T, FA, FB, 256, 256, 2, 4, EPI, GROUPING><<<grid, 512, 0, st>>>(g);
+        return hipGetLastError();
+    }
+    // (a grid's threads are counted in 32 bits)
+    constexpr int64_t MOST = 1 << 23;
+    ProductArgs part = g;
+    for (int64_t done = 0; done < all; done += MOST) {
+        part.before = (int)(done / 8);
+        const dim3 grid((unsigned)std::min(all - done, MOST), (unsigned)g.splits);
+        if (tile == TILE) product_kernel<T, FA, FB, 128, 128, 2, 2, EPI, GROUPING><<<grid, 256, 0, st>>>(part);
+        else product_kernel<T, FA, FB, 64, 64, 4, 1, EPI, GROUPING><<<grid, 256, 0, st>>>(part);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 template <class T>

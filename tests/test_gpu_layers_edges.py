@@ -89,3 +89,22 @@ def test_loss_of_more_rows_than_a_launch_has_room_for():
         C.within("loss", loss[part], *ref["loss"])
         C.within("lse", lse[part], *ref["lse"])
     assert bool(torch.isfinite(lse).all()) and not bool(loss[::words + 1].any()) and bool((loss >= 0).all())
+
+
+def test_gradients_of_more_tiles_than_a_launch_has_room_for():
+    """300000 weights for each of 4096 experts, in tiles of 128: two launches (tests/test_layers_host_side.py).  An expert has one
+    row or none, so its gradient is one product, exact in 32 bits and rounded once."""
+    g = C.gen(43)
+    rows, experts, n_in = 1500, 4096, 300000
+    has = torch.zeros(experts, dtype=torch.bool, device="cuda")
+    has[torch.randperm(experts, device="cuda", generator=g)[:rows]] = True
+    off = torch.cat([has.new_zeros(1).int(), torch.cumsum(has, 0).int()])
+    assert int(off[-1]) == rows
+    x, dy = C.normal(g, BF16, rows, n_in), C.normal(g, BF16, rows, 1)
+    w = torch.empty(experts, 1, n_in, dtype=BF16, device="cuda")               # (only its shape is used)
+    _, dw, _ = L.alpa_experts_backward(dy, x, w, off, need=("w",))
+    assert not bool(dw[~has].any())
+    for e0, t0 in ((0, 0), (experts // 2, int(off[experts // 2])), (experts - 200, int(off[experts - 200]))):
+        mine = torch.nonzero(has[e0:e0 + 200])[:, 0] + e0
+        t = torch.arange(t0, t0 + len(mine), device="cuda")
+        assert torch.equal(dw[mine, 0], (dy[t].float() * x[t].float()).to(BF16))

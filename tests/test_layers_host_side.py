@@ -21,3 +21,19 @@ def test_loss_of_many_rows_is_launched(driver, rows):
     call, = Q.calls(driver, [("loss", BF16, rows, 8, 64)])
     assert call.rc == 0 and "loss_kernel" in call.launches[-1][0]
     assert call.launches[-1][1] == min((rows + 15) // 16, 1 << 21)
+
+
+@pytest.mark.parametrize("line", [("backward", BF16, 0, 809, 3357, 922983, 7, 922983, 922983, 0, 1, 1),
+                                  ("backward", BF16, 0, 1500, 4096, 300000, 1, 300000, 300000, 0, 0, 1),
+                                  ("forward", BF16, 0, 4096, 4096, 8, 1 << 20, 8, 1 << 20, 0, 0, 0)])
+def test_products_of_many_tiles_are_launched(driver, line):
+    """Weights of 4096 experts make more tiles than one launch has threads for: every tile is in one of the launches."""
+    call, = Q.calls(driver, [line])
+    assert call.rc == 0
+    _, _, _, rows, experts, n_in, n_out = line[:7]
+    for p in Q.products(call):
+        assert p.grid <= 1 << 23
+    steps = [p for p in Q.products(call) if p.grouping == "STEPS"]
+    if steps and steps[0].tile < 256:
+        t = steps[0].tile
+        assert sum(p.grid for p in steps) == -(-(-(-n_out // t) * -(-n_in // t)) // 8) * 8 * experts
