@@ -102,6 +102,7 @@ int alpa_experts_backward(int dtype, int act, int64_t rows, int experts, int64_t
  *           are the gradients it has a part in.
  *   loss    DEVICE float [rows]: log(sum_v exp(l_v)) - l_target.
  *   lse     DEVICE float [rows]: the logarithm, which the backward pass takes back.
+ * Work memory holds two floats for every row and 64 words, an eighth of a byte a logit.
  */
 int64_t alpa_vocab_loss_forward_work(int dtype, int64_t rows, int64_t n_in, int64_t words, alpa_mat_t x, alpa_mat_t w);
 int alpa_vocab_loss_forward(int dtype, int64_t rows, int64_t n_in, int64_t words, alpa_mat_t x, alpa_mat_t w,
@@ -110,7 +111,8 @@ int alpa_vocab_loss_forward(int dtype, int64_t rows, int64_t n_in, int64_t words
 
 /*
  * Its gradients for loss gradients dloss (DEVICE float [rows]):   g = (softmax(l) - onehot(target)) * dloss,   dx = g w,   dw = g^T x.
- *   l is computed again, a piece of the words at a time.  g is rounded to `dtype` as an operand of the two products, divided by the
+ *   l is computed again, a piece of the words at a time, and with many rows a block of them: 256 MiB of work memory at most, beside what it takes to
+ *   sum dx, and dw of a piece, in 32 bits over several of them.  g is rounded to `dtype` as an operand of the two products, divided by the
  *   largest |dloss| (found on the device) so that small probabilities keep their bits in 16-bit floats.  dx or dw may be NULL.  A row without a
  *   loss is not read into dx; in dw it counts as 0 times its x.
  */

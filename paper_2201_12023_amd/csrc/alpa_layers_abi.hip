@@ -396,15 +396,22 @@ int check_experts(int experts, const int32_t *offsets)
 int64_t stripes_of(int64_t words) { return (words + STRIPE - 1) / STRIPE; }
 
 // A piece's gradient of the logits is kept to 256 MiB, what the last-level cache holds, in pieces of one size: a multiple of the columns that
-// give every compute unit the same number of the larger tiles.
+// give every compute unit the same number of the larger tiles.  A piece has 1024 words at least, as far as there are so many, so that its products
+// have depth; rows that would then make it larger (131072 in 16 bits) go in blocks, whose shares of dw are summed in 32 bits.
 struct LossWork {
     int64_t pieces, piece;              // number, words in each
-    int64_t coef, scale, x, w, grad, sum, split, total;
-    LossWork(int dtype, int64_t rows, int64_t n_in, int64_t words, const alpa_mat_t &xm, const alpa_mat_t &wm)
+    int64_t blocks, rows;               // number, rows in each
+    int64_t coef, scale, x, w, grad, sum, sum_w, split, total;
+    LossWork(int dtype, int64_t all_rows, int64_t n_in, int64_t words, const alpa_mat_t &xm, const alpa_mat_t &wm)
     {
-        const int64_t es = element(dtype), r = std::max<int64_t>(rows, 1), row_tiles = (r + BIG_TILE - 1) / BIG_TILE;
-        const int64_t most = std::min<int64_t>(std::max<int64_t>((256ll << 20) / (r * es) / BIG_TILE * BIG_TILE, 4 * BIG_TILE),
-                                               MAX_STRIDE / es);
+        constexpr int64_t ROOM = 256ll << 20;
+        const int64_t es = element(dtype), least = std::min<int64_t>(4 * BIG_TILE, round_up(words, BIG_TILE));
+        const int64_t most_rows = ROOM / (least * es);
+        blocks = std::max<int64_t>((all_rows + most_rows - 1) / most_rows, 1);
+        rows = blocks > 1 ? round_up((all_rows + blocks - 1) / blocks, BIG_TILE) : all_rows;
+        blocks = std::max<int64_t>(rows ? (all_rows + rows - 1) / rows : 1, 1);
+        const int64_t r = std::max<int64_t>(rows, 1), row_tiles = (r + BIG_TILE - 1) / BIG_TILE;
+        const int64_t most = std::min<int64_t>(std::max<int64_t>(ROOM / (r * es) / BIG_TILE * BIG_TILE, least), MAX_STRIDE / es);
         int64_t even = BIG_TILE;
         while (even * 2 <= most && even / BIG_TILE * row_tiles % 256 != 0) even *= 2;
         pieces = (words + most - 1) / most;
@@ -412,18 +419,19 @@ struct LossWork {
         pieces = (words + piece - 1) / piece;
         piece = std::min(piece, round_up(words, BIG_TILE));
         coef = 0;
-        scale = coef + block(r * 4);
+        scale = coef + block(std::max<int64_t>(all_rows, 1) * 4);
         x = scale + 256;
-        w = x + pack_bytes(xm, rows, n_in, dtype);
+        w = x + pack_bytes(xm, all_rows, n_in, dtype);
         // (of the weights, a piece at a time; those behind the first piece lie as that does or not, so there may be room for nothing)
-        grad = w + piece_bytes(wm, rows, n_in, dtype);
+        grad = w + piece_bytes(wm, all_rows, n_in, dtype);
         sum = grad + block(r * piece * es);
-        split = sum + (pieces > 1 ? block(r * n_in * 4) : 0);
-        const int64_t last = words - (pieces - 1) * piece;
-        total = split + std::max(std::max(split_bytes(Shape{rows, n_in, last, GROUP_NONE, 0}, dtype),
-                                          split_bytes(Shape{last, n_in, rows, GROUP_NONE, 0}, dtype)),
-                                 std::max(split_bytes(Shape{rows, n_in, piece, GROUP_NONE, 0}, dtype),
-                                          split_bytes(Shape{piece, n_in, rows, GROUP_NONE, 0}, dtype)));
+        sum_w = sum + (pieces > 1 ? block(all_rows * n_in * 4) : 0);
+        split = sum_w + (blocks > 1 ? block(piece * n_in * 4) : 0);
+        int64_t parts = 0;
+        for (const int64_t m : {rows, all_rows - (blocks - 1) * rows})
+            for (const int64_t n : {piece, words - (pieces - 1) * piece})
+                parts = std::max(parts, std::max(split_bytes(Shape{m, n_in, n, GROUP_NONE, 0}, dtype), split_bytes(Shape{n, n_in, m, GROUP_NONE, 0}, dtype)));
+        total = split + parts;
     }
     int64_t piece_bytes(const alpa_mat_t &wm, int64_t rows, int64_t n_in, int dtype) const
     {
@@ -575,29 +583,37 @@ int alpa_vocab_loss_backward(int dtype, int64_t rows, int64_t n_in, int64_t word
             if (p == 0) xs = packs.add(x, rows, n_in, dtype, base + at.x);
             ws = packs.add(alpa_mat_t{(char *)w.p + word0 * w.ld * es, w.ld}, n, n_in, dtype, base + at.w);
             TRY(packs.queue(st, dtype));
-            ProductArgs g = operands(FORM_RR, xs, ws, n_in, dtype);
-            result(g, alpa_mat_t{base + at.grad, at.piece});
-            g.target = target;
-            g.word0 = word0;
-            g.lse = lse;
-            g.coef = coef;
-            TRY(run_product(st, dtype, FORM_RR, EPI_GRAD, Shape{rows, n, n_in, GROUP_NONE, 0}, g, nullptr));
         }
-        if (dx.p && rows > 0) {
-            ProductArgs g = operands(FORM_RC, grad, ws, n, dtype);
-            result(g, dx);
-            g.scale = scale;
-            g.sum = (float *)(base + at.sum);
-            g.first = p == 0;
-            g.last = p + 1 == at.pieces;
-            TRY(run_product(st, dtype, FORM_RC, at.pieces > 1 ? EPI_SUM : EPI_LINE, Shape{rows, n_in, n, GROUP_NONE, 0}, g,
-                            base + at.split));
-        }
-        if (dw.p) {
-            ProductArgs g = operands(FORM_CC, grad, xs, rows, dtype);
-            result(g, alpa_mat_t{(char *)dw.p + word0 * dw.ld * es, dw.ld});
-            g.scale = scale;
-            TRY(run_product(st, dtype, FORM_CC, EPI_LINE, Shape{n, n_in, rows, GROUP_NONE, 0}, g, base + at.split));
+        for (int64_t b = 0; b < at.blocks; ++b) {
+            const int64_t row0 = b * at.rows, m = std::min(at.rows, rows - row0);
+            const Source xb{xs.p + row0 * xs.ld * es, xs.ld, xs.len};
+            if (rows > 0) {
+                ProductArgs g = operands(FORM_RR, xb, ws, n_in, dtype);
+                result(g, alpa_mat_t{base + at.grad, at.piece});
+                g.target = target + row0;
+                g.word0 = word0;
+                g.lse = lse + row0;
+                g.coef = coef + row0;
+                TRY(run_product(st, dtype, FORM_RR, EPI_GRAD, Shape{m, n, n_in, GROUP_NONE, 0}, g, nullptr));
+            }
+            if (dx.p && rows > 0) {
+                ProductArgs g = operands(FORM_RC, grad, ws, n, dtype);
+                result(g, alpa_mat_t{(char *)dx.p + row0 * dx.ld * es, dx.ld});
+                g.scale = scale;
+                g.sum = (float *)(base + at.sum) + row0 * n_in;
+                g.first = p == 0;
+                g.last = p + 1 == at.pieces;
+                TRY(run_product(st, dtype, FORM_RC, at.pieces > 1 ? EPI_SUM : EPI_LINE, Shape{m, n_in, n, GROUP_NONE, 0}, g, base + at.split));
+            }
+            if (dw.p) {
+                ProductArgs g = operands(FORM_CC, grad, xb, m, dtype);
+                result(g, alpa_mat_t{(char *)dw.p + word0 * dw.ld * es, dw.ld});
+                g.scale = scale;
+                g.sum = (float *)(base + at.sum_w);
+                g.first = b == 0;
+                g.last = b + 1 == at.blocks;
+                TRY(run_product(st, dtype, FORM_CC, at.blocks > 1 ? EPI_SUM : EPI_LINE, Shape{n, n_in, m, GROUP_NONE, 0}, g, base + at.split));
+            }
         }
     }
     return ALPA_DP_OK;

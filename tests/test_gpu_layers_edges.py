@@ -108,3 +108,28 @@ def test_gradients_of_more_tiles_than_a_launch_has_room_for():
         mine = torch.nonzero(has[e0:e0 + 200])[:, 0] + e0
         t = torch.arange(t0, t0 + len(mine), device="cuda")
         assert torch.equal(dw[mine, 0], (dy[t].float() * x[t].float()).to(BF16))
+
+
+@pytest.mark.parametrize("dtype, rows", [(BF16, 131072 + 1000), (F32, 3 * 65536 - 77)], ids=["bf16", "f32"])
+@pytest.mark.parametrize("words, n_in", [(1024, 24), (2100, 17)])
+def test_vocab_loss_in_blocks_of_rows(dtype, rows, words, n_in):
+    """Rows for which a piece of 1024 words takes more than 256 MiB: dw is the sum of two and more blocks."""
+    g = C.gen(44)
+    x, w = C.normal(g, dtype, rows, n_in), C.normal(g, dtype, words, n_in, scale=0.3)
+    t = torch.randint(-words // 10, words, (rows,), device="cuda", generator=g)
+    dloss = torch.rand(rows, device="cuda", generator=g) / rows
+    loss, lse = L.alpa_vocab_loss_forward(x, w, t)
+    dx, dw = L.alpa_vocab_loss_backward(dloss, x, w, t, lse)
+    dws, bound = torch.zeros(words, n_in, dtype=C.D, device="cuda"), torch.zeros(words, n_in, dtype=C.D, device="cuda")
+    step = 16384
+    for a in range(0, rows, step):
+        part = slice(a, a + step)
+        ref = C.vocab(x[part], w, t[part], dloss[part])
+        C.within("loss", loss[part], *ref["loss"])
+        C.within("dx", dx[part], *ref["dx"])
+        dws += ref["dw"][0]
+        bound += ref["dw"][1] * (rows / step + 1)    # (sums of `rows` terms in place of 16384)
+    C.within("dw", dw, dws, bound)
+    only, _ = L.alpa_vocab_loss_backward(dloss, x, w, t, lse, need=("x",))
+    _, other = L.alpa_vocab_loss_backward(dloss, x, w, t, lse, need=("w",))
+    assert torch.equal(only, dx) and torch.equal(other, dw)

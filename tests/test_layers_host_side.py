@@ -37,3 +37,17 @@ def test_products_of_many_tiles_are_launched(driver, line):
     if steps and steps[0].tile < 256:
         t = steps[0].tile
         assert sum(p.grid for p in steps) == -(-(-(-n_out // t) * -(-n_in // t)) // 8) * 8 * experts
+
+
+@pytest.mark.parametrize("dtype", [F32, F16])
+@pytest.mark.parametrize("rows, words", [(1, 5), (65536, 1024), (65537, 5000), (131072, 51200), (131073, 1024), (200000, 51200), (1 << 20, 2),
+                                         (1 << 24, 1030)])
+def test_work_memory_of_the_loss_backwards(driver, dtype, rows, words):
+    """The gradient of the logits is in memory 256 MiB at a time, whatever the number of rows; beside it stand a float a row, the
+    32-bit sums of dx and of a piece's dw, and the parts of products that are split (2^26 floats at most)."""
+    n_in = 8
+    call, = Q.calls(driver, [("gradient", dtype, rows, n_in, words)])
+    assert call.rc == 0
+    assert call.work <= (256 << 20) + rows * 4 + rows * n_in * 4 + words * n_in * 4 + (1 << 28) + (1 << 14)
+    pieces = [p for p in Q.products(call) if p.epilogue == "GRAD"]
+    assert len(pieces) >= rows * words * (4 if dtype == F32 else 2) / (256 << 20)
