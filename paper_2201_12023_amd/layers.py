@@ -1,17 +1,22 @@
-"""Thin ctypes binding over the C ABI in ``include/alpa_layers.h`` (argument marshalling only): the products of
-dense and expert layers and the loss over a vocabulary, forward and backward.
+"""Thin ctypes binding over the C ABI in ``include/alpa_layers.h`` (argument marshalling, and nodes of torch's graph): the
+products of dense and expert layers and the loss over a vocabulary, forward and backward.
 
 Same names as the C entry points.  Arguments and results are torch tensors on one GPU; results and work memory come from
 torch's allocator, every step runs in the HIP kernels of ``libalpa_dp.so``.  Work is queued on ``stream`` (a
 torch.cuda.Stream; the current one if None) and not waited for; tensors that belong to another stream are the caller's to
 order and to keep.  The last dimension of a tensor must be contiguous, rows may be
 any distance apart.
+
+The forward calls can be differentiated: where an argument requires a gradient their results are part of torch's graph, and its backward
+pass makes the calls of this module.  What is kept for those, z and lse, can not be: a loss that depends on them raises an error in the
+backward pass.  The backward calls themselves record nothing.
 """
 from __future__ import annotations
 
 import ctypes
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import binding
 
@@ -203,9 +208,75 @@ def _backward(dy, x, w, offsets, z, act, need, stream):
     return dx, dw, db
 
 
+def _recorded(*tensors):
+    return torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors)
+
+
+def _apply(function, stream, *args):
+    """The call as a node of torch's graph, whose backward pass runs on the stream that is current here."""
+    if stream is None:
+        return function.apply(*args, None)
+    with torch.cuda.stream(stream):
+        return function.apply(*args, stream)
+
+
+class _Product(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, w, offsets, bias, residual, act, keep_z, stream):
+        needs = ctx.needs_input_grad
+        ctx.need = tuple(name for name, wanted in (("x", needs[0]), ("w", needs[1]), ("bias", needs[3])) if wanted)
+        ctx.act = act
+        has_z = keep_z or (act != ALPA_ACT_NONE and bool(ctx.need))
+        result = _forward(x, w, offsets, bias, residual, act, has_z, stream)
+        y, z = result if has_z else (result, None)
+        # (of x and w one at least, for the sizes)
+        ctx.save_for_backward(x if needs[1] or (ctx.need and not needs[0]) else None, w if needs[0] else None, offsets,
+                              z if act != ALPA_ACT_NONE else None)
+        ctx.set_materialize_grads(False)
+        return (y, z) if keep_z else y
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dy, dz=None):
+        if dz is not None:
+            raise RuntimeError("z has no gradient: a loss may depend on y alone")
+        if dy is None:
+            return (None,) * 8
+        x, w, offsets, z = ctx.saved_tensors
+        dy = dy.contiguous()
+        dx, dw, db = _backward(dy, x, w, offsets, z, ctx.act, ctx.need, None) if ctx.need else (None, None, None)
+        dr = dy if ctx.needs_input_grad[4] else None
+        if dr is not None and offsets is not None:
+            row = torch.arange(dy.shape[0], device=dy.device)         # (rows of no expert do not have the residual)
+            dr = torch.where(((row >= offsets[0]) & (row < offsets[-1]))[:, None], dy, torch.zeros_like(dy))
+        return dx, dw, None, db, dr, None, None, None
+
+
+class _VocabLoss(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, w, target, stream):
+        loss, lse = _vocab_loss(x, w, target, stream)
+        ctx.save_for_backward(x, w, target, lse)
+        ctx.set_materialize_grads(False)
+        return loss, lse
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dloss, dlse):
+        if dlse is not None:
+            raise RuntimeError("lse has no gradient: a loss may depend on the rows' losses alone")
+        if dloss is None:
+            return (None,) * 4
+        x, w, target, lse = ctx.saved_tensors
+        need = tuple(name for name, wanted in zip(("x", "w"), ctx.needs_input_grad) if wanted)
+        return *alpa_vocab_loss_backward(dloss.contiguous(), x, w, target, lse, need), None, None
+
+
 def alpa_linear_forward(x, w, bias=None, residual=None, act=ALPA_ACT_NONE, keep_z=False, stream=None):
     """act(x w^T + bias) + residual for x [rows, in], w [out, in]; with ``keep_z`` also what stands in front of the
     activation, which the backward pass takes: (y, z)."""
+    if _recorded(x, w, bias, residual):
+        return _apply(_Product, stream, x, w, None, bias, residual, act, keep_z)
     return _forward(x, w, None, bias, residual, act, keep_z, stream)
 
 
@@ -217,6 +288,8 @@ def alpa_linear_backward(dy, x, w, z=None, act=ALPA_ACT_NONE, need=("x", "w", "b
 def alpa_experts_forward(x, w, offsets, bias=None, residual=None, act=ALPA_ACT_NONE, keep_z=False, stream=None):
     """The same for rows sorted by expert: rows offsets[e] .. offsets[e + 1] - 1 (int32 tensor [experts + 1] on the GPU)
     through w[e] of [experts, out, in] and bias[e]; rows of no expert give zeros."""
+    if _recorded(x, w, bias, residual):
+        return _apply(_Product, stream, x, w, offsets, bias, residual, act, keep_z)
     return _forward(x, w, offsets, bias, residual, act, keep_z, stream)
 
 
@@ -225,9 +298,7 @@ def alpa_experts_backward(dy, x, w, offsets, z=None, act=ALPA_ACT_NONE, need=("x
     return _backward(dy, x, w, offsets, z, act, need, stream)
 
 
-def alpa_vocab_loss_forward(x, w, target, stream=None):
-    """(loss, lse), float32 [rows]: cross entropy of softmax(x w^T) for x [rows, in], w [words, in], target int64 [rows];
-    a negative target leaves the row out (loss 0).  ``lse`` is what the backward pass takes."""
+def _vocab_loss(x, w, target, stream):
     L, d = load(), _type(x)
     rows, n_in = _two("x", x)
     words = _two("w", w)[0]
@@ -240,6 +311,14 @@ def alpa_vocab_loss_forward(x, w, target, stream=None):
         keep, p, n = _work(L.alpa_vocab_loss_forward_work(d, rows, n_in, words, xm, wm), device)
         binding._check(L.alpa_vocab_loss_forward(d, rows, n_in, words, xm, wm, t, loss.data_ptr(), lse.data_ptr(), p, n, s))
     return loss, lse
+
+
+def alpa_vocab_loss_forward(x, w, target, stream=None):
+    """(loss, lse), float32 [rows]: cross entropy of softmax(x w^T) for x [rows, in], w [words, in], target int64 [rows];
+    a negative target leaves the row out (loss 0).  ``lse`` is what the backward pass takes."""
+    if _recorded(x, w):
+        return _apply(_VocabLoss, stream, x, w, target)
+    return _vocab_loss(x, w, target, stream)
 
 
 def alpa_vocab_loss_backward(dloss, x, w, target, lse, need=("x", "w"), stream=None):
