@@ -138,6 +138,68 @@ def check_warm_register(asm_text: str) -> list:
     return bad
 
 
+# Vector instructions that write scalar registers besides their first operand (a carry, a flag).
+_SECOND_OPERAND = re.compile(r"v_(mad_u64_u32|mad_i64_i32|add_co_|addc_co_|sub_co_|subb_co_|subrev_co_|subbrev_co_|div_scale_)")
+_RANGE_STATES = 5                   # wait states between such a write and a load that takes the register for its range
+
+
+def _scalars(operand: str) -> set:
+    m = re.fullmatch(r"s(\d+)|s\[(\d+):(\d+)\]", operand)
+    if not m:
+        return set()
+    return {int(m.group(1))} if m.group(1) else set(range(int(m.group(2)), int(m.group(3)) + 1))
+
+
+def check_load_ranges(asm_text: str) -> list:
+    """The loads to LDS of the products are inline assembly, so the compiler does not see that they read the four scalar
+    registers of their range, and would not keep a vector instruction that writes one of them the five wait states away
+    that the hardware asks for.  In every product_kernel of the device assembly: no such write stands so
+    close in front of a load, on any path to it."""
+    bad = []
+    for part in re.split(r"\n(?=_ZN4alpa14product_kernel\S*:)", asm_text)[1:]:
+        name = part.split(":", 1)[0]
+        code = part[:part.find("\n.Lfunc_end")] if "\n.Lfunc_end" in part else part
+        lines = [t for t in (line.split(";", 1)[0].strip() for line in code.splitlines()[1:])
+                 if t and (not t.startswith(".") or t.startswith(".LBB"))]
+        jumps = {}
+        for i, t in enumerate(lines):
+            m = re.match(r"s_c?branch\S*\s+(\.LBB\S+)", t)
+            if m:
+                jumps.setdefault(m.group(1), []).append(i)
+
+        def behind(i, states, regs, seen):
+            """A write of `regs` fewer than `states` wait states in front of line i, or None."""
+            while i > 0 and states > 0:
+                i -= 1
+                t = lines[i]
+                if t.endswith(":"):
+                    for j in jumps.get(t[:-1], []):
+                        if (j, states) not in seen:
+                            seen.add((j, states))
+                            found = behind(j, states - 1, regs, seen)
+                            if found:
+                                return found
+                    if i > 0 and re.match(r"s_branch|s_endpgm", lines[i - 1]):
+                        return None                          # (reached by jumps alone)
+                    continue
+                op, *rest = t.split(None, 1)
+                if op.startswith("v_"):
+                    operands = [o.strip() for o in (rest[0] if rest else "").split(",")]
+                    written = _scalars(operands[0]) | (_scalars(operands[1]) if _SECOND_OPERAND.match(op) and len(operands) > 1 else set())
+                    if written & regs:
+                        return t
+                states -= int(rest[0], 0) + 1 if op == "s_nop" else 1
+            return None
+
+        for i, t in enumerate(lines):
+            m = re.match(r"buffer_load_dwordx4\s+v\d+,\s*(s\[\d+:\d+\]),.*\blds$", t)
+            if m:
+                found = behind(i, _RANGE_STATES, _scalars(m.group(1)), set())
+                if found:
+                    bad.append(f"{name}: `{found}` writes the range of `{t}` right in front of it")
+    return bad
+
+
 def build(verbose: bool = True, extra=()) -> str:
     os.makedirs(OBJ, exist_ok=True)
     srcs = sorted(glob.glob(os.path.join(CSRC, "*.hip")))
@@ -157,9 +219,9 @@ def build(verbose: bool = True, extra=()) -> str:
             raise subprocess.CalledProcessError(res.returncode, cmd)
         kernels.update(parse_resource_remarks(res.stderr))
 
-    # device assembly of the two files that instantiate the recurrence kernel, for the check above
+    # device assembly of the files that instantiate the recurrence kernel and the products, for the checks above
     asm_jobs = [(s, os.path.join(OBJ, os.path.basename(s)[:-4] + ".s")) for s in srcs
-                if os.path.basename(s).startswith("kernels_fast")]
+                if os.path.basename(s).startswith(("kernels_fast", "kernels_product"))]
     asm_bad = []
 
     def asm(pair):
@@ -172,7 +234,8 @@ def build(verbose: bool = True, extra=()) -> str:
             print(res.stderr, file=sys.stderr, flush=True)
             raise subprocess.CalledProcessError(res.returncode, cmd)
         with open(o) as f:
-            asm_bad.extend(check_warm_register(f.read()))
+            text = f.read()
+        asm_bad.extend(check_warm_register(text) + check_load_ranges(text))
         os.remove(o)
 
     with ThreadPoolExecutor(max_workers=4) as ex:
@@ -185,7 +248,7 @@ def build(verbose: bool = True, extra=()) -> str:
     if verbose:
         n_batch = sum(1 for k in kernels if _BATCH_INSTANCE.search(k))
         print(f"resource check: {len(kernels)} kernels, {n_batch} instances at 8 waves/SIMD, "
-              "no spills in the recurrence kernels, its warm-up register keeps its place", flush=True)
+              "no spills in the recurrence kernels, its warm-up register keeps its place, no vector write close to the products' loads", flush=True)
     cmd = [HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", LIB, *objs]
     if verbose:
         print(" ".join(cmd), flush=True)
