@@ -8,6 +8,7 @@
 //   backward dtype act rows experts n_in n_out ldx lddx bias dx dw        experts -1: a dense layer
 //   loss     dtype rows n_in words
 //   gradient dtype rows n_in words
+//   kernels                                     (all there are, as if they were launched)
 #include "../include/alpa_layers.h"
 
 #include <cstdio>
@@ -103,6 +104,8 @@ int main()
                 rc = alpa_vocab_loss_backward(dtype, rows, n_in, n_out, f, x, w, target, f, mat(6, n_in), mat(7, n_in), place(8), need, nullptr);
             }
         }
+        if (op == "kernels")
+            for (auto &k : kernels()) launches += " " + k.second + " 0 0 0 0;";
         printf("%d %lld%s\n", rc, (long long)need, launches.c_str());
     }
     return 0;

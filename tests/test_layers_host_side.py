@@ -4,6 +4,7 @@ import shutil
 import pytest
 
 from tests import layer_launches as Q
+from tests import layer_paths as P
 
 F32, F16, BF16 = 0, 1, 2
 
@@ -51,3 +52,21 @@ def test_work_memory_of_the_loss_backwards(driver, dtype, rows, words):
     assert call.work <= (256 << 20) + rows * 4 + rows * n_in * 4 + words * n_in * 4 + (1 << 28) + (1 << 14)
     pieces = [p for p in Q.products(call) if p.epilogue == "GRAD"]
     assert len(pieces) >= rows * words * (4 if dtype == F32 else 2) / (256 << 20)
+
+
+def test_listed_sizes_reach_every_product(driver):
+    """Each of tests/layer_paths.py's cases takes the path that it is listed for, and no compiled product is left without one."""
+    seen = set()
+    for dtype in (F32, F16, BF16):
+        cases = [small if dtype != F32 else wide for _, small, wide in P.PATHS]
+        for (path, _, _), case, call in zip(P.PATHS, cases, Q.calls(driver, [P.line(dtype, c) for c in cases])):
+            assert call.rc == 0
+            found = {(p.a, p.b, p.tile, p.epilogue, p.grouping, p.splits > 1): p for p in Q.products(call)}
+            assert path in found, (path, case)
+            p = found[path]
+            assert path[2] < 256 or path[5] or p.grid == 256
+            seen.add((p.type, *path[:5]))
+    blocks, = Q.calls(driver, [("gradient", BF16, 131072 + 28, 32776, 1000)])      # sums over blocks of rows (tests/test_gpu_layers_edges.py)
+    assert [(p.tile, p.splits) for p in Q.products(blocks) if p.epilogue == "SUM"] == [(256, 1)] * 2
+    there, = Q.calls(driver, [("kernels",)])
+    assert seen == {(p.type, p.a, p.b, p.tile, p.epilogue, p.grouping) for p in Q.products(there)} and len(seen) == 135
