@@ -70,3 +70,15 @@ def test_listed_sizes_reach_every_product(driver):
     assert [(p.tile, p.splits) for p in Q.products(blocks) if p.epilogue == "SUM"] == [(256, 1)] * 2
     there, = Q.calls(driver, [("kernels",)])
     assert seen == {(p.type, p.a, p.b, p.tile, p.epilogue, p.grouping) for p in Q.products(there)} and len(seen) == 135
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_results_that_are_not_aligned_take_a_smaller_tile(driver, dtype):
+    """The sizes of tests/test_gpu_layers_bounds.py, with rows of the result as long as they are apart, and three elements further."""
+    dense, experts = (9000, -1, 5128, 5128), (131 * 96, 4, 2568, 3592)
+    tiles = []
+    for pad in (0, 3):
+        lines = [("forward", dtype, 3, *s, s[2], s[3] + pad, 1, 1, 1) for s in (dense, experts)]
+        lines.append(("backward", dtype, 3, *dense, dense[2], dense[2] + pad, 1, 1, 0))
+        tiles.append([Q.products(call)[0].tile for call in Q.calls(driver, lines)])
+    assert tiles == [[256] * 3, [128] * 3]
