@@ -68,7 +68,7 @@ int alpa_linear_forward(int dtype, int act, int64_t rows, int64_t n_in, int64_t 
  *   Any of dx, dw, dbias may be NULL (p NULL).  z is needed unless act is ALPA_ACT_NONE, x for dw, w for dx.  dz is rounded to
  *   `dtype` as an operand of the two products (in float16, with a smooth activation, times a power of two found from the largest |dy|, so that it
  *   neither overflows nor loses bits of small dy); dbias is summed from the 32-bit values.  The slope of ALPA_ACT_RELU at 0 is 0.  (The residual's gradient is dy.)
- * With rows == 0, dw and dbias are zero.
+ * With rows == 0, dw and dbias are zero.  Work memory has room for dbias's sums, wanted or not.
  */
 int64_t alpa_linear_backward_work(int dtype, int act, int64_t rows, int64_t n_in, int64_t n_out, alpa_mat_t dy,
                                   alpa_mat_t x, alpa_mat_t w);

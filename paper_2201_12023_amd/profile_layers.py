@@ -9,7 +9,10 @@ operators of ``layers``, with every submesh's share of the work in turn; the tim
 A share is one device's of d, in two ways: "rows" (a d-th of the rows, all weights) or "weights" (all rows, a d-th of the inner
 width and of the words).  One GPU stands for each device of the mesh; what devices exchange is not run but added as bytes over
 ``link`` bytes/s: the gradients of all weights once a batch for "rows", the layer's result and its gradient once a microbatch for
-"weights".
+"weights" (not what the loss exchanges where its words are split).
+
+A layer is its two products with their activation; what else a block has, its attention, is not timed.  Times are between events around a
+layer's calls, so where the GPU waits for launches, some 12 us a call, they are the host's.
 """
 from __future__ import annotations
 

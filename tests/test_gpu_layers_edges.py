@@ -133,3 +133,25 @@ def test_vocab_loss_in_blocks_of_rows(dtype, rows, words, n_in):
     only, _ = L.alpa_vocab_loss_backward(dloss, x, w, t, lse, need=("x",))
     _, other = L.alpa_vocab_loss_backward(dloss, x, w, t, lse, need=("w",))
     assert torch.equal(only, dx) and torch.equal(other, dw)
+
+
+def test_float16_gradients_in_a_graph():
+    """The scale of dz is found anew in every replay."""
+    g = C.gen(45)
+    x, w = C.normal(g, F16, 300, 64), C.normal(g, F16, 136, 64)
+    dy, z = C.normal(g, F16, 300, 136), C.normal(g, F16, 300, 136)
+    step = lambda: L.alpa_linear_backward(dy, x, w, z=z, act=3)
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        recorded = step()
+    for factor in (1.0, 2.0 ** -16, 2.0 ** 20, 2.0 ** -7):
+        dy.mul_(factor)
+        eager = [v.clone() for v in step()]
+        for v in recorded:
+            v.fill_(float("nan"))
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(eager, recorded)) and bool(eager[1].any())
