@@ -183,7 +183,7 @@ int run_product(hipStream_t st, int dtype, Forms forms, Epilogue epi, const Shap
     g.wide = by16(g.out) && by16(g.z) && by16(g.residual) && by16(g.bias) && g.ldo * es % 16 == 0 && g.ldz * es % 16 == 0 &&
              g.ldr * es % 16 == 0 && (s.grouping == GROUP_NONE || s.n * es % 16 == 0) &&
              (s.grouping != GROUP_STEPS || g.b_expert * es % 16 == 0);
-    const bool may_split = epi != EPI_LOSS && epi != EPI_GRAD && epi != EPI_SUM;
+    const bool may_split = epi != EPI_LOSS && epi != EPI_GRAD && (epi != EPI_SUM || g.total);
     Cut cut = cut_of(s, dtype, may_split, s.n % 8 == 0 || epi == EPI_LOSS);
     // (parts of a split product and statistics go to work memory, where everything is aligned)
     if (cut.tile == BIG_TILE && cut.splits == 1 && epi != EPI_LOSS && !g.wide) cut = cut_of(s, dtype, false, false);
@@ -609,7 +609,7 @@ int alpa_vocab_loss_backward(int dtype, int64_t rows, int64_t n_in, int64_t word
                 ProductArgs g = operands(FORM_CC, grad, xb, m, dtype);
                 result(g, alpa_mat_t{(char *)dw.p + word0 * dw.ld * es, dw.ld});
                 g.scale = scale;
-                g.sum = (float *)(base + at.sum_w);
+                if (at.blocks > 1) g.sum = g.total = (float *)(base + at.sum_w);
                 g.first = b == 0;
                 g.last = b + 1 == at.blocks;
                 TRY(run_product(st, dtype, FORM_CC, at.blocks > 1 ? EPI_SUM : EPI_LINE, Shape{n, n_in, m, GROUP_NONE, 0}, g, base + at.split));

@@ -262,6 +262,18 @@ __global__ __launch_bounds__(256) void join_kernel(const ProductArgs g)
 #pragma unroll
         for (int j = 0; j < 4; ++j) v[j] += part[j];
     }
+    if (g.total) {
+        if (!g.first) {
+            float old[4];
+            load_row<float>((const char *)g.total, m * g.N + n, cnt, aligned, old);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[j] += old[j];
+        }
+        if (!g.last) {
+            store_row<float>((char *)g.total, m * g.N + n, cnt, aligned, v);
+            return;
+        }
+    }
     const float scale = g.scale ? *g.scale : 1.0f;
     if (EPI == EPI_LINE) {
 #pragma unroll

@@ -39,6 +39,7 @@ struct ProductArgs {
     float low, c1, c3;
     float *sum;                     // EPI_SUM: [split][M][N]
     int first, last;
+    float *total;                   // EPI_SUM: where `sum` goes on from product to product, if one that is split may be joined to it (NULL: none is split)
     const float *scale;             // EPI_SUM, EPI_LINE: result times *scale (NULL: 1)
     const int64_t *target;          // EPI_LOSS, EPI_GRAD
     int64_t word0;                  // EPI_GRAD: the first column's word

@@ -66,8 +66,9 @@ def test_listed_sizes_reach_every_product(driver):
             p = found[path]
             assert path[2] < 256 or path[5] or p.grid == 256
             seen.add((p.type, *path[:5]))
-    blocks, = Q.calls(driver, [("gradient", BF16, 131072 + 28, 32776, 1000)])      # sums over blocks of rows (tests/test_gpu_layers_edges.py)
-    assert [(p.tile, p.splits) for p in Q.products(blocks) if p.epilogue == "SUM"] == [(256, 1)] * 2
+    # sums over blocks of rows without parts (tests/test_gpu_layers_edges.py)
+    for call in Q.calls(driver, [("gradient", BF16, 131072 + 28, 16376, 1000), ("gradient", F32, 65536 + 28, 16376, 1000)]):
+        assert [(p.tile, p.splits) for p in Q.products(call) if p.epilogue == "SUM"] == [(256, 1)] * 2
     there, = Q.calls(driver, [("kernels",)])
     assert seen == {(p.type, p.a, p.b, p.tile, p.epilogue, p.grouping) for p in Q.products(there)} and len(seen) == 135
 
@@ -82,3 +83,14 @@ def test_results_that_are_not_aligned_take_a_smaller_tile(driver, dtype):
         lines.append(("backward", dtype, 3, *dense, dense[2], dense[2] + pad, 1, 1, 0))
         tiles.append([Q.products(call)[0].tile for call in Q.calls(driver, lines)])
     assert tiles == [[256] * 3, [128] * 3]
+
+
+@pytest.mark.parametrize("dtype, rows, n_in, words", [(BF16, 200000, 1024, 32000), (BF16, 600000, 512, 1024), (F32, 140000, 24, 1024)])
+def test_gradients_of_blocks_of_rows_fill_the_compute_units(driver, dtype, rows, n_in, words):
+    """Rows in blocks: a piece's dw has few tiles and a long contraction, which is split as it is without blocks, and joined to the blocks before."""
+    call, = Q.calls(driver, [("gradient", dtype, rows, n_in, words)])
+    assert call.rc == 0
+    dw = [p for p in Q.products(call) if (p.a, p.b) == ("COLS", "COLS")]
+    grads = [p for p in Q.products(call) if p.epilogue == "GRAD"]
+    assert len(dw) == len(grads) and all(p.splits > 1 for p in dw)
+    assert sum("join_kernel" in name for name, *_ in call.launches) >= len(dw)
