@@ -1,0 +1,777 @@
+// Attention forward and backward, instantiated per element type (kernels_attention_*.hip).
+//
+// Everything is computed transposed: a block of 32 keys x 32 rows of scores is K Qt, so that a lane holds 16 keys' scores of one row.  A row's maximum
+// and sum are then a lane's own numbers, joined once with the lane that has the row's other 16 keys, and the rounded exponentials are the second operand of
+// yt = Vt Pt as they lie in the registers: no weight goes through LDS.  The gradients are built alike: dqt = Kt dRt with a lane per row, dvt = dyt P
+// and dkt = Qt dR with a lane per key.
+//
+// The query heads that share a kv head are rows of one product: packed row r of a sequence's kv head is query r / group, head r % group.
+#pragma once
+#include "blocks.hpp"
+#include "epilogue.hpp"
+#include "slots.hpp"
+
+namespace alpa {
+
+using f32x16 = float __attribute__((ext_vector_type(16)));
+
+constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.69314718055994531f;
+
+__device__ __forceinline__ f32x16 mma32(u32x4 a, u32x4 b, f32x16 c, bf16)
+{
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x16 mma32(u32x4 a, u32x4 b, f32x16 c, f16)
+{
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x16 mma32(u32x4 a, u32x4 b, f32x16 c, float)
+{
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        c = __builtin_amdgcn_mfma_f32_32x32x2f32(__builtin_bit_cast(f32x4, a)[j], __builtin_bit_cast(f32x4, b)[j], c, 0, 0, 0);
+    return c;
+}
+
+// the row (first operand) that register i of a lane's 32 x 32 block holds
+__device__ __forceinline__ int block_row(int i, int h) { return (i >> 2) * 8 + h * 4 + (i & 3); }
+
+// Rows of a head in LDS: 16-byte chunk c of row r lies at place c ^ swz(r), so that both reads are spread over all banks: 32 rows at one chunk
+// (products over the head's elements), and four rows at four chunks that follow each other (transposed).
+template <class T, int DB>
+struct Rows {
+    static constexpr int ES = sizeof(T), WIDTH = DB <= 2 ? 64 : DB <= 4 ? 128 : 256, ROWB = WIDTH * ES, CHUNKS = ROWB / 16;
+    static constexpr int STEPS = DB * ES;              // 32 bytes of a head: 16 elements of 16 bits, 8 of 32
+    static constexpr int PER = ES == 2 ? 16 : 8;       // rows of a transposed fragment
+    static constexpr int FRAGS = 32 / PER;
+
+    static __device__ __forceinline__ int swz(int r)
+    {
+        return CHUNKS == 8 ? ((r >> 1 & 1) << 2) | (r >> 2 & 3) : ((r & 3) << 2) | (r >> 2 & 3);
+    }
+    static __device__ __forceinline__ uint32_t at(int r, int chunk) { return r * ROWB + ((chunk ^ swz(r)) << 4); }
+
+    // Lane (i, h) = (lane & 31, lane >> 5): row i, bytes 32 step + 16 h of it.
+    struct Place {
+        uint32_t row, col, col2;
+        __device__ __forceinline__ Place()
+        {
+            const int lane = threadIdx.x & 63, i = lane & 31, h = lane >> 5;
+            row = at(i, h);
+            if (ES == 2) {
+                const int r = 4 * h + ((lane & 15) >> 2), c = 2 * (lane >> 4 & 1) + ((lane & 3) >> 1);
+                col = at(r, c) + (lane & 1) * 8;
+                col2 = at(r + 8, c) + (lane & 1) * 8;
+            } else {
+                col = h * 4 * ROWB + (i & 3) * 4;
+                col2 = i >> 2;
+            }
+        }
+    };
+    // rows row0 + i, step; row0 a multiple of 32
+    static __device__ __forceinline__ u32x4 along(const char *lds, const Place &p, int row0, int step)
+    {
+        return *(const u32x4 *)(lds + ((p.row ^ (step * 32)) + row0 * ROWB));
+    }
+    // Elements d0 + i (d0 a multiple of 32) of the rows that a lane's fragment `t` of a 32 x 32 block stands for: row0 + block_row(PER / 2 * t + e, h).
+    static __device__ __forceinline__ u32x4 across(const char *lds, const Place &p, int row0, int t, int d0)
+    {
+        if constexpr (ES == 2) {
+            const uint32_t from = (uint32_t)(uintptr_t)(const ALPA_LDS char *)lds + (row0 + t * 16) * ROWB;
+            const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((ALPA_LDS i16x4 *)(uintptr_t)(from + (p.col ^ (d0 * 2))));
+            const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((ALPA_LDS i16x4 *)(uintptr_t)(from + (p.col2 ^ (d0 * 2))));
+            const u32x2 l = __builtin_bit_cast(u32x2, lo), g = __builtin_bit_cast(u32x2, hi);
+            return u32x4{l.x, l.y, g.x, g.y};
+        } else {
+            u32x4 r;
+            const int h = threadIdx.x >> 5 & 1;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int s = (e << 2) | ((2 * t + h) & 3);
+                r[e] = *(const uint32_t *)(lds + p.col + (row0 + 8 * t + e) * ROWB + ((((d0 >> 2) + p.col2) ^ s) << 4));
+            }
+            return r;
+        }
+    }
+    // A block's values, rounded to the type, as the second operand of fragment t.
+    static __device__ __forceinline__ u32x4 packed(const f32x16 &v, int t)
+    {
+        if constexpr (ES == 2) {
+            T e[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) e[j] = (T)v[8 * t + j];
+            return __builtin_bit_cast(u32x4, *(i16x8 *)e);
+        } else {
+            return u32x4{__float_as_uint(v[4 * t]), __float_as_uint(v[4 * t + 1]), __float_as_uint(v[4 * t + 2]), __float_as_uint(v[4 * t + 3])};
+        }
+    }
+    using i16x8 = short __attribute__((ext_vector_type(8)));
+};
+
+// A sequence's share of the tensors.
+struct Span {
+    int seq;                        // seqs and above: rows of no sequence, seqs + 2: none
+    int first, n;                   // its rows
+    int r0;                         // a tile's first packed row
+    int k_first, m;                 // its keys
+    int ahead;                      // m - n: the place of row 0
+    int prefix;
+};
+
+// group_rows() of slots.hpp; without offsets there is one sequence of all rows
+__device__ __forceinline__ void sequence_rows(const int32_t *offsets, int seqs, int rows, int group, int &first, int &end)
+{
+    if (offsets) return group_rows(offsets, seqs, rows, group, first, end);
+    first = 0;
+    end = group == 0 ? rows : 0;
+}
+
+__device__ __forceinline__ void find_keys(const AttentionArgs &g, Span &s)
+{
+    s.k_first = s.m = s.prefix = 0;
+    if (s.seq < g.seqs) {
+        const int32_t *at = g.k_offsets + (int64_t)s.seq * g.k_step;
+        const int a = g.k_offsets ? min(max(at[0], 0), g.k_rows) : 0, b = g.k_offsets ? min(max(at[1], 0), g.k_rows) : g.k_rows;
+        s.k_first = a;
+        s.m = max(b - a, 0);
+        if (g.prefix && g.causal) s.prefix = g.prefix[s.seq];
+    }
+    s.ahead = s.m - s.n;
+}
+
+// The tile-th run of up to `tile` packed rows of one group of rows (slots.hpp), `group` of them a row.
+__device__ __forceinline__ Span find_span(const int32_t *offsets, int seqs, int rows, int group, int tile, int index)
+{
+    const int lane = threadIdx.x & 63;
+    int before = 0;
+    for (int base = 0; base < seqs + 2; base += 64) {
+        int first, end;
+        sequence_rows(offsets, seqs, rows, base + lane, first, end);
+        const int n = ((end - first) * group + tile - 1) / tile;
+        int sum = n;
+#pragma unroll
+        for (int off = 1; off < 64; off <<= 1) {
+            const int o = __shfl_up(sum, off, 64);
+            if (lane >= off) sum += o;
+        }
+        const unsigned long long past = __ballot(before + sum > index);
+        if (past) {
+            const int l = __ffsll(past) - 1;
+            const int f = __builtin_amdgcn_readlane(first, l), e = __builtin_amdgcn_readlane(end, l), count = __builtin_amdgcn_readlane(n, l);
+            const int s = before + __builtin_amdgcn_readlane(sum, l) - count;
+            if (index < s || index - s >= count) break;          // (offsets that are none)
+            // a sequence's tiles from its last one on: with a causal mask those have most keys, and the short ones fill up the end
+            return Span{base + l, f, e - f, (count - 1 - (index - s)) * tile, 0, 0, 0, 0};
+        }
+        before += __builtin_amdgcn_readlane(sum, 63);
+    }
+    return Span{seqs + 2, 0, 0, 0, 0, 0, 0, 0};
+}
+
+// keys that row `i` of a sequence sees: those in front of this one
+__device__ __forceinline__ int limit_of(const AttentionArgs &g, const Span &s, int i)
+{
+    return min(s.m, g.causal ? max(max(i + s.ahead + 1, s.prefix), 0) : s.m);
+}
+
+// Scores in units of the binary logarithm.  EXTRA: what the formula has beside a positive factor, and the slope of the cap.
+template <class T>
+__device__ __forceinline__ float capped(const AttentionArgs &g, float r, float &bent)
+{
+    // 1 - tanh(x) = 2 / (1 + exp(2 x)), from which the slope keeps its relative error where the cap is reached
+    const float x = r / g.cap, u = divide_for<T>(2.0f, 1.0f + exp_for<T>(2.0f * fabsf(x)));
+    bent = u * (2.0f - u);
+    if (sizeof(T) == 4) return g.cap * tanhf(x);
+    return copysignf(g.cap * (1.0f - u), r);
+}
+
+__device__ __forceinline__ float other_half(float v) { return __shfl_xor(v, 32, 64); }
+
+// Rows of a tile from memory to LDS: `rows` rows that exist, row r at p + r * stride, of R; the others, and what is behind a head's bytes, are zeros.
+template <class R, int COUNT, int NT>
+__device__ __forceinline__ void fill(char *lds, const char *p, int64_t stride, int rows, int bytes)
+{
+#pragma unroll 4
+    for (int c = threadIdx.x % NT; c < COUNT * R::CHUNKS; c += NT) {
+        const int r = c / R::CHUNKS, chunk = c % R::CHUNKS;
+        u32x4 v = {0, 0, 0, 0};
+        if (r < rows && chunk * 16 < bytes) v = *(const u32x4 *)(p + r * stride + chunk * 16);
+        *(u32x4 *)(lds + R::at(r, chunk)) = v;
+    }
+}
+
+// Where packed row r of a sequence's kv head lies in a tensor of queries.
+__device__ __forceinline__ const char *packed_row(const AttentionArgs &g, const Heads &t, const Span &s, int kv, int r)
+{
+    const int i = r / g.group;
+    return t.p + (int64_t)(s.first + i) * t.row + (int64_t)(kv * g.group + r - i * g.group) * t.head;
+}
+__device__ __forceinline__ int64_t packed_item(const AttentionArgs &g, const Span &s, int kv, int r)
+{
+    const int i = r / g.group;
+    return (int64_t)(s.first + i) * g.heads + kv * g.group + r - i * g.group;
+}
+
+// 32 results of one row or key, times `by`, as a lane holds them of each block; `at` the head's first element
+template <class T, int DB>
+__device__ __forceinline__ void store_head(char *at, const f32x16 (&acc)[DB], float by, int dim, int wide)
+{
+    const int h = threadIdx.x >> 5 & 1;
+#pragma unroll
+    for (int b = 0; b < DB; ++b)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int d = b * 32 + j * 8 + h * 4;
+            const float v[4] = {acc[b][4 * j] * by, acc[b][4 * j + 1] * by, acc[b][4 * j + 2] * by, acc[b][4 * j + 3] * by};
+            if (d < dim) store_row<T>(at, d, dim - d, wide, v);
+        }
+}
+
+template <int DB>
+__device__ __forceinline__ void clear(f32x16 (&acc)[DB])
+{
+#pragma unroll
+    for (int b = 0; b < DB; ++b)
+#pragma unroll
+        for (int j = 0; j < 16; ++j) acc[b][j] = 0.0f;
+}
+
+// One row a lane, twice: what has been seen of the keys so far.
+template <class T, int DB, bool EXTRA>
+struct Running {
+    using R = Rows<T, DB>;
+    u32x4 q[R::STEPS];
+    f32x16 y[DB];
+    float top, sum;                 // in units of the binary logarithm; of this lane's half of the keys
+    int limit, place;
+    float slope;
+
+    __device__ __forceinline__ void begin(const AttentionArgs &g, const Span &s, int kv, int r)
+    {
+        const int h = threadIdx.x >> 5 & 1, last = s.n * g.group - 1, i = min(r, last);
+        const char *p = packed_row(g, g.q, s, kv, i);
+#pragma unroll
+        for (int k = 0; k < R::STEPS; ++k) {
+            const int at = k * 32 + h * 16;
+            q[k] = at < g.bytes ? *(const u32x4 *)(p + at) : u32x4{0, 0, 0, 0};
+        }
+        clear(y);
+        top = -INFINITY;
+        sum = 0.0f;
+        limit = limit_of(g, s, i / g.group);
+        place = i / g.group + s.ahead;
+        slope = EXTRA && g.slopes ? g.slopes[kv * g.group + i % g.group] : 0.0f;
+    }
+
+    // NB blocks of 32 keys from j0 on, in LDS from row `at` on
+    template <int NB>
+    __device__ __forceinline__ void step(const AttentionArgs &g, const char *k_lds, const char *v_lds, const typename R::Place &p, int j0)
+    {
+        const int h = threadIdx.x >> 5 & 1;
+        f32x16 s[NB];
+        clear(s);
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int k = 0; k < R::STEPS; ++k) s[b] = mma32(R::along(k_lds, p, b * 32, k), q[k], s[b], T{});
+        const float by = EXTRA ? 1.0f : g.scale * LOG2E;
+        if constexpr (EXTRA) {
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    float a = s[b][i] * g.scale, bent;
+                    if (g.cap != 0.0f) a = capped<T>(g, a, bent);
+                    a -= slope * fabsf((float)(place - (j0 + b * 32 + block_row(i, h))));
+                    s[b][i] = a * LOG2E;
+                }
+        }
+        if (__any(j0 + NB * 32 > limit)) {
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s[b][i] = j0 + b * 32 + block_row(i, h) < limit ? s[b][i] : -INFINITY;
+        }
+        float most = s[0][0];
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) most = fmaxf(most, s[b][i]);
+        most = fmaxf(most, other_half(most)) * by;
+        // Exponents are taken from a reference that follows the maximum once it is 8 ahead: exponentials up to 2^8 round to the type like those up to 1
+        if (__any(most > top + 8.0f)) {
+            const float next = fmaxf(top, most), down = exp2f(top - (next == -INFINITY ? 0.0f : next));
+#pragma unroll
+            for (int b = 0; b < DB; ++b)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) y[b][i] *= down;
+            sum *= down;
+            top = next;
+        }
+        const float ref = top == -INFINITY ? 0.0f : top;
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                s[b][i] = __builtin_amdgcn_exp2f(fmaf(s[b][i], by, -ref));
+                sum += s[b][i];
+            }
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int t = 0; t < R::FRAGS; ++t) {
+                const u32x4 w = R::packed(s[b], t);
+#pragma unroll
+                for (int d = 0; d < DB; ++d) y[d] = mma32(R::across(v_lds, p, b * 32, t, d * 32), w, y[d], T{});
+            }
+    }
+
+    // y and lse, or this part of them
+    __device__ __forceinline__ void end(const AttentionArgs &g, const Span &s, int kv, int r, int split)
+    {
+        const float all = sum + other_half(sum);
+        if (r >= s.n * g.group) return;
+        const int64_t item = packed_item(g, s, kv, r);
+        const bool first = (threadIdx.x & 32) == 0;
+        if (g.splits > 1) {
+            const int64_t at = (int64_t)split * g.rows * g.heads + item;
+            store_head<float, DB>((char *)(g.part + at * g.dim), y, 1.0f, g.dim, (g.dim & 3) == 0);
+            if (first) g.stat[at] = make_float2(top, all);
+            return;
+        }
+        char *out = (char *)packed_row(g, g.out, s, kv, r);
+        store_head<T, DB>(out, y, all == 0.0f ? 0.0f : 1.0f / all, g.dim, g.wide);
+        if (g.lse && first) g.lse[item] = all == 0.0f ? -INFINITY : (top + log2f(all)) * LN2;
+    }
+};
+
+// zeros for rows that belong to no sequence, packed rows r0 .. r0 + count - 1; where results are joined later, a part without weight
+template <class T>
+__device__ __forceinline__ void no_rows(const AttentionArgs &g, const Heads &out, const Span &s, int kv, int r0, int count, float *lse, int split)
+{
+    for (int r = r0 + (threadIdx.x >> 6); r < min(r0 + count, s.n * g.group); r += blockDim.x >> 6) {
+        if (g.splits > 1) {
+            if ((threadIdx.x & 63) == 0) g.stat[(int64_t)split * g.rows * g.heads + packed_item(g, s, kv, r)] = make_float2(-INFINITY, 0.0f);
+            continue;
+        }
+        T *to = (T *)packed_row(g, out, s, kv, r);
+        for (int d = threadIdx.x & 63; d < g.dim; d += 64) to[d] = (T)0.0f;
+        if (lse && (threadIdx.x & 63) == 0) lse[packed_item(g, s, kv, r)] = -INFINITY;
+    }
+}
+
+// The keys that one of `splits` workgroups takes, in whole tiles.
+__device__ __forceinline__ void share_of(int most, int tile, int splits, int split, int &from, int &to)
+{
+    const int tiles = (most + tile - 1) / tile, per = (tiles + splits - 1) / splits;
+    from = min(split * per, tiles) * tile;
+    to = min(min(split * per + per, tiles) * tile, most);
+}
+
+// Many rows: a wave has 32 packed rows, the waves share tiles of 64 keys.
+template <class T, int DB, bool EXTRA, int WAVES>
+__global__ __launch_bounds__(WAVES * 64, 2) void attention_kernel(const AttentionArgs g)
+{
+    using R = Rows<T, DB>;
+    constexpr int KEYS = 64, NT = WAVES * 64;
+    __shared__ __align__(1024) char lds[2 * KEYS * R::ROWB];
+    const int kv = (int)((blockIdx.x + g.before) % g.kv_heads);
+    Span s = find_span(g.offsets, g.seqs, g.rows, g.group, WAVES * 32, (int)((blockIdx.x + g.before) / g.kv_heads));
+    if (s.seq >= g.seqs) {
+        if (s.n > 0) no_rows<T>(g, g.out, s, kv, s.r0, WAVES * 32, g.lse, blockIdx.y);
+        return;
+    }
+    find_keys(g, s);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = s.r0 + wave * 32 + (threadIdx.x & 31);
+    Running<T, DB, EXTRA> run;
+    run.begin(g, s, kv, r);
+    const typename R::Place place;
+    // (rows see more keys the later they are)
+    const int last = min(s.r0 + WAVES * 32, s.n * g.group) - 1, most = limit_of(g, s, last / g.group);
+    const int mine = __builtin_amdgcn_readlane(run.limit, 31);
+    int from, to;
+    share_of(most, KEYS, g.splits, blockIdx.y, from, to);
+    const char *k = g.k.p + (int64_t)s.k_first * g.k.row + (int64_t)kv * g.k.head, *v = g.v.p + (int64_t)s.k_first * g.v.row + (int64_t)kv * g.v.head;
+    for (int j0 = from; j0 < to; j0 += KEYS) {
+        __syncthreads();
+        fill<R, KEYS, NT>(lds, k + j0 * g.k.row, g.k.row, s.m - j0, g.bytes);
+        fill<R, KEYS, NT>(lds + KEYS * R::ROWB, v + j0 * g.v.row, g.v.row, s.m - j0, g.bytes);
+        __syncthreads();
+        if (j0 < mine) run.template step<KEYS / 32>(g, lds, lds + KEYS * R::ROWB, place, j0);
+    }
+    run.end(g, s, kv, r, blockIdx.y);
+}
+
+// Few rows: the waves of a workgroup have the same 32 packed rows and take tiles of 32 keys in turn, each from its own part of LDS; in the end their sums
+// are joined.  A workgroup goes through its sequence's rows; one more sequence stands for the rows of none.
+template <class T, int DB>
+struct FewShape {
+    using R = Rows<T, DB>;
+    static constexpr int WAVES = R::ROWB <= 256 ? 4 : R::ROWB == 512 ? 2 : 1, SHARE = 2 * 32 * R::ROWB;
+};
+
+template <class T, int DB, bool EXTRA>
+__global__ __launch_bounds__((FewShape<T, DB>::WAVES * 64)) void attention_few_kernel(const AttentionArgs g)
+{
+    using F = FewShape<T, DB>;
+    using R = Rows<T, DB>;
+    constexpr int WAVES = F::WAVES;
+    __shared__ __align__(1024) char lds[WAVES * F::SHARE];
+    __shared__ float tops[WAVES][32], sums[WAVES][32];
+    const int kv = (int)((blockIdx.x + g.before) % g.kv_heads), lane = threadIdx.x & 63;
+    Span s;
+    s.seq = (int)((blockIdx.x + g.before) / g.kv_heads);
+    if (s.seq >= g.seqs) {
+        for (int k = g.seqs; k < g.seqs + 2; ++k) {
+            int first, end;
+            sequence_rows(g.offsets, g.seqs, g.rows, k, first, end);
+            s.first = first;
+            s.n = end - first;
+            no_rows<T>(g, g.out, s, kv, 0, s.n * g.group, g.lse, blockIdx.y);
+        }
+        return;
+    }
+    int first, end;
+    sequence_rows(g.offsets, g.seqs, g.rows, s.seq, first, end);
+    s.first = first;
+    s.n = end - first;
+    find_keys(g, s);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const typename R::Place place;
+    char *const mine = lds + wave * F::SHARE;
+    const char *k = g.k.p + (int64_t)s.k_first * g.k.row + (int64_t)kv * g.k.head, *v = g.v.p + (int64_t)s.k_first * g.v.row + (int64_t)kv * g.v.head;
+    for (int r0 = 0; r0 < s.n * g.group; r0 += 32) {
+        const int r = r0 + (lane & 31);
+        Running<T, DB, EXTRA> run;
+        run.begin(g, s, kv, r);
+        int from, to;
+        share_of(__builtin_amdgcn_readlane(run.limit, 31), 32 * WAVES, g.splits, blockIdx.y, from, to);
+        for (int j0 = from; j0 < to; j0 += 32 * WAVES) {
+            const int j = j0 + wave * 32;
+            __syncthreads();
+            fill<R, 32, 64>(mine, k + j * g.k.row, g.k.row, s.m - j, g.bytes);
+            fill<R, 32, 64>(mine + 32 * R::ROWB, v + j * g.v.row, g.v.row, s.m - j, g.bytes);
+            __syncthreads();
+            if (j < to) run.template step<1>(g, mine, mine + 32 * R::ROWB, place, j);
+        }
+        if constexpr (WAVES > 1) {
+            // the waves' sums, each brought to the common maximum; wave 0 goes on with them
+            __syncthreads();
+            const float all = run.sum + other_half(run.sum);
+            if (lane < 32) {
+                tops[wave][lane] = run.top;
+                sums[wave][lane] = all;
+            }
+            __syncthreads();
+            float top = tops[0][lane & 31];
+#pragma unroll
+            for (int w = 1; w < WAVES; ++w) top = fmaxf(top, tops[w][lane & 31]);
+            const float ref = top == -INFINITY ? 0.0f : top, down = exp2f(run.top - ref);
+            float total = 0.0f;
+#pragma unroll
+            for (int w = 0; w < WAVES; ++w) total += sums[w][lane & 31] * exp2f(tops[w][lane & 31] - ref);
+            // (a block at a time: 4 KB a wave)
+#pragma unroll
+            for (int b = 0; b < DB; ++b) {
+                float *to_lds = (float *)lds + wave * 1024 + lane;
+                __syncthreads();
+#pragma unroll
+                for (int i = 0; i < 16; ++i) to_lds[i * 64] = run.y[b][i] * down;
+                __syncthreads();
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    float v = 0.0f;
+#pragma unroll
+                    for (int w = 0; w < WAVES; ++w) v += ((float *)lds)[w * 1024 + i * 64 + lane];
+                    run.y[b][i] = v;
+                }
+            }
+            run.top = top;
+            run.sum = (threadIdx.x & 32) ? 0.0f : total;
+        }
+        if (wave == 0) run.end(g, s, kv, r, blockIdx.y);
+    }
+}
+
+// In float16 dR has neither room for large gradients nor bits for small ones.  A lane's dR are kept times a power of two (its row's, or its key's), found from
+// the largest |dR| so far; when a larger one comes, what has been summed is brought to the new one.  The two lanes of a row go together.
+template <class T, int DB>
+__device__ __forceinline__ void keep_in_range(f32x16 &d, f32x16 (&acc)[DB], float &by)
+{
+    if constexpr (std::is_same_v<T, f16>) {
+        float most = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) most = fmaxf(most, fabsf(d[i]));
+        most = fmaxf(most, other_half(most));
+        most = most < INFINITY ? most : 0.0f;
+        if (__any(most * by > 32768.0f)) {
+            // the new factor leaves room for 2^4 more
+            int e;
+            (void)frexpf(most, &e);
+            const float next = most * by > 32768.0f ? ldexpf(1.0f, max(11 - e, -100)) : by, down = next / by;
+#pragma unroll
+            for (int b = 0; b < DB; ++b)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) acc[b][i] *= down;
+            by = next;
+        }
+#pragma unroll
+        for (int i = 0; i < 16; ++i) d[i] *= by;
+    }
+}
+template <class T>
+__device__ __forceinline__ float first_factor() { return std::is_same_v<T, f16> ? 0x1p60f : 1.0f; }
+
+// dq, and the sums of dy y on the way: a wave has 32 packed rows, the waves share tiles of 32 keys.
+template <class T, int DB, bool EXTRA, int WAVES>
+__global__ __launch_bounds__(WAVES * 64) void attention_dq_kernel(const AttentionArgs g)
+{
+    using R = Rows<T, DB>;
+    constexpr int KEYS = 32, NT = WAVES * 64;
+    __shared__ __align__(1024) char lds[2 * KEYS * R::ROWB];
+    const int kv = (int)((blockIdx.x + g.before) % g.kv_heads), lane = threadIdx.x & 63, h = lane >> 5;
+    Span s = find_span(g.offsets, g.seqs, g.rows, g.group, WAVES * 32, (int)((blockIdx.x + g.before) / g.kv_heads));
+    if (s.seq >= g.seqs) {
+        if (s.n > 0 && g.out.p) no_rows<T>(g, g.out, s, kv, s.r0, WAVES * 32, nullptr, 0);
+        return;
+    }
+    find_keys(g, s);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = s.r0 + wave * 32 + (lane & 31), i = min(r, s.n * g.group - 1);
+    const char *qp = packed_row(g, g.q, s, kv, i), *dp = packed_row(g, g.dy, s, kv, i), *yp = packed_row(g, g.y, s, kv, i);
+    u32x4 q[R::STEPS], dy[R::STEPS];
+    float delta = 0.0f;
+#pragma unroll
+    for (int k = 0; k < R::STEPS; ++k) {
+        const int at = k * 32 + h * 16;
+        q[k] = dy[k] = u32x4{0, 0, 0, 0};
+        if (at >= g.bytes) continue;
+        q[k] = *(const u32x4 *)(qp + at);
+        dy[k] = *(const u32x4 *)(dp + at);
+        const u32x4 y = *(const u32x4 *)(yp + at);
+        T a[16 / sizeof(T)], b[16 / sizeof(T)];
+        __builtin_memcpy(a, &dy[k], 16);
+        __builtin_memcpy(b, &y, 16);
+#pragma unroll
+        for (int j = 0; j < (int)(16 / sizeof(T)); ++j) delta += (float)a[j] * (float)b[j];
+    }
+    delta += other_half(delta);
+    const int64_t item = packed_item(g, s, kv, i);
+    if (h == 0 && r == i) g.delta[item] = delta;
+    if (!g.out.p) return;
+    float lse = g.lse[item] * LOG2E;
+    lse = lse == -INFINITY ? INFINITY : lse;           // (no key seen: all exponentials are zero)
+    const int limit = limit_of(g, s, i / g.group), where = i / g.group + s.ahead, end = min(s.r0 + WAVES * 32, s.n * g.group) - 1;
+    const float slope = EXTRA && g.slopes ? g.slopes[kv * g.group + i % g.group] : 0.0f;
+    const int most = limit_of(g, s, end / g.group), mine = __builtin_amdgcn_readlane(limit, 31);
+    f32x16 dq[DB];
+    clear(dq);
+    const typename R::Place place;
+    const char *k = g.k.p + (int64_t)s.k_first * g.k.row + (int64_t)kv * g.k.head, *v = g.v.p + (int64_t)s.k_first * g.v.row + (int64_t)kv * g.v.head;
+    const char *const k_lds = lds, *const v_lds = lds + KEYS * R::ROWB;
+    float by = first_factor<T>();
+    for (int j0 = 0; j0 < most; j0 += KEYS) {
+        __syncthreads();
+        fill<R, KEYS, NT>(lds, k + j0 * g.k.row, g.k.row, s.m - j0, g.bytes);
+        fill<R, KEYS, NT>(lds + KEYS * R::ROWB, v + j0 * g.v.row, g.v.row, s.m - j0, g.bytes);
+        __syncthreads();
+        if (j0 >= mine) continue;
+        f32x16 a, d;
+#pragma unroll
+        for (int j = 0; j < 16; ++j) a[j] = d[j] = 0.0f;
+#pragma unroll
+        for (int c = 0; c < R::STEPS; ++c) a = mma32(R::along(k_lds, place, 0, c), q[c], a, T{});
+#pragma unroll
+        for (int c = 0; c < R::STEPS; ++c) d = mma32(R::along(v_lds, place, 0, c), dy[c], d, T{});
+        const bool whole = !__any(j0 + KEYS > limit);
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+            const int key = j0 + block_row(j, h);
+            float e = a[j] * g.scale, bent = 1.0f;
+            if constexpr (EXTRA) {
+                if (g.cap != 0.0f) e = capped<T>(g, e, bent);
+                e -= slope * fabsf((float)(where - key));
+            }
+            const float p = __builtin_amdgcn_exp2f(fmaf(e, LOG2E, -lse));
+            float w = p * (d[j] - delta);
+            if constexpr (EXTRA) w *= bent;
+            d[j] = whole || key < limit ? w : 0.0f;
+        }
+        keep_in_range<T>(d, dq, by);
+#pragma unroll
+        for (int t = 0; t < R::FRAGS; ++t) {
+            const u32x4 w = R::packed(d, t);
+#pragma unroll
+            for (int b = 0; b < DB; ++b) dq[b] = mma32(R::across(k_lds, place, 0, t, b * 32), w, dq[b], T{});
+        }
+    }
+    if (r == i) store_head<T, DB>((char *)packed_row(g, g.out, s, kv, r), dq, g.scale / by, g.dim, g.wide);
+}
+
+// dk and dv: a wave has 32 keys, the waves share tiles of 32 packed rows of the kv head.
+template <class T, int DB, bool EXTRA, int WAVES>
+__global__ __launch_bounds__(WAVES * 64) void attention_dkv_kernel(const AttentionArgs g)
+{
+    using R = Rows<T, DB>;
+    constexpr int ROWS_AT_ONCE = 32, NT = WAVES * 64;
+    __shared__ __align__(1024) char lds[2 * ROWS_AT_ONCE * R::ROWB];
+    __shared__ __align__(16) float lses[32], deltas[32], slopes[32];
+    __shared__ __align__(16) int limits[32], places[32];
+    const int kv = (int)((blockIdx.x + g.before) % g.kv_heads), lane = threadIdx.x & 63, h = lane >> 5;
+    Span s = find_span(g.k_offsets, g.seqs, g.k_rows, 1, WAVES * 32, (int)((blockIdx.x + g.before) / g.kv_heads));
+    const int key0 = s.r0;
+    if (s.seq >= g.seqs) {
+        for (int c = threadIdx.x / 64; c < min(WAVES * 32, s.n - key0); c += WAVES)
+            for (int d = lane; d < g.dim; d += 64) {
+                const int64_t row = s.first + key0 + c, at = (((int64_t)blockIdx.y * g.k_rows + row) * g.kv_heads + kv) * g.dim + d;
+                if (g.out.p && g.splits > 1) g.part[at] = 0.0f;
+                else if (g.out.p) *((T *)(g.out.p + row * g.out.row + kv * g.out.head) + d) = (T)0.0f;
+                if (g.out2.p && g.splits > 1) g.part2[at] = 0.0f;
+                else if (g.out2.p) *((T *)(g.out2.p + row * g.out2.row + kv * g.out2.head) + d) = (T)0.0f;
+            }
+        return;
+    }
+    s.k_first = s.first;
+    s.m = s.n;
+    int first, stop;
+    sequence_rows(g.offsets, g.seqs, g.rows, s.seq, first, stop);
+    s.first = first;
+    s.n = stop - first;
+    s.ahead = s.m - s.n;
+    s.prefix = g.prefix && g.causal ? g.prefix[s.seq] : 0;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), key_w = key0 + wave * 32, key = key_w + (lane & 31);
+    const int64_t key_row = s.k_first + min(key, s.m - 1);
+    const char *kp = g.k.p + key_row * g.k.row + kv * g.k.head, *vp = g.v.p + key_row * g.v.row + kv * g.v.head;
+    u32x4 k[R::STEPS], v[R::STEPS];
+#pragma unroll
+    for (int c = 0; c < R::STEPS; ++c) {
+        const int at = c * 32 + h * 16;
+        const bool here = at < g.bytes;
+        k[c] = here ? *(const u32x4 *)(kp + at) : u32x4{0, 0, 0, 0};
+        v[c] = here ? *(const u32x4 *)(vp + at) : u32x4{0, 0, 0, 0};
+    }
+    f32x16 dk[DB], dv[DB];
+    clear(dk);
+    clear(dv);
+    const typename R::Place place;
+    const char *const q_lds = lds, *const dy_lds = lds + ROWS_AT_ONCE * R::ROWB;
+    float by = first_factor<T>();
+    // the first row that sees one of the tile's keys: row i sees key j in front of the prefix or where j <= i + ahead
+    const int all = s.n * g.group, begin = !g.causal || key0 < s.prefix ? 0 : min(max(key0 - s.ahead, 0), s.n) * g.group;
+    int from, to;
+    share_of(all - begin, ROWS_AT_ONCE, g.splits, blockIdx.y, from, to);
+    for (int r0 = begin + from; r0 < begin + to; r0 += ROWS_AT_ONCE) {
+        __syncthreads();
+        for (int c = threadIdx.x; c < ROWS_AT_ONCE * R::CHUNKS; c += NT) {
+            const int row = c / R::CHUNKS, chunk = c % R::CHUNKS;
+            u32x4 a = {0, 0, 0, 0}, b = {0, 0, 0, 0};
+            if (r0 + row < all && chunk * 16 < g.bytes) {
+                a = *(const u32x4 *)(packed_row(g, g.q, s, kv, r0 + row) + chunk * 16);
+                b = *(const u32x4 *)(packed_row(g, g.dy, s, kv, r0 + row) + chunk * 16);
+            }
+            *(u32x4 *)(lds + R::at(row, chunk)) = a;
+            *(u32x4 *)(lds + ROWS_AT_ONCE * R::ROWB + R::at(row, chunk)) = b;
+        }
+        if (threadIdx.x < 32) {
+            const int r = r0 + threadIdx.x, i = min(r, all - 1);
+            const int64_t item = packed_item(g, s, kv, i);
+            const float lse = g.lse[item] * LOG2E;
+            lses[threadIdx.x] = r > i || lse == -INFINITY ? INFINITY : lse;
+            deltas[threadIdx.x] = r > i ? 0.0f : g.delta[item];
+            limits[threadIdx.x] = limit_of(g, s, i / g.group);
+            places[threadIdx.x] = i / g.group + s.ahead;
+            slopes[threadIdx.x] = EXTRA && g.slopes ? g.slopes[kv * g.group + i % g.group] : 0.0f;
+        }
+        __syncthreads();
+        if (limits[31] <= key_w) continue;             // (no row of these sees a key of this wave)
+        f32x16 a, d, p;
+#pragma unroll
+        for (int j = 0; j < 16; ++j) a[j] = d[j] = 0.0f;
+#pragma unroll
+        for (int c = 0; c < R::STEPS; ++c) a = mma32(R::along(q_lds, place, 0, c), k[c], a, T{});
+#pragma unroll
+        for (int c = 0; c < R::STEPS; ++c) d = mma32(R::along(dy_lds, place, 0, c), v[c], d, T{});
+        const bool whole = limits[0] >= key_w + 32;
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+            const int r = block_row(j, h);
+            float e = a[j] * g.scale, bent = 1.0f;
+            if constexpr (EXTRA) {
+                if (g.cap != 0.0f) e = capped<T>(g, e, bent);
+                e -= slopes[r] * fabsf((float)(places[r] - key));
+            }
+            const bool seen = whole || key < limits[r];
+            p[j] = seen ? __builtin_amdgcn_exp2f(fmaf(e, LOG2E, -lses[r])) : 0.0f;
+            float w = p[j] * (d[j] - deltas[r]);
+            if constexpr (EXTRA) w *= bent;
+            d[j] = seen ? w : 0.0f;
+        }
+        keep_in_range<T>(d, dk, by);
+#pragma unroll
+        for (int t = 0; t < R::FRAGS; ++t) {
+            const u32x4 w = R::packed(p, t), u = R::packed(d, t);
+#pragma unroll
+            for (int b = 0; b < DB; ++b) {
+                dv[b] = mma32(R::across(dy_lds, place, 0, t, b * 32), w, dv[b], T{});
+                dk[b] = mma32(R::across(q_lds, place, 0, t, b * 32), u, dk[b], T{});
+            }
+        }
+    }
+    if (key >= s.m) return;
+    const int64_t row = s.k_first + key;
+    if (g.splits > 1) {
+        const int64_t at = ((int64_t)blockIdx.y * g.k_rows + row) * g.kv_heads + kv;
+        const int wide = (g.dim & 3) == 0;
+        if (g.out.p) store_head<float, DB>((char *)(g.part + at * g.dim), dk, g.scale / by, g.dim, wide);
+        if (g.out2.p) store_head<float, DB>((char *)(g.part2 + at * g.dim), dv, 1.0f, g.dim, wide);
+        return;
+    }
+    if (g.out.p) store_head<T, DB>(g.out.p + row * g.out.row + kv * g.out.head, dk, g.scale / by, g.dim, g.wide);
+    if (g.out2.p) store_head<T, DB>(g.out2.p + row * g.out2.row + kv * g.out2.head, dv, 1.0f, g.dim, g.wide);
+}
+
+inline bool extra(const AttentionArgs &g) { return g.cap != 0.0f || g.slopes || !(g.scale > 0.0f); }
+
+// (a grid's threads are counted in 32 bits)
+template <class Launch>
+hipError_t in_launches(const AttentionArgs &g, int64_t workgroups, Launch launch)
+{
+    constexpr int64_t MOST = 1 << 22;
+    AttentionArgs part = g;
+    for (int64_t done = 0; done < workgroups; done += MOST) {
+        part.before = (uint32_t)done;
+        launch(part, dim3((unsigned)std::min(workgroups - done, MOST), (unsigned)g.splits));
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+
+template <class T, int DB, bool EXTRA>
+hipError_t launch_rows(hipStream_t st, int few, const AttentionArgs &g)
+{
+    if (few)
+        return in_launches(g, ((int64_t)g.seqs + 1) * g.kv_heads, [&](const AttentionArgs &p, dim3 grid) {
+            attention_few_kernel<T, DB, EXTRA><<<grid, FewShape<T, DB>::WAVES * 64, 0, st>>>(p);
+        });
+    return in_launches(g, (int64_t)g.tiles * g.kv_heads, [&](const AttentionArgs &p, dim3 grid) { attention_kernel<T, DB, EXTRA, 4><<<grid, 256, 0, st>>>(p); });
+}
+template <class T, int DB, bool EXTRA>
+hipError_t launch_dq(hipStream_t st, const AttentionArgs &g)
+{
+    return in_launches(g, (int64_t)g.tiles * g.kv_heads, [&](const AttentionArgs &p, dim3 grid) { attention_dq_kernel<T, DB, EXTRA, 4><<<grid, 256, 0, st>>>(p); });
+}
+template <class T, int DB, bool EXTRA>
+hipError_t launch_dkv(hipStream_t st, const AttentionArgs &g)
+{
+    return in_launches(g, (int64_t)g.tiles * g.kv_heads, [&](const AttentionArgs &p, dim3 grid) { attention_dkv_kernel<T, DB, EXTRA, 4><<<grid, 256, 0, st>>>(p); });
+}
+
+#define ALPA_BY_DIM(call, T, g, ...)                                                                           \
+    switch (dim_blocks((g).dim)) {                                                                             \
+    case 2: return extra(g) ? call<T, 2, true>(__VA_ARGS__) : call<T, 2, false>(__VA_ARGS__);                  \
+    case 3: return extra(g) ? call<T, 3, true>(__VA_ARGS__) : call<T, 3, false>(__VA_ARGS__);                  \
+    case 4: return extra(g) ? call<T, 4, true>(__VA_ARGS__) : call<T, 4, false>(__VA_ARGS__);                  \
+    default: return extra(g) ? call<T, 8, true>(__VA_ARGS__) : call<T, 8, false>(__VA_ARGS__);                 \
+    }
+
+}  // namespace alpa
