@@ -151,12 +151,12 @@ def _scalars(operand: str) -> set:
 
 
 def check_load_ranges(asm_text: str) -> list:
-    """The loads to LDS of the products are inline assembly, so the compiler does not see that they read the four scalar
+    """The loads to LDS of the products and of attention are inline assembly, so the compiler does not see that they read the four scalar
     registers of their range, and would not keep a vector instruction that writes one of them the five wait states away
-    that the hardware asks for.  In every product_kernel of the device assembly: no such write stands so
+    that the hardware asks for.  In every product_kernel and attention kernel of the device assembly: no such write stands so
     close in front of a load, on any path to it."""
     bad = []
-    for part in re.split(r"\n(?=_ZN4alpa14product_kernel\S*:)", asm_text)[1:]:
+    for part in re.split(r"\n(?=_ZN4alpa\d+(?:product|attention\w*)_kernel\S*:)", asm_text)[1:]:
         name = part.split(":", 1)[0]
         code = part[:part.find("\n.Lfunc_end")] if "\n.Lfunc_end" in part else part
         lines = [t for t in (line.split(";", 1)[0].strip() for line in code.splitlines()[1:])
@@ -219,9 +219,9 @@ def build(verbose: bool = True, extra=()) -> str:
             raise subprocess.CalledProcessError(res.returncode, cmd)
         kernels.update(parse_resource_remarks(res.stderr))
 
-    # device assembly of the files that instantiate the recurrence kernel and the products, for the checks above
+    # device assembly of the files that instantiate the recurrence kernel, the products and attention, for the checks above
     asm_jobs = [(s, os.path.join(OBJ, os.path.basename(s)[:-4] + ".s")) for s in srcs
-                if os.path.basename(s).startswith(("kernels_fast", "kernels_product"))]
+                if os.path.basename(s).startswith(("kernels_fast", "kernels_product", "kernels_attention"))]
     asm_bad = []
 
     def asm(pair):
@@ -248,7 +248,7 @@ def build(verbose: bool = True, extra=()) -> str:
     if verbose:
         n_batch = sum(1 for k in kernels if _BATCH_INSTANCE.search(k))
         print(f"resource check: {len(kernels)} kernels, {n_batch} instances at 8 waves/SIMD, "
-              "no spills in the recurrence kernels, its warm-up register keeps its place, no vector write close to the products' loads", flush=True)
+              "no spills in the recurrence kernels, its warm-up register keeps its place, no vector write close to the loads to LDS", flush=True)
     cmd = [HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", LIB, *objs]
     if verbose:
         print(" ".join(cmd), flush=True)

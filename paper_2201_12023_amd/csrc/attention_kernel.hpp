@@ -187,18 +187,89 @@ __device__ __forceinline__ float capped(const AttentionArgs &g, float r, float &
 
 __device__ __forceinline__ float other_half(float v) { return __shfl_xor(v, 32, 64); }
 
-// Rows of a tile from memory to LDS: `rows` rows that exist, row r at p + r * stride, of R; the others, and what is behind a head's bytes, are zeros.
-template <class R, int COUNT, int NT>
-__device__ __forceinline__ void fill(char *lds, const char *p, int64_t stride, int rows, int bytes)
+// Sixteen bytes a lane from memory to LDS, written there by the load unit itself: the wave's go to `lds` and the 1008 bytes behind, in the order of its lanes; those
+// whose offset is out of range are zeros.  Assembly without a result register, as in product.hpp: what has arrived is known by counting.
+__device__ __forceinline__ void load_chunk(uint32_t lds, uint32_t off, u32x4 range)
 {
-#pragma unroll 4
-    for (int c = threadIdx.x % NT; c < COUNT * R::CHUNKS; c += NT) {
-        const int r = c / R::CHUNKS, chunk = c % R::CHUNKS;
-        u32x4 v = {0, 0, 0, 0};
-        if (r < rows && chunk * 16 < bytes) v = *(const u32x4 *)(p + r * stride + chunk * 16);
-        *(u32x4 *)(lds + R::at(r, chunk)) = v;
-    }
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"         // (m0 is reserved, and said to be overwritten all the same)
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+                 :
+                 : "s"(__builtin_amdgcn_readfirstlane(lds)), "v"(off), "s"(range)
+                 : "m0");
+#pragma clang diagnostic pop
 }
+__device__ __forceinline__ u32x4 range_of(const char *p, uint32_t bytes)
+{
+    const uint64_t at = (uint64_t)p;
+    return u32x4{(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)at), (uint32_t)__builtin_amdgcn_readfirstlane((int)((uint32_t)(at >> 32) & 0xffffu)),
+                 (uint32_t)__builtin_amdgcn_readfirstlane((int)bytes), 0x00020000u};
+}
+__device__ __forceinline__ uint32_t lds_at(const char *p) { return (uint32_t)(uintptr_t)(const ALPA_LDS char *)p; }
+
+// The COUNT rows of a tile that follow each other in memory, brought to LDS by NT threads: keys or values.
+template <class R, int COUNT, int NT>
+struct KeyLoader {
+    static constexpr int N = COUNT * R::CHUNKS / NT, APART = NT / R::CHUNKS;          // a thread's chunks are so many rows apart
+    static constexpr int KINDS = APART >= 16 ? 1 : 16 / APART < N ? 16 / APART : N;       // and lie at the same place of rows sixteen apart
+    static_assert(COUNT * R::CHUNKS % NT == 0 && (APART & (APART - 1)) == 0 && APART > 0, "chunks are dealt evenly");
+    const char *p;
+    int64_t stride;
+    int bytes;
+    uint32_t off[KINDS];
+
+    __device__ __forceinline__ KeyLoader(const char *first, int64_t row, int head_bytes) : p(first), stride(row), bytes(head_bytes)
+    {
+        const int t = threadIdx.x % NT;
+#pragma unroll
+        for (int j = 0; j < KINDS; ++j) {
+            const int r = t / R::CHUNKS + j * APART, chunk = (t % R::CHUNKS) ^ R::swz(r);
+            off[j] = chunk * 16 < bytes ? (uint32_t)(r * (int)row + chunk * 16) : OUT_OF_RANGE;
+        }
+    }
+    // rows j0 .. of which those from `end` on do not exist
+    __device__ __forceinline__ void load(uint32_t lds, int j0, int end) const
+    {
+        const int rows = min(end - j0, COUNT);
+        const u32x4 range = range_of(p + j0 * stride, rows > 0 ? (uint32_t)((rows - 1) * (int)stride + bytes) : 0u);
+        const uint32_t to = lds + __builtin_amdgcn_readfirstlane(threadIdx.x % NT / 64) * 1024;
+#pragma unroll
+        for (int j = 0; j < N; ++j) load_chunk(to + j * NT * 16, off[j % KINDS] + (uint32_t)(j / KINDS * KINDS * APART * (int)stride), range);
+    }
+};
+
+// COUNT packed rows of two tensors of queries.
+template <class R, int COUNT, int NT>
+struct PackedLoader {
+    static constexpr int N = COUNT * R::CHUNKS / NT, APART = NT / R::CHUNKS;
+    static_assert(COUNT * R::CHUNKS % NT == 0, "chunks are dealt evenly");
+    const char *a, *b;              // the kv head's first head of the sequence's row 0
+    int a_row, a_head, b_row, b_head, group, bytes;
+    int64_t a_long, b_long;
+    uint32_t inverse;
+
+    __device__ __forceinline__ PackedLoader(const AttentionArgs &g, const Heads &x, const Heads &y, int first, int kv)
+        : a(x.p + (int64_t)first * x.row + (int64_t)kv * g.group * x.head), b(y.p + (int64_t)first * y.row + (int64_t)kv * g.group * y.head), a_row((int)x.row),
+          a_head((int)x.head), b_row((int)y.row), b_head((int)y.head), group(g.group), bytes(g.bytes), a_long(x.row), b_long(y.row),
+          inverse(0xffffffffu / (uint32_t)g.group + 1)
+    {
+    }
+    __device__ __forceinline__ void load(uint32_t a_lds, uint32_t b_lds, int r0, int end) const
+    {
+        const int i0 = r0 / group, rest = r0 - i0 * group, t = threadIdx.x % NT;
+        const u32x4 ra = range_of(a + i0 * a_long, 0x7fffffffu), rb = range_of(b + i0 * b_long, 0x7fffffffu);
+        const uint32_t to = __builtin_amdgcn_readfirstlane(t / 64) * 1024;
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            const int r = t / R::CHUNKS + j * APART, chunk = (t % R::CHUNKS) ^ R::swz(r);
+            // (a quotient of at most 4160 by at most 4096; one head a row: the inverse has no room)
+            const int x = rest + r, i = group == 1 ? x : (int)__umulhi((uint32_t)x, inverse), h = x - i * group;
+            const bool here = r0 + r < end && chunk * 16 < bytes;
+            load_chunk(a_lds + to + j * NT * 16, here ? (uint32_t)(i * a_row + h * a_head + chunk * 16) : OUT_OF_RANGE, ra);
+            load_chunk(b_lds + to + j * NT * 16, here ? (uint32_t)(i * b_row + h * b_head + chunk * 16) : OUT_OF_RANGE, rb);
+        }
+    }
+};
 
 // Where packed row r of a sequence's kv head lies in a tensor of queries.
 __device__ __forceinline__ const char *packed_row(const AttentionArgs &g, const Heads &t, const Span &s, int kv, int r)
@@ -368,13 +439,13 @@ __device__ __forceinline__ void share_of(int most, int tile, int splits, int spl
     to = min(min(split * per + per, tiles) * tile, most);
 }
 
-// Many rows: a wave has 32 packed rows, the waves share tiles of 64 keys.
+// Many rows: a wave has 32 packed rows, the waves share tiles of keys, of which one is worked on and the next one under way.
 template <class T, int DB, bool EXTRA, int WAVES>
 __global__ __launch_bounds__(WAVES * 64, 2) void attention_kernel(const AttentionArgs g)
 {
     using R = Rows<T, DB>;
-    constexpr int KEYS = 64, NT = WAVES * 64;
-    __shared__ __align__(1024) char lds[2 * KEYS * R::ROWB];
+    constexpr int KEYS = R::ROWB <= 256 ? 64 : 32, NT = WAVES * 64, HALF = KEYS * R::ROWB;
+    __shared__ __align__(1024) char lds[4 * HALF];
     const int kv = (int)((blockIdx.x + g.before) % g.kv_heads);
     Span s = find_span(g.offsets, g.seqs, g.rows, g.group, WAVES * 32, (int)((blockIdx.x + g.before) / g.kv_heads));
     if (s.seq >= g.seqs) {
@@ -391,13 +462,20 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attention_kernel(const Attentio
     const int mine = __builtin_amdgcn_readlane(run.limit, 31);
     int from, to;
     share_of(most, KEYS, g.splits, blockIdx.y, from, to);
-    const char *k = g.k.p + (int64_t)s.k_first * g.k.row + (int64_t)kv * g.k.head, *v = g.v.p + (int64_t)s.k_first * g.v.row + (int64_t)kv * g.v.head;
-    for (int j0 = from; j0 < to; j0 += KEYS) {
-        __syncthreads();
-        fill<R, KEYS, NT>(lds, k + j0 * g.k.row, g.k.row, s.m - j0, g.bytes);
-        fill<R, KEYS, NT>(lds + KEYS * R::ROWB, v + j0 * g.v.row, g.v.row, s.m - j0, g.bytes);
-        __syncthreads();
-        if (j0 < mine) run.template step<KEYS / 32>(g, lds, lds + KEYS * R::ROWB, place, j0);
+    const KeyLoader<R, KEYS, NT> k(g.k.p + (int64_t)s.k_first * g.k.row + (int64_t)kv * g.k.head, g.k.row, g.bytes);
+    const KeyLoader<R, KEYS, NT> v(g.v.p + (int64_t)s.k_first * g.v.row + (int64_t)kv * g.v.head, g.v.row, g.bytes);
+    uint32_t here = 0;
+    if (from < to) {
+        k.load(lds_at(lds), from, s.m);
+        v.load(lds_at(lds) + HALF, from, s.m);
+    }
+    for (int j0 = from; j0 < to; j0 += KEYS, here ^= 2 * HALF) {
+        arrived<0>();
+        if (j0 + KEYS < to) {
+            k.load(lds_at(lds) + (here ^ 2 * HALF), j0 + KEYS, s.m);
+            v.load(lds_at(lds) + (here ^ 2 * HALF) + HALF, j0 + KEYS, s.m);
+        }
+        if (j0 < mine) run.template step<KEYS / 32>(g, lds + here, lds + here + HALF, place, j0);
     }
     run.end(g, s, kv, r, blockIdx.y);
 }
@@ -407,7 +485,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attention_kernel(const Attentio
 template <class T, int DB>
 struct FewShape {
     using R = Rows<T, DB>;
-    static constexpr int WAVES = R::ROWB <= 256 ? 4 : R::ROWB == 512 ? 2 : 1, SHARE = 2 * 32 * R::ROWB;
+    static constexpr int WAVES = R::ROWB <= 256 ? 4 : R::ROWB == 512 ? 2 : 1, SHARE = 32 * R::ROWB;          // (two tiles of keys and two of values a wave)
 };
 
 template <class T, int DB, bool EXTRA>
@@ -416,7 +494,7 @@ __global__ __launch_bounds__((FewShape<T, DB>::WAVES * 64)) void attention_few_k
     using F = FewShape<T, DB>;
     using R = Rows<T, DB>;
     constexpr int WAVES = F::WAVES;
-    __shared__ __align__(1024) char lds[WAVES * F::SHARE];
+    __shared__ __align__(1024) char lds[WAVES * 4 * F::SHARE];
     __shared__ float tops[WAVES][32], sums[WAVES][32];
     const int kv = (int)((blockIdx.x + g.before) % g.kv_heads), lane = threadIdx.x & 63;
     Span s;
@@ -438,21 +516,30 @@ __global__ __launch_bounds__((FewShape<T, DB>::WAVES * 64)) void attention_few_k
     find_keys(g, s);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const typename R::Place place;
-    char *const mine = lds + wave * F::SHARE;
-    const char *k = g.k.p + (int64_t)s.k_first * g.k.row + (int64_t)kv * g.k.head, *v = g.v.p + (int64_t)s.k_first * g.v.row + (int64_t)kv * g.v.head;
+    const uint32_t mine = lds_at(lds) + wave * 4 * F::SHARE;
+    const KeyLoader<R, 32, 64> k(g.k.p + (int64_t)s.k_first * g.k.row + (int64_t)kv * g.k.head, g.k.row, g.bytes);
+    const KeyLoader<R, 32, 64> v(g.v.p + (int64_t)s.k_first * g.v.row + (int64_t)kv * g.v.head, g.v.row, g.bytes);
     for (int r0 = 0; r0 < s.n * g.group; r0 += 32) {
         const int r = r0 + (lane & 31);
         Running<T, DB, EXTRA> run;
         run.begin(g, s, kv, r);
         int from, to;
         share_of(__builtin_amdgcn_readlane(run.limit, 31), 32 * WAVES, g.splits, blockIdx.y, from, to);
-        for (int j0 = from; j0 < to; j0 += 32 * WAVES) {
-            const int j = j0 + wave * 32;
-            __syncthreads();
-            fill<R, 32, 64>(mine, k + j * g.k.row, g.k.row, s.m - j, g.bytes);
-            fill<R, 32, 64>(mine + 32 * R::ROWB, v + j * g.v.row, g.v.row, s.m - j, g.bytes);
-            __syncthreads();
-            if (j < to) run.template step<1>(g, mine, mine + 32 * R::ROWB, place, j);
+        // each wave waits for its own loads alone
+        const int j1 = from + wave * 32;
+        uint32_t here = 0;
+        __syncthreads();                                   // (the rows before are done with)
+        if (j1 < to) {
+            k.load(mine, j1, s.m);
+            v.load(mine + F::SHARE, j1, s.m);
+        }
+        for (int j0 = j1; j0 < to; j0 += 32 * WAVES, here ^= 2 * F::SHARE) {
+            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+            if (j0 + 32 * WAVES < to) {
+                k.load(mine + (here ^ 2 * F::SHARE), j0 + 32 * WAVES, s.m);
+                v.load(mine + (here ^ 2 * F::SHARE) + F::SHARE, j0 + 32 * WAVES, s.m);
+            }
+            run.template step<1>(g, lds + wave * 4 * F::SHARE + here, lds + wave * 4 * F::SHARE + here + F::SHARE, place, j0);
         }
         if constexpr (WAVES > 1) {
             // the waves' sums, each brought to the common maximum; wave 0 goes on with them
@@ -527,8 +614,8 @@ template <class T, int DB, bool EXTRA, int WAVES>
 __global__ __launch_bounds__(WAVES * 64) void attention_dq_kernel(const AttentionArgs g)
 {
     using R = Rows<T, DB>;
-    constexpr int KEYS = 32, NT = WAVES * 64;
-    __shared__ __align__(1024) char lds[2 * KEYS * R::ROWB];
+    constexpr int KEYS = R::ROWB <= 256 ? 64 : 32, NT = WAVES * 64, HALF = KEYS * R::ROWB;
+    __shared__ __align__(1024) char lds[4 * HALF];
     const int kv = (int)((blockIdx.x + g.before) % g.kv_heads), lane = threadIdx.x & 63, h = lane >> 5;
     Span s = find_span(g.offsets, g.seqs, g.rows, g.group, WAVES * 32, (int)((blockIdx.x + g.before) / g.kv_heads));
     if (s.seq >= g.seqs) {
@@ -566,42 +653,52 @@ __global__ __launch_bounds__(WAVES * 64) void attention_dq_kernel(const Attentio
     f32x16 dq[DB];
     clear(dq);
     const typename R::Place place;
-    const char *k = g.k.p + (int64_t)s.k_first * g.k.row + (int64_t)kv * g.k.head, *v = g.v.p + (int64_t)s.k_first * g.v.row + (int64_t)kv * g.v.head;
-    const char *const k_lds = lds, *const v_lds = lds + KEYS * R::ROWB;
+    const KeyLoader<R, KEYS, NT> k(g.k.p + (int64_t)s.k_first * g.k.row + (int64_t)kv * g.k.head, g.k.row, g.bytes);
+    const KeyLoader<R, KEYS, NT> v(g.v.p + (int64_t)s.k_first * g.v.row + (int64_t)kv * g.v.head, g.v.row, g.bytes);
     float by = first_factor<T>();
-    for (int j0 = 0; j0 < most; j0 += KEYS) {
-        __syncthreads();
-        fill<R, KEYS, NT>(lds, k + j0 * g.k.row, g.k.row, s.m - j0, g.bytes);
-        fill<R, KEYS, NT>(lds + KEYS * R::ROWB, v + j0 * g.v.row, g.v.row, s.m - j0, g.bytes);
-        __syncthreads();
-        if (j0 >= mine) continue;
-        f32x16 a, d;
-#pragma unroll
-        for (int j = 0; j < 16; ++j) a[j] = d[j] = 0.0f;
-#pragma unroll
-        for (int c = 0; c < R::STEPS; ++c) a = mma32(R::along(k_lds, place, 0, c), q[c], a, T{});
-#pragma unroll
-        for (int c = 0; c < R::STEPS; ++c) d = mma32(R::along(v_lds, place, 0, c), dy[c], d, T{});
-        const bool whole = !__any(j0 + KEYS > limit);
-#pragma unroll
-        for (int j = 0; j < 16; ++j) {
-            const int key = j0 + block_row(j, h);
-            float e = a[j] * g.scale, bent = 1.0f;
-            if constexpr (EXTRA) {
-                if (g.cap != 0.0f) e = capped<T>(g, e, bent);
-                e -= slope * fabsf((float)(where - key));
-            }
-            const float p = __builtin_amdgcn_exp2f(fmaf(e, LOG2E, -lse));
-            float w = p * (d[j] - delta);
-            if constexpr (EXTRA) w *= bent;
-            d[j] = whole || key < limit ? w : 0.0f;
+    uint32_t here = 0;
+    if (most > 0) {
+        k.load(lds_at(lds), 0, s.m);
+        v.load(lds_at(lds) + HALF, 0, s.m);
+    }
+    for (int j0 = 0; j0 < most; j0 += KEYS, here ^= 2 * HALF) {
+        arrived<0>();
+        if (j0 + KEYS < most) {
+            k.load(lds_at(lds) + (here ^ 2 * HALF), j0 + KEYS, s.m);
+            v.load(lds_at(lds) + (here ^ 2 * HALF) + HALF, j0 + KEYS, s.m);
         }
-        keep_in_range<T>(d, dq, by);
+        const char *const k_lds = lds + here, *const v_lds = lds + here + HALF;
 #pragma unroll
-        for (int t = 0; t < R::FRAGS; ++t) {
-            const u32x4 w = R::packed(d, t);
+        for (int at = 0; at < KEYS; at += 32) {
+            if (j0 + at >= mine) continue;
+            f32x16 a, d;
 #pragma unroll
-            for (int b = 0; b < DB; ++b) dq[b] = mma32(R::across(k_lds, place, 0, t, b * 32), w, dq[b], T{});
+            for (int j = 0; j < 16; ++j) a[j] = d[j] = 0.0f;
+#pragma unroll
+            for (int c = 0; c < R::STEPS; ++c) a = mma32(R::along(k_lds, place, at, c), q[c], a, T{});
+#pragma unroll
+            for (int c = 0; c < R::STEPS; ++c) d = mma32(R::along(v_lds, place, at, c), dy[c], d, T{});
+            const bool whole = !__any(j0 + at + 32 > limit);
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+                const int key = j0 + at + block_row(j, h);
+                float e = a[j] * g.scale, bent = 1.0f;
+                if constexpr (EXTRA) {
+                    if (g.cap != 0.0f) e = capped<T>(g, e, bent);
+                    e -= slope * fabsf((float)(where - key));
+                }
+                const float p = __builtin_amdgcn_exp2f(fmaf(e, LOG2E, -lse));
+                float w = p * (d[j] - delta);
+                if constexpr (EXTRA) w *= bent;
+                d[j] = whole || key < limit ? w : 0.0f;
+            }
+            keep_in_range<T>(d, dq, by);
+#pragma unroll
+            for (int t = 0; t < R::FRAGS; ++t) {
+                const u32x4 w = R::packed(d, t);
+#pragma unroll
+                for (int b = 0; b < DB; ++b) dq[b] = mma32(R::across(k_lds, place, at, t, b * 32), w, dq[b], T{});
+            }
         }
     }
     if (r == i) store_head<T, DB>((char *)packed_row(g, g.out, s, kv, r), dq, g.scale / by, g.dim, g.wide);
@@ -612,10 +709,10 @@ template <class T, int DB, bool EXTRA, int WAVES>
 __global__ __launch_bounds__(WAVES * 64) void attention_dkv_kernel(const AttentionArgs g)
 {
     using R = Rows<T, DB>;
-    constexpr int ROWS_AT_ONCE = 32, NT = WAVES * 64;
-    __shared__ __align__(1024) char lds[2 * ROWS_AT_ONCE * R::ROWB];
-    __shared__ __align__(16) float lses[32], deltas[32], slopes[32];
-    __shared__ __align__(16) int limits[32], places[32];
+    constexpr int TILE = 32, NT = WAVES * 64, HALF = TILE * R::ROWB;
+    struct RowsInfo { float lse[TILE], delta[TILE], slope[TILE]; int limit[TILE], place[TILE]; };
+    __shared__ __align__(1024) char lds[4 * HALF];
+    __shared__ __align__(16) RowsInfo infos[2];
     const int kv = (int)((blockIdx.x + g.before) % g.kv_heads), lane = threadIdx.x & 63, h = lane >> 5;
     Span s = find_span(g.k_offsets, g.seqs, g.k_rows, 1, WAVES * 32, (int)((blockIdx.x + g.before) / g.kv_heads));
     const int key0 = s.r0;
@@ -653,68 +750,79 @@ __global__ __launch_bounds__(WAVES * 64) void attention_dkv_kernel(const Attenti
     clear(dk);
     clear(dv);
     const typename R::Place place;
-    const char *const q_lds = lds, *const dy_lds = lds + ROWS_AT_ONCE * R::ROWB;
     float by = first_factor<T>();
     // the first row that sees one of the tile's keys: row i sees key j in front of the prefix or where j <= i + ahead
     const int all = s.n * g.group, begin = !g.causal || key0 < s.prefix ? 0 : min(max(key0 - s.ahead, 0), s.n) * g.group;
     int from, to;
-    share_of(all - begin, ROWS_AT_ONCE, g.splits, blockIdx.y, from, to);
-    for (int r0 = begin + from; r0 < begin + to; r0 += ROWS_AT_ONCE) {
-        __syncthreads();
-        for (int c = threadIdx.x; c < ROWS_AT_ONCE * R::CHUNKS; c += NT) {
-            const int row = c / R::CHUNKS, chunk = c % R::CHUNKS;
-            u32x4 a = {0, 0, 0, 0}, b = {0, 0, 0, 0};
-            if (r0 + row < all && chunk * 16 < g.bytes) {
-                a = *(const u32x4 *)(packed_row(g, g.q, s, kv, r0 + row) + chunk * 16);
-                b = *(const u32x4 *)(packed_row(g, g.dy, s, kv, r0 + row) + chunk * 16);
+    share_of(all - begin, TILE, g.splits, blockIdx.y, from, to);
+    from += begin;
+    to += begin;
+    const PackedLoader<R, TILE, NT> loader(g, g.q, g.dy, s.first, kv);
+    // What is known of a tile's rows, by one thread each: asked for in front of a step, put to LDS behind it.
+    float lse_next = 0.0f, delta_next = 0.0f;
+    const auto ask = [&](int r0) {
+        const int64_t item = packed_item(g, s, kv, min(r0 + (int)threadIdx.x % TILE, all - 1));
+        lse_next = g.lse[item];
+        delta_next = g.delta[item];
+    };
+    const auto put = [&](int r0, RowsInfo &info) {
+        if (threadIdx.x >= TILE) return;
+        const int t = threadIdx.x, r = r0 + t, i = min(r, all - 1), row = i / g.group;
+        info.lse[t] = r > i || lse_next == -INFINITY ? INFINITY : lse_next * LOG2E;
+        info.delta[t] = r > i ? 0.0f : delta_next;
+        info.limit[t] = limit_of(g, s, row);
+        info.place[t] = row + s.ahead;
+        info.slope[t] = EXTRA && g.slopes ? g.slopes[kv * g.group + i - row * g.group] : 0.0f;
+    };
+    int here = 0;
+    if (from < to) {
+        ask(from);
+        loader.load(lds_at(lds), lds_at(lds) + HALF, from, all);
+        put(from, infos[0]);
+    }
+    for (int r0 = from; r0 < to; r0 += TILE, here ^= 1) {
+        arrived<0>();
+        if (r0 + TILE < to) {
+            ask(r0 + TILE);
+            loader.load(lds_at(lds) + (here ^ 1) * 2 * HALF, lds_at(lds) + (here ^ 1) * 2 * HALF + HALF, r0 + TILE, all);
+        }
+        const RowsInfo &info = infos[here];
+        const char *const q_lds = lds + here * 2 * HALF, *const dy_lds = q_lds + HALF;
+        if (info.limit[TILE - 1] > key_w) {                      // (else no row of these sees a key of this wave)
+            f32x16 a, d, p;
+#pragma unroll
+            for (int j = 0; j < 16; ++j) a[j] = d[j] = 0.0f;
+#pragma unroll
+            for (int c = 0; c < R::STEPS; ++c) a = mma32(R::along(q_lds, place, 0, c), k[c], a, T{});
+#pragma unroll
+            for (int c = 0; c < R::STEPS; ++c) d = mma32(R::along(dy_lds, place, 0, c), v[c], d, T{});
+            const bool whole = info.limit[0] >= key_w + 32;
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+                const int r = block_row(j, h);
+                float e = a[j] * g.scale, bent = 1.0f;
+                if constexpr (EXTRA) {
+                    if (g.cap != 0.0f) e = capped<T>(g, e, bent);
+                    e -= info.slope[r] * fabsf((float)(info.place[r] - key));
+                }
+                const bool seen = whole || key < info.limit[r];
+                p[j] = seen ? __builtin_amdgcn_exp2f(fmaf(e, LOG2E, -info.lse[r])) : 0.0f;
+                float w = p[j] * (d[j] - info.delta[r]);
+                if constexpr (EXTRA) w *= bent;
+                d[j] = seen ? w : 0.0f;
             }
-            *(u32x4 *)(lds + R::at(row, chunk)) = a;
-            *(u32x4 *)(lds + ROWS_AT_ONCE * R::ROWB + R::at(row, chunk)) = b;
-        }
-        if (threadIdx.x < 32) {
-            const int r = r0 + threadIdx.x, i = min(r, all - 1);
-            const int64_t item = packed_item(g, s, kv, i);
-            const float lse = g.lse[item] * LOG2E;
-            lses[threadIdx.x] = r > i || lse == -INFINITY ? INFINITY : lse;
-            deltas[threadIdx.x] = r > i ? 0.0f : g.delta[item];
-            limits[threadIdx.x] = limit_of(g, s, i / g.group);
-            places[threadIdx.x] = i / g.group + s.ahead;
-            slopes[threadIdx.x] = EXTRA && g.slopes ? g.slopes[kv * g.group + i % g.group] : 0.0f;
-        }
-        __syncthreads();
-        if (limits[31] <= key_w) continue;             // (no row of these sees a key of this wave)
-        f32x16 a, d, p;
+            keep_in_range<T>(d, dk, by);
 #pragma unroll
-        for (int j = 0; j < 16; ++j) a[j] = d[j] = 0.0f;
+            for (int t = 0; t < R::FRAGS; ++t) {
+                const u32x4 w = R::packed(p, t), u = R::packed(d, t);
 #pragma unroll
-        for (int c = 0; c < R::STEPS; ++c) a = mma32(R::along(q_lds, place, 0, c), k[c], a, T{});
-#pragma unroll
-        for (int c = 0; c < R::STEPS; ++c) d = mma32(R::along(dy_lds, place, 0, c), v[c], d, T{});
-        const bool whole = limits[0] >= key_w + 32;
-#pragma unroll
-        for (int j = 0; j < 16; ++j) {
-            const int r = block_row(j, h);
-            float e = a[j] * g.scale, bent = 1.0f;
-            if constexpr (EXTRA) {
-                if (g.cap != 0.0f) e = capped<T>(g, e, bent);
-                e -= slopes[r] * fabsf((float)(places[r] - key));
-            }
-            const bool seen = whole || key < limits[r];
-            p[j] = seen ? __builtin_amdgcn_exp2f(fmaf(e, LOG2E, -lses[r])) : 0.0f;
-            float w = p[j] * (d[j] - deltas[r]);
-            if constexpr (EXTRA) w *= bent;
-            d[j] = seen ? w : 0.0f;
-        }
-        keep_in_range<T>(d, dk, by);
-#pragma unroll
-        for (int t = 0; t < R::FRAGS; ++t) {
-            const u32x4 w = R::packed(p, t), u = R::packed(d, t);
-#pragma unroll
-            for (int b = 0; b < DB; ++b) {
-                dv[b] = mma32(R::across(dy_lds, place, 0, t, b * 32), w, dv[b], T{});
-                dk[b] = mma32(R::across(q_lds, place, 0, t, b * 32), u, dk[b], T{});
+                for (int b = 0; b < DB; ++b) {
+                    dv[b] = mma32(R::across(dy_lds, place, 0, t, b * 32), w, dv[b], T{});
+                    dk[b] = mma32(R::across(q_lds, place, 0, t, b * 32), u, dk[b], T{});
+                }
             }
         }
+        if (r0 + TILE < to) put(r0 + TILE, infos[here ^ 1]);
     }
     if (key >= s.m) return;
     const int64_t row = s.k_first + key;
