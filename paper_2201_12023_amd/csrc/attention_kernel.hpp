@@ -108,6 +108,25 @@ struct Rows {
     using i16x8 = short __attribute__((ext_vector_type(8)));
 };
 
+// acc += (32 rows in LDS from row0 on) x (a fragment a step): reads go ahead of the products by groups of four.
+template <class R, class T>
+__device__ __forceinline__ void along_product(const char *lds, const typename R::Place &p, int row0, const u32x4 (&b)[R::STEPS], f32x16 &acc)
+{
+    constexpr int GROUP = 4;
+    u32x4 f[2][GROUP];
+#pragma unroll
+    for (int c = 0; c < GROUP && c < R::STEPS; ++c) f[0][c] = R::along(lds, p, row0, c);
+#pragma unroll
+    for (int k = 0; k < R::STEPS; k += GROUP) {
+#pragma unroll
+        for (int c = 0; c < GROUP; ++c)
+            if (k + GROUP + c < R::STEPS) f[(k / GROUP + 1) & 1][c] = R::along(lds, p, row0, k + GROUP + c);
+#pragma unroll
+        for (int c = 0; c < GROUP; ++c)
+            if (k + c < R::STEPS) acc = mma32(f[(k / GROUP) & 1][c], b[k + c], acc, T{});
+    }
+}
+
 // A sequence's share of the tensors.
 struct Span {
     int seq;                        // seqs and above: rows of no sequence, seqs + 2: none
@@ -611,7 +630,7 @@ __device__ __forceinline__ float first_factor() { return std::is_same_v<T, f16> 
 
 // dq, and the sums of dy y on the way: a wave has 32 packed rows, the waves share tiles of 32 keys.
 template <class T, int DB, bool EXTRA, int WAVES>
-__global__ __launch_bounds__(WAVES * 64) void attention_dq_kernel(const AttentionArgs g)
+__global__ __launch_bounds__(WAVES * 64, sizeof(T) == 2 && DB <= 4 ? 2 : 1) void attention_dq_kernel(const AttentionArgs g)
 {
     using R = Rows<T, DB>;
     constexpr int KEYS = R::ROWB <= 256 ? 64 : 32, NT = WAVES * 64, HALF = KEYS * R::ROWB;
@@ -674,23 +693,27 @@ __global__ __launch_bounds__(WAVES * 64) void attention_dq_kernel(const Attentio
             f32x16 a, d;
 #pragma unroll
             for (int j = 0; j < 16; ++j) a[j] = d[j] = 0.0f;
+            along_product<R, T>(k_lds, place, at, q, a);
+            along_product<R, T>(v_lds, place, at, dy, d);
+            float by_log = g.scale * LOG2E;
+            if constexpr (EXTRA) {
 #pragma unroll
-            for (int c = 0; c < R::STEPS; ++c) a = mma32(R::along(k_lds, place, at, c), q[c], a, T{});
+                for (int j = 0; j < 16; ++j) {
+                    float e = a[j] * g.scale, bent = 1.0f;
+                    if (g.cap != 0.0f) e = capped<T>(g, e, bent);
+                    a[j] = e - slope * fabsf((float)(where - (j0 + at + block_row(j, h))));
+                    d[j] = (d[j] - delta) * bent;
+                }
+                by_log = LOG2E;
+            }
+            if (__any(j0 + at + 32 > limit)) {
 #pragma unroll
-            for (int c = 0; c < R::STEPS; ++c) d = mma32(R::along(v_lds, place, at, c), dy[c], d, T{});
-            const bool whole = !__any(j0 + at + 32 > limit);
+                for (int j = 0; j < 16; ++j) a[j] = j0 + at + block_row(j, h) < limit ? a[j] : -INFINITY;
+            }
 #pragma unroll
             for (int j = 0; j < 16; ++j) {
-                const int key = j0 + at + block_row(j, h);
-                float e = a[j] * g.scale, bent = 1.0f;
-                if constexpr (EXTRA) {
-                    if (g.cap != 0.0f) e = capped<T>(g, e, bent);
-                    e -= slope * fabsf((float)(where - key));
-                }
-                const float p = __builtin_amdgcn_exp2f(fmaf(e, LOG2E, -lse));
-                float w = p * (d[j] - delta);
-                if constexpr (EXTRA) w *= bent;
-                d[j] = whole || key < limit ? w : 0.0f;
+                const float p = __builtin_amdgcn_exp2f(fmaf(a[j], by_log, -lse));
+                d[j] = p * (EXTRA ? d[j] : d[j] - delta);
             }
             keep_in_range<T>(d, dq, by);
 #pragma unroll
@@ -706,13 +729,16 @@ __global__ __launch_bounds__(WAVES * 64) void attention_dq_kernel(const Attentio
 
 // dk and dv: a wave has 32 keys, the waves share tiles of 32 packed rows of the kv head.
 template <class T, int DB, bool EXTRA, int WAVES>
-__global__ __launch_bounds__(WAVES * 64) void attention_dkv_kernel(const AttentionArgs g)
+__global__ __launch_bounds__(WAVES * 64, sizeof(T) == 2 && DB <= 4 ? 2 : 1) void attention_dkv_kernel(const AttentionArgs g)
 {
     using R = Rows<T, DB>;
     constexpr int TILE = 32, NT = WAVES * 64, HALF = TILE * R::ROWB;
+    // (in registers the keys would leave room for one wave a SIMD)
+    constexpr bool K_IN_LDS = sizeof(T) == 2 && DB == 4;
     struct RowsInfo { float lse[TILE], delta[TILE], slope[TILE]; int limit[TILE], place[TILE]; };
-    __shared__ __align__(1024) char lds[4 * HALF];
+    __shared__ __align__(1024) char lds[4 * HALF + (K_IN_LDS ? WAVES * 32 * R::ROWB : 0)];
     __shared__ __align__(16) RowsInfo infos[2];
+    const char *const k_lds = lds + 4 * HALF;
     const int kv = (int)((blockIdx.x + g.before) % g.kv_heads), lane = threadIdx.x & 63, h = lane >> 5;
     Span s = find_span(g.k_offsets, g.seqs, g.k_rows, 1, WAVES * 32, (int)((blockIdx.x + g.before) / g.kv_heads));
     const int key0 = s.r0;
@@ -738,12 +764,12 @@ __global__ __launch_bounds__(WAVES * 64) void attention_dkv_kernel(const Attenti
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), key_w = key0 + wave * 32, key = key_w + (lane & 31);
     const int64_t key_row = s.k_first + min(key, s.m - 1);
     const char *kp = g.k.p + key_row * g.k.row + kv * g.k.head, *vp = g.v.p + key_row * g.v.row + kv * g.v.head;
-    u32x4 k[R::STEPS], v[R::STEPS];
+    u32x4 k[K_IN_LDS ? 1 : R::STEPS], v[R::STEPS];
 #pragma unroll
     for (int c = 0; c < R::STEPS; ++c) {
         const int at = c * 32 + h * 16;
         const bool here = at < g.bytes;
-        k[c] = here ? *(const u32x4 *)(kp + at) : u32x4{0, 0, 0, 0};
+        if (!K_IN_LDS) k[K_IN_LDS ? 0 : c] = here ? *(const u32x4 *)(kp + at) : u32x4{0, 0, 0, 0};
         v[c] = here ? *(const u32x4 *)(vp + at) : u32x4{0, 0, 0, 0};
     }
     f32x16 dk[DB], dv[DB];
@@ -776,6 +802,10 @@ __global__ __launch_bounds__(WAVES * 64) void attention_dkv_kernel(const Attenti
     };
     int here = 0;
     if (from < to) {
+        if constexpr (K_IN_LDS) {
+            const KeyLoader<R, WAVES * 32, NT> keys(g.k.p + (int64_t)s.k_first * g.k.row + (int64_t)kv * g.k.head, g.k.row, g.bytes);
+            keys.load(lds_at(k_lds), key0, s.m);
+        }
         ask(from);
         loader.load(lds_at(lds), lds_at(lds) + HALF, from, all);
         put(from, infos[0]);
@@ -789,37 +819,50 @@ __global__ __launch_bounds__(WAVES * 64) void attention_dkv_kernel(const Attenti
         const RowsInfo &info = infos[here];
         const char *const q_lds = lds + here * 2 * HALF, *const dy_lds = q_lds + HALF;
         if (info.limit[TILE - 1] > key_w) {                      // (else no row of these sees a key of this wave)
-            f32x16 a, d, p;
+            f32x16 a, d;
 #pragma unroll
             for (int j = 0; j < 16; ++j) a[j] = d[j] = 0.0f;
+            if constexpr (K_IN_LDS) {
 #pragma unroll
-            for (int c = 0; c < R::STEPS; ++c) a = mma32(R::along(q_lds, place, 0, c), k[c], a, T{});
+                for (int c = 0; c < R::STEPS; ++c) a = mma32(R::along(q_lds, place, 0, c), R::along(k_lds, place, wave * 32, c), a, T{});
+            } else {
+                along_product<R, T>(q_lds, place, 0, k, a);
+            }
+            along_product<R, T>(dy_lds, place, 0, v, d);
+            float by_log = g.scale * LOG2E;
+            if constexpr (EXTRA) {
 #pragma unroll
-            for (int c = 0; c < R::STEPS; ++c) d = mma32(R::along(dy_lds, place, 0, c), v[c], d, T{});
-            const bool whole = info.limit[0] >= key_w + 32;
+                for (int j = 0; j < 16; ++j) {
+                    const int r = block_row(j, h);
+                    float e = a[j] * g.scale, bent = 1.0f;
+                    if (g.cap != 0.0f) e = capped<T>(g, e, bent);
+                    a[j] = e - info.slope[r] * fabsf((float)(info.place[r] - key));
+                    d[j] = (d[j] - info.delta[r]) * bent;
+                }
+                by_log = LOG2E;
+            }
+            if (info.limit[0] < key_w + 32) {
+#pragma unroll
+                for (int j = 0; j < 16; ++j) a[j] = key < info.limit[block_row(j, h)] ? a[j] : -INFINITY;
+            }
 #pragma unroll
             for (int j = 0; j < 16; ++j) {
                 const int r = block_row(j, h);
-                float e = a[j] * g.scale, bent = 1.0f;
-                if constexpr (EXTRA) {
-                    if (g.cap != 0.0f) e = capped<T>(g, e, bent);
-                    e -= info.slope[r] * fabsf((float)(info.place[r] - key));
-                }
-                const bool seen = whole || key < info.limit[r];
-                p[j] = seen ? __builtin_amdgcn_exp2f(fmaf(e, LOG2E, -info.lse[r])) : 0.0f;
-                float w = p[j] * (d[j] - info.delta[r]);
-                if constexpr (EXTRA) w *= bent;
-                d[j] = seen ? w : 0.0f;
+                a[j] = __builtin_amdgcn_exp2f(fmaf(a[j], by_log, -info.lse[r]));
+                d[j] = a[j] * (EXTRA ? d[j] : d[j] - info.delta[r]);
+            }
+#pragma unroll
+            for (int t = 0; t < R::FRAGS; ++t) {
+                const u32x4 w = R::packed(a, t);
+#pragma unroll
+                for (int b = 0; b < DB; ++b) dv[b] = mma32(R::across(dy_lds, place, 0, t, b * 32), w, dv[b], T{});
             }
             keep_in_range<T>(d, dk, by);
 #pragma unroll
             for (int t = 0; t < R::FRAGS; ++t) {
-                const u32x4 w = R::packed(p, t), u = R::packed(d, t);
+                const u32x4 w = R::packed(d, t);
 #pragma unroll
-                for (int b = 0; b < DB; ++b) {
-                    dv[b] = mma32(R::across(dy_lds, place, 0, t, b * 32), w, dv[b], T{});
-                    dk[b] = mma32(R::across(q_lds, place, 0, t, b * 32), u, dk[b], T{});
-                }
+                for (int b = 0; b < DB; ++b) dk[b] = mma32(R::across(q_lds, place, 0, t, b * 32), w, dk[b], T{});
             }
         }
         if (r0 + TILE < to) put(r0 + TILE, infos[here ^ 1]);
