@@ -158,7 +158,9 @@ __device__ __forceinline__ void find_keys(const AttentionArgs &g, Span &s)
     s.ahead = s.m - s.n;
 }
 
-// The tile-th run of up to `tile` packed rows of one group of rows (slots.hpp), `group` of them a row.
+// The index-th run of up to `tile` packed rows of one group of rows (slots.hpp), `group` of them a row.  LAST_FIRST: a sequence's runs from its last one on.
+// With a causal mask the last rows have most keys, and the first keys most rows: those go first, and the short ones fill up the end.
+template <bool LAST_FIRST>
 __device__ __forceinline__ Span find_span(const int32_t *offsets, int seqs, int rows, int group, int tile, int index)
 {
     const int lane = threadIdx.x & 63;
@@ -179,8 +181,7 @@ __device__ __forceinline__ Span find_span(const int32_t *offsets, int seqs, int 
             const int f = __builtin_amdgcn_readlane(first, l), e = __builtin_amdgcn_readlane(end, l), count = __builtin_amdgcn_readlane(n, l);
             const int s = before + __builtin_amdgcn_readlane(sum, l) - count;
             if (index < s || index - s >= count) break;          // (offsets that are none)
-            // a sequence's tiles from its last one on: with a causal mask those have most keys, and the short ones fill up the end
-            return Span{base + l, f, e - f, (count - 1 - (index - s)) * tile, 0, 0, 0, 0};
+            return Span{base + l, f, e - f, (LAST_FIRST ? count - 1 - (index - s) : index - s) * tile, 0, 0, 0, 0};
         }
         before += __builtin_amdgcn_readlane(sum, 63);
     }
@@ -272,6 +273,13 @@ struct PackedLoader {
           a_head((int)x.head), b_row((int)y.row), b_head((int)y.head), group(g.group), bytes(g.bytes), a_long(x.row), b_long(y.row),
           inverse(0xffffffffu / (uint32_t)g.group + 1)
     {
+    }
+    // packed row r0 + t as row and head of the group
+    __device__ __forceinline__ void place(int r0, int t, int &row, int &head) const
+    {
+        const int i0 = r0 / group, x = r0 - i0 * group + t, i = group == 1 ? x : (int)__umulhi((uint32_t)x, inverse);
+        row = i0 + i;
+        head = x - i * group;
     }
     __device__ __forceinline__ void load(uint32_t a_lds, uint32_t b_lds, int r0, int end) const
     {
@@ -466,7 +474,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attention_kernel(const Attentio
     constexpr int KEYS = R::ROWB <= 256 ? 64 : 32, NT = WAVES * 64, HALF = KEYS * R::ROWB;
     __shared__ __align__(1024) char lds[4 * HALF];
     const int kv = (int)((blockIdx.x + g.before) % g.kv_heads);
-    Span s = find_span(g.offsets, g.seqs, g.rows, g.group, WAVES * 32, (int)((blockIdx.x + g.before) / g.kv_heads));
+    Span s = find_span<true>(g.offsets, g.seqs, g.rows, g.group, WAVES * 32, (int)((blockIdx.x + g.before) / g.kv_heads));
     if (s.seq >= g.seqs) {
         if (s.n > 0) no_rows<T>(g, g.out, s, kv, s.r0, WAVES * 32, g.lse, blockIdx.y);
         return;
@@ -599,6 +607,30 @@ __global__ __launch_bounds__((FewShape<T, DB>::WAVES * 64)) void attention_few_k
     }
 }
 
+// The packed rows that see a tile's keys, and the parts they are dealt in: of a causal sequence the first keys have most rows, and their tiles alone would
+// be what the call waits for.  Parts are `chunk` rows, counted from the last one, so that a tile with few rows is one part and needs no join.
+struct RowParts {
+    int all, begin, chunk, count;
+
+    // `s` as find_span() gives it for keys; it is turned into rows and keys
+    __device__ __forceinline__ RowParts(const AttentionArgs &g, Span &s, int key0)
+    {
+        s.k_first = s.first;
+        s.m = s.n;
+        int first, stop;
+        sequence_rows(g.offsets, g.seqs, g.rows, s.seq, first, stop);
+        s.first = first;
+        s.n = stop - first;
+        s.ahead = s.m - s.n;
+        s.prefix = g.prefix && g.causal ? g.prefix[s.seq] : 0;
+        all = s.n * g.group;
+        // row i sees key j in front of the prefix or where j <= i + ahead
+        begin = !g.causal || key0 < s.prefix ? 0 : min(max(key0 - s.ahead, 0), s.n) * g.group;
+        chunk = max((all + g.splits * 32 - 1) / (g.splits * 32) * 32, 32);
+        count = (all - begin + chunk - 1) / chunk;
+    }
+};
+
 // In float16 dR has neither room for large gradients nor bits for small ones.  A lane's dR are kept times a power of two (its row's, or its key's), found from
 // the largest |dR| so far; when a larger one comes, what has been summed is brought to the new one.  The two lanes of a row go together.
 template <class T, int DB>
@@ -636,7 +668,7 @@ __global__ __launch_bounds__(WAVES * 64, sizeof(T) == 2 && DB <= 4 ? 2 : 1) void
     constexpr int KEYS = R::ROWB <= 256 ? 64 : 32, NT = WAVES * 64, HALF = KEYS * R::ROWB;
     __shared__ __align__(1024) char lds[4 * HALF];
     const int kv = (int)((blockIdx.x + g.before) % g.kv_heads), lane = threadIdx.x & 63, h = lane >> 5;
-    Span s = find_span(g.offsets, g.seqs, g.rows, g.group, WAVES * 32, (int)((blockIdx.x + g.before) / g.kv_heads));
+    Span s = find_span<true>(g.offsets, g.seqs, g.rows, g.group, WAVES * 32, (int)((blockIdx.x + g.before) / g.kv_heads));
     if (s.seq >= g.seqs) {
         if (s.n > 0 && g.out.p) no_rows<T>(g, g.out, s, kv, s.r0, WAVES * 32, nullptr, 0);
         return;
@@ -740,27 +772,21 @@ __global__ __launch_bounds__(WAVES * 64, sizeof(T) == 2 && DB <= 4 ? 2 : 1) void
     __shared__ __align__(16) RowsInfo infos[2];
     const char *const k_lds = lds + 4 * HALF;
     const int kv = (int)((blockIdx.x + g.before) % g.kv_heads), lane = threadIdx.x & 63, h = lane >> 5;
-    Span s = find_span(g.k_offsets, g.seqs, g.k_rows, 1, WAVES * 32, (int)((blockIdx.x + g.before) / g.kv_heads));
+    Span s = find_span<false>(g.k_offsets, g.seqs, g.k_rows, 1, WAVES * 32, (int)((blockIdx.x + g.before) / g.kv_heads));
     const int key0 = s.r0;
     if (s.seq >= g.seqs) {
-        for (int c = threadIdx.x / 64; c < min(WAVES * 32, s.n - key0); c += WAVES)
+        for (int c = threadIdx.x / 64; c < min(WAVES * 32, s.n - key0) && blockIdx.y == 0; c += WAVES)
             for (int d = lane; d < g.dim; d += 64) {
-                const int64_t row = s.first + key0 + c, at = (((int64_t)blockIdx.y * g.k_rows + row) * g.kv_heads + kv) * g.dim + d;
-                if (g.out.p && g.splits > 1) g.part[at] = 0.0f;
-                else if (g.out.p) *((T *)(g.out.p + row * g.out.row + kv * g.out.head) + d) = (T)0.0f;
-                if (g.out2.p && g.splits > 1) g.part2[at] = 0.0f;
-                else if (g.out2.p) *((T *)(g.out2.p + row * g.out2.row + kv * g.out2.head) + d) = (T)0.0f;
+                const int64_t row = s.first + key0 + c;
+                if (g.out.p) *((T *)(g.out.p + row * g.out.row + kv * g.out.head) + d) = (T)0.0f;
+                if (g.out2.p) *((T *)(g.out2.p + row * g.out2.row + kv * g.out2.head) + d) = (T)0.0f;
             }
         return;
     }
-    s.k_first = s.first;
-    s.m = s.n;
-    int first, stop;
-    sequence_rows(g.offsets, g.seqs, g.rows, s.seq, first, stop);
-    s.first = first;
-    s.n = stop - first;
-    s.ahead = s.m - s.n;
-    s.prefix = g.prefix && g.causal ? g.prefix[s.seq] : 0;
+    // (the parts of the last rows, which end with the shortest ones, go last and fill up the end)
+    const int index = g.splits - 1 - (int)blockIdx.y;
+    const RowParts part(g, s, key0);
+    if (index >= max(part.count, 1)) return;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), key_w = key0 + wave * 32, key = key_w + (lane & 31);
     const int64_t key_row = s.k_first + min(key, s.m - 1);
     const char *kp = g.k.p + key_row * g.k.row + kv * g.k.head, *vp = g.v.p + key_row * g.v.row + kv * g.v.head;
@@ -777,28 +803,30 @@ __global__ __launch_bounds__(WAVES * 64, sizeof(T) == 2 && DB <= 4 ? 2 : 1) void
     clear(dv);
     const typename R::Place place;
     float by = first_factor<T>();
-    // the first row that sees one of the tile's keys: row i sees key j in front of the prefix or where j <= i + ahead
-    const int all = s.n * g.group, begin = !g.causal || key0 < s.prefix ? 0 : min(max(key0 - s.ahead, 0), s.n) * g.group;
-    int from, to;
-    share_of(all - begin, TILE, g.splits, blockIdx.y, from, to);
-    from += begin;
-    to += begin;
+    const int to = part.all - index * part.chunk, from = max(part.begin, to - part.chunk);
+    // From the last tile of rows to the first one: all workgroups of a sequence begin at the same rows, so that what is under way is shared in the
+    // caches, and end where their keys are no longer seen.
+    const int top = from + (max(to - from, 1) - 1) / TILE * TILE;
     const PackedLoader<R, TILE, NT> loader(g, g.q, g.dy, s.first, kv);
     // What is known of a tile's rows, by one thread each: asked for in front of a step, put to LDS behind it.
     float lse_next = 0.0f, delta_next = 0.0f;
+    int row_next = 0, head_next = 0;
     const auto ask = [&](int r0) {
-        const int64_t item = packed_item(g, s, kv, min(r0 + (int)threadIdx.x % TILE, all - 1));
+        if (threadIdx.x >= TILE) return;
+        loader.place(r0, min((int)threadIdx.x, to - 1 - r0), row_next, head_next);
+        const int64_t item = (int64_t)(s.first + row_next) * g.heads + kv * g.group + head_next;
         lse_next = g.lse[item];
         delta_next = g.delta[item];
     };
     const auto put = [&](int r0, RowsInfo &info) {
         if (threadIdx.x >= TILE) return;
-        const int t = threadIdx.x, r = r0 + t, i = min(r, all - 1), row = i / g.group;
-        info.lse[t] = r > i || lse_next == -INFINITY ? INFINITY : lse_next * LOG2E;
-        info.delta[t] = r > i ? 0.0f : delta_next;
-        info.limit[t] = limit_of(g, s, row);
-        info.place[t] = row + s.ahead;
-        info.slope[t] = EXTRA && g.slopes ? g.slopes[kv * g.group + i - row * g.group] : 0.0f;
+        const int t = threadIdx.x;
+        const bool none = r0 + t >= to;
+        info.lse[t] = none || lse_next == -INFINITY ? INFINITY : lse_next * LOG2E;
+        info.delta[t] = none ? 0.0f : delta_next;
+        info.limit[t] = limit_of(g, s, row_next);
+        info.place[t] = row_next + s.ahead;
+        info.slope[t] = EXTRA && g.slopes ? g.slopes[kv * g.group + head_next] : 0.0f;
     };
     int here = 0;
     if (from < to) {
@@ -806,15 +834,15 @@ __global__ __launch_bounds__(WAVES * 64, sizeof(T) == 2 && DB <= 4 ? 2 : 1) void
             const KeyLoader<R, WAVES * 32, NT> keys(g.k.p + (int64_t)s.k_first * g.k.row + (int64_t)kv * g.k.head, g.k.row, g.bytes);
             keys.load(lds_at(k_lds), key0, s.m);
         }
-        ask(from);
-        loader.load(lds_at(lds), lds_at(lds) + HALF, from, all);
-        put(from, infos[0]);
+        ask(top);
+        loader.load(lds_at(lds), lds_at(lds) + HALF, top, to);
+        put(top, infos[0]);
     }
-    for (int r0 = from; r0 < to; r0 += TILE, here ^= 1) {
+    for (int r0 = from < to ? top : from - 1; r0 >= from; r0 -= TILE, here ^= 1) {
         arrived<0>();
-        if (r0 + TILE < to) {
-            ask(r0 + TILE);
-            loader.load(lds_at(lds) + (here ^ 1) * 2 * HALF, lds_at(lds) + (here ^ 1) * 2 * HALF + HALF, r0 + TILE, all);
+        if (r0 > from) {
+            ask(r0 - TILE);
+            loader.load(lds_at(lds) + (here ^ 1) * 2 * HALF, lds_at(lds) + (here ^ 1) * 2 * HALF + HALF, r0 - TILE, to);
         }
         const RowsInfo &info = infos[here];
         const char *const q_lds = lds + here * 2 * HALF, *const dy_lds = q_lds + HALF;
@@ -865,12 +893,12 @@ __global__ __launch_bounds__(WAVES * 64, sizeof(T) == 2 && DB <= 4 ? 2 : 1) void
                 for (int b = 0; b < DB; ++b) dk[b] = mma32(R::across(q_lds, place, 0, t, b * 32), w, dk[b], T{});
             }
         }
-        if (r0 + TILE < to) put(r0 + TILE, infos[here ^ 1]);
+        if (r0 > from) put(r0 - TILE, infos[here ^ 1]);
     }
     if (key >= s.m) return;
     const int64_t row = s.k_first + key;
-    if (g.splits > 1) {
-        const int64_t at = ((int64_t)blockIdx.y * g.k_rows + row) * g.kv_heads + kv;
+    if (part.count > 1) {
+        const int64_t at = ((int64_t)index * g.k_rows + row) * g.kv_heads + kv;
         const int wide = (g.dim & 3) == 0;
         if (g.out.p) store_head<float, DB>((char *)(g.part + at * g.dim), dk, g.scale / by, g.dim, wide);
         if (g.out2.p) store_head<float, DB>((char *)(g.part2 + at * g.dim), dv, 1.0f, g.dim, wide);
@@ -878,6 +906,35 @@ __global__ __launch_bounds__(WAVES * 64, sizeof(T) == 2 && DB <= 4 ? 2 : 1) void
     }
     if (g.out.p) store_head<T, DB>(g.out.p + row * g.out.row + kv * g.out.head, dk, g.scale / by, g.dim, g.wide);
     if (g.out2.p) store_head<T, DB>(g.out2.p + row * g.out2.row + kv * g.out2.head, dv, 1.0f, g.dim, g.wide);
+}
+
+// dk and dv of tiles whose rows went in several parts, which are added in their order: four elements a thread.
+template <class T>
+__global__ __launch_bounds__(256) void attention_sum_kernel(const AttentionArgs g)
+{
+    const int kv = (int)((blockIdx.x + g.before) % g.kv_heads);
+    Span s = find_span<false>(g.k_offsets, g.seqs, g.k_rows, 1, ATTENTION_TILE, (int)((blockIdx.x + g.before) / g.kv_heads));
+    if (s.seq >= g.seqs) return;
+    const int key0 = s.r0;
+    const RowParts part(g, s, key0);
+    const Heads &out = blockIdx.y ? g.out2 : g.out;
+    const float *const sums = blockIdx.y ? g.part2 : g.part;
+    if (part.count < 2 || !out.p) return;
+    const int per = (g.dim + 3) / 4, keys = min(ATTENTION_TILE, s.m - key0);
+    const int64_t items = (int64_t)g.k_rows * g.kv_heads;
+    for (int c = threadIdx.x; c < keys * per; c += 256) {
+        const int key = c / per, d = (c - key * per) * 4, cnt = g.dim - d, wide = (g.dim & 3) == 0;
+        const int64_t row = s.k_first + key0 + key;
+        float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 4
+        for (int k = 0; k < part.count; ++k) {
+            float one[4];
+            load_row<float>((const char *)sums, (k * items + row * g.kv_heads + kv) * g.dim + d, cnt, wide, one);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[j] += one[j];
+        }
+        store_row<T>(out.p + row * out.row + kv * out.head, d, cnt, g.wide, v);
+    }
 }
 
 inline bool extra(const AttentionArgs &g) { return g.cap != 0.0f || g.slopes || !(g.scale > 0.0f); }
@@ -914,7 +971,10 @@ hipError_t launch_dq(hipStream_t st, const AttentionArgs &g)
 template <class T, int DB, bool EXTRA>
 hipError_t launch_dkv(hipStream_t st, const AttentionArgs &g)
 {
-    return in_launches(g, (int64_t)g.tiles * g.kv_heads, [&](const AttentionArgs &p, dim3 grid) { attention_dkv_kernel<T, DB, EXTRA, 4><<<grid, 256, 0, st>>>(p); });
+    const int64_t tiles = (int64_t)g.tiles * g.kv_heads;
+    const hipError_t e = in_launches(g, tiles, [&](const AttentionArgs &p, dim3 grid) { attention_dkv_kernel<T, DB, EXTRA, 4><<<grid, 256, 0, st>>>(p); });
+    if (e != hipSuccess || g.splits == 1) return e;
+    return in_launches(g, tiles, [&](const AttentionArgs &p, dim3 grid) { attention_sum_kernel<T><<<dim3(grid.x, 2), 256, 0, st>>>(p); });
 }
 
 #define ALPA_BY_DIM(call, T, g, ...)                                                                           \

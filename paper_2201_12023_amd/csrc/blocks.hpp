@@ -1,6 +1,6 @@
 // What the kernels between a block's products take, and how they are launched (device code: attention_kernel.hpp, kernels_blocks.hip).
 #pragma once
-#include "internal.hpp"
+#include "layers.hpp"
 
 namespace alpa {
 
@@ -43,9 +43,8 @@ ALPA_ATTENTION_LAUNCHES(bf16)
 // rows of a head's dim padded to blocks of 32, as the kernels are compiled for them: 2, 3, 4 or 8
 inline int dim_blocks(int dim) { return dim <= 64 ? 2 : dim <= 96 ? 3 : dim <= 128 ? 4 : 8; }
 
-// y and lse from the parts of the keys; sums of dk and dv from the parts of the rows
+// y and lse from the parts of the keys
 hipError_t launch_attention_join(hipStream_t st, int dtype, const AttentionArgs &a);
-hipError_t launch_attention_sum(hipStream_t st, int dtype, const AttentionArgs &a);
 
 // Copies tensors to [rows][heads][to_len] elements (a multiple of 16 bytes), zeros behind len.
 struct HeadPack {

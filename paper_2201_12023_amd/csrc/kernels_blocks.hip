@@ -59,38 +59,6 @@ hipError_t launch_attention_join(hipStream_t st, int dtype, const AttentionArgs 
     return by_type(dtype, [&](auto t) { attention_join_kernel<decltype(t)><<<blocks, 256, 0, st>>>(g); });
 }
 
-// Four elements a thread, of dk (blockIdx.y 0) or dv.
-template <class T>
-__global__ __launch_bounds__(256) void attention_sum_kernel(const AttentionArgs g)
-{
-    const Heads &out = blockIdx.y ? g.out2 : g.out;
-    const float *const parts = blockIdx.y ? g.part2 : g.part;
-    if (!out.p) return;
-    const int per = (g.dim + 3) / 4;
-    const int64_t items = (int64_t)g.k_rows * g.kv_heads;
-    for (int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x; c < items * per; c += (int64_t)gridDim.x * 256) {
-        const int64_t item = c / per;
-        const int d = (int)(c - item * per) * 4, cnt = g.dim - d, wide = (g.dim & 3) == 0;
-        float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll 4
-        for (int s = 0; s < g.splits; ++s) {
-            float part[4];
-            load_row<float>((const char *)parts, (s * items + item) * g.dim + d, cnt, wide, part);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) v[j] += part[j];
-        }
-        const int64_t row = item / g.kv_heads;
-        store_row<T>(out.p + row * out.row + (item - row * g.kv_heads) * out.head, d, cnt, g.wide, v);
-    }
-}
-
-hipError_t launch_attention_sum(hipStream_t st, int dtype, const AttentionArgs &g)
-{
-    const int64_t threads = (int64_t)g.k_rows * g.kv_heads * ((g.dim + 3) / 4);
-    const dim3 grid(blocks_for((threads + 255) / 256, 1 << 20), 2);
-    return by_type(dtype, [&](auto t) { attention_sum_kernel<decltype(t)><<<grid, 256, 0, st>>>(g); });
-}
-
 // ---------------------------------------------------------------- heads in 16-byte units
 
 // A thread writes sixteen bytes; all of a call's tensors in one launch.
