@@ -123,6 +123,7 @@ struct Plan {
         g.causal = a.causal != 0;
         g.scale = a.scale;
         g.cap = a.cap;
+        g.twice = a.cap > 0.0f ? (float)(2.0 * a.scale * 1.4426950408889634 / a.cap) : 0.0f;
         g.splits = 1;
         pack.len = a.dim;
         pack.to_len = (int)(g.bytes / es);
@@ -176,7 +177,7 @@ int row_splits(const alpa_attention_t &a)
     const int64_t rows = a.rows * (a.heads / a.kv_heads) / a.seqs;
     const int64_t tiles = std::max<int64_t>((a.k_rows / ATTENTION_TILE + a.seqs / 2) * a.kv_heads, a.kv_heads), slots = 2 * COMPUTE_UNITS;
     const int64_t even = a.causal ? std::max<int64_t>(2 * slots / tiles - 1, tiles <= 2 * slots ? 2 : 1) : slots / tiles;
-    return (int)std::max<int64_t>(1, std::min({(int64_t)16, even, rows / 256}));
+    return (int)std::max<int64_t>(1, std::min({(int64_t)32, even, rows / 256}));
 }
 
 void plan_forward(Plan &p, const alpa_heads_t &q, const alpa_heads_t &k, const alpa_heads_t &v)

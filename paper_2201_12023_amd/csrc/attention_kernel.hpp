@@ -194,15 +194,20 @@ __device__ __forceinline__ int limit_of(const AttentionArgs &g, const Span &s, i
     return min(s.m, g.causal ? max(max(i + s.ahead + 1, s.prefix), 0) : s.m);
 }
 
-// Scores in units of the binary logarithm.  EXTRA: what the formula has beside a positive factor, and the slope of the cap.
+// A capped score from the product of q and k, in units of the binary logarithm, and the slope of the cap.  1 - tanh(x) = 2 / (1 + exp(2 x)) = 2 u, and the
+// slope is 4 u^2 exp(2 x), which keeps its relative error where the cap is reached; tanh is off by a few units of 2^-24 absolute so, which float32 gets better.
 template <class T>
-__device__ __forceinline__ float capped(const AttentionArgs &g, float r, float &bent)
+__device__ __forceinline__ float capped(const AttentionArgs &g, float s, float &bent)
 {
-    // 1 - tanh(x) = 2 / (1 + exp(2 x)), from which the slope keeps its relative error where the cap is reached
-    const float x = r / g.cap, u = divide_for<T>(2.0f, 1.0f + exp_for<T>(2.0f * fabsf(x)));
-    bent = u * (2.0f - u);
-    if (sizeof(T) == 4) return g.cap * tanhf(x);
-    return copysignf(g.cap * (1.0f - u), r);
+    if constexpr (sizeof(T) == 4) {
+        const float x = s * g.scale / g.cap, u = 1.0f / (1.0f + expf(2.0f * fabsf(x)));
+        bent = 4.0f * u * (1.0f - u);
+        return g.cap * tanhf(x) * LOG2E;
+    } else {
+        const float e = __builtin_amdgcn_exp2f(fminf(s * g.twice, 60.0f)), u = __builtin_amdgcn_rcpf(1.0f + e);
+        bent = 4.0f * e * u * u;
+        return fmaf(-2.0f * LOG2E * g.cap, u, LOG2E * g.cap);
+    }
 }
 
 __device__ __forceinline__ float other_half(float v) { return __shfl_xor(v, 32, 64); }
@@ -358,7 +363,7 @@ struct Running {
         sum = 0.0f;
         limit = limit_of(g, s, i / g.group);
         place = i / g.group + s.ahead;
-        slope = EXTRA && g.slopes ? g.slopes[kv * g.group + i % g.group] : 0.0f;
+        slope = EXTRA && g.slopes ? g.slopes[kv * g.group + i % g.group] * LOG2E : 0.0f;
     }
 
     // NB blocks of 32 keys from j0 on, in LDS from row `at` on
@@ -374,15 +379,22 @@ struct Running {
             for (int k = 0; k < R::STEPS; ++k) s[b] = mma32(R::along(k_lds, p, b * 32, k), q[k], s[b], T{});
         const float by = EXTRA ? 1.0f : g.scale * LOG2E;
         if constexpr (EXTRA) {
+            float bent;
+            const float far = (float)(place - j0 - 4 * h);
 #pragma unroll
-            for (int b = 0; b < NB; ++b)
+            for (int b = 0; b < NB; ++b) {
+                if (g.cap != 0.0f) {
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    float a = s[b][i] * g.scale, bent;
-                    if (g.cap != 0.0f) a = capped<T>(g, a, bent);
-                    a -= slope * fabsf((float)(place - (j0 + b * 32 + block_row(i, h))));
-                    s[b][i] = a * LOG2E;
+                    for (int i = 0; i < 16; ++i) s[b][i] = capped<T>(g, s[b][i], bent);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) s[b][i] *= g.scale * LOG2E;
                 }
+                if (g.slopes) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) s[b][i] = fmaf(-slope, fabsf(far - (float)(b * 32 + block_row(i, 0))), s[b][i]);
+                }
+            }
         }
         if (__any(j0 + NB * 32 > limit)) {
 #pragma unroll
@@ -699,7 +711,7 @@ __global__ __launch_bounds__(WAVES * 64, sizeof(T) == 2 && DB <= 4 ? 2 : 1) void
     float lse = g.lse[item] * LOG2E;
     lse = lse == -INFINITY ? INFINITY : lse;           // (no key seen: all exponentials are zero)
     const int limit = limit_of(g, s, i / g.group), where = i / g.group + s.ahead, end = min(s.r0 + WAVES * 32, s.n * g.group) - 1;
-    const float slope = EXTRA && g.slopes ? g.slopes[kv * g.group + i % g.group] : 0.0f;
+    const float slope = EXTRA && g.slopes ? g.slopes[kv * g.group + i % g.group] * LOG2E : 0.0f;
     const int most = limit_of(g, s, end / g.group), mine = __builtin_amdgcn_readlane(limit, 31);
     f32x16 dq[DB];
     clear(dq);
@@ -727,16 +739,27 @@ __global__ __launch_bounds__(WAVES * 64, sizeof(T) == 2 && DB <= 4 ? 2 : 1) void
             for (int j = 0; j < 16; ++j) a[j] = d[j] = 0.0f;
             along_product<R, T>(k_lds, place, at, q, a);
             along_product<R, T>(v_lds, place, at, dy, d);
-            float by_log = g.scale * LOG2E;
+            const float by_log = EXTRA ? 1.0f : g.scale * LOG2E;
             if constexpr (EXTRA) {
+                if (g.cap != 0.0f) {
 #pragma unroll
-                for (int j = 0; j < 16; ++j) {
-                    float e = a[j] * g.scale, bent = 1.0f;
-                    if (g.cap != 0.0f) e = capped<T>(g, e, bent);
-                    a[j] = e - slope * fabsf((float)(where - (j0 + at + block_row(j, h))));
-                    d[j] = (d[j] - delta) * bent;
+                    for (int j = 0; j < 16; ++j) {
+                        float bent;
+                        a[j] = capped<T>(g, a[j], bent);
+                        d[j] = (d[j] - delta) * bent;
+                    }
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) {
+                        a[j] *= g.scale * LOG2E;
+                        d[j] -= delta;
+                    }
                 }
-                by_log = LOG2E;
+                if (g.slopes) {
+                    const float far = (float)(where - j0 - at - 4 * h);
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) a[j] = fmaf(-slope, fabsf(far - (float)block_row(j, 0)), a[j]);
+                }
             }
             if (__any(j0 + at + 32 > limit)) {
 #pragma unroll
@@ -826,7 +849,7 @@ __global__ __launch_bounds__(WAVES * 64, sizeof(T) == 2 && DB <= 4 ? 2 : 1) void
         info.delta[t] = none ? 0.0f : delta_next;
         info.limit[t] = limit_of(g, s, row_next);
         info.place[t] = row_next + s.ahead;
-        info.slope[t] = EXTRA && g.slopes ? g.slopes[kv * g.group + head_next] : 0.0f;
+        info.slope[t] = EXTRA && g.slopes ? g.slopes[kv * g.group + head_next] * LOG2E : 0.0f;
     };
     int here = 0;
     if (from < to) {
@@ -857,17 +880,29 @@ __global__ __launch_bounds__(WAVES * 64, sizeof(T) == 2 && DB <= 4 ? 2 : 1) void
                 along_product<R, T>(q_lds, place, 0, k, a);
             }
             along_product<R, T>(dy_lds, place, 0, v, d);
-            float by_log = g.scale * LOG2E;
+            const float by_log = EXTRA ? 1.0f : g.scale * LOG2E;
             if constexpr (EXTRA) {
+                if (g.cap != 0.0f) {
 #pragma unroll
-                for (int j = 0; j < 16; ++j) {
-                    const int r = block_row(j, h);
-                    float e = a[j] * g.scale, bent = 1.0f;
-                    if (g.cap != 0.0f) e = capped<T>(g, e, bent);
-                    a[j] = e - info.slope[r] * fabsf((float)(info.place[r] - key));
-                    d[j] = (d[j] - info.delta[r]) * bent;
+                    for (int j = 0; j < 16; ++j) {
+                        float bent;
+                        a[j] = capped<T>(g, a[j], bent);
+                        d[j] = (d[j] - info.delta[block_row(j, h)]) * bent;
+                    }
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) {
+                        a[j] *= g.scale * LOG2E;
+                        d[j] -= info.delta[block_row(j, h)];
+                    }
                 }
-                by_log = LOG2E;
+                if (g.slopes) {
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) {
+                        const int r = block_row(j, h);
+                        a[j] = fmaf(-info.slope[r], fabsf((float)(info.place[r] - key)), a[j]);
+                    }
+                }
             }
             if (info.limit[0] < key_w + 32) {
 #pragma unroll
@@ -908,7 +943,7 @@ __global__ __launch_bounds__(WAVES * 64, sizeof(T) == 2 && DB <= 4 ? 2 : 1) void
     if (g.out2.p) store_head<T, DB>(g.out2.p + row * g.out2.row + kv * g.out2.head, dv, 1.0f, g.dim, g.wide);
 }
 
-// dk and dv of tiles whose rows went in several parts, which are added in their order: four elements a thread.
+// dk and dv of tiles whose rows went in several parts, which are added in their order: four elements a thread, sixteen keys a workgroup.
 template <class T>
 __global__ __launch_bounds__(256) void attention_sum_kernel(const AttentionArgs g)
 {
@@ -917,14 +952,14 @@ __global__ __launch_bounds__(256) void attention_sum_kernel(const AttentionArgs 
     if (s.seq >= g.seqs) return;
     const int key0 = s.r0;
     const RowParts part(g, s, key0);
-    const Heads &out = blockIdx.y ? g.out2 : g.out;
-    const float *const sums = blockIdx.y ? g.part2 : g.part;
+    const Heads &out = blockIdx.y & 1 ? g.out2 : g.out;
+    const float *const sums = blockIdx.y & 1 ? g.part2 : g.part;
     if (part.count < 2 || !out.p) return;
-    const int per = (g.dim + 3) / 4, keys = min(ATTENTION_TILE, s.m - key0);
+    const int per = (g.dim + 3) / 4, key1 = key0 + (blockIdx.y >> 1) * 16, keys = min(16, s.m - key1);
     const int64_t items = (int64_t)g.k_rows * g.kv_heads;
     for (int c = threadIdx.x; c < keys * per; c += 256) {
         const int key = c / per, d = (c - key * per) * 4, cnt = g.dim - d, wide = (g.dim & 3) == 0;
-        const int64_t row = s.k_first + key0 + key;
+        const int64_t row = s.k_first + key1 + key;
         float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll 4
         for (int k = 0; k < part.count; ++k) {
@@ -974,7 +1009,7 @@ hipError_t launch_dkv(hipStream_t st, const AttentionArgs &g)
     const int64_t tiles = (int64_t)g.tiles * g.kv_heads;
     const hipError_t e = in_launches(g, tiles, [&](const AttentionArgs &p, dim3 grid) { attention_dkv_kernel<T, DB, EXTRA, 4><<<grid, 256, 0, st>>>(p); });
     if (e != hipSuccess || g.splits == 1) return e;
-    return in_launches(g, tiles, [&](const AttentionArgs &p, dim3 grid) { attention_sum_kernel<T><<<dim3(grid.x, 2), 256, 0, st>>>(p); });
+    return in_launches(g, tiles, [&](const AttentionArgs &p, dim3 grid) { attention_sum_kernel<T><<<dim3(grid.x, 2 * ATTENTION_TILE / 16), 256, 0, st>>>(p); });
 }
 
 #define ALPA_BY_DIM(call, T, g, ...)                                                                           \

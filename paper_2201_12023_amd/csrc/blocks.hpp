@@ -20,7 +20,7 @@ struct AttentionArgs {
     const int32_t *offsets, *k_offsets, *prefix;
     const float *slopes;
     int k_step, causal;
-    float scale, cap;
+    float scale, cap, twice;        // twice: 2 scale / cap, times the binary logarithm of e
     int tiles;                      // grid: row tiles of all sequences, at most
     uint32_t before;                // of the grid, workgroups of earlier launches
     int splits;                     // of the keys (forward), of the rows (dk, dv)
