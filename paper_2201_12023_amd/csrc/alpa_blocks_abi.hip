@@ -154,20 +154,33 @@ struct Plan {
         return Heads{(char *)t.p, t.row * es, t.head * es};
     }
     // tiles that the sequences' packed rows can make at most, rows of none among them
-    static int64_t tiles_of(int64_t packed, int64_t seqs) { return packed / ATTENTION_TILE + std::min(seqs + 2, packed); }
+    static int64_t tiles_of(int64_t packed, int64_t seqs, int tile) { return packed / tile + std::min(seqs + 2, packed); }
 };
 
-// Few rows of a sequence: they fit in one or two blocks of 32, and the keys, not the products, are what takes time.
-bool few_rows(const alpa_attention_t &a) { return a.rows * (a.heads / a.kv_heads) <= 64 * (int64_t)a.seqs; }
+// What a call's rows are to the kernels.
+struct Shape {
+    int64_t packed, tiles;          // rows of a kv head; tiles of many rows, about
+    bool few, direct;               // tiles of 32 rows whose keys the waves share; without a search among the sequences
+
+    explicit Shape(const alpa_attention_t &a)
+        : packed(a.rows * (a.heads / a.kv_heads)), tiles((packed / ATTENTION_TILE + std::min<int64_t>(a.seqs, packed)) * a.kv_heads)
+    {
+        // few rows of a sequence, so that the keys and not the products are what takes time; or few tiles, so that waves are short of work
+        const bool short_rows = packed <= 64 * (int64_t)a.seqs;
+        few = short_rows || tiles <= COMPUTE_UNITS;
+        direct = short_rows && a.seqs > 512;
+    }
+};
 
 // Parts of the keys: enough workgroups to fill the compute units twice, each with a few tiles.
-int key_splits(const alpa_attention_t &a)
+int key_splits(const alpa_attention_t &a, const Shape &shape)
 {
-    const int64_t keys = a.k_rows / a.seqs, group = a.heads / a.kv_heads;
-    const int64_t tiles = few_rows(a) ? (int64_t)a.seqs * a.kv_heads : (a.rows * group / ATTENTION_TILE + a.seqs) * a.kv_heads;
-    const int64_t least = few_rows(a) ? 128 : 256;
+    const int64_t keys = a.k_rows / a.seqs;
+    const int64_t tiles = shape.few ? std::max<int64_t>(shape.packed / FEW_TILE, a.seqs) * a.kv_heads : shape.tiles;
+    const int64_t least = shape.few ? 128 : 256;
     return (int)std::max<int64_t>(1, std::min({(int64_t)64, 512 / tiles, keys / least}));
 }
+
 // Parts of the rows for dk and dv (RowParts in attention_kernel.hpp): as many workgroups as are on the compute units at once, two each.  With a causal mask a
 // tile has half of all parts on average, and where one part each fills the units, two are better, as the tile with most rows is what is waited for
 // (8192 rows, 32 heads on 8 kv heads: 1963 us in one part, 1260 in two, 1435 in three; 2048 rows: 265 in two, 168 in four, 136 in six, 165 in eight;
@@ -177,7 +190,7 @@ int row_splits(const alpa_attention_t &a)
     const int64_t rows = a.rows * (a.heads / a.kv_heads) / a.seqs;
     const int64_t tiles = std::max<int64_t>((a.k_rows / ATTENTION_TILE + a.seqs / 2) * a.kv_heads, a.kv_heads), slots = 2 * COMPUTE_UNITS;
     const int64_t even = a.causal ? std::max<int64_t>(2 * slots / tiles - 1, tiles <= 2 * slots ? 2 : 1) : slots / tiles;
-    return (int)std::max<int64_t>(1, std::min({(int64_t)32, even, rows / 256}));
+    return (int)std::max<int64_t>(1, std::min({(int64_t)32, even, rows / (a.dtype == ALPA_F32 ? 64 : 128)}));
 }
 
 void plan_forward(Plan &p, const alpa_heads_t &q, const alpa_heads_t &k, const alpa_heads_t &v)
@@ -186,8 +199,9 @@ void plan_forward(Plan &p, const alpa_heads_t &q, const alpa_heads_t &k, const a
     g.q = p.operand(q, true);
     g.k = p.operand(k, false);
     g.v = p.operand(v, false);
-    g.splits = key_splits(p.a);
-    g.tiles = (int)Plan::tiles_of(p.a.rows * g.group, p.a.seqs);
+    const Shape shape(p.a);
+    g.splits = key_splits(p.a, shape);
+    g.tiles = shape.direct ? 0 : (int)Plan::tiles_of(shape.packed, p.a.seqs, shape.few ? FEW_TILE : ATTENTION_TILE);
     if (g.splits > 1) {
         const int64_t items = (int64_t)g.splits * p.a.rows * p.a.heads;
         g.part = p.take<float>(items * p.a.dim);
@@ -216,9 +230,9 @@ hipError_t launch_rows_of(hipStream_t st, int dtype, int few, const AttentionArg
 {
     return dtype == ALPA_F32 ? launch_attention_f32(st, few, g) : dtype == ALPA_F16 ? launch_attention_f16(st, few, g) : launch_attention_bf16(st, few, g);
 }
-hipError_t launch_dq_of(hipStream_t st, int dtype, const AttentionArgs &g)
+hipError_t launch_dq_of(hipStream_t st, int dtype, int few, const AttentionArgs &g)
 {
-    return dtype == ALPA_F32 ? launch_attention_dq_f32(st, g) : dtype == ALPA_F16 ? launch_attention_dq_f16(st, g) : launch_attention_dq_bf16(st, g);
+    return dtype == ALPA_F32 ? launch_attention_dq_f32(st, few, g) : dtype == ALPA_F16 ? launch_attention_dq_f16(st, few, g) : launch_attention_dq_bf16(st, few, g);
 }
 hipError_t launch_dkv_of(hipStream_t st, int dtype, const AttentionArgs &g)
 {
@@ -304,7 +318,7 @@ int alpa_attention_forward(const alpa_attention_t *how, alpa_heads_t q, alpa_hea
     g.wide = wide_heads(y, a.dtype, 4 * element(a.dtype));
     g.lse = lse;
     if (p.pack.count) HIPCHK(launch_head_pack(st, a.dtype, p.pack));
-    HIPCHK(launch_rows_of(st, a.dtype, few_rows(a), g));
+    HIPCHK(launch_rows_of(st, a.dtype, Shape(a).few, g));
     if (g.splits > 1) HIPCHK(launch_attention_join(st, a.dtype, g));
     return ALPA_DP_OK;
 }
@@ -346,15 +360,16 @@ int alpa_attention_backward(const alpa_attention_t *how, alpa_heads_t dy, alpa_h
         if (p.pack.count) HIPCHK(launch_head_pack(st, a.dtype, p.pack));
         g.out = p.result(dq);
         g.wide = wide_heads(dq, a.dtype, bytes);
-        g.tiles = (int)Plan::tiles_of(a.rows * g.group, a.seqs);
+        const Shape shape(a);
+        g.tiles = (int)Plan::tiles_of(shape.packed, a.seqs, shape.few ? FEW_TILE : ATTENTION_TILE);
         g.splits = 1;
-        HIPCHK(launch_dq_of(st, a.dtype, g));
+        HIPCHK(launch_dq_of(st, a.dtype, shape.few, g));
     }
     if (a.k_rows > 0 && (dk.p || dv.p)) {
         g.out = p.result(dk);
         g.out2 = p.result(dv);
         g.wide = wide_heads(dk, a.dtype, bytes) && wide_heads(dv, a.dtype, bytes);
-        g.tiles = (int)Plan::tiles_of(a.k_rows, a.seqs);
+        g.tiles = (int)Plan::tiles_of(a.k_rows, a.seqs, ATTENTION_TILE);
         g.splits = splits;
         HIPCHK(launch_dkv_of(st, a.dtype, g));
     }

@@ -520,12 +520,33 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attention_kernel(const Attentio
 }
 
 // Few rows: the waves of a workgroup have the same 32 packed rows and take tiles of 32 keys in turn, each from its own part of LDS; in the end their sums
-// are joined.  A workgroup goes through its sequence's rows; one more sequence stands for the rows of none.
+// are joined.  A workgroup has one tile of rows (g.tiles), or, of very many sequences, goes through one's rows, and one more stands for the rows of none.
 template <class T, int DB>
 struct FewShape {
     using R = Rows<T, DB>;
     static constexpr int WAVES = R::ROWB <= 256 ? 4 : R::ROWB == 512 ? 2 : 1, SHARE = 32 * R::ROWB;          // (two tiles of keys and two of values a wave)
 };
+
+// Adds up the waves' blocks, each times `by`, a block at a time: 4 KB a wave.  What was in LDS has been read.
+template <int WAVES, int DB>
+__device__ __forceinline__ void join_waves(char *lds, f32x16 (&acc)[DB], float by)
+{
+    float *const all = (float *)lds + (threadIdx.x & 63), *const mine = all + (threadIdx.x >> 6) * 1024;
+#pragma unroll
+    for (int b = 0; b < DB; ++b) {
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 16; ++i) mine[i * 64] = acc[b][i] * by;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            float v = 0.0f;
+#pragma unroll
+            for (int w = 0; w < WAVES; ++w) v += all[w * 1024 + i * 64];
+            acc[b][i] = v;
+        }
+    }
+}
 
 template <class T, int DB, bool EXTRA>
 __global__ __launch_bounds__((FewShape<T, DB>::WAVES * 64)) void attention_few_kernel(const AttentionArgs g)
@@ -537,28 +558,39 @@ __global__ __launch_bounds__((FewShape<T, DB>::WAVES * 64)) void attention_few_k
     __shared__ float tops[WAVES][32], sums[WAVES][32];
     const int kv = (int)((blockIdx.x + g.before) % g.kv_heads), lane = threadIdx.x & 63;
     Span s;
-    s.seq = (int)((blockIdx.x + g.before) / g.kv_heads);
-    if (s.seq >= g.seqs) {
-        for (int k = g.seqs; k < g.seqs + 2; ++k) {
+    int r_begin = 0, r_end;
+    if (g.tiles) {
+        s = find_span<true>(g.offsets, g.seqs, g.rows, g.group, 32, (int)((blockIdx.x + g.before) / g.kv_heads));
+        r_begin = s.r0;
+        r_end = min(s.r0 + 32, s.n * g.group);
+        if (s.seq >= g.seqs) {
+            if (s.n > 0) no_rows<T>(g, g.out, s, kv, s.r0, 32, g.lse, blockIdx.y);
+            return;
+        }
+    } else {
+        s.seq = (int)((blockIdx.x + g.before) / g.kv_heads);
+        const auto rows_of = [&](int k) {
             int first, end;
             sequence_rows(g.offsets, g.seqs, g.rows, k, first, end);
             s.first = first;
             s.n = end - first;
+        };
+        rows_of(s.seq);
+        if (s.seq == g.seqs) {
             no_rows<T>(g, g.out, s, kv, 0, s.n * g.group, g.lse, blockIdx.y);
+            rows_of(g.seqs + 1);
+            no_rows<T>(g, g.out, s, kv, 0, s.n * g.group, g.lse, blockIdx.y);
+            return;
         }
-        return;
+        r_end = s.n * g.group;
     }
-    int first, end;
-    sequence_rows(g.offsets, g.seqs, g.rows, s.seq, first, end);
-    s.first = first;
-    s.n = end - first;
     find_keys(g, s);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const typename R::Place place;
     const uint32_t mine = lds_at(lds) + wave * 4 * F::SHARE;
     const KeyLoader<R, 32, 64> k(g.k.p + (int64_t)s.k_first * g.k.row + (int64_t)kv * g.k.head, g.k.row, g.bytes);
     const KeyLoader<R, 32, 64> v(g.v.p + (int64_t)s.k_first * g.v.row + (int64_t)kv * g.v.head, g.v.row, g.bytes);
-    for (int r0 = 0; r0 < s.n * g.group; r0 += 32) {
+    for (int r0 = r_begin; r0 < r_end; r0 += 32) {
         const int r = r0 + (lane & 31);
         Running<T, DB, EXTRA> run;
         run.begin(g, s, kv, r);
@@ -596,22 +628,7 @@ __global__ __launch_bounds__((FewShape<T, DB>::WAVES * 64)) void attention_few_k
             float total = 0.0f;
 #pragma unroll
             for (int w = 0; w < WAVES; ++w) total += sums[w][lane & 31] * exp2f(tops[w][lane & 31] - ref);
-            // (a block at a time: 4 KB a wave)
-#pragma unroll
-            for (int b = 0; b < DB; ++b) {
-                float *to_lds = (float *)lds + wave * 1024 + lane;
-                __syncthreads();
-#pragma unroll
-                for (int i = 0; i < 16; ++i) to_lds[i * 64] = run.y[b][i] * down;
-                __syncthreads();
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    float v = 0.0f;
-#pragma unroll
-                    for (int w = 0; w < WAVES; ++w) v += ((float *)lds)[w * 1024 + i * 64 + lane];
-                    run.y[b][i] = v;
-                }
-            }
+            join_waves<WAVES>(lds, run.y, down);
             run.top = top;
             run.sum = (threadIdx.x & 32) ? 0.0f : total;
         }
@@ -672,53 +689,123 @@ __device__ __forceinline__ void keep_in_range(f32x16 &d, f32x16 (&acc)[DB], floa
 template <class T>
 __device__ __forceinline__ float first_factor() { return std::is_same_v<T, f16> ? 0x1p60f : 1.0f; }
 
-// dq, and the sums of dy y on the way: a wave has 32 packed rows, the waves share tiles of 32 keys.
+// One row a lane, twice: what of its gradient the keys so far have given; the sum of dy y on the way.
+template <class T, int DB, bool EXTRA>
+struct Backward {
+    using R = Rows<T, DB>;
+    u32x4 q[R::STEPS], dy[R::STEPS];
+    f32x16 dq[DB];
+    float delta, lse, slope, by;
+    int limit, where;
+
+    // false: dq is not wanted
+    __device__ __forceinline__ bool begin(const AttentionArgs &g, const Span &s, int kv, int r)
+    {
+        const int h = threadIdx.x >> 5 & 1, i = min(r, s.n * g.group - 1);
+        const char *qp = packed_row(g, g.q, s, kv, i), *dp = packed_row(g, g.dy, s, kv, i), *yp = packed_row(g, g.y, s, kv, i);
+        delta = 0.0f;
+#pragma unroll
+        for (int k = 0; k < R::STEPS; ++k) {
+            const int at = k * 32 + h * 16;
+            const bool here = at < g.bytes;
+            const u32x4 none = {0, 0, 0, 0}, y = here ? *(const u32x4 *)(yp + at) : none;
+            q[k] = here ? *(const u32x4 *)(qp + at) : none;
+            dy[k] = here ? *(const u32x4 *)(dp + at) : none;
+            T a[16 / sizeof(T)], b[16 / sizeof(T)];
+            __builtin_memcpy(a, &dy[k], 16);
+            __builtin_memcpy(b, &y, 16);
+#pragma unroll
+            for (int j = 0; j < (int)(16 / sizeof(T)); ++j) delta += (float)a[j] * (float)b[j];
+        }
+        delta += other_half(delta);
+        const int64_t item = packed_item(g, s, kv, i);
+        if (h == 0 && r == i) g.delta[item] = delta;
+        lse = g.lse[item] * LOG2E;
+        lse = lse == -INFINITY ? INFINITY : lse;           // (no key seen: all exponentials are zero)
+        limit = limit_of(g, s, i / g.group);
+        where = i / g.group + s.ahead;
+        slope = EXTRA && g.slopes ? g.slopes[kv * g.group + i % g.group] * LOG2E : 0.0f;
+        by = first_factor<T>();
+        clear(dq);
+        return g.out.p != nullptr;
+    }
+
+    // 32 keys from j0 on, in LDS from row `at` on
+    __device__ __forceinline__ void step(const AttentionArgs &g, const char *k_lds, const char *v_lds, const typename R::Place &place, int j0, int at)
+    {
+        const int h = threadIdx.x >> 5 & 1;
+        f32x16 a, d;
+#pragma unroll
+        for (int j = 0; j < 16; ++j) a[j] = d[j] = 0.0f;
+        along_product<R, T>(k_lds, place, at, q, a);
+        along_product<R, T>(v_lds, place, at, dy, d);
+        const float by_log = EXTRA ? 1.0f : g.scale * LOG2E;
+        if constexpr (EXTRA) {
+            if (g.cap != 0.0f) {
+#pragma unroll
+                for (int j = 0; j < 16; ++j) {
+                    float bent;
+                    a[j] = capped<T>(g, a[j], bent);
+                    d[j] = (d[j] - delta) * bent;
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < 16; ++j) {
+                    a[j] *= g.scale * LOG2E;
+                    d[j] -= delta;
+                }
+            }
+            if (g.slopes) {
+                const float far = (float)(where - j0 - 4 * h);
+#pragma unroll
+                for (int j = 0; j < 16; ++j) a[j] = fmaf(-slope, fabsf(far - (float)block_row(j, 0)), a[j]);
+            }
+        }
+        if (__any(j0 + 32 > limit)) {
+#pragma unroll
+            for (int j = 0; j < 16; ++j) a[j] = j0 + block_row(j, h) < limit ? a[j] : -INFINITY;
+        }
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+            const float p = __builtin_amdgcn_exp2f(fmaf(a[j], by_log, -lse));
+            d[j] = p * (EXTRA ? d[j] : d[j] - delta);
+        }
+        keep_in_range<T>(d, dq, by);
+#pragma unroll
+        for (int t = 0; t < R::FRAGS; ++t) {
+            const u32x4 w = R::packed(d, t);
+#pragma unroll
+            for (int b = 0; b < DB; ++b) dq[b] = mma32(R::across(k_lds, place, at, t, b * 32), w, dq[b], T{});
+        }
+    }
+
+    __device__ __forceinline__ void end(const AttentionArgs &g, const Span &s, int kv, int r, float scale)
+    {
+        if (r < s.n * g.group) store_head<T, DB>((char *)packed_row(g, g.out, s, kv, r), dq, scale, g.dim, g.wide);
+    }
+};
+
+// dq of many rows: a wave has 32 packed rows, the waves share tiles of keys.
 template <class T, int DB, bool EXTRA, int WAVES>
 __global__ __launch_bounds__(WAVES * 64, sizeof(T) == 2 && DB <= 4 ? 2 : 1) void attention_dq_kernel(const AttentionArgs g)
 {
     using R = Rows<T, DB>;
     constexpr int KEYS = R::ROWB <= 256 ? 64 : 32, NT = WAVES * 64, HALF = KEYS * R::ROWB;
     __shared__ __align__(1024) char lds[4 * HALF];
-    const int kv = (int)((blockIdx.x + g.before) % g.kv_heads), lane = threadIdx.x & 63, h = lane >> 5;
+    const int kv = (int)((blockIdx.x + g.before) % g.kv_heads), lane = threadIdx.x & 63;
     Span s = find_span<true>(g.offsets, g.seqs, g.rows, g.group, WAVES * 32, (int)((blockIdx.x + g.before) / g.kv_heads));
     if (s.seq >= g.seqs) {
         if (s.n > 0 && g.out.p) no_rows<T>(g, g.out, s, kv, s.r0, WAVES * 32, nullptr, 0);
         return;
     }
     find_keys(g, s);
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = s.r0 + wave * 32 + (lane & 31), i = min(r, s.n * g.group - 1);
-    const char *qp = packed_row(g, g.q, s, kv, i), *dp = packed_row(g, g.dy, s, kv, i), *yp = packed_row(g, g.y, s, kv, i);
-    u32x4 q[R::STEPS], dy[R::STEPS];
-    float delta = 0.0f;
-#pragma unroll
-    for (int k = 0; k < R::STEPS; ++k) {
-        const int at = k * 32 + h * 16;
-        q[k] = dy[k] = u32x4{0, 0, 0, 0};
-        if (at >= g.bytes) continue;
-        q[k] = *(const u32x4 *)(qp + at);
-        dy[k] = *(const u32x4 *)(dp + at);
-        const u32x4 y = *(const u32x4 *)(yp + at);
-        T a[16 / sizeof(T)], b[16 / sizeof(T)];
-        __builtin_memcpy(a, &dy[k], 16);
-        __builtin_memcpy(b, &y, 16);
-#pragma unroll
-        for (int j = 0; j < (int)(16 / sizeof(T)); ++j) delta += (float)a[j] * (float)b[j];
-    }
-    delta += other_half(delta);
-    const int64_t item = packed_item(g, s, kv, i);
-    if (h == 0 && r == i) g.delta[item] = delta;
-    if (!g.out.p) return;
-    float lse = g.lse[item] * LOG2E;
-    lse = lse == -INFINITY ? INFINITY : lse;           // (no key seen: all exponentials are zero)
-    const int limit = limit_of(g, s, i / g.group), where = i / g.group + s.ahead, end = min(s.r0 + WAVES * 32, s.n * g.group) - 1;
-    const float slope = EXTRA && g.slopes ? g.slopes[kv * g.group + i % g.group] * LOG2E : 0.0f;
-    const int most = limit_of(g, s, end / g.group), mine = __builtin_amdgcn_readlane(limit, 31);
-    f32x16 dq[DB];
-    clear(dq);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = s.r0 + wave * 32 + (lane & 31);
+    Backward<T, DB, EXTRA> run;
+    if (!run.begin(g, s, kv, r)) return;
+    const int most = limit_of(g, s, (min(s.r0 + WAVES * 32, s.n * g.group) - 1) / g.group), mine = __builtin_amdgcn_readlane(run.limit, 31);
     const typename R::Place place;
     const KeyLoader<R, KEYS, NT> k(g.k.p + (int64_t)s.k_first * g.k.row + (int64_t)kv * g.k.head, g.k.row, g.bytes);
     const KeyLoader<R, KEYS, NT> v(g.v.p + (int64_t)s.k_first * g.v.row + (int64_t)kv * g.v.head, g.v.row, g.bytes);
-    float by = first_factor<T>();
     uint32_t here = 0;
     if (most > 0) {
         k.load(lds_at(lds), 0, s.m);
@@ -730,56 +817,57 @@ __global__ __launch_bounds__(WAVES * 64, sizeof(T) == 2 && DB <= 4 ? 2 : 1) void
             k.load(lds_at(lds) + (here ^ 2 * HALF), j0 + KEYS, s.m);
             v.load(lds_at(lds) + (here ^ 2 * HALF) + HALF, j0 + KEYS, s.m);
         }
-        const char *const k_lds = lds + here, *const v_lds = lds + here + HALF;
 #pragma unroll
-        for (int at = 0; at < KEYS; at += 32) {
-            if (j0 + at >= mine) continue;
-            f32x16 a, d;
-#pragma unroll
-            for (int j = 0; j < 16; ++j) a[j] = d[j] = 0.0f;
-            along_product<R, T>(k_lds, place, at, q, a);
-            along_product<R, T>(v_lds, place, at, dy, d);
-            const float by_log = EXTRA ? 1.0f : g.scale * LOG2E;
-            if constexpr (EXTRA) {
-                if (g.cap != 0.0f) {
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) {
-                        float bent;
-                        a[j] = capped<T>(g, a[j], bent);
-                        d[j] = (d[j] - delta) * bent;
-                    }
-                } else {
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) {
-                        a[j] *= g.scale * LOG2E;
-                        d[j] -= delta;
-                    }
-                }
-                if (g.slopes) {
-                    const float far = (float)(where - j0 - at - 4 * h);
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) a[j] = fmaf(-slope, fabsf(far - (float)block_row(j, 0)), a[j]);
-                }
-            }
-            if (__any(j0 + at + 32 > limit)) {
-#pragma unroll
-                for (int j = 0; j < 16; ++j) a[j] = j0 + at + block_row(j, h) < limit ? a[j] : -INFINITY;
-            }
-#pragma unroll
-            for (int j = 0; j < 16; ++j) {
-                const float p = __builtin_amdgcn_exp2f(fmaf(a[j], by_log, -lse));
-                d[j] = p * (EXTRA ? d[j] : d[j] - delta);
-            }
-            keep_in_range<T>(d, dq, by);
-#pragma unroll
-            for (int t = 0; t < R::FRAGS; ++t) {
-                const u32x4 w = R::packed(d, t);
-#pragma unroll
-                for (int b = 0; b < DB; ++b) dq[b] = mma32(R::across(k_lds, place, at, t, b * 32), w, dq[b], T{});
-            }
-        }
+        for (int at = 0; at < KEYS; at += 32)
+            if (j0 + at < mine) run.step(g, lds + here, lds + here + HALF, place, j0 + at, at);
     }
-    if (r == i) store_head<T, DB>((char *)packed_row(g, g.out, s, kv, r), dq, g.scale / by, g.dim, g.wide);
+    run.end(g, s, kv, r, g.scale / run.by);
+}
+
+// dq of few rows: as in attention_few_kernel, the waves have the same 32 packed rows and take tiles of 32 keys in turn.
+template <class T, int DB, bool EXTRA>
+__global__ __launch_bounds__((FewShape<T, DB>::WAVES * 64)) void attention_dq_few_kernel(const AttentionArgs g)
+{
+    using F = FewShape<T, DB>;
+    using R = Rows<T, DB>;
+    constexpr int WAVES = F::WAVES;
+    __shared__ __align__(1024) char lds[WAVES * 4 * F::SHARE];
+    const int kv = (int)((blockIdx.x + g.before) % g.kv_heads), lane = threadIdx.x & 63;
+    Span s = find_span<true>(g.offsets, g.seqs, g.rows, g.group, 32, (int)((blockIdx.x + g.before) / g.kv_heads));
+    if (s.seq >= g.seqs) {
+        if (s.n > 0 && g.out.p) no_rows<T>(g, g.out, s, kv, s.r0, 32, nullptr, 0);
+        return;
+    }
+    find_keys(g, s);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = s.r0 + (lane & 31);
+    Backward<T, DB, EXTRA> run;
+    if (!run.begin(g, s, kv, r)) return;
+    const int most = __builtin_amdgcn_readlane(run.limit, 31);
+    const typename R::Place place;
+    const KeyLoader<R, 32, 64> k(g.k.p + (int64_t)s.k_first * g.k.row + (int64_t)kv * g.k.head, g.k.row, g.bytes);
+    const KeyLoader<R, 32, 64> v(g.v.p + (int64_t)s.k_first * g.v.row + (int64_t)kv * g.v.head, g.v.row, g.bytes);
+    const uint32_t mine = lds_at(lds) + wave * 4 * F::SHARE;
+    uint32_t here = 0;
+    if (wave * 32 < most) {
+        k.load(mine, wave * 32, s.m);
+        v.load(mine + F::SHARE, wave * 32, s.m);
+    }
+    for (int j0 = wave * 32; j0 < most; j0 += 32 * WAVES, here ^= 2 * F::SHARE) {
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        if (j0 + 32 * WAVES < most) {
+            k.load(mine + (here ^ 2 * F::SHARE), j0 + 32 * WAVES, s.m);
+            v.load(mine + (here ^ 2 * F::SHARE) + F::SHARE, j0 + 32 * WAVES, s.m);
+        }
+        const char *const at = lds + wave * 4 * F::SHARE + here;
+        run.step(g, at, at + F::SHARE, place, j0, 0);
+    }
+    const float scale = g.scale / run.by;
+    if constexpr (WAVES > 1) {
+        join_waves<WAVES>(lds, run.dq, scale);
+        if (wave == 0) run.end(g, s, kv, r, 1.0f);
+    } else {
+        run.end(g, s, kv, r, scale);
+    }
 }
 
 // dk and dv: a wave has 32 keys, the waves share tiles of 32 packed rows of the kv head.
@@ -993,14 +1081,18 @@ template <class T, int DB, bool EXTRA>
 hipError_t launch_rows(hipStream_t st, int few, const AttentionArgs &g)
 {
     if (few)
-        return in_launches(g, ((int64_t)g.seqs + 1) * g.kv_heads, [&](const AttentionArgs &p, dim3 grid) {
+        return in_launches(g, (g.tiles ? g.tiles : (int64_t)g.seqs + 1) * g.kv_heads, [&](const AttentionArgs &p, dim3 grid) {
             attention_few_kernel<T, DB, EXTRA><<<grid, FewShape<T, DB>::WAVES * 64, 0, st>>>(p);
         });
     return in_launches(g, (int64_t)g.tiles * g.kv_heads, [&](const AttentionArgs &p, dim3 grid) { attention_kernel<T, DB, EXTRA, 4><<<grid, 256, 0, st>>>(p); });
 }
 template <class T, int DB, bool EXTRA>
-hipError_t launch_dq(hipStream_t st, const AttentionArgs &g)
+hipError_t launch_dq(hipStream_t st, int few, const AttentionArgs &g)
 {
+    if (few)
+        return in_launches(g, (int64_t)g.tiles * g.kv_heads, [&](const AttentionArgs &p, dim3 grid) {
+            attention_dq_few_kernel<T, DB, EXTRA><<<grid, FewShape<T, DB>::WAVES * 64, 0, st>>>(p);
+        });
     return in_launches(g, (int64_t)g.tiles * g.kv_heads, [&](const AttentionArgs &p, dim3 grid) { attention_dq_kernel<T, DB, EXTRA, 4><<<grid, 256, 0, st>>>(p); });
 }
 template <class T, int DB, bool EXTRA>

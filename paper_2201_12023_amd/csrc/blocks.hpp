@@ -29,12 +29,12 @@ struct AttentionArgs {
     float *part2;
 };
 
-constexpr int ATTENTION_TILE = 128;                 // packed rows, or keys, of a workgroup
+constexpr int ATTENTION_TILE = 128, FEW_TILE = 32;     // packed rows, or keys, of a workgroup
 
 // An element type's kernels (one file each, to build them side by side).
 #define ALPA_ATTENTION_LAUNCHES(type)                                                 \
     hipError_t launch_attention_##type(hipStream_t, int few, const AttentionArgs &);       \
-    hipError_t launch_attention_dq_##type(hipStream_t, const AttentionArgs &);        \
+    hipError_t launch_attention_dq_##type(hipStream_t, int few, const AttentionArgs &); \
     hipError_t launch_attention_dkv_##type(hipStream_t, const AttentionArgs &);
 ALPA_ATTENTION_LAUNCHES(f32)
 ALPA_ATTENTION_LAUNCHES(f16)

@@ -94,6 +94,25 @@ def test_few_rows_with_many_keys(dtype, rows, keys, heads, kv):
     check_attention(gen(9), dtype, rows, keys, heads, kv, 64, train=False, causal=True)
 
 
+@pytest.mark.parametrize("keys", [1, 70])
+def test_very_many_sequences(keys):
+    """One row of each of 700 sequences, some without keys, rows of none on both sides."""
+    g, seqs = gen(11), 700
+    lens = torch.randint(0, keys + 1, (seqs,), device="cuda", generator=g, dtype=torch.int32)
+    ends = torch.cumsum(lens, 0).to(torch.int32)
+    k_off = torch.cat([torch.zeros_like(ends[:1]), ends])
+    off = torch.arange(seqs + 1, device="cuda", dtype=torch.int32) + 2
+    check_attention(g, BF16, seqs + 7, int(ends[-1]) + 3, 4, 2, 64, offsets=off, k_offsets=k_off, causal=True)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("causal", [False, True])
+def test_tiles_of_many_rows(dtype, causal):
+    """Enough rows for the kernels that share tiles of keys among rows, forward and backward."""
+    off = ints(1, 1300, 1300, 2000, 2950)
+    check_attention(gen(12), dtype, 2960, 2960, 24, 12, 64, offsets=off, causal=causal, cap=8.0 if causal else 0.0)
+
+
 @pytest.mark.parametrize("dtype", TYPES, ids=str)
 def test_many_rows_with_few_keys(dtype):
     """Gradients of keys whose rows go in parts that are added."""
