@@ -160,7 +160,7 @@ struct Plan {
 // What a call's rows are to the kernels.
 struct Shape {
     int64_t packed, tiles;          // rows of a kv head; tiles of many rows, about
-    bool few, direct;               // tiles of 32 rows whose keys the waves share; without a search among the sequences
+    bool few, direct;               // tiles of 32 rows whose keys the waves share; forward, a sequence a workgroup, without a search
 
     explicit Shape(const alpa_attention_t &a)
         : packed(a.rows * (a.heads / a.kv_heads)), tiles((packed / ATTENTION_TILE + std::min<int64_t>(a.seqs, packed)) * a.kv_heads)
@@ -168,29 +168,38 @@ struct Shape {
         // few rows of a sequence, so that the keys and not the products are what takes time; or few tiles, so that waves are short of work
         const bool short_rows = packed <= 64 * (int64_t)a.seqs;
         few = short_rows || tiles <= COMPUTE_UNITS;
-        direct = short_rows && a.seqs > 512;
+        direct = packed <= 32 * (int64_t)a.seqs;
     }
 };
 
-// Parts of the keys: enough workgroups to fill the compute units twice, each with a few tiles.
-int key_splits(const alpa_attention_t &a, const Shape &shape)
+// As many workgroups as are on the compute units at once.  With a causal mask a tile has half of all parts on average, and where one part each fills the units,
+// two are better, as the tile with most work is what is waited for.
+int64_t parts_for(int64_t tiles, int64_t slots, bool causal)
 {
-    const int64_t keys = a.k_rows / a.seqs;
-    const int64_t tiles = shape.few ? std::max<int64_t>(shape.packed / FEW_TILE, a.seqs) * a.kv_heads : shape.tiles;
-    const int64_t least = shape.few ? 128 : 256;
-    return (int)std::max<int64_t>(1, std::min({(int64_t)64, 512 / tiles, keys / least}));
+    return causal ? std::max<int64_t>(2 * slots / tiles - 1, tiles <= 2 * slots ? 2 : 1) : slots / tiles;
 }
 
-// Parts of the rows for dk and dv (RowParts in attention_kernel.hpp): as many workgroups as are on the compute units at once, two each.  With a causal mask a
-// tile has half of all parts on average, and where one part each fills the units, two are better, as the tile with most rows is what is waited for
-// (8192 rows, 32 heads on 8 kv heads: 1963 us in one part, 1260 in two, 1435 in three; 2048 rows: 265 in two, 168 in four, 136 in six, 165 in eight;
+// Parts of the keys for y and dq (KeyParts in attention_kernel.hpp).
+int key_splits(const alpa_attention_t &a, const Shape &shape, bool backward)
+{
+    const int64_t keys = a.k_rows / a.seqs;
+    if (!shape.few) {
+        if (backward && a.dtype == ALPA_F32) return 1;           // (4096 rows, 16 heads: dq 879 us, 933 in two parts; forward 799 and 579)
+        return (int)std::max<int64_t>(1, std::min({(int64_t)64, parts_for(shape.tiles, 2 * COMPUTE_UNITS, a.causal), keys / 2048}));
+    }
+    // (one workgroup a unit where its tiles fill the LDS; rows that are few in front of their keys see nearly all of them)
+    const int64_t slots = dim_blocks(a.dim) == 2 && a.dtype != ALPA_F32 ? 2 * COMPUTE_UNITS : COMPUTE_UNITS;
+    const int64_t tiles = std::max<int64_t>(shape.packed / FEW_TILE, a.seqs) * a.kv_heads;
+    return (int)std::max<int64_t>(1, std::min({(int64_t)64, parts_for(tiles, slots, a.causal && a.rows > a.k_rows / 4), keys / (a.dtype == ALPA_F32 ? 64 : 128)}));
+}
+
+// Parts of the rows for dk and dv (RowParts in attention_kernel.hpp; causal, 8192 rows, 32 heads on 8 kv heads: 1963 us in one part, 1260 in two, 1435 in three; 2048 rows: 265 in two, 168 in four, 136 in six, 165 in eight;
 // without the mask 8 heads of 8192 rows: 605, 634 in two; 32 on 8 of 2048: 294 in two, 182 in four, 227 in six).
 int row_splits(const alpa_attention_t &a)
 {
     const int64_t rows = a.rows * (a.heads / a.kv_heads) / a.seqs;
-    const int64_t tiles = std::max<int64_t>((a.k_rows / ATTENTION_TILE + a.seqs / 2) * a.kv_heads, a.kv_heads), slots = 2 * COMPUTE_UNITS;
-    const int64_t even = a.causal ? std::max<int64_t>(2 * slots / tiles - 1, tiles <= 2 * slots ? 2 : 1) : slots / tiles;
-    return (int)std::max<int64_t>(1, std::min({(int64_t)32, even, rows / (a.dtype == ALPA_F32 ? 64 : 128)}));
+    const int64_t tiles = std::max<int64_t>((a.k_rows / ATTENTION_TILE + a.seqs / 2) * a.kv_heads, a.kv_heads);
+    return (int)std::max<int64_t>(1, std::min({(int64_t)32, parts_for(tiles, 2 * COMPUTE_UNITS, a.causal), rows / (a.dtype == ALPA_F32 ? 64 : 128)}));
 }
 
 void plan_forward(Plan &p, const alpa_heads_t &q, const alpa_heads_t &k, const alpa_heads_t &v)
@@ -200,7 +209,7 @@ void plan_forward(Plan &p, const alpa_heads_t &q, const alpa_heads_t &k, const a
     g.k = p.operand(k, false);
     g.v = p.operand(v, false);
     const Shape shape(p.a);
-    g.splits = key_splits(p.a, shape);
+    g.splits = key_splits(p.a, shape, false);
     g.tiles = shape.direct ? 0 : (int)Plan::tiles_of(shape.packed, p.a.seqs, shape.few ? FEW_TILE : ATTENTION_TILE);
     if (g.splits > 1) {
         const int64_t items = (int64_t)g.splits * p.a.rows * p.a.heads;
@@ -218,12 +227,11 @@ void plan_backward(Plan &p, const alpa_heads_t &dy, const alpa_heads_t &q, const
     g.v = p.operand(v, false);
     g.y = p.operand(y, true);
     g.delta = p.take<float>(p.a.rows * p.a.heads);
-    g.splits = row_splits(p.a);
-    if (g.splits > 1) {
-        const int64_t items = (int64_t)g.splits * p.a.k_rows * p.a.kv_heads;
-        g.part = p.take<float>(items * p.a.dim);
-        g.part2 = p.take<float>(items * p.a.dim);
-    }
+    const int rows = row_splits(p.a), keys = key_splits(p.a, Shape(p.a), true);
+    g.splits = rows;
+    const int64_t items = rows > 1 ? (int64_t)rows * p.a.k_rows * p.a.kv_heads : 0, q_items = keys > 1 ? (int64_t)keys * p.a.rows * p.a.heads : 0;
+    if (items || q_items) g.part = p.take<float>(std::max(items, q_items) * p.a.dim);          // (dq's are done with when dk's come)
+    if (items) g.part2 = p.take<float>(items * p.a.dim);
 }
 
 hipError_t launch_rows_of(hipStream_t st, int dtype, int few, const AttentionArgs &g)
@@ -319,7 +327,6 @@ int alpa_attention_forward(const alpa_attention_t *how, alpa_heads_t q, alpa_hea
     g.lse = lse;
     if (p.pack.count) HIPCHK(launch_head_pack(st, a.dtype, p.pack));
     HIPCHK(launch_rows_of(st, a.dtype, Shape(a).few, g));
-    if (g.splits > 1) HIPCHK(launch_attention_join(st, a.dtype, g));
     return ALPA_DP_OK;
 }
 
@@ -362,7 +369,7 @@ int alpa_attention_backward(const alpa_attention_t *how, alpa_heads_t dy, alpa_h
         g.wide = wide_heads(dq, a.dtype, bytes);
         const Shape shape(a);
         g.tiles = (int)Plan::tiles_of(shape.packed, a.seqs, shape.few ? FEW_TILE : ATTENTION_TILE);
-        g.splits = 1;
+        g.splits = key_splits(a, shape, true);
         HIPCHK(launch_dq_of(st, a.dtype, shape.few, g));
     }
     if (a.k_rows > 0 && (dk.p || dv.p)) {

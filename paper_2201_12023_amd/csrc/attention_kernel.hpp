@@ -213,15 +213,31 @@ __device__ __forceinline__ float capped(const AttentionArgs &g, float s, float &
 __device__ __forceinline__ float other_half(float v) { return __shfl_xor(v, 32, 64); }
 
 // Sixteen bytes a lane from memory to LDS, written there by the load unit itself: the wave's go to `lds` and the 1008 bytes behind, in the order of its lanes; those
-// whose offset is out of range are zeros.  Assembly without a result register, as in product.hpp: what has arrived is known by counting.
+// whose offset is out of range are zeros.  Assembly without a result register, as in product.hpp: what has arrived is known by counting.  (The hardware wants five
+// wait states between a vector instruction that writes a scalar register and a load that reads it, which the compiler does not see: the move and the wait.)
 __device__ __forceinline__ void load_chunk(uint32_t lds, uint32_t off, u32x4 range)
 {
 #pragma clang diagnostic push
 #pragma clang diagnostic ignored "-Winline-asm"         // (m0 is reserved, and said to be overwritten all the same)
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
                  :
                  : "s"(__builtin_amdgcn_readfirstlane(lds)), "v"(off), "s"(range)
                  : "m0");
+#pragma clang diagnostic pop
+}
+// Four of them, `APART` bytes apart in LDS.
+template <int APART>
+__device__ __forceinline__ void load_chunks(uint32_t lds, uint32_t a, uint32_t b, uint32_t c, uint32_t d, u32x4 range)
+{
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tbuffer_load_dwordx4 %1, %5, 0 offen lds\n\t"
+                 "s_add_u32 m0, m0, %6\n\ts_nop 0\n\tbuffer_load_dwordx4 %2, %5, 0 offen lds\n\t"
+                 "s_add_u32 m0, m0, %6\n\ts_nop 0\n\tbuffer_load_dwordx4 %3, %5, 0 offen lds\n\t"
+                 "s_add_u32 m0, m0, %6\n\ts_nop 0\n\tbuffer_load_dwordx4 %4, %5, 0 offen lds"
+                 :
+                 : "s"(__builtin_amdgcn_readfirstlane(lds)), "v"(a), "v"(b), "v"(c), "v"(d), "s"(range), "n"(APART)
+                 : "m0", "scc");
 #pragma clang diagnostic pop
 }
 __device__ __forceinline__ u32x4 range_of(const char *p, uint32_t bytes)
@@ -258,8 +274,14 @@ struct KeyLoader {
         const int rows = min(end - j0, COUNT);
         const u32x4 range = range_of(p + j0 * stride, rows > 0 ? (uint32_t)((rows - 1) * (int)stride + bytes) : 0u);
         const uint32_t to = lds + __builtin_amdgcn_readfirstlane(threadIdx.x % NT / 64) * 1024;
+        const auto from = [&](int j) { return off[j % KINDS] + (uint32_t)(j / KINDS * KINDS * APART * (int)stride); };
+        if constexpr (N % 4 == 0) {
 #pragma unroll
-        for (int j = 0; j < N; ++j) load_chunk(to + j * NT * 16, off[j % KINDS] + (uint32_t)(j / KINDS * KINDS * APART * (int)stride), range);
+            for (int j = 0; j < N; j += 4) load_chunks<NT * 16>(to + j * NT * 16, from(j), from(j + 1), from(j + 2), from(j + 3), range);
+        } else {
+#pragma unroll
+            for (int j = 0; j < N; ++j) load_chunk(to + j * NT * 16, from(j), range);
+        }
     }
 };
 
@@ -302,6 +324,15 @@ struct PackedLoader {
         }
     }
 };
+
+// Fragments that are waited for here: to the compiler a load is under way until its register is used, which is in the loop, where it would wait for the loads to
+// LDS as well (a tenth of a forward pass's time).
+template <int N>
+__device__ __forceinline__ void settle(const u32x4 (&f)[N])
+{
+#pragma unroll
+    for (int k = 0; k < N; ++k) asm volatile("" ::"v"(f[k]));
+}
 
 // Where packed row r of a sequence's kv head lies in a tensor of queries.
 __device__ __forceinline__ const char *packed_row(const AttentionArgs &g, const Heads &t, const Span &s, int kv, int r)
@@ -358,12 +389,14 @@ struct Running {
             const int at = k * 32 + h * 16;
             q[k] = at < g.bytes ? *(const u32x4 *)(p + at) : u32x4{0, 0, 0, 0};
         }
+        settle(q);
         clear(y);
         top = -INFINITY;
         sum = 0.0f;
         limit = limit_of(g, s, i / g.group);
         place = i / g.group + s.ahead;
         slope = EXTRA && g.slopes ? g.slopes[kv * g.group + i % g.group] * LOG2E : 0.0f;
+        asm volatile("" ::"v"(slope));
     }
 
     // NB blocks of 32 keys from j0 on, in LDS from row `at` on
@@ -437,14 +470,14 @@ struct Running {
     }
 
     // y and lse, or this part of them
-    __device__ __forceinline__ void end(const AttentionArgs &g, const Span &s, int kv, int r, int split)
+    __device__ __forceinline__ void end(const AttentionArgs &g, const Span &s, int kv, int r, int part, int parts)
     {
         const float all = sum + other_half(sum);
         if (r >= s.n * g.group) return;
         const int64_t item = packed_item(g, s, kv, r);
         const bool first = (threadIdx.x & 32) == 0;
-        if (g.splits > 1) {
-            const int64_t at = (int64_t)split * g.rows * g.heads + item;
+        if (parts > 1) {
+            const int64_t at = (int64_t)part * g.rows * g.heads + item;
             store_head<float, DB>((char *)(g.part + at * g.dim), y, 1.0f, g.dim, (g.dim & 3) == 0);
             if (first) g.stat[at] = make_float2(top, all);
             return;
@@ -455,28 +488,32 @@ struct Running {
     }
 };
 
-// zeros for rows that belong to no sequence, packed rows r0 .. r0 + count - 1; where results are joined later, a part without weight
+// zeros for rows that belong to no sequence, packed rows r0 .. r0 + count - 1
 template <class T>
-__device__ __forceinline__ void no_rows(const AttentionArgs &g, const Heads &out, const Span &s, int kv, int r0, int count, float *lse, int split)
+__device__ __forceinline__ void no_rows(const AttentionArgs &g, const Heads &out, const Span &s, int kv, int r0, int count, float *lse)
 {
-    for (int r = r0 + (threadIdx.x >> 6); r < min(r0 + count, s.n * g.group); r += blockDim.x >> 6) {
-        if (g.splits > 1) {
-            if ((threadIdx.x & 63) == 0) g.stat[(int64_t)split * g.rows * g.heads + packed_item(g, s, kv, r)] = make_float2(-INFINITY, 0.0f);
-            continue;
-        }
+    for (int r = r0 + (threadIdx.x >> 6); r < min(r0 + count, s.n * g.group) && blockIdx.y == 0; r += blockDim.x >> 6) {
         T *to = (T *)packed_row(g, out, s, kv, r);
         for (int d = threadIdx.x & 63; d < g.dim; d += 64) to[d] = (T)0.0f;
         if (lse && (threadIdx.x & 63) == 0) lse[packed_item(g, s, kv, r)] = -INFINITY;
     }
 }
 
-// The keys that one of `splits` workgroups takes, in whole tiles.
-__device__ __forceinline__ void share_of(int most, int tile, int splits, int split, int &from, int &to)
-{
-    const int tiles = (most + tile - 1) / tile, per = (tiles + splits - 1) / splits;
-    from = min(split * per, tiles) * tile;
-    to = min(min(split * per + per, tiles) * tile, most);
-}
+// The keys that a tile of rows sees, `most`, and the parts they are dealt in: of a causal sequence the last rows have most keys, and their tiles alone would be
+// what the call waits for; of one new token a tile is all there is.  Parts are `chunk` keys, an even share of the sequence's in steps of the
+// kernel, so that a tile with few
+// keys is one part and needs no join.
+struct KeyParts {
+    int most, chunk, count;
+
+    // the tile's packed rows are those from s.r0 on, `rows` at most
+    __device__ __forceinline__ KeyParts(const AttentionArgs &g, const Span &s, int rows)
+    {
+        most = limit_of(g, s, (min(s.r0 + rows, s.n * g.group) - 1) / g.group);
+        chunk = max(((s.m + g.unit - 1) / g.unit + g.splits - 1) / g.splits, 1) * g.unit;
+        count = max((most + chunk - 1) / chunk, 1);
+    }
+};
 
 // Many rows: a wave has 32 packed rows, the waves share tiles of keys, of which one is worked on and the next one under way.
 template <class T, int DB, bool EXTRA, int WAVES>
@@ -488,19 +525,18 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attention_kernel(const Attentio
     const int kv = (int)((blockIdx.x + g.before) % g.kv_heads);
     Span s = find_span<true>(g.offsets, g.seqs, g.rows, g.group, WAVES * 32, (int)((blockIdx.x + g.before) / g.kv_heads));
     if (s.seq >= g.seqs) {
-        if (s.n > 0) no_rows<T>(g, g.out, s, kv, s.r0, WAVES * 32, g.lse, blockIdx.y);
+        if (s.n > 0) no_rows<T>(g, g.out, s, kv, s.r0, WAVES * 32, g.lse);
         return;
     }
     find_keys(g, s);
+    const KeyParts part(g, s, WAVES * 32);
+    const int index = g.splits - 1 - (int)blockIdx.y, from = index * part.chunk, to = min(from + part.chunk, part.most);
+    if (index >= part.count) return;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = s.r0 + wave * 32 + (threadIdx.x & 31);
     Running<T, DB, EXTRA> run;
     run.begin(g, s, kv, r);
     const typename R::Place place;
-    // (rows see more keys the later they are)
-    const int last = min(s.r0 + WAVES * 32, s.n * g.group) - 1, most = limit_of(g, s, last / g.group);
     const int mine = __builtin_amdgcn_readlane(run.limit, 31);
-    int from, to;
-    share_of(most, KEYS, g.splits, blockIdx.y, from, to);
     const KeyLoader<R, KEYS, NT> k(g.k.p + (int64_t)s.k_first * g.k.row + (int64_t)kv * g.k.head, g.k.row, g.bytes);
     const KeyLoader<R, KEYS, NT> v(g.v.p + (int64_t)s.k_first * g.v.row + (int64_t)kv * g.v.head, g.v.row, g.bytes);
     uint32_t here = 0;
@@ -516,11 +552,40 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attention_kernel(const Attentio
         }
         if (j0 < mine) run.template step<KEYS / 32>(g, lds + here, lds + here + HALF, place, j0);
     }
-    run.end(g, s, kv, r, blockIdx.y);
+    run.end(g, s, kv, r, index, part.count);
 }
 
+// A workgroup's rows: one tile of a sequence's (g.tiles of them), or all rows of one sequence, without a search; the rows of none are one sequence more then,
+// with those in front of the first sequence in `other`.
+struct Share {
+    Span s, other;
+    int begin, end;
+
+    __device__ __forceinline__ Share(const AttentionArgs &g, int tile)
+    {
+        const int index = (int)((blockIdx.x + g.before) / g.kv_heads);
+        if (g.tiles) {
+            s = find_span<true>(g.offsets, g.seqs, g.rows, g.group, tile, index);
+            begin = s.r0;
+            end = min(s.r0 + tile, s.n * g.group);
+            return;
+        }
+        const auto rows_of = [&](int k, Span &to) {
+            int last;
+            sequence_rows(g.offsets, g.seqs, g.rows, k, to.first, last);
+            to.seq = k;
+            to.n = last - to.first;
+            to.r0 = 0;
+        };
+        rows_of(index, s);
+        if (index == g.seqs) rows_of(index + 1, other);
+        begin = 0;
+        end = s.n * g.group;
+    }
+};
+
 // Few rows: the waves of a workgroup have the same 32 packed rows and take tiles of 32 keys in turn, each from its own part of LDS; in the end their sums
-// are joined.  A workgroup has one tile of rows (g.tiles), or, of very many sequences, goes through one's rows, and one more stands for the rows of none.
+// are joined.
 template <class T, int DB>
 struct FewShape {
     using R = Rows<T, DB>;
@@ -557,32 +622,12 @@ __global__ __launch_bounds__((FewShape<T, DB>::WAVES * 64)) void attention_few_k
     __shared__ __align__(1024) char lds[WAVES * 4 * F::SHARE];
     __shared__ float tops[WAVES][32], sums[WAVES][32];
     const int kv = (int)((blockIdx.x + g.before) % g.kv_heads), lane = threadIdx.x & 63;
-    Span s;
-    int r_begin = 0, r_end;
-    if (g.tiles) {
-        s = find_span<true>(g.offsets, g.seqs, g.rows, g.group, 32, (int)((blockIdx.x + g.before) / g.kv_heads));
-        r_begin = s.r0;
-        r_end = min(s.r0 + 32, s.n * g.group);
-        if (s.seq >= g.seqs) {
-            if (s.n > 0) no_rows<T>(g, g.out, s, kv, s.r0, 32, g.lse, blockIdx.y);
-            return;
-        }
-    } else {
-        s.seq = (int)((blockIdx.x + g.before) / g.kv_heads);
-        const auto rows_of = [&](int k) {
-            int first, end;
-            sequence_rows(g.offsets, g.seqs, g.rows, k, first, end);
-            s.first = first;
-            s.n = end - first;
-        };
-        rows_of(s.seq);
-        if (s.seq == g.seqs) {
-            no_rows<T>(g, g.out, s, kv, 0, s.n * g.group, g.lse, blockIdx.y);
-            rows_of(g.seqs + 1);
-            no_rows<T>(g, g.out, s, kv, 0, s.n * g.group, g.lse, blockIdx.y);
-            return;
-        }
-        r_end = s.n * g.group;
+    const Share share(g, 32);
+    Span s = share.s;
+    if (s.seq >= g.seqs) {
+        no_rows<T>(g, g.out, s, kv, share.begin, share.end - share.begin, g.lse);
+        if (s.seq == g.seqs && !g.tiles) no_rows<T>(g, g.out, share.other, kv, 0, share.other.n * g.group, g.lse);
+        return;
     }
     find_keys(g, s);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -590,12 +635,14 @@ __global__ __launch_bounds__((FewShape<T, DB>::WAVES * 64)) void attention_few_k
     const uint32_t mine = lds_at(lds) + wave * 4 * F::SHARE;
     const KeyLoader<R, 32, 64> k(g.k.p + (int64_t)s.k_first * g.k.row + (int64_t)kv * g.k.head, g.k.row, g.bytes);
     const KeyLoader<R, 32, 64> v(g.v.p + (int64_t)s.k_first * g.v.row + (int64_t)kv * g.v.head, g.v.row, g.bytes);
-    for (int r0 = r_begin; r0 < r_end; r0 += 32) {
+    for (int r0 = share.begin; r0 < share.end; r0 += 32) {
         const int r = r0 + (lane & 31);
+        s.r0 = r0;
+        const KeyParts part(g, s, 32);
+        const int index = g.splits - 1 - (int)blockIdx.y, from = index * part.chunk, to = min(from + part.chunk, part.most);
+        if (index >= part.count) continue;
         Running<T, DB, EXTRA> run;
         run.begin(g, s, kv, r);
-        int from, to;
-        share_of(__builtin_amdgcn_readlane(run.limit, 31), 32 * WAVES, g.splits, blockIdx.y, from, to);
         // each wave waits for its own loads alone
         const int j1 = from + wave * 32;
         uint32_t here = 0;
@@ -632,7 +679,7 @@ __global__ __launch_bounds__((FewShape<T, DB>::WAVES * 64)) void attention_few_k
             run.top = top;
             run.sum = (threadIdx.x & 32) ? 0.0f : total;
         }
-        if (wave == 0) run.end(g, s, kv, r, blockIdx.y);
+        if (wave == 0) run.end(g, s, kv, r, index, part.count);
     }
 }
 
@@ -701,7 +748,7 @@ struct Backward {
     // false: dq is not wanted
     __device__ __forceinline__ bool begin(const AttentionArgs &g, const Span &s, int kv, int r)
     {
-        const int h = threadIdx.x >> 5 & 1, i = min(r, s.n * g.group - 1);
+        const int h = threadIdx.x >> 5 & 1, i = min(r, s.n * g.group - 1);          // (of several parts each puts down the sum of dy y, the same bits)
         const char *qp = packed_row(g, g.q, s, kv, i), *dp = packed_row(g, g.dy, s, kv, i), *yp = packed_row(g, g.y, s, kv, i);
         delta = 0.0f;
 #pragma unroll
@@ -717,6 +764,8 @@ struct Backward {
 #pragma unroll
             for (int j = 0; j < (int)(16 / sizeof(T)); ++j) delta += (float)a[j] * (float)b[j];
         }
+        settle(q);
+        settle(dy);
         delta += other_half(delta);
         const int64_t item = packed_item(g, s, kv, i);
         if (h == 0 && r == i) g.delta[item] = delta;
@@ -726,6 +775,7 @@ struct Backward {
         where = i / g.group + s.ahead;
         slope = EXTRA && g.slopes ? g.slopes[kv * g.group + i % g.group] * LOG2E : 0.0f;
         by = first_factor<T>();
+        asm volatile("" ::"v"(lse), "v"(slope));
         clear(dq);
         return g.out.p != nullptr;
     }
@@ -779,9 +829,11 @@ struct Backward {
         }
     }
 
-    __device__ __forceinline__ void end(const AttentionArgs &g, const Span &s, int kv, int r, float scale)
+    __device__ __forceinline__ void end(const AttentionArgs &g, const Span &s, int kv, int r, float scale, int part, int parts)
     {
-        if (r < s.n * g.group) store_head<T, DB>((char *)packed_row(g, g.out, s, kv, r), dq, scale, g.dim, g.wide);
+        if (r >= s.n * g.group) return;
+        if (parts > 1) store_head<float, DB>((char *)(g.part + ((int64_t)part * g.rows * g.heads + packed_item(g, s, kv, r)) * g.dim), dq, scale, g.dim, (g.dim & 3) == 0);
+        else store_head<T, DB>((char *)packed_row(g, g.out, s, kv, r), dq, scale, g.dim, g.wide);
     }
 };
 
@@ -795,25 +847,28 @@ __global__ __launch_bounds__(WAVES * 64, sizeof(T) == 2 && DB <= 4 ? 2 : 1) void
     const int kv = (int)((blockIdx.x + g.before) % g.kv_heads), lane = threadIdx.x & 63;
     Span s = find_span<true>(g.offsets, g.seqs, g.rows, g.group, WAVES * 32, (int)((blockIdx.x + g.before) / g.kv_heads));
     if (s.seq >= g.seqs) {
-        if (s.n > 0 && g.out.p) no_rows<T>(g, g.out, s, kv, s.r0, WAVES * 32, nullptr, 0);
+        if (s.n > 0 && g.out.p) no_rows<T>(g, g.out, s, kv, s.r0, WAVES * 32, nullptr);
         return;
     }
     find_keys(g, s);
+    const KeyParts part(g, s, WAVES * 32);
+    const int index = g.splits - 1 - (int)blockIdx.y, from = index * part.chunk, to = min(from + part.chunk, part.most);
+    if (index >= part.count) return;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = s.r0 + wave * 32 + (lane & 31);
     Backward<T, DB, EXTRA> run;
     if (!run.begin(g, s, kv, r)) return;
-    const int most = limit_of(g, s, (min(s.r0 + WAVES * 32, s.n * g.group) - 1) / g.group), mine = __builtin_amdgcn_readlane(run.limit, 31);
+    const int mine = __builtin_amdgcn_readlane(run.limit, 31);
     const typename R::Place place;
     const KeyLoader<R, KEYS, NT> k(g.k.p + (int64_t)s.k_first * g.k.row + (int64_t)kv * g.k.head, g.k.row, g.bytes);
     const KeyLoader<R, KEYS, NT> v(g.v.p + (int64_t)s.k_first * g.v.row + (int64_t)kv * g.v.head, g.v.row, g.bytes);
     uint32_t here = 0;
-    if (most > 0) {
-        k.load(lds_at(lds), 0, s.m);
-        v.load(lds_at(lds) + HALF, 0, s.m);
+    if (from < to) {
+        k.load(lds_at(lds), from, s.m);
+        v.load(lds_at(lds) + HALF, from, s.m);
     }
-    for (int j0 = 0; j0 < most; j0 += KEYS, here ^= 2 * HALF) {
+    for (int j0 = from; j0 < to; j0 += KEYS, here ^= 2 * HALF) {
         arrived<0>();
-        if (j0 + KEYS < most) {
+        if (j0 + KEYS < to) {
             k.load(lds_at(lds) + (here ^ 2 * HALF), j0 + KEYS, s.m);
             v.load(lds_at(lds) + (here ^ 2 * HALF) + HALF, j0 + KEYS, s.m);
         }
@@ -821,7 +876,7 @@ __global__ __launch_bounds__(WAVES * 64, sizeof(T) == 2 && DB <= 4 ? 2 : 1) void
         for (int at = 0; at < KEYS; at += 32)
             if (j0 + at < mine) run.step(g, lds + here, lds + here + HALF, place, j0 + at, at);
     }
-    run.end(g, s, kv, r, g.scale / run.by);
+    run.end(g, s, kv, r, g.scale / run.by, index, part.count);
 }
 
 // dq of few rows: as in attention_few_kernel, the waves have the same 32 packed rows and take tiles of 32 keys in turn.
@@ -835,26 +890,28 @@ __global__ __launch_bounds__((FewShape<T, DB>::WAVES * 64)) void attention_dq_fe
     const int kv = (int)((blockIdx.x + g.before) % g.kv_heads), lane = threadIdx.x & 63;
     Span s = find_span<true>(g.offsets, g.seqs, g.rows, g.group, 32, (int)((blockIdx.x + g.before) / g.kv_heads));
     if (s.seq >= g.seqs) {
-        if (s.n > 0 && g.out.p) no_rows<T>(g, g.out, s, kv, s.r0, 32, nullptr, 0);
+        if (s.n > 0 && g.out.p) no_rows<T>(g, g.out, s, kv, s.r0, 32, nullptr);
         return;
     }
     find_keys(g, s);
+    const KeyParts part(g, s, 32);
+    const int index = g.splits - 1 - (int)blockIdx.y, from = index * part.chunk, to = min(from + part.chunk, part.most);
+    if (index >= part.count) return;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = s.r0 + (lane & 31);
     Backward<T, DB, EXTRA> run;
     if (!run.begin(g, s, kv, r)) return;
-    const int most = __builtin_amdgcn_readlane(run.limit, 31);
     const typename R::Place place;
     const KeyLoader<R, 32, 64> k(g.k.p + (int64_t)s.k_first * g.k.row + (int64_t)kv * g.k.head, g.k.row, g.bytes);
     const KeyLoader<R, 32, 64> v(g.v.p + (int64_t)s.k_first * g.v.row + (int64_t)kv * g.v.head, g.v.row, g.bytes);
     const uint32_t mine = lds_at(lds) + wave * 4 * F::SHARE;
     uint32_t here = 0;
-    if (wave * 32 < most) {
-        k.load(mine, wave * 32, s.m);
-        v.load(mine + F::SHARE, wave * 32, s.m);
+    if (from + wave * 32 < to) {
+        k.load(mine, from + wave * 32, s.m);
+        v.load(mine + F::SHARE, from + wave * 32, s.m);
     }
-    for (int j0 = wave * 32; j0 < most; j0 += 32 * WAVES, here ^= 2 * F::SHARE) {
+    for (int j0 = from + wave * 32; j0 < to; j0 += 32 * WAVES, here ^= 2 * F::SHARE) {
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-        if (j0 + 32 * WAVES < most) {
+        if (j0 + 32 * WAVES < to) {
             k.load(mine + (here ^ 2 * F::SHARE), j0 + 32 * WAVES, s.m);
             v.load(mine + (here ^ 2 * F::SHARE) + F::SHARE, j0 + 32 * WAVES, s.m);
         }
@@ -864,15 +921,16 @@ __global__ __launch_bounds__((FewShape<T, DB>::WAVES * 64)) void attention_dq_fe
     const float scale = g.scale / run.by;
     if constexpr (WAVES > 1) {
         join_waves<WAVES>(lds, run.dq, scale);
-        if (wave == 0) run.end(g, s, kv, r, 1.0f);
+        if (wave == 0) run.end(g, s, kv, r, 1.0f, index, part.count);
     } else {
-        run.end(g, s, kv, r, scale);
+        run.end(g, s, kv, r, scale, index, part.count);
     }
 }
 
 // dk and dv: a wave has 32 keys, the waves share tiles of 32 packed rows of the kv head.
-template <class T, int DB, bool EXTRA, int WAVES>
-__global__ __launch_bounds__(WAVES * 64, sizeof(T) == 2 && DB <= 4 ? 2 : 1) void attention_dkv_kernel(const AttentionArgs g)
+// DK, DV: which of the two; heads of 256 elements have no registers for both at once.
+template <class T, int DB, bool EXTRA, int WAVES, bool DK, bool DV>
+__global__ __launch_bounds__(WAVES * 64, sizeof(T) == 2 && (DB <= 4 || !DK) ? 2 : 1) void attention_dkv_kernel(const AttentionArgs g)
 {
     using R = Rows<T, DB>;
     constexpr int TILE = 32, NT = WAVES * 64, HALF = TILE * R::ROWB;
@@ -889,8 +947,8 @@ __global__ __launch_bounds__(WAVES * 64, sizeof(T) == 2 && DB <= 4 ? 2 : 1) void
         for (int c = threadIdx.x / 64; c < min(WAVES * 32, s.n - key0) && blockIdx.y == 0; c += WAVES)
             for (int d = lane; d < g.dim; d += 64) {
                 const int64_t row = s.first + key0 + c;
-                if (g.out.p) *((T *)(g.out.p + row * g.out.row + kv * g.out.head) + d) = (T)0.0f;
-                if (g.out2.p) *((T *)(g.out2.p + row * g.out2.row + kv * g.out2.head) + d) = (T)0.0f;
+                if (DK && g.out.p) *((T *)(g.out.p + row * g.out.row + kv * g.out.head) + d) = (T)0.0f;
+                if (DV && g.out2.p) *((T *)(g.out2.p + row * g.out2.row + kv * g.out2.head) + d) = (T)0.0f;
             }
         return;
     }
@@ -907,11 +965,13 @@ __global__ __launch_bounds__(WAVES * 64, sizeof(T) == 2 && DB <= 4 ? 2 : 1) void
         const int at = c * 32 + h * 16;
         const bool here = at < g.bytes;
         if (!K_IN_LDS) k[K_IN_LDS ? 0 : c] = here ? *(const u32x4 *)(kp + at) : u32x4{0, 0, 0, 0};
-        v[c] = here ? *(const u32x4 *)(vp + at) : u32x4{0, 0, 0, 0};
+        if (DK) v[c] = here ? *(const u32x4 *)(vp + at) : u32x4{0, 0, 0, 0};
     }
+    if constexpr (!K_IN_LDS) settle(k);
+    if constexpr (DK) settle(v);
     f32x16 dk[DB], dv[DB];
-    clear(dk);
-    clear(dv);
+    if (DK) clear(dk);
+    if (DV) clear(dv);
     const typename R::Place place;
     float by = first_factor<T>();
     const int to = part.all - index * part.chunk, from = max(part.begin, to - part.chunk);
@@ -967,7 +1027,7 @@ __global__ __launch_bounds__(WAVES * 64, sizeof(T) == 2 && DB <= 4 ? 2 : 1) void
             } else {
                 along_product<R, T>(q_lds, place, 0, k, a);
             }
-            along_product<R, T>(dy_lds, place, 0, v, d);
+            if constexpr (DK) along_product<R, T>(dy_lds, place, 0, v, d);
             const float by_log = EXTRA ? 1.0f : g.scale * LOG2E;
             if constexpr (EXTRA) {
                 if (g.cap != 0.0f) {
@@ -1002,18 +1062,22 @@ __global__ __launch_bounds__(WAVES * 64, sizeof(T) == 2 && DB <= 4 ? 2 : 1) void
                 a[j] = __builtin_amdgcn_exp2f(fmaf(a[j], by_log, -info.lse[r]));
                 d[j] = a[j] * (EXTRA ? d[j] : d[j] - info.delta[r]);
             }
+            if constexpr (DV) {
 #pragma unroll
-            for (int t = 0; t < R::FRAGS; ++t) {
-                const u32x4 w = R::packed(a, t);
+                for (int t = 0; t < R::FRAGS; ++t) {
+                    const u32x4 w = R::packed(a, t);
 #pragma unroll
-                for (int b = 0; b < DB; ++b) dv[b] = mma32(R::across(dy_lds, place, 0, t, b * 32), w, dv[b], T{});
+                    for (int b = 0; b < DB; ++b) dv[b] = mma32(R::across(dy_lds, place, 0, t, b * 32), w, dv[b], T{});
+                }
             }
-            keep_in_range<T>(d, dk, by);
+            if constexpr (DK) {
+                keep_in_range<T>(d, dk, by);
 #pragma unroll
-            for (int t = 0; t < R::FRAGS; ++t) {
-                const u32x4 w = R::packed(d, t);
+                for (int t = 0; t < R::FRAGS; ++t) {
+                    const u32x4 w = R::packed(d, t);
 #pragma unroll
-                for (int b = 0; b < DB; ++b) dk[b] = mma32(R::across(q_lds, place, 0, t, b * 32), w, dk[b], T{});
+                    for (int b = 0; b < DB; ++b) dk[b] = mma32(R::across(q_lds, place, 0, t, b * 32), w, dk[b], T{});
+                }
             }
         }
         if (r0 > from) put(r0 - TILE, infos[here ^ 1]);
@@ -1023,12 +1087,59 @@ __global__ __launch_bounds__(WAVES * 64, sizeof(T) == 2 && DB <= 4 ? 2 : 1) void
     if (part.count > 1) {
         const int64_t at = ((int64_t)index * g.k_rows + row) * g.kv_heads + kv;
         const int wide = (g.dim & 3) == 0;
-        if (g.out.p) store_head<float, DB>((char *)(g.part + at * g.dim), dk, g.scale / by, g.dim, wide);
-        if (g.out2.p) store_head<float, DB>((char *)(g.part2 + at * g.dim), dv, 1.0f, g.dim, wide);
+        if constexpr (DK) if (g.out.p) store_head<float, DB>((char *)(g.part + at * g.dim), dk, g.scale / by, g.dim, wide);
+        if constexpr (DV) if (g.out2.p) store_head<float, DB>((char *)(g.part2 + at * g.dim), dv, 1.0f, g.dim, wide);
         return;
     }
-    if (g.out.p) store_head<T, DB>(g.out.p + row * g.out.row + kv * g.out.head, dk, g.scale / by, g.dim, g.wide);
-    if (g.out2.p) store_head<T, DB>(g.out2.p + row * g.out2.row + kv * g.out2.head, dv, 1.0f, g.dim, g.wide);
+    if constexpr (DK) if (g.out.p) store_head<T, DB>(g.out.p + row * g.out.row + kv * g.out.head, dk, g.scale / by, g.dim, g.wide);
+    if constexpr (DV) if (g.out2.p) store_head<T, DB>(g.out2.p + row * g.out2.row + kv * g.out2.head, dv, 1.0f, g.dim, g.wide);
+}
+
+// Rows of tiles whose keys went in several parts, eight a workgroup and a wave each: y and lse, each part brought to the common maximum, or (SUM) dq.  Four
+// elements a lane, the parts in their order.
+template <class T, bool SUM>
+__global__ __launch_bounds__(256) void attention_join_kernel(const AttentionArgs g, int tile)
+{
+    const int kv = (int)((blockIdx.x + g.before) % g.kv_heads), lane = threadIdx.x & 63;
+    const Share share(g, tile);
+    Span s = share.s;
+    if (s.seq >= g.seqs) return;
+    find_keys(g, s);
+    const int64_t items = (int64_t)g.rows * g.heads;
+    const int d = lane * 4, cnt = g.dim - d, wide = (g.dim & 3) == 0;
+    for (int r0 = share.begin; r0 < share.end; r0 += tile)
+    for (int r = r0 + blockIdx.y * 8 + (threadIdx.x >> 6); r < min(r0 + (int)blockIdx.y * 8 + 8, share.end); r += 4) {
+        s.r0 = r0;
+        const KeyParts part(g, s, tile);
+        if (part.count < 2) break;
+        const int64_t item = packed_item(g, s, kv, r);
+        float weight = 1.0f, sum = 1.0f, top = 0.0f;
+        if constexpr (!SUM) {
+            const float2 mine = lane < part.count ? g.stat[lane * items + item] : make_float2(-INFINITY, 0.0f);
+            top = mine.x;
+#pragma unroll
+            for (int off = 32; off; off >>= 1) top = fmaxf(top, __shfl_xor(top, off, 64));
+            weight = mine.y == 0.0f ? 0.0f : exp2f(mine.x - (top == -INFINITY ? 0.0f : top));
+            sum = mine.y * weight;
+#pragma unroll
+            for (int off = 32; off; off >>= 1) sum += __shfl_xor(sum, off, 64);
+        }
+        float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 4
+        for (int k = 0; k < part.count; ++k) {
+            const float w = SUM ? 1.0f : __shfl(weight, k, 64);
+            if (cnt <= 0) continue;
+            float one[4];
+            load_row<float>((const char *)g.part, (k * items + item) * g.dim + d, cnt, wide, one);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[j] += w == 0.0f ? 0.0f : w * one[j];
+        }
+        const float by = sum == 0.0f ? 0.0f : 1.0f / sum;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] *= by;
+        if (cnt > 0) store_row<T>((char *)packed_row(g, g.out, s, kv, r), d, cnt, g.wide, v);
+        if (!SUM && g.lse && lane == 0) g.lse[item] = sum == 0.0f ? -INFINITY : (top + log2f(sum)) * LN2;
+    }
 }
 
 // dk and dv of tiles whose rows went in several parts, which are added in their order: four elements a thread, sixteen keys a workgroup.
@@ -1077,29 +1188,52 @@ hipError_t in_launches(const AttentionArgs &g, int64_t workgroups, Launch launch
     return hipSuccess;
 }
 
-template <class T, int DB, bool EXTRA>
-hipError_t launch_rows(hipStream_t st, int few, const AttentionArgs &g)
+template <class T, bool SUM>
+hipError_t launch_join(hipStream_t st, int few, const AttentionArgs &g)
 {
-    if (few)
-        return in_launches(g, (g.tiles ? g.tiles : (int64_t)g.seqs + 1) * g.kv_heads, [&](const AttentionArgs &p, dim3 grid) {
-            attention_few_kernel<T, DB, EXTRA><<<grid, FewShape<T, DB>::WAVES * 64, 0, st>>>(p);
-        });
-    return in_launches(g, (int64_t)g.tiles * g.kv_heads, [&](const AttentionArgs &p, dim3 grid) { attention_kernel<T, DB, EXTRA, 4><<<grid, 256, 0, st>>>(p); });
+    const int tile = few ? FEW_TILE : ATTENTION_TILE;
+    return in_launches(g, (g.tiles ? g.tiles : (int64_t)g.seqs) * g.kv_heads,
+                       [&](const AttentionArgs &p, dim3 grid) { attention_join_kernel<T, SUM><<<dim3(grid.x, tile / 8), 256, 0, st>>>(p, tile); });
+}
+// keys of a step of the kernels of rows
+template <class T, int DB>
+AttentionArgs with_unit(int few, AttentionArgs g)
+{
+    g.unit = few ? 32 * FewShape<T, DB>::WAVES : 64;
+    return g;
 }
 template <class T, int DB, bool EXTRA>
-hipError_t launch_dq(hipStream_t st, int few, const AttentionArgs &g)
+hipError_t launch_rows(hipStream_t st, int few, const AttentionArgs &args)
 {
-    if (few)
-        return in_launches(g, (int64_t)g.tiles * g.kv_heads, [&](const AttentionArgs &p, dim3 grid) {
-            attention_dq_few_kernel<T, DB, EXTRA><<<grid, FewShape<T, DB>::WAVES * 64, 0, st>>>(p);
-        });
-    return in_launches(g, (int64_t)g.tiles * g.kv_heads, [&](const AttentionArgs &p, dim3 grid) { attention_dq_kernel<T, DB, EXTRA, 4><<<grid, 256, 0, st>>>(p); });
+    const AttentionArgs g = with_unit<T, DB>(few, args);
+    const hipError_t e = in_launches(g, (g.tiles ? g.tiles : (int64_t)g.seqs + 1) * g.kv_heads, [&](const AttentionArgs &p, dim3 grid) {
+        if (few) attention_few_kernel<T, DB, EXTRA><<<grid, FewShape<T, DB>::WAVES * 64, 0, st>>>(p);
+        else attention_kernel<T, DB, EXTRA, 4><<<grid, 256, 0, st>>>(p);
+    });
+    return e != hipSuccess || g.splits == 1 ? e : launch_join<T, false>(st, few, g);
+}
+template <class T, int DB, bool EXTRA>
+hipError_t launch_dq(hipStream_t st, int few, const AttentionArgs &args)
+{
+    const AttentionArgs g = with_unit<T, DB>(few, args);
+    const hipError_t e = in_launches(g, (int64_t)g.tiles * g.kv_heads, [&](const AttentionArgs &p, dim3 grid) {
+        if (few) attention_dq_few_kernel<T, DB, EXTRA><<<grid, FewShape<T, DB>::WAVES * 64, 0, st>>>(p);
+        else attention_dq_kernel<T, DB, EXTRA, 4><<<grid, 256, 0, st>>>(p);
+    });
+    return e != hipSuccess || g.splits == 1 || !g.out.p ? e : launch_join<T, true>(st, few, g);
 }
 template <class T, int DB, bool EXTRA>
 hipError_t launch_dkv(hipStream_t st, const AttentionArgs &g)
 {
     const int64_t tiles = (int64_t)g.tiles * g.kv_heads;
-    const hipError_t e = in_launches(g, tiles, [&](const AttentionArgs &p, dim3 grid) { attention_dkv_kernel<T, DB, EXTRA, 4><<<grid, 256, 0, st>>>(p); });
+    const hipError_t e = in_launches(g, tiles, [&](const AttentionArgs &p, dim3 grid) {
+        if constexpr (DB <= 4) {
+            attention_dkv_kernel<T, DB, EXTRA, 4, true, true><<<grid, 256, 0, st>>>(p);
+        } else {
+            if (p.out.p) attention_dkv_kernel<T, DB, EXTRA, 4, true, false><<<grid, 256, 0, st>>>(p);
+            if (p.out2.p) attention_dkv_kernel<T, DB, EXTRA, 4, false, true><<<grid, 256, 0, st>>>(p);
+        }
+    });
     if (e != hipSuccess || g.splits == 1) return e;
     return in_launches(g, tiles, [&](const AttentionArgs &p, dim3 grid) { attention_sum_kernel<T><<<dim3(grid.x, 2 * ATTENTION_TILE / 16), 256, 0, st>>>(p); });
 }

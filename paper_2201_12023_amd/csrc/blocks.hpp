@@ -23,10 +23,11 @@ struct AttentionArgs {
     float scale, cap, twice;        // twice: 2 scale / cap, times the binary logarithm of e
     int tiles;                      // grid: row tiles of all sequences, at most
     uint32_t before;                // of the grid, workgroups of earlier launches
-    int splits;                     // of the keys (forward), of the rows (dk, dv)
-    float *part;                    // splits > 1: [split][item][dim] sums, forward: and
-    float2 *stat;                   // [split][item] (maximum, sum); items: rows x heads, or key rows x kv heads
-    float *part2;
+    int unit;                       // keys of a step: what parts of them are multiples of
+    int splits;                     // parts, at most, of the keys (y, dq) or of the rows (dk, dv)
+    float *part;                    // splits > 1: [part][item][dim] sums, of dk or else; items: rows x heads, or key rows x kv heads
+    float2 *stat;                   // forward: [part][item] (maximum, sum)
+    float *part2;                   // of dv
 };
 
 constexpr int ATTENTION_TILE = 128, FEW_TILE = 32;     // packed rows, or keys, of a workgroup
@@ -43,8 +44,6 @@ ALPA_ATTENTION_LAUNCHES(bf16)
 // rows of a head's dim padded to blocks of 32, as the kernels are compiled for them: 2, 3, 4 or 8
 inline int dim_blocks(int dim) { return dim <= 64 ? 2 : dim <= 96 ? 3 : dim <= 128 ? 4 : 8; }
 
-// y and lse from the parts of the keys
-hipError_t launch_attention_join(hipStream_t st, int dtype, const AttentionArgs &a);
 
 // Copies tensors to [rows][heads][to_len] elements (a multiple of 16 bytes), zeros behind len.
 struct HeadPack {

@@ -1,4 +1,4 @@
-// The kernels between a block's products beside attention itself: joins of attention's parts, copies to aligned memory, rotary positions, layer norm.
+// The kernels between a block's products beside attention itself: copies to aligned memory, rotary positions, layer norm.
 #include "blocks.hpp"
 #include "epilogue.hpp"
 
@@ -15,49 +15,6 @@ hipError_t by_type(int dtype, Call call)
 
 // (a grid's threads are counted in 32 bits)
 unsigned blocks_for(int64_t work, int64_t most) { return (unsigned)std::max<int64_t>(std::min(work, most), 1); }
-
-// ---------------------------------------------------------------- attention's parts
-
-// A wave an item, four elements a lane; the parts are added in their order, each brought to the common maximum.
-template <class T>
-__global__ __launch_bounds__(256) void attention_join_kernel(const AttentionArgs g)
-{
-    const int64_t items = (int64_t)g.rows * g.heads;
-    const int lane = threadIdx.x & 63;
-    for (int64_t item = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); item < items; item += (int64_t)gridDim.x * 4) {
-        const float2 none = make_float2(-INFINITY, 0.0f), mine = lane < g.splits ? g.stat[lane * items + item] : none;
-        float top = mine.x;
-#pragma unroll
-        for (int off = 32; off; off >>= 1) top = fmaxf(top, __shfl_xor(top, off, 64));
-        const float weight = mine.y == 0.0f ? 0.0f : exp2f(mine.x - (top == -INFINITY ? 0.0f : top));
-        float sum = mine.y * weight;
-#pragma unroll
-        for (int off = 32; off; off >>= 1) sum += __shfl_xor(sum, off, 64);
-        const int d = lane * 4, cnt = g.dim - d, wide = (g.dim & 3) == 0;
-        float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-        for (int s = 0; s < g.splits; ++s) {
-            const float w = __shfl(weight, s, 64);
-            if (w == 0.0f || cnt <= 0) continue;
-            float part[4];
-            load_row<float>((const char *)g.part, (s * items + item) * g.dim + d, cnt, wide, part);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) v[j] += w * part[j];
-        }
-        const float by = sum == 0.0f ? 0.0f : 1.0f / sum;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) v[j] *= by;
-        const int64_t row = item / g.heads;
-        const int head = (int)(item - row * g.heads);
-        if (cnt > 0) store_row<T>(g.out.p + row * g.out.row + head * g.out.head, d, cnt, g.wide, v);
-        if (g.lse && lane == 0) g.lse[item] = sum == 0.0f ? -INFINITY : (top + log2f(sum)) * 0.69314718055994531f;
-    }
-}
-
-hipError_t launch_attention_join(hipStream_t st, int dtype, const AttentionArgs &g)
-{
-    const unsigned blocks = blocks_for(((int64_t)g.rows * g.heads + 3) / 4, 1 << 20);
-    return by_type(dtype, [&](auto t) { attention_join_kernel<decltype(t)><<<blocks, 256, 0, st>>>(g); });
-}
 
 // ---------------------------------------------------------------- heads in 16-byte units
 
