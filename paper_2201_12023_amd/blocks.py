@@ -70,6 +70,35 @@ def load():
 _NONE = alpa_heads_t(None, 0, 0)
 
 
+def _on(call, x, stream, *args):
+    """``call`` with the stream's handle and ``args``, the tensors' device and the stream being torch's current ones.  (Calls of a few microseconds of the GPU's
+    time wait for the host: nothing is done here that would not change anything.)"""
+    device = x.device
+    _l._type(x)
+    if stream is None and device.type == "cuda" and device.index == torch.cuda.current_device():
+        return call(torch._C._cuda_getCurrentRawStream(device.index), *args)
+    with _l._On(x, stream) as s:
+        return call(s, *args)
+
+
+def _vec(name, t, shape, dtype, device):
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.device != device or t.shape != shape or not t.is_contiguous():
+        return _l._vec(name, t, shape, dtype, device)              # (which says what is wrong)
+    return t.data_ptr()
+
+
+def _mat(name, t, shape, dtype, device):
+    if t.dtype is not dtype or t.device != device or t.shape != shape or not t.is_contiguous():
+        return _l._mat(name, t, shape, dtype, device)
+    return _l.alpa_mat_t(t.data_ptr(), shape[1])
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
 def _three(name, x):
     if x.dim() != 3:
         raise ValueError(f"{name} must have three dimensions, not {x.dim()}")
@@ -78,10 +107,12 @@ def _three(name, x):
 
 def _heads(name, t, shape, dtype, device):
     """A tensor [rows, heads, dim] as the library takes it."""
-    _l._check(name, t, shape, dtype, device)
-    if shape[2] > 1 and t.stride(2) != 1:
-        raise ValueError(f"{name} must have contiguous heads; strides are {tuple(t.stride())}")
-    return alpa_heads_t(t.data_ptr(), t.stride(0), t.stride(1))
+    if t.dtype is not dtype or t.device != device or t.shape != shape:
+        _l._check(name, t, shape, dtype, device)
+    row, head, one = t.stride()
+    if one != 1 and shape[2] > 1:
+        raise ValueError(f"{name} must have contiguous heads; strides are {(row, head, one)}")
+    return alpa_heads_t(t.data_ptr(), row, head)
 
 
 def _new(t):
@@ -103,22 +134,27 @@ def _how(q, k, offsets, k_offsets, scale, cap, slopes, causal, prefix):
         k_offsets = offsets
     pairs = k_offsets is not None and k_offsets.dim() == 2
     a = alpa_attention_t(_l._type(q), seqs, heads, kv_heads, dim, bool(causal), 2 if pairs else 1, dim ** -0.5 if scale is None else scale, cap,
-                         rows, k_rows, _l._vec("offsets", offsets, (seqs + 1,), ints, device),
-                         _l._vec("k_offsets", k_offsets, (seqs, 2) if pairs else (seqs + 1,), ints, device),
-                         _l._vec("prefix", prefix, (seqs,), ints, device), _l._vec("slopes", slopes, (heads,), torch.float32, device))
+                         rows, k_rows, _vec("offsets", offsets, (seqs + 1,), ints, device),
+                         _vec("k_offsets", k_offsets, (seqs, 2) if pairs else (seqs + 1,), ints, device), _vec("prefix", prefix, (seqs,), ints, device),
+                         _vec("slopes", slopes, (heads,), torch.float32, device))
     return a
 
 
 def _attention(q, k, v, offsets, k_offsets, scale, cap, slopes, causal, prefix, keep_lse, stream):
-    L = load()
-    with _l._On(q, stream) as s:
-        a = _how(q, k, offsets, k_offsets, scale, cap, slopes, causal, prefix)
-        shape = (a.k_rows, a.kv_heads, a.dim)
-        qm, km, vm = _heads("q", q, q.shape, q.dtype, q.device), _heads("k", k, shape, q.dtype, q.device), _heads("v", v, shape, q.dtype, q.device)
-        y = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device) if keep_lse else None
-        held, p, n = _l._work(L.alpa_attention_forward_work(a, qm, km, vm), q.device)
-        binding._check(L.alpa_attention_forward(a, qm, km, vm, _new(y), None if lse is None else lse.data_ptr(), p, n, s))
+    return _on(_attention_on, q, stream, q, k, v, offsets, k_offsets, scale, cap, slopes, causal, prefix, keep_lse)
+
+
+def _attention_on(s, q, k, v, offsets, k_offsets, scale, cap, slopes, causal, prefix, keep_lse):
+    L = _ready or load()
+    a = _how(q, k, offsets, k_offsets, scale, cap, slopes, causal, prefix)
+    shape, dtype, device = k.shape, q.dtype, q.device
+    if shape[2] != a.dim:
+        raise ValueError(f"k has heads of {shape[2]} elements, q of {a.dim}")
+    qm, km, vm = _heads("q", q, q.shape, dtype, device), _heads("k", k, shape, dtype, device), _heads("v", v, shape, dtype, device)
+    y = q.new_empty(q.shape)
+    lse = q.new_empty(q.shape[:2], dtype=torch.float32) if keep_lse else None
+    held, p, n = _l._work(L.alpa_attention_forward_work(a, qm, km, vm), device)
+    binding._check(L.alpa_attention_forward(a, qm, km, vm, _new(y), _ptr(lse), p, n, s))
     return (y, lse) if keep_lse else y
 
 
@@ -168,21 +204,23 @@ def alpa_attention_forward(q, k, v, offsets=None, k_offsets=None, scale=None, ca
 def alpa_attention_backward(dy, q, k, v, y, lse, offsets=None, k_offsets=None, scale=None, cap=0.0, slopes=None, causal=False, prefix=None,
                             need=("q", "k", "v"), stream=None):
     """(dq, dk, dv) of alpa_attention_forward, None for those not in ``need``; y and lse are its results."""
-    L = load()
     if not set(need) <= {"q", "k", "v"}:
         raise ValueError(f"need is {need!r}: names out of 'q', 'k', 'v' expected")
     if k_offsets is not None and k_offsets.dim() == 2:
         raise ValueError("keys that are not packed have no gradient")
-    with _l._On(q, stream) as s:
-        a = _how(q, k, offsets, k_offsets, scale, cap, slopes, causal, prefix)
-        shape, dtype, device = (a.k_rows, a.kv_heads, a.dim), q.dtype, q.device
-        mats = [_heads(name, t, size, dtype, device) for name, t, size in (("dy", dy, q.shape), ("q", q, q.shape), ("k", k, shape), ("v", v, shape),
-                                                                           ("y", y, q.shape))]
-        l = _l._vec("lse", lse, q.shape[:2], torch.float32, device)
-        dq, dk, dv = (torch.empty(size, dtype=dtype, device=device) if name in need else None
-                      for name, size in (("q", q.shape), ("k", shape), ("v", shape)))
-        held, p, n = _l._work(L.alpa_attention_backward_work(a, *mats), device)
-        binding._check(L.alpa_attention_backward(a, *mats, l, _new(dq), _new(dk), _new(dv), p, n, s))
+    return _on(_attention_backward_on, q, stream, dy, q, k, v, y, lse, offsets, k_offsets, scale, cap, slopes, causal, prefix, need)
+
+
+def _attention_backward_on(s, dy, q, k, v, y, lse, offsets, k_offsets, scale, cap, slopes, causal, prefix, need):
+    L = _ready or load()
+    a = _how(q, k, offsets, k_offsets, scale, cap, slopes, causal, prefix)
+    shape, dtype, device = (a.k_rows, a.kv_heads, a.dim), q.dtype, q.device
+    mats = [_heads(name, t, size, dtype, device) for name, t, size in (("dy", dy, q.shape), ("q", q, q.shape), ("k", k, shape), ("v", v, shape),
+                                                                       ("y", y, q.shape))]
+    l = _vec("lse", lse, q.shape[:2], torch.float32, device)
+    dq, dk, dv = (q.new_empty(size) if name in need else None for name, size in (("q", q.shape), ("k", shape), ("v", shape)))
+    held, p, n = _l._work(L.alpa_attention_backward_work(a, *mats), device)
+    binding._check(L.alpa_attention_backward(a, *mats, l, _new(dq), _new(dk), _new(dv), p, n, s))
     return dq, dk, dv
 
 
@@ -198,15 +236,17 @@ def alpa_rotary_frequencies(rot, base=10000.0, factor=1.0, context=0.0, low=1.0,
 
 
 def _rotary(name, x, positions, frequencies, interleaved, scale, out, stream):
-    L = load()
-    rows, heads, dim = _three("x", x)
-    with _l._On(x, stream) as s:
-        xm = _heads("x", x, x.shape, x.dtype, x.device)
-        p = _l._vec("positions", positions, (rows,), torch.int64, x.device)
-        f = _l._vec("frequencies", frequencies, (frequencies.numel(),), torch.float64, x.device)
-        y = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else out
-        ym = _new(y) if out is None else _heads("out", out, x.shape, x.dtype, x.device)
-        binding._check(getattr(L, name)(_l._type(x), rows, heads, dim, 2 * frequencies.numel(), interleaved, scale, p, f, xm, ym, s))
+    return _on(_rotary_on, x, stream, name, x, positions, frequencies, interleaved, scale, out)
+
+
+def _rotary_on(s, name, x, positions, frequencies, interleaved, scale, out):
+    L = _ready or load()
+    shape, dtype, device = _three("x", x), x.dtype, x.device
+    xm, half = _heads("x", x, shape, dtype, device), frequencies.numel()
+    p, f = _vec("positions", positions, shape[:1], torch.int64, device), _vec("frequencies", frequencies, (half,), torch.float64, device)
+    y = x.new_empty(shape) if out is None else out
+    ym = _new(y) if out is None else _heads("out", out, shape, dtype, device)
+    binding._check(getattr(L, name)(_l._type(x), *shape, 2 * half, interleaved, scale, p, f, xm, ym, s))
     return y
 
 
@@ -243,16 +283,16 @@ def alpa_rotary_backward(dy, positions, frequencies, interleaved=False, scale=1.
 # ------------------------------------------------------------------ layer norm
 
 def _norm(x, weight, bias, eps, keep, stream):
-    L, d = load(), _l._type(x)
-    rows, n = _l._two("x", x)
-    dtype, device = x.dtype, x.device
-    with _l._On(x, stream) as s:
-        xm = _l._mat("x", x, (rows, n), dtype, device)
-        w, b = _l._vec("weight", weight, (n,), dtype, device), _l._vec("bias", bias, (n,), dtype, device)
-        y = torch.empty((rows, n), dtype=dtype, device=device)
-        mean, rstd = (torch.empty((rows,), dtype=torch.float32, device=device) if keep else None for _ in range(2))
-        ptr = lambda t: None if t is None else t.data_ptr()
-        binding._check(L.alpa_norm_forward(d, rows, n, eps, xm, w, b, _l._new(y), ptr(mean), ptr(rstd), s))
+    return _on(_norm_on, x, stream, x, weight, bias, eps, keep)
+
+
+def _norm_on(s, x, weight, bias, eps, keep):
+    L = _ready or load()
+    shape, dtype, device = _l._two("x", x), x.dtype, x.device
+    xm, w, b = _mat("x", x, shape, dtype, device), _vec("weight", weight, shape[1:], dtype, device), _vec("bias", bias, shape[1:], dtype, device)
+    y = x.new_empty(shape)
+    mean, rstd = (x.new_empty(shape[:1], dtype=torch.float32) for _ in range(2)) if keep else (None, None)
+    binding._check(L.alpa_norm_forward(_l._type(x), *shape, eps, xm, w, b, _l._new(y), _ptr(mean), _ptr(rstd), s))
     return (y, mean, rstd) if keep else y
 
 
@@ -286,18 +326,19 @@ def alpa_norm_forward(x, weight=None, bias=None, eps=1e-5, keep=False, stream=No
 
 def alpa_norm_backward(dy, x, mean, rstd, weight=None, need=("x", "weight", "bias"), stream=None):
     """(dx, dweight, dbias) of alpa_norm_forward, None for those not in ``need``."""
-    L, d = load(), _l._type(x)
     if not set(need) <= {"x", "weight", "bias"}:
         raise ValueError(f"need is {need!r}: names out of 'x', 'weight', 'bias' expected")
-    rows, n = _l._two("x", x)
-    dtype, device = x.dtype, x.device
-    with _l._On(x, stream) as s:
-        dym, xm = _l._mat("dy", dy, (rows, n), dtype, device), _l._mat("x", x, (rows, n), dtype, device)
-        m, r = (_l._vec(k, t, (rows,), torch.float32, device) for k, t in (("mean", mean), ("rstd", rstd)))
-        w = _l._vec("weight", weight, (n,), dtype, device)
-        dx = torch.empty((rows, n), dtype=dtype, device=device) if "x" in need else None
-        dw, db = (torch.empty((n,), dtype=dtype, device=device) if name in need else None for name in ("weight", "bias"))
-        ptr = lambda t: None if t is None else t.data_ptr()
-        held, p, size = _l._work(L.alpa_norm_backward_work(d, rows, n), device)
-        binding._check(L.alpa_norm_backward(d, rows, n, dym, xm, m, r, w, _l._new(dx), ptr(dw), ptr(db), p, size, s))
+    return _on(_norm_backward_on, x, stream, dy, x, mean, rstd, weight, need)
+
+
+def _norm_backward_on(s, dy, x, mean, rstd, weight, need):
+    L, d = _ready or load(), _l._type(x)
+    shape, dtype, device = _l._two("x", x), x.dtype, x.device
+    dym, xm = _mat("dy", dy, shape, dtype, device), _mat("x", x, shape, dtype, device)
+    m, r = _vec("mean", mean, shape[:1], torch.float32, device), _vec("rstd", rstd, shape[:1], torch.float32, device)
+    w = _vec("weight", weight, shape[1:], dtype, device)
+    dx = x.new_empty(shape) if "x" in need else None
+    dw, db = (x.new_empty(shape[1:]) if name in need else None for name in ("weight", "bias"))
+    held, p, size = _l._work(L.alpa_norm_backward_work(d, *shape), device)
+    binding._check(L.alpa_norm_backward(d, *shape, dym, xm, m, r, w, _l._new(dx), _ptr(dw), _ptr(db), p, size, s))
     return dx, dw, db

@@ -265,7 +265,7 @@ int rotary(int dtype, int64_t rows, int heads, int dim, int rot, int interleaved
     TRY(check_heads(y, rows, heads, dim, dtype, true, false, "y or dx is null"));
     const bool in_place = x.p == y.p;
     if (in_place && (x.row != y.row || x.head != y.head)) return fail(ALPA_DP_EINVAL, "turned in place, x and y need the same strides");
-    const int64_t es = element(dtype), unit = 16 / es;
+    const int64_t es = element(dtype);
     RotaryArgs g{};
     g.x = Heads{(char *)x.p, x.row, x.head};
     g.y = Heads{(char *)y.p, y.row, y.head};
@@ -279,8 +279,11 @@ int rotary(int dtype, int64_t rows, int heads, int dim, int rot, int interleaved
     g.sign = sign;
     g.positions = positions;
     g.frequencies = frequencies;
-    // sixteen bytes at once: of halves each starts and ends there, of interleaved pairs the whole does, and so does what is copied
-    g.wide = wide_heads(x, dtype, 16) && wide_heads(y, dtype, 16) && (interleaved ? rot : rot / 2) % unit == 0 && (!g.copy || dim % unit == 0);
+    // bytes at once: of halves each starts and ends at a multiple of them, of interleaved pairs the whole does, and so does what is copied
+    const auto fits = [&](int64_t b) {
+        return wide_heads(x, dtype, b) && wide_heads(y, dtype, b) && (interleaved ? rot : rot / 2) * es % b == 0 && (!g.copy || dim * es % b == 0);
+    };
+    g.wide = fits(16) ? 16 : fits(8) ? 8 : 0;
     HIPCHK(launch_rotary(st, dtype, g));
     return ALPA_DP_OK;
 }

@@ -346,15 +346,17 @@ __device__ __forceinline__ int64_t packed_item(const AttentionArgs &g, const Spa
     return (int64_t)(s.first + i) * g.heads + kv * g.group + r - i * g.group;
 }
 
-// 32 results of one row or key, times `by`, as a lane holds them of each block; `at` the head's first element
-template <class T, int DB>
+// The results of one row or key, times `by`, as a lane holds them of each block; `at` the head's first element.  With several waves that have the same rows
+// (WAVES) each writes every so-many-th block.
+template <class T, int DB, int WAVES = 1>
 __device__ __forceinline__ void store_head(char *at, const f32x16 (&acc)[DB], float by, int dim, int wide)
 {
-    const int h = threadIdx.x >> 5 & 1;
+    const int h = threadIdx.x >> 5 & 1, wave = WAVES > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0;
 #pragma unroll
     for (int b = 0; b < DB; ++b)
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
+            if (WAVES > 1 && b % WAVES != wave) continue;
             const int d = b * 32 + j * 8 + h * 4;
             const float v[4] = {acc[b][4 * j] * by, acc[b][4 * j + 1] * by, acc[b][4 * j + 2] * by, acc[b][4 * j + 3] * by};
             if (d < dim) store_row<T>(at, d, dim - d, wide, v);
@@ -470,20 +472,21 @@ struct Running {
     }
 
     // y and lse, or this part of them
+    template <int WAVES = 1>
     __device__ __forceinline__ void end(const AttentionArgs &g, const Span &s, int kv, int r, int part, int parts)
     {
         const float all = sum + other_half(sum);
         if (r >= s.n * g.group) return;
         const int64_t item = packed_item(g, s, kv, r);
-        const bool first = (threadIdx.x & 32) == 0;
+        const bool first = (threadIdx.x & (WAVES > 1 ? ~31u : 32u)) == 0;
         if (parts > 1) {
             const int64_t at = (int64_t)part * g.rows * g.heads + item;
-            store_head<float, DB>((char *)(g.part + at * g.dim), y, 1.0f, g.dim, (g.dim & 3) == 0);
+            store_head<float, DB, WAVES>((char *)(g.part + at * g.dim), y, 1.0f, g.dim, (g.dim & 3) == 0);
             if (first) g.stat[at] = make_float2(top, all);
             return;
         }
         char *out = (char *)packed_row(g, g.out, s, kv, r);
-        store_head<T, DB>(out, y, all == 0.0f ? 0.0f : 1.0f / all, g.dim, g.wide);
+        store_head<T, DB, WAVES>(out, y, all == 0.0f ? 0.0f : 1.0f / all, g.dim, g.wide);
         if (g.lse && first) g.lse[item] = all == 0.0f ? -INFINITY : (top + log2f(all)) * LN2;
     }
 };
@@ -533,10 +536,6 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attention_kernel(const Attentio
     const int index = g.splits - 1 - (int)blockIdx.y, from = index * part.chunk, to = min(from + part.chunk, part.most);
     if (index >= part.count) return;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = s.r0 + wave * 32 + (threadIdx.x & 31);
-    Running<T, DB, EXTRA> run;
-    run.begin(g, s, kv, r);
-    const typename R::Place place;
-    const int mine = __builtin_amdgcn_readlane(run.limit, 31);
     const KeyLoader<R, KEYS, NT> k(g.k.p + (int64_t)s.k_first * g.k.row + (int64_t)kv * g.k.head, g.k.row, g.bytes);
     const KeyLoader<R, KEYS, NT> v(g.v.p + (int64_t)s.k_first * g.v.row + (int64_t)kv * g.v.head, g.v.row, g.bytes);
     uint32_t here = 0;
@@ -544,6 +543,10 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attention_kernel(const Attentio
         k.load(lds_at(lds), from, s.m);
         v.load(lds_at(lds) + HALF, from, s.m);
     }
+    Running<T, DB, EXTRA> run;
+    run.begin(g, s, kv, r);
+    const typename R::Place place;
+    const int mine = __builtin_amdgcn_readlane(run.limit, 31);
     for (int j0 = from; j0 < to; j0 += KEYS, here ^= 2 * HALF) {
         arrived<0>();
         if (j0 + KEYS < to) {
@@ -592,23 +595,28 @@ struct FewShape {
     static constexpr int WAVES = R::ROWB <= 256 ? 4 : R::ROWB == 512 ? 2 : 1, SHARE = 32 * R::ROWB;          // (two tiles of keys and two of values a wave)
 };
 
-// Adds up the waves' blocks, each times `by`, a block at a time: 4 KB a wave.  What was in LDS has been read.
+// Adds up the waves' blocks, each times `by`: a wave has every so-many-th one then.  What was in LDS has been read; the sums' 16 KB a wave for heads of 128 lie in the
+// room of the tiles.
 template <int WAVES, int DB>
 __device__ __forceinline__ void join_waves(char *lds, f32x16 (&acc)[DB], float by)
 {
-    float *const all = (float *)lds + (threadIdx.x & 63), *const mine = all + (threadIdx.x >> 6) * 1024;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    f32x4 *const all = (f32x4 *)lds + (threadIdx.x & 63), *const mine = all + wave * DB * 256;
+#pragma unroll
+    for (int b = 0; b < DB; ++b)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) mine[(b * 4 + i) * 64] = f32x4{acc[b][4 * i] * by, acc[b][4 * i + 1] * by, acc[b][4 * i + 2] * by, acc[b][4 * i + 3] * by};
+    __syncthreads();
 #pragma unroll
     for (int b = 0; b < DB; ++b) {
-        __syncthreads();
+        if (b % WAVES != wave) continue;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) mine[i * 64] = acc[b][i] * by;
-        __syncthreads();
+        for (int i = 0; i < 4; ++i) {
+            f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            float v = 0.0f;
+            for (int w = 0; w < WAVES; ++w) v += all[(w * DB * 4 + b * 4 + i) * 64];
 #pragma unroll
-            for (int w = 0; w < WAVES; ++w) v += all[w * 1024 + i * 64];
-            acc[b][i] = v;
+            for (int j = 0; j < 4; ++j) acc[b][4 * i + j] = v[j];
         }
     }
 }
@@ -641,8 +649,6 @@ __global__ __launch_bounds__((FewShape<T, DB>::WAVES * 64)) void attention_few_k
         const KeyParts part(g, s, 32);
         const int index = g.splits - 1 - (int)blockIdx.y, from = index * part.chunk, to = min(from + part.chunk, part.most);
         if (index >= part.count) continue;
-        Running<T, DB, EXTRA> run;
-        run.begin(g, s, kv, r);
         // each wave waits for its own loads alone
         const int j1 = from + wave * 32;
         uint32_t here = 0;
@@ -651,6 +657,8 @@ __global__ __launch_bounds__((FewShape<T, DB>::WAVES * 64)) void attention_few_k
             k.load(mine, j1, s.m);
             v.load(mine + F::SHARE, j1, s.m);
         }
+        Running<T, DB, EXTRA> run;
+        run.begin(g, s, kv, r);
         for (int j0 = j1; j0 < to; j0 += 32 * WAVES, here ^= 2 * F::SHARE) {
             asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
             if (j0 + 32 * WAVES < to) {
@@ -679,7 +687,7 @@ __global__ __launch_bounds__((FewShape<T, DB>::WAVES * 64)) void attention_few_k
             run.top = top;
             run.sum = (threadIdx.x & 32) ? 0.0f : total;
         }
-        if (wave == 0) run.end(g, s, kv, r, index, part.count);
+        run.template end<WAVES>(g, s, kv, r, index, part.count);
     }
 }
 
@@ -745,8 +753,7 @@ struct Backward {
     float delta, lse, slope, by;
     int limit, where;
 
-    // false: dq is not wanted
-    __device__ __forceinline__ bool begin(const AttentionArgs &g, const Span &s, int kv, int r)
+    __device__ __forceinline__ void begin(const AttentionArgs &g, const Span &s, int kv, int r)
     {
         const int h = threadIdx.x >> 5 & 1, i = min(r, s.n * g.group - 1);          // (of several parts each puts down the sum of dy y, the same bits)
         const char *qp = packed_row(g, g.q, s, kv, i), *dp = packed_row(g, g.dy, s, kv, i), *yp = packed_row(g, g.y, s, kv, i);
@@ -777,7 +784,6 @@ struct Backward {
         by = first_factor<T>();
         asm volatile("" ::"v"(lse), "v"(slope));
         clear(dq);
-        return g.out.p != nullptr;
     }
 
     // 32 keys from j0 on, in LDS from row `at` on
@@ -829,11 +835,12 @@ struct Backward {
         }
     }
 
+    template <int WAVES = 1>
     __device__ __forceinline__ void end(const AttentionArgs &g, const Span &s, int kv, int r, float scale, int part, int parts)
     {
         if (r >= s.n * g.group) return;
-        if (parts > 1) store_head<float, DB>((char *)(g.part + ((int64_t)part * g.rows * g.heads + packed_item(g, s, kv, r)) * g.dim), dq, scale, g.dim, (g.dim & 3) == 0);
-        else store_head<T, DB>((char *)packed_row(g, g.out, s, kv, r), dq, scale, g.dim, g.wide);
+        if (parts > 1) store_head<float, DB, WAVES>((char *)(g.part + ((int64_t)part * g.rows * g.heads + packed_item(g, s, kv, r)) * g.dim), dq, scale, g.dim, (g.dim & 3) == 0);
+        else store_head<T, DB, WAVES>((char *)packed_row(g, g.out, s, kv, r), dq, scale, g.dim, g.wide);
     }
 };
 
@@ -855,17 +862,19 @@ __global__ __launch_bounds__(WAVES * 64, sizeof(T) == 2 && DB <= 4 ? 2 : 1) void
     const int index = g.splits - 1 - (int)blockIdx.y, from = index * part.chunk, to = min(from + part.chunk, part.most);
     if (index >= part.count) return;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = s.r0 + wave * 32 + (lane & 31);
-    Backward<T, DB, EXTRA> run;
-    if (!run.begin(g, s, kv, r)) return;
-    const int mine = __builtin_amdgcn_readlane(run.limit, 31);
-    const typename R::Place place;
     const KeyLoader<R, KEYS, NT> k(g.k.p + (int64_t)s.k_first * g.k.row + (int64_t)kv * g.k.head, g.k.row, g.bytes);
     const KeyLoader<R, KEYS, NT> v(g.v.p + (int64_t)s.k_first * g.v.row + (int64_t)kv * g.v.head, g.v.row, g.bytes);
     uint32_t here = 0;
-    if (from < to) {
+    const bool wanted = g.out.p != nullptr;
+    if (wanted && from < to) {
         k.load(lds_at(lds), from, s.m);
         v.load(lds_at(lds) + HALF, from, s.m);
     }
+    Backward<T, DB, EXTRA> run;
+    run.begin(g, s, kv, r);
+    if (!wanted) return;
+    const int mine = __builtin_amdgcn_readlane(run.limit, 31);
+    const typename R::Place place;
     for (int j0 = from; j0 < to; j0 += KEYS, here ^= 2 * HALF) {
         arrived<0>();
         if (j0 + KEYS < to) {
@@ -898,17 +907,19 @@ __global__ __launch_bounds__((FewShape<T, DB>::WAVES * 64)) void attention_dq_fe
     const int index = g.splits - 1 - (int)blockIdx.y, from = index * part.chunk, to = min(from + part.chunk, part.most);
     if (index >= part.count) return;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = s.r0 + (lane & 31);
-    Backward<T, DB, EXTRA> run;
-    if (!run.begin(g, s, kv, r)) return;
-    const typename R::Place place;
     const KeyLoader<R, 32, 64> k(g.k.p + (int64_t)s.k_first * g.k.row + (int64_t)kv * g.k.head, g.k.row, g.bytes);
     const KeyLoader<R, 32, 64> v(g.v.p + (int64_t)s.k_first * g.v.row + (int64_t)kv * g.v.head, g.v.row, g.bytes);
     const uint32_t mine = lds_at(lds) + wave * 4 * F::SHARE;
     uint32_t here = 0;
-    if (from + wave * 32 < to) {
+    const bool wanted = g.out.p != nullptr;
+    if (wanted && from + wave * 32 < to) {
         k.load(mine, from + wave * 32, s.m);
         v.load(mine + F::SHARE, from + wave * 32, s.m);
     }
+    Backward<T, DB, EXTRA> run;
+    run.begin(g, s, kv, r);
+    if (!wanted) return;
+    const typename R::Place place;
     for (int j0 = from + wave * 32; j0 < to; j0 += 32 * WAVES, here ^= 2 * F::SHARE) {
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
         if (j0 + 32 * WAVES < to) {
@@ -920,8 +931,9 @@ __global__ __launch_bounds__((FewShape<T, DB>::WAVES * 64)) void attention_dq_fe
     }
     const float scale = g.scale / run.by;
     if constexpr (WAVES > 1) {
+        __syncthreads();
         join_waves<WAVES>(lds, run.dq, scale);
-        if (wave == 0) run.end(g, s, kv, r, 1.0f, index, part.count);
+        run.template end<WAVES>(g, s, kv, r, 1.0f, index, part.count);
     } else {
         run.end(g, s, kv, r, scale, index, part.count);
     }
@@ -1106,7 +1118,9 @@ __global__ __launch_bounds__(256) void attention_join_kernel(const AttentionArgs
     if (s.seq >= g.seqs) return;
     find_keys(g, s);
     const int64_t items = (int64_t)g.rows * g.heads;
-    const int d = lane * 4, cnt = g.dim - d, wide = (g.dim & 3) == 0;
+    // (a head's elements take 16, 32 or 64 lanes; the others go through other parts)
+    const int lanes = g.dim <= 64 ? 16 : g.dim <= 128 ? 32 : 64, sub = lane / lanes, subs = 64 / lanes;
+    const int d = lane % lanes * 4, cnt = g.dim - d, wide = (g.dim & 3) == 0;
     for (int r0 = share.begin; r0 < share.end; r0 += tile)
     for (int r = r0 + blockIdx.y * 8 + (threadIdx.x >> 6); r < min(r0 + (int)blockIdx.y * 8 + 8, share.end); r += 4) {
         s.r0 = r0;
@@ -1126,18 +1140,22 @@ __global__ __launch_bounds__(256) void attention_join_kernel(const AttentionArgs
         }
         float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll 4
-        for (int k = 0; k < part.count; ++k) {
-            const float w = SUM ? 1.0f : __shfl(weight, k, 64);
-            if (cnt <= 0) continue;
+        for (int k0 = 0; k0 < part.count; k0 += subs) {
+            const int k = k0 + sub;
+            const float w = SUM ? 1.0f : __shfl(weight, min(k, 63), 64);
+            if (cnt <= 0 || k >= part.count) continue;
             float one[4];
             load_row<float>((const char *)g.part, (k * items + item) * g.dim + d, cnt, wide, one);
 #pragma unroll
             for (int j = 0; j < 4; ++j) v[j] += w == 0.0f ? 0.0f : w * one[j];
         }
+        for (int off = lanes; off < 64; off <<= 1)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[j] += __shfl_xor(v[j], off, 64);
         const float by = sum == 0.0f ? 0.0f : 1.0f / sum;
 #pragma unroll
         for (int j = 0; j < 4; ++j) v[j] *= by;
-        if (cnt > 0) store_row<T>((char *)packed_row(g, g.out, s, kv, r), d, cnt, g.wide, v);
+        if (cnt > 0 && sub == 0) store_row<T>((char *)packed_row(g, g.out, s, kv, r), d, cnt, g.wide, v);
         if (!SUM && g.lse && lane == 0) g.lse[item] = sum == 0.0f ? -INFINITY : (top + log2f(sum)) * LN2;
     }
 }

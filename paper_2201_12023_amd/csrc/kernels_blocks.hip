@@ -129,14 +129,16 @@ hipError_t launch_rotary(hipStream_t st, int dtype, const RotaryArgs &g)
     const size_t bytes = (size_t)per * half * sizeof(float2);
     return by_type(dtype, [&](auto t) {
         using T = decltype(t);
-        if (g.wide) rotary_kernel<T, 16 / sizeof(T)><<<grid, 256, bytes, st>>>(g, per);
+        constexpr int ES = sizeof(T);
+        if (g.wide == 16) rotary_kernel<T, 16 / ES><<<grid, 256, bytes, st>>>(g, per);
+        else if (g.wide == 8) rotary_kernel<T, 8 / ES><<<grid, 256, bytes, st>>>(g, per);
         else rotary_kernel<T, 1><<<grid, 256, bytes, st>>>(g, per);
     });
 }
 
 // ---------------------------------------------------------------- layer norm
 
-// Sums over the threads of a row: a wave, or a workgroup.
+// Sums over the threads of a row: a wave, or a workgroup.  `lds`: THREADS / 64 floats for each of N, not those of the sums before.
 template <int THREADS, int N>
 __device__ __forceinline__ void row_sums(float (&v)[N], float *lds)
 {
@@ -146,7 +148,6 @@ __device__ __forceinline__ void row_sums(float (&v)[N], float *lds)
         for (int off = 32; off; off >>= 1) v[k] += __shfl_xor(v[k], off, 64);
     if constexpr (THREADS > 64) {
         constexpr int WAVES = THREADS / 64;
-        __syncthreads();                                           // (the sums before have been read)
         if ((threadIdx.x & 63) == 0)
 #pragma unroll
             for (int k = 0; k < N; ++k) lds[k * WAVES + (threadIdx.x >> 6)] = v[k];
@@ -160,44 +161,56 @@ __device__ __forceinline__ void row_sums(float (&v)[N], float *lds)
     }
 }
 
-// A row's elements in the registers of THREADS threads, C times V each; `wide`: V at once.
-template <class T, int THREADS, int C>
+// A row's elements as THREADS threads hold them, C times V each, as they were read, so that a row can be under way while another one is worked on.
+// WIDE: V at once.
+template <class T, int THREADS, int C, bool WIDE>
 struct RowOf {
     static constexpr int V = 16 / sizeof(T), N = C * V;
-    static __device__ __forceinline__ int column(int c, int j, int wide, int t) { return wide ? (c * THREADS + t) * V + j : (c * V + j) * THREADS + t; }
-    static __device__ __forceinline__ void load(const char *p, int n, int wide, int t, float (&v)[N])
+    u32x4 raw[WIDE ? C : 1];
+    T one[WIDE ? 1 : N];
+
+    static __device__ __forceinline__ int column(int c, int j, int t) { return WIDE ? (c * THREADS + t) * V + j : (c * V + j) * THREADS + t; }
+    __device__ __forceinline__ void load(const char *p, int n, int t)
     {
 #pragma unroll
         for (int c = 0; c < C; ++c) {
-            if (wide) {
-                float e[V];
-                const int at = column(c, 0, 1, t);
-                load_row<T>(p, at, n - at, 1, e);
-#pragma unroll
-                for (int j = 0; j < V; ++j) v[c * V + j] = e[j];
+            if constexpr (WIDE) {
+                const int at = column(c, 0, t);
+                raw[c] = u32x4{0, 0, 0, 0};
+                if (at < n) raw[c] = *(const u32x4 *)((const T *)p + at);
             } else {
 #pragma unroll
                 for (int j = 0; j < V; ++j) {
-                    const int at = column(c, j, 0, t);
-                    v[c * V + j] = at < n ? (float)((const T *)p)[at] : 0.0f;
+                    const int at = column(c, j, t);
+                    one[c * V + j] = at < n ? ((const T *)p)[at] : (T)0.0f;
                 }
             }
         }
     }
-    static __device__ __forceinline__ void store(char *p, int n, int wide, int t, const float (&v)[N])
+    __device__ __forceinline__ void values(float (&v)[N]) const
     {
 #pragma unroll
         for (int c = 0; c < C; ++c) {
-            if (wide) {
+            T e[V];
+            if constexpr (WIDE) __builtin_memcpy(e, &raw[c], 16);
+#pragma unroll
+            for (int j = 0; j < V; ++j) v[c * V + j] = (float)(WIDE ? e[j] : one[WIDE ? 0 : c * V + j]);
+        }
+    }
+    static __device__ __forceinline__ void store(char *p, int n, int t, const float (&v)[N])
+    {
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            if constexpr (WIDE) {
                 float e[V];
-                const int at = column(c, 0, 1, t);
+                const int at = column(c, 0, t);
 #pragma unroll
                 for (int j = 0; j < V; ++j) e[j] = v[c * V + j];
-                store_row<T>(p, at, n - at, 1, e);
+                if (at < n) store_row<T>(p, at, V, 1, e);
             } else {
 #pragma unroll
                 for (int j = 0; j < V; ++j) {
-                    const int at = column(c, j, 0, t);
+                    const int at = column(c, j, t);
                     if (at < n) ((T *)p)[at] = (T)v[c * V + j];
                 }
             }
@@ -205,47 +218,56 @@ struct RowOf {
     }
 };
 
-// The variance is summed from the differences to the mean, which is known by then, as the row is in registers.
-template <class T, int THREADS, int C>
+// Rows one after the other, the next one under way; weight and bias stay in registers.  The variance is summed from the differences to the mean, which is known
+// by then, as the row is in registers.  Memory bounds it: 8192 rows of 4096 in 16 bits, see FWD.
+template <class T, int THREADS, int C, bool WIDE>
 __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void norm_kernel(const NormArgs g)
 {
-    using R = RowOf<T, THREADS, C>;
+    using R = RowOf<T, THREADS, C, WIDE>;
     constexpr int AT_ONCE = THREADS < 256 ? 256 / THREADS : 1;
-    __shared__ float lds[16];
+    __shared__ float lds[2][16];
     const int t = threadIdx.x % THREADS;
-    // (a wave or the whole workgroup goes on to the next row)
-    for (int64_t row = (int64_t)blockIdx.x * AT_ONCE + threadIdx.x / THREADS; row < g.rows; row += (int64_t)gridDim.x * AT_ONCE) {
-        float x[R::N], v[R::N];
-        R::load(g.x + row * g.ldx * (int64_t)sizeof(T), g.n, g.wide, t, x);
+    const int64_t apart = (int64_t)gridDim.x * AT_ONCE;
+    int64_t row = (int64_t)blockIdx.x * AT_ONCE + threadIdx.x / THREADS;
+    if (row >= g.rows) return;                                     // (whole waves, where a wave has a row)
+    R next, weight, bias;
+    next.load(g.x + row * g.ldx * (int64_t)sizeof(T), g.n, t);
+    if (g.weight) weight.load(g.weight, g.n, t);
+    if (g.bias) bias.load(g.bias, g.n, t);
+    for (; row < g.rows; row += apart) {
+        float x[R::N];
+        next.values(x);
+        if (row + apart < g.rows) next.load(g.x + (row + apart) * g.ldx * (int64_t)sizeof(T), g.n, t);
         float sum[1] = {0.0f};
 #pragma unroll
         for (int j = 0; j < R::N; ++j) sum[0] += x[j];
-        row_sums<THREADS>(sum, lds);
+        row_sums<THREADS>(sum, lds[0]);
         const float mean = sum[0] / (float)g.n;
         sum[0] = 0.0f;
 #pragma unroll
         for (int c = 0; c < C; ++c)
 #pragma unroll
             for (int j = 0; j < R::V; ++j) {
-                const float d = R::column(c, j, g.wide, t) < g.n ? x[c * R::V + j] - mean : 0.0f;
+                const float d = R::column(c, j, t) < g.n ? x[c * R::V + j] - mean : 0.0f;
                 x[c * R::V + j] = d;
                 sum[0] += d * d;
             }
-        row_sums<THREADS>(sum, lds);
+        row_sums<THREADS>(sum, lds[1]);
         const float rstd = 1.0f / sqrtf(sum[0] / (float)g.n + g.eps);
+        float v[R::N];
 #pragma unroll
         for (int j = 0; j < R::N; ++j) x[j] *= rstd;
         if (g.weight) {
-            R::load(g.weight, g.n, g.wide, t, v);
+            weight.values(v);
 #pragma unroll
             for (int j = 0; j < R::N; ++j) x[j] *= v[j];
         }
         if (g.bias) {
-            R::load(g.bias, g.n, g.wide, t, v);
+            bias.values(v);
 #pragma unroll
             for (int j = 0; j < R::N; ++j) x[j] += v[j];
         }
-        R::store(g.y + row * g.ldy * (int64_t)sizeof(T), g.n, g.wide, t, x);
+        R::store(g.y + row * g.ldy * (int64_t)sizeof(T), g.n, t, x);
         if (g.mean && t == 0) {
             g.mean[row] = mean;
             g.rstd[row] = rstd;
@@ -257,19 +279,19 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void norm_kernel(con
 template <class T>
 __global__ __launch_bounds__(1024) void norm_long_kernel(const NormArgs g)
 {
-    __shared__ float lds[16];
+    __shared__ float lds[2][16];
     for (int64_t row = blockIdx.x; row < g.rows; row += gridDim.x) {
         const T *x = (const T *)g.x + row * g.ldx;
         float sum[1] = {0.0f};
         for (int k = threadIdx.x; k < g.n; k += 1024) sum[0] += (float)x[k];
-        row_sums<1024>(sum, lds);
+        row_sums<1024>(sum, lds[0]);
         const float mean = sum[0] / (float)g.n;
         sum[0] = 0.0f;
         for (int k = threadIdx.x; k < g.n; k += 1024) {
             const float d = (float)x[k] - mean;
             sum[0] += d * d;
         }
-        row_sums<1024>(sum, lds);
+        row_sums<1024>(sum, lds[1]);
         const float rstd = 1.0f / sqrtf(sum[0] / (float)g.n + g.eps);
         T *y = (T *)g.y + row * g.ldy;
         for (int k = threadIdx.x; k < g.n; k += 1024) {
@@ -285,52 +307,61 @@ __global__ __launch_bounds__(1024) void norm_long_kernel(const NormArgs g)
     }
 }
 
-// A group's rows one after the other: dx, and the sums for dweight and dbias in registers, as a thread has the same columns of all of them.
-template <class T, int THREADS, int C>
+// A group's rows one after the other, the next one under way: dx, and the sums for dweight and dbias in registers, as a thread has the same columns of all
+// of them.
+template <class T, int THREADS, int C, bool WIDE>
 __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void norm_backward_kernel(const NormArgs g)
 {
-    using R = RowOf<T, THREADS, C>;
+    using R = RowOf<T, THREADS, C, WIDE>;
     constexpr int AT_ONCE = THREADS < 256 ? 256 / THREADS : 1;
-    __shared__ float lds[32];
+    __shared__ float lds[2][32];
     const int t = threadIdx.x % THREADS, group = blockIdx.x * AT_ONCE + threadIdx.x / THREADS;
     if (group >= g.groups) return;
-    float w[R::N], dw[R::N], db[R::N];
+    R next_x, next_dy, weight;
+    float dw[R::N], db[R::N], next_mean = 0.0f, next_rstd = 0.0f;
+    const auto ask = [&](int64_t row) {
+        next_x.load(g.x + row * g.ldx * (int64_t)sizeof(T), g.n, t);
+        next_dy.load(g.dy + row * g.lddy * (int64_t)sizeof(T), g.n, t);
+        next_mean = g.mean[row];
+        next_rstd = g.rstd[row];
+    };
+    if (group < g.rows) ask(group);
+    if (g.weight) weight.load(g.weight, g.n, t);
 #pragma unroll
-    for (int j = 0; j < R::N; ++j) {
-        w[j] = 1.0f;
-        dw[j] = db[j] = 0.0f;
-    }
-    if (g.weight) R::load(g.weight, g.n, g.wide, t, w);
-    for (int64_t row = group; row < g.rows; row += g.groups) {
-        float x[R::N], dy[R::N];
-        R::load(g.x + row * g.ldx * (int64_t)sizeof(T), g.n, g.wide, t, x);
-        R::load(g.dy + row * g.lddy * (int64_t)sizeof(T), g.n, g.wide, t, dy);
-        const float mean = g.mean[row], rstd = g.rstd[row];
+    for (int j = 0; j < R::N; ++j) dw[j] = db[j] = 0.0f;
+    int turn = 0;
+    for (int64_t row = group; row < g.rows; row += g.groups, turn ^= 1) {
+        float x[R::N], dy[R::N], w[R::N];
+        next_x.values(x);
+        next_dy.values(dy);
+        const float mean = next_mean, rstd = next_rstd;
+        if (row + g.groups < g.rows) ask(row + g.groups);
+        if (g.weight) weight.values(w);
         float sum[2] = {0.0f, 0.0f};
 #pragma unroll
         for (int c = 0; c < C; ++c)
 #pragma unroll
             for (int j = 0; j < R::V; ++j) {
                 const int k = c * R::V + j;
-                x[k] = R::column(c, j, g.wide, t) < g.n ? (x[k] - mean) * rstd : 0.0f;
+                x[k] = R::column(c, j, t) < g.n ? (x[k] - mean) * rstd : 0.0f;
                 dw[k] += dy[k] * x[k];
                 db[k] += dy[k];
-                dy[k] *= w[k];
+                if (g.weight) dy[k] *= w[k];
                 sum[0] += dy[k];
                 sum[1] += dy[k] * x[k];
             }
         if (!g.y) continue;
-        row_sums<THREADS>(sum, lds);
+        row_sums<THREADS>(sum, lds[turn]);
         const float a = sum[0] / (float)g.n, b = sum[1] / (float)g.n;
 #pragma unroll
         for (int k = 0; k < R::N; ++k) x[k] = rstd * (dy[k] - a - x[k] * b);
-        R::store(g.y + row * g.ldy * (int64_t)sizeof(T), g.n, g.wide, t, x);
+        R::store(g.y + row * g.ldy * (int64_t)sizeof(T), g.n, t, x);
     }
 #pragma unroll
     for (int c = 0; c < C; ++c)
 #pragma unroll
         for (int j = 0; j < R::V; ++j) {
-            const int at = R::column(c, j, g.wide, t);
+            const int at = R::column(c, j, t);
             if (at >= g.n) continue;
             if (g.part_w) g.part_w[(int64_t)group * g.n + at] = dw[c * R::V + j];
             if (g.part_b) g.part_b[(int64_t)group * g.n + at] = db[c * R::V + j];
@@ -341,8 +372,9 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void norm_backward_k
 template <class T>
 __global__ __launch_bounds__(1024) void norm_backward_long_kernel(const NormArgs g)
 {
-    __shared__ float lds[32];
-    for (int64_t row = blockIdx.x; row < g.rows; row += gridDim.x) {
+    __shared__ float lds[2][32];
+    int turn = 0;
+    for (int64_t row = blockIdx.x; row < g.rows; row += gridDim.x, turn ^= 1) {
         const T *x = (const T *)g.x + row * g.ldx, *dy = (const T *)g.dy + row * g.lddy, *w = (const T *)g.weight;
         const float mean = g.mean[row], rstd = g.rstd[row];
         float sum[2] = {0.0f, 0.0f};
@@ -351,7 +383,7 @@ __global__ __launch_bounds__(1024) void norm_backward_long_kernel(const NormArgs
             sum[0] += d;
             sum[1] += d * ((float)x[k] - mean) * rstd;
         }
-        row_sums<1024>(sum, lds);
+        row_sums<1024>(sum, lds[turn]);
         const float a = sum[0] / (float)g.n, b = sum[1] / (float)g.n;
         T *dx = (T *)g.y + row * g.ldy;
         for (int k = threadIdx.x; k < g.n; k += 1024) {
@@ -425,13 +457,15 @@ hipError_t launch_norm(hipStream_t st, int dtype, const NormArgs &g)
         using T = decltype(type);
         const bool done = with_shape<T, 16>(g.n, [&](auto threads, auto c) {
             constexpr int THREADS = threads(), AT_ONCE = THREADS < 256 ? 256 / THREADS : 1;
-            norm_kernel<T, THREADS, c()><<<blocks_for((g.rows + AT_ONCE - 1) / AT_ONCE, 1 << 20), THREADS * AT_ONCE, 0, st>>>(g);
+            const unsigned blocks = blocks_for((g.rows + AT_ONCE - 1) / AT_ONCE, THREADS == 1024 ? 512 : 2048);
+            if (g.wide) norm_kernel<T, THREADS, c(), true><<<blocks, THREADS * AT_ONCE, 0, st>>>(g);
+            else norm_kernel<T, THREADS, c(), false><<<blocks, THREADS * AT_ONCE, 0, st>>>(g);
         });
         if (!done) norm_long_kernel<T><<<blocks_for(g.rows, 1 << 20), 1024, 0, st>>>(g);
     });
 }
 
-int norm_groups(int64_t rows, int64_t n) { return (int)std::min<int64_t>(std::max<int64_t>(rows, 1), n <= 1024 ? 2048 : n <= 8192 ? 1024 : 512); }
+int norm_groups(int64_t rows, int64_t n) { return (int)std::min<int64_t>(std::max<int64_t>(rows, 1), n <= 4096 ? 1024 : 512); }
 
 hipError_t launch_norm_backward(hipStream_t st, int dtype, const NormArgs &g)
 {
@@ -439,7 +473,9 @@ hipError_t launch_norm_backward(hipStream_t st, int dtype, const NormArgs &g)
         using T = decltype(type);
         const bool done = with_shape<T, sizeof(T) == 4 ? 8 : 16>(g.n, [&](auto threads, auto c) {
             constexpr int THREADS = threads(), AT_ONCE = THREADS < 256 ? 256 / THREADS : 1;
-            norm_backward_kernel<T, THREADS, c()><<<(unsigned)((g.groups + AT_ONCE - 1) / AT_ONCE), THREADS * AT_ONCE, 0, st>>>(g);
+            const unsigned blocks = (unsigned)((g.groups + AT_ONCE - 1) / AT_ONCE);
+            if (g.wide) norm_backward_kernel<T, THREADS, c(), true><<<blocks, THREADS * AT_ONCE, 0, st>>>(g);
+            else norm_backward_kernel<T, THREADS, c(), false><<<blocks, THREADS * AT_ONCE, 0, st>>>(g);
         });
         if (!done) {
             if (g.y) norm_backward_long_kernel<T><<<blocks_for(g.rows, 1 << 20), 1024, 0, st>>>(g);
