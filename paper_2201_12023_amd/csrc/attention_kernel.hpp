@@ -210,7 +210,17 @@ __device__ __forceinline__ float capped(const AttentionArgs &g, float s, float &
     }
 }
 
-__device__ __forceinline__ float other_half(float v) { return __shfl_xor(v, 32, 64); }
+// The maximum and the sum with the lane that has the row's other half, by exchanging the halves of the wave (through LDS it would take a hundred cycles more).
+__device__ __forceinline__ float max_halves(float v)
+{
+    const u32x2 both = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(both.x), __uint_as_float(both.y));
+}
+__device__ __forceinline__ float add_halves(float v)
+{
+    const u32x2 both = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(both.x) + __uint_as_float(both.y);
+}
 
 // Sixteen bytes a lane from memory to LDS, written there by the load unit itself: the wave's go to `lds` and the 1008 bytes behind, in the order of its lanes; those
 // whose offset is out of range are zeros.  Assembly without a result register, as in product.hpp: what has arrived is known by counting.  (The hardware wants five
@@ -442,7 +452,7 @@ struct Running {
         for (int b = 0; b < NB; ++b)
 #pragma unroll
             for (int i = 0; i < 16; ++i) most = fmaxf(most, s[b][i]);
-        most = fmaxf(most, other_half(most)) * by;
+        most = max_halves(most) * by;
         // Exponents are taken from a reference that follows the maximum once it is 8 ahead: exponentials up to 2^8 round to the type like those up to 1
         if (__any(most > top + 8.0f)) {
             const float next = fmaxf(top, most), down = exp2f(top - (next == -INFINITY ? 0.0f : next));
@@ -475,7 +485,7 @@ struct Running {
     template <int WAVES = 1>
     __device__ __forceinline__ void end(const AttentionArgs &g, const Span &s, int kv, int r, int part, int parts)
     {
-        const float all = sum + other_half(sum);
+        const float all = add_halves(sum);
         if (r >= s.n * g.group) return;
         const int64_t item = packed_item(g, s, kv, r);
         const bool first = (threadIdx.x & (WAVES > 1 ? ~31u : 32u)) == 0;
@@ -670,7 +680,7 @@ __global__ __launch_bounds__((FewShape<T, DB>::WAVES * 64)) void attention_few_k
         if constexpr (WAVES > 1) {
             // the waves' sums, each brought to the common maximum; wave 0 goes on with them
             __syncthreads();
-            const float all = run.sum + other_half(run.sum);
+            const float all = add_halves(run.sum);
             if (lane < 32) {
                 tops[wave][lane] = run.top;
                 sums[wave][lane] = all;
@@ -724,7 +734,7 @@ __device__ __forceinline__ void keep_in_range(f32x16 &d, f32x16 (&acc)[DB], floa
         float most = 0.0f;
 #pragma unroll
         for (int i = 0; i < 16; ++i) most = fmaxf(most, fabsf(d[i]));
-        most = fmaxf(most, other_half(most));
+        most = max_halves(most);
         most = most < INFINITY ? most : 0.0f;
         if (__any(most * by > 32768.0f)) {
             // the new factor leaves room for 2^4 more
@@ -773,7 +783,7 @@ struct Backward {
         }
         settle(q);
         settle(dy);
-        delta += other_half(delta);
+        delta = add_halves(delta);
         const int64_t item = packed_item(g, s, kv, i);
         if (h == 0 && r == i) g.delta[item] = delta;
         lse = g.lse[item] * LOG2E;
@@ -1160,9 +1170,9 @@ __global__ __launch_bounds__(256) void attention_join_kernel(const AttentionArgs
     }
 }
 
-// dk and dv of tiles whose rows went in several parts, which are added in their order: four elements a thread, sixteen keys a workgroup.
+// dk and dv of tiles whose rows went in several parts, which are added in their order: four elements a thread, `keys_each` keys a workgroup.
 template <class T>
-__global__ __launch_bounds__(256) void attention_sum_kernel(const AttentionArgs g)
+__global__ __launch_bounds__(256) void attention_sum_kernel(const AttentionArgs g, int keys_each)
 {
     const int kv = (int)((blockIdx.x + g.before) % g.kv_heads);
     Span s = find_span<false>(g.k_offsets, g.seqs, g.k_rows, 1, ATTENTION_TILE, (int)((blockIdx.x + g.before) / g.kv_heads));
@@ -1172,7 +1182,7 @@ __global__ __launch_bounds__(256) void attention_sum_kernel(const AttentionArgs 
     const Heads &out = blockIdx.y & 1 ? g.out2 : g.out;
     const float *const sums = blockIdx.y & 1 ? g.part2 : g.part;
     if (part.count < 2 || !out.p) return;
-    const int per = (g.dim + 3) / 4, key1 = key0 + (blockIdx.y >> 1) * 16, keys = min(16, s.m - key1);
+    const int per = (g.dim + 3) / 4, key1 = key0 + (blockIdx.y >> 1) * keys_each, keys = min(keys_each, s.m - key1);
     const int64_t items = (int64_t)g.k_rows * g.kv_heads;
     for (int c = threadIdx.x; c < keys * per; c += 256) {
         const int key = c / per, d = (c - key * per) * 4, cnt = g.dim - d, wide = (g.dim & 3) == 0;
@@ -1253,7 +1263,10 @@ hipError_t launch_dkv(hipStream_t st, const AttentionArgs &g)
         }
     });
     if (e != hipSuccess || g.splits == 1) return e;
-    return in_launches(g, tiles, [&](const AttentionArgs &p, dim3 grid) { attention_sum_kernel<T><<<dim3(grid.x, 2 * ATTENTION_TILE / 16), 256, 0, st>>>(p); });
+    const int keys_each = tiles >= COMPUTE_UNITS ? 64 : 16;
+    return in_launches(g, tiles, [&](const AttentionArgs &p, dim3 grid) {
+        attention_sum_kernel<T><<<dim3(grid.x, 2 * ATTENTION_TILE / keys_each), 256, 0, st>>>(p, keys_each);
+    });
 }
 
 #define ALPA_BY_DIM(call, T, g, ...)                                                                           \
