@@ -202,26 +202,35 @@ def alpa_attention_forward(q, k, v, offsets=None, k_offsets=None, scale=None, ca
 
 
 def alpa_attention_backward(dy, q, k, v, y, lse, offsets=None, k_offsets=None, scale=None, cap=0.0, slopes=None, causal=False, prefix=None,
-                            need=("q", "k", "v"), stream=None):
-    """(dq, dk, dv) of alpa_attention_forward, None for those not in ``need``; y and lse are its results."""
+                            need=("q", "k", "v"), out=None, stream=None):
+    """(dq, dk, dv) of alpa_attention_forward, None for those not in ``need``; y and lse are its results.  ``out``: three tensors to put them in (None where
+    one is not needed), such as the slices of one product's gradient."""
     if not set(need) <= {"q", "k", "v"}:
         raise ValueError(f"need is {need!r}: names out of 'q', 'k', 'v' expected")
     if k_offsets is not None and k_offsets.dim() == 2:
         raise ValueError("keys that are not packed have no gradient")
-    return _on(_attention_backward_on, q, stream, dy, q, k, v, y, lse, offsets, k_offsets, scale, cap, slopes, causal, prefix, need)
+    return _on(_attention_backward_on, q, stream, dy, q, k, v, y, lse, offsets, k_offsets, scale, cap, slopes, causal, prefix, need, out)
 
 
-def _attention_backward_on(s, dy, q, k, v, y, lse, offsets, k_offsets, scale, cap, slopes, causal, prefix, need):
+def _attention_backward_on(s, dy, q, k, v, y, lse, offsets, k_offsets, scale, cap, slopes, causal, prefix, need, out):
     L = _ready or load()
     a = _how(q, k, offsets, k_offsets, scale, cap, slopes, causal, prefix)
     shape, dtype, device = (a.k_rows, a.kv_heads, a.dim), q.dtype, q.device
     mats = [_heads(name, t, size, dtype, device) for name, t, size in (("dy", dy, q.shape), ("q", q, q.shape), ("k", k, shape), ("v", v, shape),
                                                                        ("y", y, q.shape))]
     l = _vec("lse", lse, q.shape[:2], torch.float32, device)
-    dq, dk, dv = (q.new_empty(size) if name in need else None for name, size in (("q", q.shape), ("k", shape), ("v", shape)))
+    sizes = (("q", q.shape), ("k", shape), ("v", shape))
+    if out is None:
+        grads = tuple(q.new_empty(size) if name in need else None for name, size in sizes)
+        results = [_new(t) for t in grads]
+    else:
+        grads = tuple(t if name in need else None for t, (name, _) in zip(out, sizes))
+        if any(t is None for t, (name, _) in zip(grads, sizes) if name in need):
+            raise ValueError("out lacks a gradient that is needed")
+        results = [_NONE if t is None else _heads("d" + name, t, size, dtype, device) for t, (name, size) in zip(grads, sizes)]
     held, p, n = _l._work(L.alpa_attention_backward_work(a, *mats), device)
-    binding._check(L.alpa_attention_backward(a, *mats, l, _new(dq), _new(dk), _new(dv), p, n, s))
-    return dq, dk, dv
+    binding._check(L.alpa_attention_backward(a, *mats, l, *results, p, n, s))
+    return grads
 
 
 # ------------------------------------------------------------------ rotary positions

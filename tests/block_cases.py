@@ -3,12 +3,16 @@
 Bounds are worst cases, not fits (tests/layer_cases.py has the units).  A sum of n products in 32 bits is off by at most n * STEP * (sum of the absolute
 values); a score's exponential is off, relatively, by the score's error and by STEP for each unit of the exponent; weights and score gradients
 are rounded once to the type as operands (U relative, and what float16 loses below its normal numbers, TINY of the largest), results once more.
+Exponentials below 2^-126, the smallest normal number of 32 bits, may be zero, and so may a product or a sum: FLUSH for a weight, times what it is
+multiplied with, and for a result.
 """
 import math
 
 import torch
 
 from tests.layer_cases import D, STEP, TINY, U
+
+FLUSH = 2.0 ** -125
 
 
 def spans(rows, offsets):
@@ -68,7 +72,7 @@ def attention(q, k, v, dy=None, offsets=None, k_offsets=None, scale=None, cap=0.
             spread = torch.where(seen, (x - lse).abs(), torch.zeros_like(x)).amax(1, keepdim=True)
             e_w = top + STEP * (spread + 16)                       # of a weight, relative
             y = p @ V
-            e_y = (p * (2 * e_w + u + (m + 16) * STEP)) @ V.abs() + tiny * (seen.to(D) @ V.abs())
+            e_y = (p * (2 * e_w + u + (m + 16) * STEP)) @ V.abs() + (tiny + FLUSH) * (seen.to(D) @ V.abs()) + FLUSH
             y_off = e_y + u * (y.abs() + e_y) + TINY[t]
             lse_off = e_w + STEP * (lse.abs() + m + 16)
             out["y"][0][a:b, h], out["y"][1][a:b, h] = y, y_off
@@ -81,18 +85,18 @@ def attention(q, k, v, dy=None, offsets=None, k_offsets=None, scale=None, cap=0.
             e_delta = (E.abs() * y_off).sum(1, keepdim=True) + (dim + 4) * STEP * (E.abs() * (y.abs() + y_off)).sum(1, keepdim=True)
             e_p = e_a + torch.where(some, lse_off, torch.zeros_like(lse_off)) + STEP * (torch.where(seen, (x - lse).abs(), torch.zeros_like(x)) + 16)
             w = p * (dp - delta)
-            e_ds = p * e_p * (dp - delta).abs() + p * (e_dp + e_delta) * (1 + e_p) + 4 * STEP * w.abs()
+            e_ds = p * e_p * (dp - delta).abs() + p * (e_dp + e_delta) * (1 + e_p) + 4 * STEP * w.abs() + FLUSH * seen * (1 + (dp - delta).abs())
             ds = w * bent
             e_ds = e_ds * bent + (w.abs() + e_ds) * e_bent
             ds_off = e_ds + u * (ds.abs() + e_ds)
             row_off, key_off = (ds_off + tiny * ds.abs().amax(i, keepdim=True) for i in (1, 0))
-            v_, e_ = scale * ds @ K, abs(scale) * (row_off + (m + 4) * STEP * (ds.abs() + row_off)) @ K.abs()
+            v_, e_ = scale * ds @ K, FLUSH + abs(scale) * (row_off + (m + 4) * STEP * (ds.abs() + row_off)) @ K.abs()
             out["dq"][0][a:b, h], out["dq"][1][a:b, h] = v_, e_ + u * (v_.abs() + e_) + TINY[t]
             N = n * group + 64
             out["dk"][0][c:e, g] += scale * ds.t() @ Q
-            out["dk"][1][c:e, g] += abs(scale) * (key_off + N * STEP * (ds.abs() + key_off)).t() @ Q.abs()
+            out["dk"][1][c:e, g] += FLUSH + abs(scale) * (key_off + N * STEP * (ds.abs() + key_off)).t() @ Q.abs()
             out["dv"][0][c:e, g] += p.t() @ E
-            out["dv"][1][c:e, g] += (p * (e_p + u + N * STEP) + tiny * seen).t() @ E.abs()
+            out["dv"][1][c:e, g] += (p * (e_p + u + N * STEP) + (tiny + FLUSH) * seen).t() @ E.abs() + FLUSH
     for name in ("dk", "dv"):
         if name in out:
             v_, e_ = out[name]
