@@ -411,17 +411,43 @@ struct Running {
         asm volatile("" ::"v"(slope));
     }
 
-    // NB blocks of 32 keys from j0 on, in LDS from row `at` on
+    // The fragments that products of 16-bit types read go through two sets of DB registers of four, in the order of their use: a set is read from LDS
+    // while the products of the other one run (read as they were needed, a product waited for LDS three times as long as it takes).
+    static constexpr bool AHEAD = sizeof(T) == 2 && DB <= 4;
+
+    // NB blocks of 32 keys from j0 on
     template <int NB>
     __device__ __forceinline__ void step(const AttentionArgs &g, const char *k_lds, const char *v_lds, const typename R::Place &p, int j0)
     {
         const int h = threadIdx.x >> 5 & 1;
         f32x16 s[NB];
         clear(s);
+        u32x4 f[2][DB];
+        const auto k_read = [&](int n) {                           // the n-th set of DB steps
 #pragma unroll
-        for (int b = 0; b < NB; ++b)
+            for (int c = 0; c < DB; ++c) f[n & 1][c] = R::along(k_lds, p, n / 2 * 32, n % 2 * DB + c);
+        };
+        const auto v_read = [&](int n) {                           // the n-th fragment of a block's weights, all blocks of y
 #pragma unroll
-            for (int k = 0; k < R::STEPS; ++k) s[b] = mma32(R::along(k_lds, p, b * 32, k), q[k], s[b], T{});
+            for (int c = 0; c < DB; ++c) f[n & 1][c] = R::across(v_lds, p, n / 2 * 32, n % 2, c * 32);
+        };
+        if constexpr (AHEAD) {
+            k_read(0);
+#pragma unroll
+            for (int n = 0; n < 2 * NB; ++n) {
+                if (n + 1 < 2 * NB) k_read(n + 1);
+                else v_read(0);
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int c = 0; c < DB; ++c) s[n / 2] = mma32(f[n & 1][c], q[n % 2 * DB + c], s[n / 2], T{});
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        } else {
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+                for (int k = 0; k < R::STEPS; ++k) s[b] = mma32(R::along(k_lds, p, b * 32, k), q[k], s[b], T{});
+        }
         const float by = EXTRA ? 1.0f : g.scale * LOG2E;
         if constexpr (EXTRA) {
             float bent;
@@ -464,21 +490,45 @@ struct Running {
             top = next;
         }
         const float ref = top == -INFINITY ? 0.0f : top;
+        if constexpr (AHEAD) {
+            // the exponentials of the next eight keys go between the products of these
+            const auto weigh = [&](int n, int from, int to) {
 #pragma unroll
-        for (int b = 0; b < NB; ++b)
+                for (int i = from; i < to; ++i) {
+                    const float e = __builtin_amdgcn_exp2f(fmaf(s[n / 2][n % 2 * 8 + i], by, -ref));
+                    s[n / 2][n % 2 * 8 + i] = e;
+                    sum += e;
+                }
+            };
+            weigh(0, 0, 8);
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                s[b][i] = __builtin_amdgcn_exp2f(fmaf(s[b][i], by, -ref));
-                sum += s[b][i];
+            for (int n = 0; n < 2 * NB; ++n) {
+                const u32x4 w = R::packed(s[n / 2], n % 2);
+                if (n + 1 < 2 * NB) v_read(n + 1);
+#pragma unroll
+                for (int d = 0; d < DB; ++d) {
+                    y[d] = mma32(f[n & 1][d], w, y[d], T{});
+                    if (n + 1 < 2 * NB) weigh(n + 1, d * 8 / DB, (d + 1) * 8 / DB);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
             }
+        } else {
 #pragma unroll
-        for (int b = 0; b < NB; ++b)
+            for (int b = 0; b < NB; ++b)
 #pragma unroll
-            for (int t = 0; t < R::FRAGS; ++t) {
-                const u32x4 w = R::packed(s[b], t);
+                for (int i = 0; i < 16; ++i) {
+                    s[b][i] = __builtin_amdgcn_exp2f(fmaf(s[b][i], by, -ref));
+                    sum += s[b][i];
+                }
 #pragma unroll
-                for (int d = 0; d < DB; ++d) y[d] = mma32(R::across(v_lds, p, b * 32, t, d * 32), w, y[d], T{});
-            }
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+                for (int t = 0; t < R::FRAGS; ++t) {
+                    const u32x4 w = R::packed(s[b], t);
+#pragma unroll
+                    for (int d = 0; d < DB; ++d) y[d] = mma32(R::across(v_lds, p, b * 32, t, d * 32), w, y[d], T{});
+                }
+        }
     }
 
     // y and lse, or this part of them
