@@ -193,13 +193,22 @@ int key_splits(const alpa_attention_t &a, const Shape &shape, bool backward)
     return (int)std::max<int64_t>(1, std::min({(int64_t)64, parts_for(tiles, slots, a.causal && a.rows > a.k_rows / 4), keys / (a.dtype == ALPA_F32 ? 64 : 128)}));
 }
 
+// Keys of a workgroup for dk and dv: 256, one workgroup a compute unit, read queries and dy half as often as 128, two a unit, and have twice the time to
+// bring a tile of rows; where tiles are few or sequences short, 128 fill the units better (causal, 8192 rows: 32 heads on 32 kv heads 1292 us with 128, 1155 with
+// 256; 32 on 4 1439 and 1260; 2048 rows, 32 on 8 136 and 183; 4096 rows, 16 on 1 287 and 300).
+int key_tile(const alpa_attention_t &a)
+{
+    const bool wide = a.dtype != ALPA_F32 && a.dim <= 128 && a.k_rows / a.seqs >= 512 && a.k_rows / 256 * a.kv_heads >= COMPUTE_UNITS / 2;
+    return wide ? 256 : 128;
+}
+
 // Parts of the rows for dk and dv (RowParts in attention_kernel.hpp; causal, 8192 rows, 32 heads on 8 kv heads: 1963 us in one part, 1260 in two, 1435 in three; 2048 rows: 265 in two, 168 in four, 136 in six, 165 in eight;
 // without the mask 8 heads of 8192 rows: 605, 634 in two; 32 on 8 of 2048: 294 in two, 182 in four, 227 in six).
-int row_splits(const alpa_attention_t &a)
+int row_splits(const alpa_attention_t &a, int key_tile)
 {
     const int64_t rows = a.rows * (a.heads / a.kv_heads) / a.seqs;
-    const int64_t tiles = std::max<int64_t>((a.k_rows / ATTENTION_TILE + a.seqs / 2) * a.kv_heads, a.kv_heads);
-    return (int)std::max<int64_t>(1, std::min({(int64_t)32, parts_for(tiles, 2 * COMPUTE_UNITS, a.causal), rows / (a.dtype == ALPA_F32 ? 64 : 128)}));
+    const int64_t tiles = std::max<int64_t>((a.k_rows / key_tile + a.seqs / 2) * a.kv_heads, a.kv_heads);
+    return (int)std::max<int64_t>(1, std::min({(int64_t)32, parts_for(tiles, (key_tile == 256 ? 1 : 2) * COMPUTE_UNITS, a.causal), rows / (a.dtype == ALPA_F32 ? 64 : 128)}));
 }
 
 void plan_forward(Plan &p, const alpa_heads_t &q, const alpa_heads_t &k, const alpa_heads_t &v)
@@ -227,7 +236,8 @@ void plan_backward(Plan &p, const alpa_heads_t &dy, const alpa_heads_t &q, const
     g.v = p.operand(v, false);
     g.y = p.operand(y, true);
     g.delta = p.take<float>(p.a.rows * p.a.heads);
-    const int rows = row_splits(p.a), keys = key_splits(p.a, Shape(p.a), true);
+    g.key_tile = key_tile(p.a);
+    const int rows = row_splits(p.a, g.key_tile), keys = key_splits(p.a, Shape(p.a), true);
     g.splits = rows;
     const int64_t items = rows > 1 ? (int64_t)rows * p.a.k_rows * p.a.kv_heads : 0, q_items = keys > 1 ? (int64_t)keys * p.a.rows * p.a.heads : 0;
     if (items || q_items) g.part = p.take<float>(std::max(items, q_items) * p.a.dim);          // (dq's are done with when dk's come)
@@ -379,7 +389,7 @@ int alpa_attention_backward(const alpa_attention_t *how, alpa_heads_t dy, alpa_h
         g.out = p.result(dk);
         g.out2 = p.result(dv);
         g.wide = wide_heads(dk, a.dtype, bytes) && wide_heads(dv, a.dtype, bytes);
-        g.tiles = (int)Plan::tiles_of(a.k_rows, a.seqs, ATTENTION_TILE);
+        g.tiles = (int)Plan::tiles_of(a.k_rows, a.seqs, g.key_tile);
         g.splits = splits;
         HIPCHK(launch_dkv_of(st, a.dtype, g));
     }

@@ -1005,7 +1005,7 @@ template <class T, int DB, bool EXTRA, int WAVES, bool DK, bool DV>
 __global__ __launch_bounds__(WAVES * 64, sizeof(T) == 2 && (DB <= 4 || !DK) ? 2 : 1) void attention_dkv_kernel(const AttentionArgs g)
 {
     using R = Rows<T, DB>;
-    constexpr int TILE = 32, NT = WAVES * 64, HALF = TILE * R::ROWB;
+    constexpr int TILE = WAVES == 8 ? 64 : 32, NT = WAVES * 64, HALF = TILE * R::ROWB;
     // (in registers the keys would leave room for one wave a SIMD)
     constexpr bool K_IN_LDS = sizeof(T) == 2 && DB == 4;
     struct RowsInfo { float lse[TILE], delta[TILE], slope[TILE]; int limit[TILE], place[TILE]; };
@@ -1089,17 +1089,19 @@ __global__ __launch_bounds__(WAVES * 64, sizeof(T) == 2 && (DB <= 4 || !DK) ? 2 
         }
         const RowsInfo &info = infos[here];
         const char *const q_lds = lds + here * 2 * HALF, *const dy_lds = q_lds + HALF;
-        if (info.limit[TILE - 1] > key_w) {                      // (else no row of these sees a key of this wave)
+#pragma unroll
+        for (int at = 0; at < TILE; at += 32) {
+            if (info.limit[at + 31] <= key_w) continue;          // (no row of these sees a key of this wave)
             f32x16 a, d;
 #pragma unroll
             for (int j = 0; j < 16; ++j) a[j] = d[j] = 0.0f;
             if constexpr (K_IN_LDS) {
 #pragma unroll
-                for (int c = 0; c < R::STEPS; ++c) a = mma32(R::along(q_lds, place, 0, c), R::along(k_lds, place, wave * 32, c), a, T{});
+                for (int c = 0; c < R::STEPS; ++c) a = mma32(R::along(q_lds, place, at, c), R::along(k_lds, place, wave * 32, c), a, T{});
             } else {
-                along_product<R, T>(q_lds, place, 0, k, a);
+                along_product<R, T>(q_lds, place, at, k, a);
             }
-            if constexpr (DK) along_product<R, T>(dy_lds, place, 0, v, d);
+            if constexpr (DK) along_product<R, T>(dy_lds, place, at, v, d);
             const float by_log = EXTRA ? 1.0f : g.scale * LOG2E;
             if constexpr (EXTRA) {
                 if (g.cap != 0.0f) {
@@ -1107,30 +1109,30 @@ __global__ __launch_bounds__(WAVES * 64, sizeof(T) == 2 && (DB <= 4 || !DK) ? 2 
                     for (int j = 0; j < 16; ++j) {
                         float bent;
                         a[j] = capped<T>(g, a[j], bent);
-                        d[j] = (d[j] - info.delta[block_row(j, h)]) * bent;
+                        d[j] = (d[j] - info.delta[at + block_row(j, h)]) * bent;
                     }
                 } else {
 #pragma unroll
                     for (int j = 0; j < 16; ++j) {
                         a[j] *= g.scale * LOG2E;
-                        d[j] -= info.delta[block_row(j, h)];
+                        d[j] -= info.delta[at + block_row(j, h)];
                     }
                 }
                 if (g.slopes) {
 #pragma unroll
                     for (int j = 0; j < 16; ++j) {
-                        const int r = block_row(j, h);
+                        const int r = at + block_row(j, h);
                         a[j] = fmaf(-info.slope[r], fabsf((float)(info.place[r] - key)), a[j]);
                     }
                 }
             }
-            if (info.limit[0] < key_w + 32) {
+            if (info.limit[at] < key_w + 32) {
 #pragma unroll
-                for (int j = 0; j < 16; ++j) a[j] = key < info.limit[block_row(j, h)] ? a[j] : -INFINITY;
+                for (int j = 0; j < 16; ++j) a[j] = key < info.limit[at + block_row(j, h)] ? a[j] : -INFINITY;
             }
 #pragma unroll
             for (int j = 0; j < 16; ++j) {
-                const int r = block_row(j, h);
+                const int r = at + block_row(j, h);
                 a[j] = __builtin_amdgcn_exp2f(fmaf(a[j], by_log, -info.lse[r]));
                 d[j] = a[j] * (EXTRA ? d[j] : d[j] - info.delta[r]);
             }
@@ -1139,7 +1141,7 @@ __global__ __launch_bounds__(WAVES * 64, sizeof(T) == 2 && (DB <= 4 || !DK) ? 2 
                 for (int t = 0; t < R::FRAGS; ++t) {
                     const u32x4 w = R::packed(a, t);
 #pragma unroll
-                    for (int b = 0; b < DB; ++b) dv[b] = mma32(R::across(dy_lds, place, 0, t, b * 32), w, dv[b], T{});
+                    for (int b = 0; b < DB; ++b) dv[b] = mma32(R::across(dy_lds, place, at, t, b * 32), w, dv[b], T{});
                 }
             }
             if constexpr (DK) {
@@ -1148,7 +1150,7 @@ __global__ __launch_bounds__(WAVES * 64, sizeof(T) == 2 && (DB <= 4 || !DK) ? 2 
                 for (int t = 0; t < R::FRAGS; ++t) {
                     const u32x4 w = R::packed(d, t);
 #pragma unroll
-                    for (int b = 0; b < DB; ++b) dk[b] = mma32(R::across(q_lds, place, 0, t, b * 32), w, dk[b], T{});
+                    for (int b = 0; b < DB; ++b) dk[b] = mma32(R::across(q_lds, place, at, t, b * 32), w, dk[b], T{});
                 }
             }
         }
@@ -1225,7 +1227,7 @@ template <class T>
 __global__ __launch_bounds__(256) void attention_sum_kernel(const AttentionArgs g, int keys_each)
 {
     const int kv = (int)((blockIdx.x + g.before) % g.kv_heads);
-    Span s = find_span<false>(g.k_offsets, g.seqs, g.k_rows, 1, ATTENTION_TILE, (int)((blockIdx.x + g.before) / g.kv_heads));
+    Span s = find_span<false>(g.k_offsets, g.seqs, g.k_rows, 1, g.key_tile, (int)((blockIdx.x + g.before) / g.kv_heads));
     if (s.seq >= g.seqs) return;
     const int key0 = s.r0;
     const RowParts part(g, s, key0);
@@ -1306,6 +1308,12 @@ hipError_t launch_dkv(hipStream_t st, const AttentionArgs &g)
     const int64_t tiles = (int64_t)g.tiles * g.kv_heads;
     const hipError_t e = in_launches(g, tiles, [&](const AttentionArgs &p, dim3 grid) {
         if constexpr (DB <= 4) {
+            if constexpr (sizeof(T) == 2) {
+                if (p.key_tile == 256) {
+                    attention_dkv_kernel<T, DB, EXTRA, 8, true, true><<<grid, 512, 0, st>>>(p);
+                    return;
+                }
+            }
             attention_dkv_kernel<T, DB, EXTRA, 4, true, true><<<grid, 256, 0, st>>>(p);
         } else {
             if (p.out.p) attention_dkv_kernel<T, DB, EXTRA, 4, true, false><<<grid, 256, 0, st>>>(p);
@@ -1315,7 +1323,7 @@ hipError_t launch_dkv(hipStream_t st, const AttentionArgs &g)
     if (e != hipSuccess || g.splits == 1) return e;
     const int keys_each = tiles >= COMPUTE_UNITS ? 64 : 16;
     return in_launches(g, tiles, [&](const AttentionArgs &p, dim3 grid) {
-        attention_sum_kernel<T><<<dim3(grid.x, 2 * ATTENTION_TILE / keys_each), 256, 0, st>>>(p, keys_each);
+        attention_sum_kernel<T><<<dim3(grid.x, 2 * p.key_tile / keys_each), 256, 0, st>>>(p, keys_each);
     });
 }
 

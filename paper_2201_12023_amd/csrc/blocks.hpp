@@ -23,6 +23,7 @@ struct AttentionArgs {
     float scale, cap, twice;        // twice: 2 scale / cap, times the binary logarithm of e
     int tiles;                      // grid: row tiles of all sequences, at most
     uint32_t before;                // of the grid, workgroups of earlier launches
+    int key_tile;                   // dk, dv: keys of a workgroup
     int unit;                       // keys of a step: what parts of them are multiples of
     int splits;                     // parts, at most, of the keys (y, dq) or of the rows (dk, dv)
     float *part;                    // splits > 1: [part][item][dim] sums, of dk or else; items: rows x heads, or key rows x kv heads

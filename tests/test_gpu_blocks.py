@@ -113,6 +113,15 @@ def test_tiles_of_many_rows(dtype, causal):
     check_attention(gen(12), dtype, 2960, 2960, 24, 12, 64, offsets=off, causal=causal, cap=8.0 if causal else 0.0)
 
 
+@pytest.mark.parametrize("dtype", [BF16, F16], ids=str)
+@pytest.mark.parametrize("dim, extra", [(64, True), (80, False), (128, False), (128, True)])
+def test_tiles_of_256_keys(dtype, dim, extra):
+    """Long sequences of many kv heads: keys in tiles of 256, of which some end inside, behind rows and keys of no sequence."""
+    off, k_off = ints(7, 607, 1807), ints(2, 777, 1990)
+    slopes = torch.linspace(0.01, 0.5, 20, device="cuda") if extra else None
+    check_attention(gen(13), dtype, 1815, 2000, 20, 20, dim, offsets=off, k_offsets=k_off, causal=True, prefix=ints(300, 0), cap=10.0 if extra else 0.0, slopes=slopes)
+
+
 @pytest.mark.parametrize("dtype", TYPES, ids=str)
 def test_many_rows_with_few_keys(dtype):
     """Gradients of keys whose rows go in parts that are added."""
