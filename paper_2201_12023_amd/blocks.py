@@ -7,7 +7,8 @@ be any distance apart, so that queries, keys and values may be slices of one pro
 
 The forward calls can be differentiated: where an argument requires a gradient their results are part of torch's graph, and its backward pass makes
 the calls of this module.  What is kept for those (lse; mean and rstd) has no gradient: a loss that depends on it raises an error in the backward pass.
-The backward calls themselves record nothing.
+The backward calls themselves record nothing.  All calls may be recorded into a HIP graph; a backward pass of torch's graph only if that graph was built in the
+same recording.
 """
 from __future__ import annotations
 

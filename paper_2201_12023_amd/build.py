@@ -40,7 +40,9 @@ _OTHER_INSTANCES = [(re.compile(r"sparse_eval_kernelI"), 3, 0), (re.compile(r"sp
                     (re.compile(r"cluster_rows_kernelI"), 2, 0),
                     # products of the layer operators: two waves, whose accumulators and fragments fill the registers; a spill's reload
                     # in the steps would make the compiler wait for all loads under way
-                    (re.compile(r"14product_kernelI"), 2, 0)]
+                    (re.compile(r"14product_kernelI"), 2, 0),
+                    # attention on 16-bit types, heads of up to 128 elements, scores as they are: the same but for a few registers outside the loops
+                    (re.compile(r"attention_(?:dq_|dkv_)?kernelIDF16[b_]Li[234]ELb0"), 2, 16)]
 
 
 def parse_resource_remarks(text: str) -> dict:

@@ -25,7 +25,7 @@ int fail(int code, const char *msg) { return alpa_dp_set_error_(code, msg); }
 
 constexpr int64_t MAX_STRIDE = 1 << 22;                  // bytes, of matrices
 constexpr int64_t FAR = (int64_t)1 << 40;                // bytes, of heads and their rows
-constexpr int64_t NEAR_ROW = 1 << 24, NEAR_HEADS = 1 << 29;    // bytes: tensors that are further spread are copied, so that a tile's offsets stay in 32 bits
+constexpr int64_t NEAR_ROW = 1 << 22, NEAR_HEADS = 1 << 29;    // bytes: tensors that are further spread are copied, so that a tile's offsets stay in 31 bits
 
 int64_t element(int dtype) { return dtype == ALPA_F32 ? 4 : 2; }
 int64_t round_up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
@@ -165,7 +165,8 @@ struct Shape {
     explicit Shape(const alpa_attention_t &a)
         : packed(a.rows * (a.heads / a.kv_heads)), tiles((packed / ATTENTION_TILE + std::min<int64_t>(a.seqs, packed)) * a.kv_heads)
     {
-        // few rows of a sequence, so that the keys and not the products are what takes time; or few tiles, so that waves are short of work
+        // few rows of a sequence, so that the keys and not the products are what takes time; or few tiles, so that waves are short of work (777 rows, 6 heads of
+        // 75 in 32 bits, 42 tiles: forward 73 and 47 us, dq 107 and 59)
         const bool short_rows = packed <= 64 * (int64_t)a.seqs;
         few = short_rows || tiles <= COMPUTE_UNITS;
         direct = packed <= 32 * (int64_t)a.seqs;
@@ -179,12 +180,14 @@ int64_t parts_for(int64_t tiles, int64_t slots, bool causal)
     return causal ? std::max<int64_t>(2 * slots / tiles - 1, tiles <= 2 * slots ? 2 : 1) : slots / tiles;
 }
 
-// Parts of the keys for y and dq (KeyParts in attention_kernel.hpp).
+// Parts of the keys for y and dq (KeyParts in attention_kernel.hpp; causal, 4096 rows, 8 heads of 256: forward 280 us in one part, 164 in two, dq 308 and 222; parts
+// of fewer than 2048 keys cost more than they save: 2048 rows, 16 heads on 1 kv head, 48 us in one, 60 in two).
 int key_splits(const alpa_attention_t &a, const Shape &shape, bool backward)
 {
     const int64_t keys = a.k_rows / a.seqs;
     if (!shape.few) {
         if (backward && a.dtype == ALPA_F32) return 1;           // (4096 rows, 16 heads: dq 879 us, 933 in two parts; forward 799 and 579)
+        if (!backward && a.dtype != ALPA_F32 && 2 * shape.tiles > 3 * COMPUTE_UNITS && keys < 8192) return 1;       // (4096 rows, 16 heads: 101 us, 113 in two)
         return (int)std::max<int64_t>(1, std::min({(int64_t)64, parts_for(shape.tiles, 2 * COMPUTE_UNITS, a.causal), keys / 2048}));
     }
     // (one workgroup a unit where its tiles fill the LDS; rows that are few in front of their keys see nearly all of them)
@@ -202,8 +205,9 @@ int key_tile(const alpa_attention_t &a)
     return wide ? 256 : 128;
 }
 
-// Parts of the rows for dk and dv (RowParts in attention_kernel.hpp; causal, 8192 rows, 32 heads on 8 kv heads: 1963 us in one part, 1260 in two, 1435 in three; 2048 rows: 265 in two, 168 in four, 136 in six, 165 in eight;
-// without the mask 8 heads of 8192 rows: 605, 634 in two; 32 on 8 of 2048: 294 in two, 182 in four, 227 in six).
+// Parts of the rows for dk and dv (RowParts in attention_kernel.hpp; tiles of 128 keys, causal, 8192 rows, 32 heads on 8 kv heads: 1963 us in one part, 1260 in two,
+// 1435 in three; 2048 rows: 265 in two, 168 in four, 136 in six, 165 in eight; without the mask 8 heads of 8192 rows: 605, 634 in two; 32 on 8 of 2048: 294 in
+// two, 182 in four, 227 in six).
 int row_splits(const alpa_attention_t &a, int key_tile)
 {
     const int64_t rows = a.rows * (a.heads / a.kv_heads) / a.seqs;

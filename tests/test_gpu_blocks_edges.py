@@ -112,6 +112,25 @@ def test_a_cache_longer_than_32_bits_reach():
     assert bool((y[0] == 0).all())
 
 
+@pytest.mark.parametrize("apart", [1 << 21, (1 << 21) + 8])
+def test_rows_far_apart(apart):
+    """Rows 2^22 bytes apart, the most that is read in place, and further: the same as from rows behind one another."""
+    g, room = gen(31), torch.empty(300 * apart, dtype=BF16, device="cuda")
+    tensors = [normal(g, BF16, 300, n, 128) for n in (4, 2, 2, 4)]
+    ref = both(*tensors, causal=True)
+    far = [room.as_strided(t.shape, (apart, 128, 1), k * 1024) for k, t in enumerate(tensors)]
+    for t, f in zip(tensors, far):
+        f.copy_(t)
+    for a, b in zip(both(*far, causal=True), ref):
+        assert torch.equal(a, b)
+    # heads far apart, rows beside one another
+    far = [room.as_strided(t.shape, (512, apart * 40, 1), k * 128) for k, t in enumerate(tensors)]
+    for t, f in zip(tensors, far):
+        f.copy_(t)
+    for a, b in zip(both(*far, causal=True), ref):
+        assert torch.equal(a, b)
+
+
 @pytest.mark.parametrize("dtype", TYPES, ids=str)
 def test_the_same_bits_twice(dtype):
     g = gen(25)
