@@ -122,7 +122,8 @@ __global__ __launch_bounds__(256) void rotary_kernel(const RotaryArgs g, int per
 
 hipError_t launch_rotary(hipStream_t st, int dtype, const RotaryArgs &g)
 {
-    const int half = g.rot / 2, per = std::max(1, 256 / half);
+    // (a workgroup's units are counted in 32 bits)
+    const int half = g.rot / 2, per = (int)std::max<int64_t>(1, std::min<int64_t>(256 / half, (1 << 24) / ((int64_t)g.heads * g.dim)));
     const int64_t groups = (g.rows + per - 1) / per;
     const int64_t work = (int64_t)per * g.heads * ((g.dim + 15) / 16);
     const dim3 grid(blocks_for(groups, 1 << 20), groups < 512 ? blocks_for(work / 256, 8) : 1);

@@ -298,6 +298,16 @@ def test_many_rows():
     C.within("t", t[at], C.rotary(x.view(rows, 1, 8)[at], pos[at], f, False, 1.0))
 
 
+def test_rotary_of_wide_rows():
+    """As many heads as allowed, as long as allowed, of which two elements are turned: more units than 32 bits count for 256 rows."""
+    x = torch.empty(256, 4096, 4096, dtype=BF16, device="cuda").random_(-100, 100)
+    pos, f = torch.arange(256, device="cuda"), B.alpa_rotary_frequencies(2)
+    y = B.alpa_rotary_forward(x, pos, f)
+    at = [0, 100, 255]
+    C.within("y", y[at][:, ::1000], C.rotary(x[at][:, ::1000], pos[at], f, False, 1.0))
+    assert torch.equal(y[..., 2:], x[..., 2:])
+
+
 def test_positions_far_away():
     """Positions of 2^40 and negative ones: the angle is reduced in 64 bits."""
     g = gen(30)
