@@ -93,6 +93,19 @@ struct Rows {
             return r;
         }
     }
+    // s + the sum of a fragment's eight values of 16 bits.  (Assembly, as the compiler's builtin read one of the four registers four times; the three wait states
+    // that the hardware wants between such a sum and another instruction that uses it are in it.)
+    static __device__ __forceinline__ float added(u32x4 f, float s)
+    {
+        constexpr uint32_t ONES = std::is_same_v<T, bf16> ? 0x3f803f80u : 0x3c003c00u;
+        if constexpr (std::is_same_v<T, bf16>)
+            asm("v_dot2c_f32_bf16 %0, %1, %5\n\tv_dot2c_f32_bf16 %0, %2, %5\n\tv_dot2c_f32_bf16 %0, %3, %5\n\tv_dot2c_f32_bf16 %0, %4, %5\n\ts_nop 2"
+                : "+v"(s) : "v"(f.x), "v"(f.y), "v"(f.z), "v"(f.w), "v"(ONES));
+        else
+            asm("v_dot2c_f32_f16 %0, %1, %5\n\tv_dot2c_f32_f16 %0, %2, %5\n\tv_dot2c_f32_f16 %0, %3, %5\n\tv_dot2c_f32_f16 %0, %4, %5\n\ts_nop 2"
+                : "+v"(s) : "v"(f.x), "v"(f.y), "v"(f.z), "v"(f.w), "v"(ONES));
+        return s;
+    }
     // A block's values, rounded to the type, as the second operand of fragment t.
     static __device__ __forceinline__ u32x4 packed(const f32x16 &v, int t)
     {
@@ -389,6 +402,9 @@ struct Running {
     u32x4 q[R::STEPS];
     f32x16 y[DB];
     float top, sum;                 // in units of the binary logarithm; of this lane's half of the keys
+    // The sum of the exponentials as they were rounded for the product with v, which y is divided by: with few keys that count the roundings of a sum and of
+    // its weights cancel then (one key: none is left).  lse takes the sum of those that were not rounded.
+    float rounded;
     int limit, place;
     float slope;
 
@@ -404,7 +420,7 @@ struct Running {
         settle(q);
         clear(y);
         top = -INFINITY;
-        sum = 0.0f;
+        sum = rounded = 0.0f;
         limit = limit_of(g, s, i / g.group);
         place = i / g.group + s.ahead;
         slope = EXTRA && g.slopes ? g.slopes[kv * g.group + i % g.group] * LOG2E : 0.0f;
@@ -487,6 +503,7 @@ struct Running {
 #pragma unroll
                 for (int i = 0; i < 16; ++i) y[b][i] *= down;
             sum *= down;
+            rounded *= down;
             top = next;
         }
         const float ref = top == -INFINITY ? 0.0f : top;
@@ -504,6 +521,7 @@ struct Running {
 #pragma unroll
             for (int n = 0; n < 2 * NB; ++n) {
                 const u32x4 w = R::packed(s[n / 2], n % 2);
+                rounded = R::added(w, rounded);
                 if (n + 1 < 2 * NB) v_read(n + 1);
 #pragma unroll
                 for (int d = 0; d < DB; ++d) {
@@ -525,28 +543,37 @@ struct Running {
 #pragma unroll
                 for (int t = 0; t < R::FRAGS; ++t) {
                     const u32x4 w = R::packed(s[b], t);
+                    if constexpr (sizeof(T) == 2) rounded = R::added(w, rounded);
 #pragma unroll
                     for (int d = 0; d < DB; ++d) y[d] = mma32(R::across(v_lds, p, b * 32, t, d * 32), w, y[d], T{});
                 }
         }
     }
 
+    // what makes of the sum over the rounded exponentials one over all
+    __device__ __forceinline__ float evened() const
+    {
+        if constexpr (sizeof(T) == 4) return 1.0f;
+        const float all = add_halves(sum), r = add_halves(rounded);
+        return r > 0.0f ? all / r : 1.0f;
+    }
+
     // y and lse, or this part of them
     template <int WAVES = 1>
     __device__ __forceinline__ void end(const AttentionArgs &g, const Span &s, int kv, int r, int part, int parts)
     {
-        const float all = add_halves(sum);
+        const float all = add_halves(sum), even = WAVES > 1 ? 1.0f : evened();      // (of several waves that has been done)
         if (r >= s.n * g.group) return;
         const int64_t item = packed_item(g, s, kv, r);
         const bool first = (threadIdx.x & (WAVES > 1 ? ~31u : 32u)) == 0;
         if (parts > 1) {
             const int64_t at = (int64_t)part * g.rows * g.heads + item;
-            store_head<float, DB, WAVES>((char *)(g.part + at * g.dim), y, 1.0f, g.dim, (g.dim & 3) == 0);
+            store_head<float, DB, WAVES>((char *)(g.part + at * g.dim), y, even, g.dim, (g.dim & 3) == 0);
             if (first) g.stat[at] = make_float2(top, all);
             return;
         }
         char *out = (char *)packed_row(g, g.out, s, kv, r);
-        store_head<T, DB, WAVES>(out, y, all == 0.0f ? 0.0f : 1.0f / all, g.dim, g.wide);
+        store_head<T, DB, WAVES>(out, y, all == 0.0f ? 0.0f : even / all, g.dim, g.wide);
         if (g.lse && first) g.lse[item] = all == 0.0f ? -INFINITY : (top + log2f(all)) * LN2;
     }
 };
@@ -743,7 +770,7 @@ __global__ __launch_bounds__((FewShape<T, DB>::WAVES * 64)) void attention_few_k
             float total = 0.0f;
 #pragma unroll
             for (int w = 0; w < WAVES; ++w) total += sums[w][lane & 31] * exp2f(tops[w][lane & 31] - ref);
-            join_waves<WAVES>(lds, run.y, down);
+            join_waves<WAVES>(lds, run.y, down * run.evened());
             run.top = top;
             run.sum = (threadIdx.x & 32) ? 0.0f : total;
         }
