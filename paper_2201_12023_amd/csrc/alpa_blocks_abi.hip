@@ -462,7 +462,7 @@ int alpa_norm_forward(int dtype, int64_t rows, int64_t n, float eps, alpa_mat_t 
 int64_t alpa_norm_backward_work(int dtype, int64_t rows, int64_t n)
 {
     if (!type_ok(dtype) || rows < 0 || rows > ALPA_LAYER_MAX_ROWS || n < 1 || n > ALPA_LAYER_MAX_WIDTH) return 0;
-    return 2 * block(norm_groups(rows, n) * n * 4);
+    return 2 * block(norm_groups(rows) * n * 4);
 }
 
 int alpa_norm_backward(int dtype, int64_t rows, int64_t n, alpa_mat_t dy, alpa_mat_t x, const float *mean,
@@ -494,7 +494,7 @@ int alpa_norm_backward(int dtype, int64_t rows, int64_t n, alpa_mat_t dy, alpa_m
     g.n = (int)n;
     g.mean = (float *)mean;
     g.rstd = (float *)rstd;
-    g.groups = norm_groups(rows, n);
+    g.groups = norm_groups(rows);
     g.dweight = (char *)dweight;
     g.dbias = (char *)dbias;
     if (dweight) g.part_w = (float *)work;

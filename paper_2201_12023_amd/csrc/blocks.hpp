@@ -76,6 +76,6 @@ struct NormArgs {
 };
 hipError_t launch_norm(hipStream_t st, int dtype, const NormArgs &a);
 hipError_t launch_norm_backward(hipStream_t st, int dtype, const NormArgs &a);
-int norm_groups(int64_t rows, int64_t n);
+int norm_groups(int64_t rows);
 
 }  // namespace alpa

@@ -139,7 +139,7 @@ hipError_t launch_rotary(hipStream_t st, int dtype, const RotaryArgs &g)
 
 // ---------------------------------------------------------------- layer norm
 
-// Sums over the threads of a row: a wave, or a workgroup.  `lds`: THREADS / 64 floats for each of N, not those of the sums before.
+// Sums over the threads of a row: a wave, or several.  `lds`: a float for each wave of the workgroup and each of N, not those of the sums before.
 template <int THREADS, int N>
 __device__ __forceinline__ void row_sums(float (&v)[N], float *lds)
 {
@@ -149,9 +149,10 @@ __device__ __forceinline__ void row_sums(float (&v)[N], float *lds)
         for (int off = 32; off; off >>= 1) v[k] += __shfl_xor(v[k], off, 64);
     if constexpr (THREADS > 64) {
         constexpr int WAVES = THREADS / 64;
+        lds += threadIdx.x / THREADS * (WAVES * N);
         if ((threadIdx.x & 63) == 0)
 #pragma unroll
-            for (int k = 0; k < N; ++k) lds[k * WAVES + (threadIdx.x >> 6)] = v[k];
+            for (int k = 0; k < N; ++k) lds[k * WAVES + (threadIdx.x % THREADS >> 6)] = v[k];
         __syncthreads();
 #pragma unroll
         for (int k = 0; k < N; ++k) {
@@ -309,65 +310,103 @@ __global__ __launch_bounds__(1024) void norm_long_kernel(const NormArgs g)
     }
 }
 
-// A group's rows one after the other, the next one under way: dx, and the sums for dweight and dbias in registers, as a thread has the same columns of all
-// of them.
+// Rows that a workgroup of the backward pass works on at once.  (Two of 256 threads with four times 16 bytes each need more registers than there are.)
+constexpr int rows_at_once(int threads, int c) { return threads == 64 ? 4 : threads == 256 && c <= 2 ? 2 : 1; }
+
+// A workgroup's rows, some at once, the next ones under way: dx, and the sums for dweight and dbias in registers, as a thread has the same columns of all of
+// them.  The rows' sums are joined through LDS, so that few parts go to memory: bound by memory and by the sums of parts, 8192 rows of 4096 in 16 bits take
+// 40 us with the sums of parts, 65536 of 768 60 us (a part to memory for each of the rows at once: 57 and 105).
 template <class T, int THREADS, int C, bool WIDE>
-__global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void norm_backward_kernel(const NormArgs g)
+__global__ __launch_bounds__(THREADS * rows_at_once(THREADS, C)) void norm_backward_kernel(const NormArgs g)
 {
     using R = RowOf<T, THREADS, C, WIDE>;
-    constexpr int AT_ONCE = THREADS < 256 ? 256 / THREADS : 1;
+    constexpr int AT_ONCE = rows_at_once(THREADS, C);
     __shared__ float lds[2][32];
-    const int t = threadIdx.x % THREADS, group = blockIdx.x * AT_ONCE + threadIdx.x / THREADS;
-    if (group >= g.groups) return;
+    __shared__ float joined[AT_ONCE > 1 ? (AT_ONCE - 1) * THREADS * R::N : 1];
+    const int t = threadIdx.x % THREADS, sub = threadIdx.x / THREADS;
+    const int64_t apart = (int64_t)g.groups * AT_ONCE, own = (int64_t)g.groups * sub;
     R next_x, next_dy, weight;
     float dw[R::N], db[R::N], next_mean = 0.0f, next_rstd = 0.0f;
     const auto ask = [&](int64_t row) {
+        if (row >= g.rows) return;
         next_x.load(g.x + row * g.ldx * (int64_t)sizeof(T), g.n, t);
         next_dy.load(g.dy + row * g.lddy * (int64_t)sizeof(T), g.n, t);
         next_mean = g.mean[row];
         next_rstd = g.rstd[row];
     };
-    if (group < g.rows) ask(group);
+    ask(blockIdx.x + own);
     if (g.weight) weight.load(g.weight, g.n, t);
 #pragma unroll
     for (int j = 0; j < R::N; ++j) dw[j] = db[j] = 0.0f;
     int turn = 0;
-    for (int64_t row = group; row < g.rows; row += g.groups, turn ^= 1) {
+    for (int64_t at = blockIdx.x; at < g.rows; at += apart, turn ^= 1) {
+        const int64_t row = at + own;
+        const bool here = row < g.rows;                            // (the others only take part in the sums)
         float x[R::N], dy[R::N], w[R::N];
-        next_x.values(x);
-        next_dy.values(dy);
-        const float mean = next_mean, rstd = next_rstd;
-        if (row + g.groups < g.rows) ask(row + g.groups);
-        if (g.weight) weight.values(w);
         float sum[2] = {0.0f, 0.0f};
+        const float mean = next_mean, rstd = next_rstd;
+        if (here) {
+            next_x.values(x);
+            next_dy.values(dy);
+        }
+        ask(row + apart);
+        if (here) {
+            if (g.weight) weight.values(w);
 #pragma unroll
-        for (int c = 0; c < C; ++c)
+            for (int c = 0; c < C; ++c)
 #pragma unroll
-            for (int j = 0; j < R::V; ++j) {
-                const int k = c * R::V + j;
-                x[k] = R::column(c, j, t) < g.n ? (x[k] - mean) * rstd : 0.0f;
-                dw[k] += dy[k] * x[k];
-                db[k] += dy[k];
-                if (g.weight) dy[k] *= w[k];
-                sum[0] += dy[k];
-                sum[1] += dy[k] * x[k];
-            }
+                for (int j = 0; j < R::V; ++j) {
+                    const int k = c * R::V + j;
+                    x[k] = R::column(c, j, t) < g.n ? (x[k] - mean) * rstd : 0.0f;
+                    dw[k] += dy[k] * x[k];
+                    db[k] += dy[k];
+                    if (g.weight) dy[k] *= w[k];
+                    sum[0] += dy[k];
+                    sum[1] += dy[k] * x[k];
+                }
+        }
         if (!g.y) continue;
         row_sums<THREADS>(sum, lds[turn]);
+        if (!here) continue;
         const float a = sum[0] / (float)g.n, b = sum[1] / (float)g.n;
 #pragma unroll
         for (int k = 0; k < R::N; ++k) x[k] = rstd * (dy[k] - a - x[k] * b);
         R::store(g.y + row * g.ldy * (int64_t)sizeof(T), g.n, t, x);
     }
+    const auto finish = [&](float (&v)[R::N], float *part) {
+        if (!part) return;
+        if constexpr (AT_ONCE > 1) {
+            __syncthreads();                                       // (the other sums have been read)
+            if (sub)
 #pragma unroll
-    for (int c = 0; c < C; ++c)
+                for (int k = 0; k < R::N; ++k) joined[((sub - 1) * R::N + k) * THREADS + t] = v[k];
+            __syncthreads();
+            if (sub) return;
 #pragma unroll
-        for (int j = 0; j < R::V; ++j) {
-            const int at = R::column(c, j, t);
-            if (at >= g.n) continue;
-            if (g.part_w) g.part_w[(int64_t)group * g.n + at] = dw[c * R::V + j];
-            if (g.part_b) g.part_b[(int64_t)group * g.n + at] = db[c * R::V + j];
+            for (int k = 0; k < R::N; ++k)
+                for (int o = 0; o < AT_ONCE - 1; ++o) v[k] += joined[(o * R::N + k) * THREADS + t];
         }
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            if constexpr (WIDE) {
+                float e[R::V];
+                const int at = R::column(c, 0, t);
+#pragma unroll
+                for (int j = 0; j < R::V; ++j) e[j] = v[c * R::V + j];
+                if (at < g.n)
+#pragma unroll
+                    for (int j = 0; j < R::V; j += 4) *(f32x4 *)(part + (int64_t)blockIdx.x * g.n + at + j) = f32x4{e[j], e[j + 1], e[j + 2], e[j + 3]};
+            } else {
+#pragma unroll
+                for (int j = 0; j < R::V; ++j) {
+                    const int at = R::column(c, j, t);
+                    if (at < g.n) part[(int64_t)blockIdx.x * g.n + at] = v[c * R::V + j];
+                }
+            }
+        }
+    };
+    finish(dw, g.part_w);
+    finish(db, g.part_b);
 }
 
 // Long rows: dx alone, and the sums by columns.
@@ -467,17 +506,16 @@ hipError_t launch_norm(hipStream_t st, int dtype, const NormArgs &g)
     });
 }
 
-int norm_groups(int64_t rows, int64_t n) { return (int)std::min<int64_t>(std::max<int64_t>(rows, 1), n <= 4096 ? 1024 : 512); }
+int norm_groups(int64_t rows) { return (int)std::min<int64_t>(std::max<int64_t>(rows, 1), 512); }
 
 hipError_t launch_norm_backward(hipStream_t st, int dtype, const NormArgs &g)
 {
     return by_type(dtype, [&](auto type) {
         using T = decltype(type);
         const bool done = with_shape<T, sizeof(T) == 4 ? 8 : 16>(g.n, [&](auto threads, auto c) {
-            constexpr int THREADS = threads(), AT_ONCE = THREADS < 256 ? 256 / THREADS : 1;
-            const unsigned blocks = (unsigned)((g.groups + AT_ONCE - 1) / AT_ONCE);
-            if (g.wide) norm_backward_kernel<T, THREADS, c(), true><<<blocks, THREADS * AT_ONCE, 0, st>>>(g);
-            else norm_backward_kernel<T, THREADS, c(), false><<<blocks, THREADS * AT_ONCE, 0, st>>>(g);
+            constexpr int THREADS = threads();
+            if (g.wide) norm_backward_kernel<T, THREADS, c(), true><<<(unsigned)g.groups, THREADS * rows_at_once(THREADS, c()), 0, st>>>(g);
+            else norm_backward_kernel<T, THREADS, c(), false><<<(unsigned)g.groups, THREADS * rows_at_once(THREADS, c()), 0, st>>>(g);
         });
         if (!done) {
             if (g.y) norm_backward_long_kernel<T><<<blocks_for(g.rows, 1 << 20), 1024, 0, st>>>(g);

@@ -158,3 +158,18 @@ def test_norm(dtype, rows, n, weight, bias):
     got = {"y": y, "mean": mean, "rstd": rstd, **dict(zip(("dx", "dweight", "dbias"), B.alpa_norm_backward(dy, x, mean, rstd, w)))}
     for name, value in got.items():
         C.within(name, value, ref[name])
+
+
+@pytest.mark.parametrize("dtype,n", [(BF16, 72), (BF16, 1000), (F16, 1024), (BF16, 2049), (BF16, 4096), (F16, 4095), (BF16, 8192), (BF16, 10001), (F32, 65), (F32, 1001), (F32, 2048)])
+@pytest.mark.parametrize("rows", [511, 513, 1025, 2047, 2055])
+def test_gradients_of_norm_rows_that_share_a_workgroup(dtype, n, rows):
+    """A workgroup takes some rows at once, the last of them not in all of its threads; what one of dx, dweight and dbias is does not depend on the others."""
+    g = gen(rows * 7 + n)
+    x, dy, w = normal(g, dtype, rows, n), normal(g, dtype, rows, n), normal(g, dtype, n)
+    ref = C.norm(x, w, None, 1e-5, dy)
+    _, mean, rstd = B.alpa_norm_forward(x, w, keep=True)
+    got = B.alpa_norm_backward(dy, x, mean, rstd, w)
+    for name, t in zip(("dx", "dweight", "dbias"), got):
+        C.within(name, t, ref[name])
+    for i, name in enumerate(("x", "weight", "bias")):
+        assert torch.equal(B.alpa_norm_backward(dy, x, mean, rstd, w, need=(name,))[i], got[i])
