@@ -166,7 +166,7 @@ struct Shape {
         : packed(a.rows * (a.heads / a.kv_heads)), tiles((packed / ATTENTION_TILE + std::min<int64_t>(a.seqs, packed)) * a.kv_heads)
     {
         // few rows of a sequence, so that the keys and not the products are what takes time; or few tiles, so that waves are short of work (777 rows, 6 heads of
-        // 75 in 32 bits, 42 tiles: forward 73 and 47 us, dq 107 and 59)
+        // 75 in 32 bits, 42 tiles: forward 73 and 33 us, dq 107 and 42)
         const bool short_rows = packed <= 64 * (int64_t)a.seqs;
         few = short_rows || tiles <= COMPUTE_UNITS;
         direct = packed <= 32 * (int64_t)a.seqs;

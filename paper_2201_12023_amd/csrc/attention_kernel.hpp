@@ -395,6 +395,10 @@ __device__ __forceinline__ void clear(f32x16 (&acc)[DB])
         for (int j = 0; j < 16; ++j) acc[b][j] = 0.0f;
 }
 
+struct Nothing {
+    __device__ __forceinline__ void operator()() const {}
+};
+
 // One row a lane, twice: what has been seen of the keys so far.
 template <class T, int DB, bool EXTRA>
 struct Running {
@@ -431,10 +435,11 @@ struct Running {
     // while the products of the other one run (read as they were needed, a product waited for LDS three times as long as it takes).
     static constexpr bool AHEAD = sizeof(T) == 2 && DB <= 4;
 
-    // NB blocks of 32 keys from j0 on
-    template <int NB>
-    __device__ __forceinline__ void step(const AttentionArgs &g, const char *k_lds, const char *v_lds, const typename R::Place &p, int j0)
+    // NB blocks of 32 keys from j0 on; `between` runs once the keys have been read and before the values are
+    template <int NB, class Between = Nothing>
+    __device__ __forceinline__ void step(const AttentionArgs &g, const char *k_lds, const char *v_lds, const typename R::Place &p, int j0, const Between &between = {})
     {
+        static_assert(!AHEAD || std::is_same<Between, Nothing>::value, "the values are read among the keys");
         const int h = threadIdx.x >> 5 & 1;
         f32x16 s[NB];
         clear(s);
@@ -463,6 +468,7 @@ struct Running {
             for (int b = 0; b < NB; ++b)
 #pragma unroll
                 for (int k = 0; k < R::STEPS; ++k) s[b] = mma32(R::along(k_lds, p, b * 32, k), q[k], s[b], T{});
+            between();
         }
         const float by = EXTRA ? 1.0f : g.scale * LOG2E;
         if constexpr (EXTRA) {
@@ -675,12 +681,45 @@ struct Share {
 };
 
 // Few rows: the waves of a workgroup have the same 32 packed rows and take tiles of 32 keys in turn, each from its own part of LDS; in the end their sums
-// are joined.
+// are joined.  A wave has room for two tiles of keys and two of values; or, where rows are wide (STAGES 1), for one, so that there are twice as many waves: the
+// next keys are under way while the values are worked on, and the other way round (32 bits, heads of 75: y 43 and 28 us, dq 53 and 36; of 128, 64 rows on 2048
+// keys each: 170 and 111; 16 bits, heads of 256, a row on 4095 keys: 41 and 29).
 template <class T, int DB>
 struct FewShape {
     using R = Rows<T, DB>;
-    static constexpr int WAVES = R::ROWB <= 256 ? 4 : R::ROWB == 512 ? 2 : 1, SHARE = 32 * R::ROWB;          // (two tiles of keys and two of values a wave)
+    static constexpr int STAGES = R::ROWB <= 256 ? 2 : 1, WAVES = R::ROWB <= 512 ? 4 : 2, TILE = 32 * R::ROWB, LDS = WAVES * STAGES * 2 * TILE;
+    using Loader = KeyLoader<R, 32, 64>;
 };
+
+// Waits until the loads have arrived that came before the last LEFT, and what was asked of LDS.
+template <int LEFT>
+__device__ __forceinline__ void arrived_but()
+{
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(LEFT) : "memory");
+}
+
+// A wave's tiles of 32 keys, each with room for one tile of `a` and one of `b`: work(j0, between) reads `a`, calls between, and reads `b` (or `a` no more
+// before it ends).  Both loads of the first tile are under way.
+template <class Loader, class Work>
+__device__ __forceinline__ void in_turn(const Loader &a, uint32_t a_lds, const Loader &b, uint32_t b_lds, int j0, int to, int apart, int end, const Work &work)
+{
+    for (; j0 < to; j0 += apart) {
+        const int next = j0 + apart;
+        arrived_but<Loader::N>();
+        work(j0, [&] {
+            // (a's reads have ended before its place is written to)
+            arrived_but<63>();
+            if (next < to) {
+                a.load(a_lds, next, end);
+                arrived_but<Loader::N>();
+            } else {
+                arrived_but<0>();
+            }
+        });
+        arrived_but<63>();
+        if (next < to) b.load(b_lds, next, end);
+    }
+}
 
 // Adds up the waves' blocks, each times `by`: a wave has every so-many-th one then.  What was in LDS has been read; the sums' 16 KB a wave for heads of 128 lie in the
 // room of the tiles.
@@ -714,7 +753,7 @@ __global__ __launch_bounds__((FewShape<T, DB>::WAVES * 64)) void attention_few_k
     using F = FewShape<T, DB>;
     using R = Rows<T, DB>;
     constexpr int WAVES = F::WAVES;
-    __shared__ __align__(1024) char lds[WAVES * 4 * F::SHARE];
+    __shared__ __align__(1024) char lds[F::LDS];
     __shared__ float tops[WAVES][32], sums[WAVES][32];
     const int kv = (int)((blockIdx.x + g.before) % g.kv_heads), lane = threadIdx.x & 63;
     const Share share(g, 32);
@@ -727,9 +766,10 @@ __global__ __launch_bounds__((FewShape<T, DB>::WAVES * 64)) void attention_few_k
     find_keys(g, s);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const typename R::Place place;
-    const uint32_t mine = lds_at(lds) + wave * 4 * F::SHARE;
-    const KeyLoader<R, 32, 64> k(g.k.p + (int64_t)s.k_first * g.k.row + (int64_t)kv * g.k.head, g.k.row, g.bytes);
-    const KeyLoader<R, 32, 64> v(g.v.p + (int64_t)s.k_first * g.v.row + (int64_t)kv * g.v.head, g.v.row, g.bytes);
+    const char *const own = lds + wave * F::STAGES * 2 * F::TILE;
+    const uint32_t mine = lds_at(lds) + wave * F::STAGES * 2 * F::TILE;
+    const typename F::Loader k(g.k.p + (int64_t)s.k_first * g.k.row + (int64_t)kv * g.k.head, g.k.row, g.bytes);
+    const typename F::Loader v(g.v.p + (int64_t)s.k_first * g.v.row + (int64_t)kv * g.v.head, g.v.row, g.bytes);
     for (int r0 = share.begin; r0 < share.end; r0 += 32) {
         const int r = r0 + (lane & 31);
         s.r0 = r0;
@@ -738,21 +778,25 @@ __global__ __launch_bounds__((FewShape<T, DB>::WAVES * 64)) void attention_few_k
         if (index >= part.count) continue;
         // each wave waits for its own loads alone
         const int j1 = from + wave * 32;
-        uint32_t here = 0;
         __syncthreads();                                   // (the rows before are done with)
         if (j1 < to) {
             k.load(mine, j1, s.m);
-            v.load(mine + F::SHARE, j1, s.m);
+            v.load(mine + F::TILE, j1, s.m);
         }
         Running<T, DB, EXTRA> run;
         run.begin(g, s, kv, r);
-        for (int j0 = j1; j0 < to; j0 += 32 * WAVES, here ^= 2 * F::SHARE) {
-            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-            if (j0 + 32 * WAVES < to) {
-                k.load(mine + (here ^ 2 * F::SHARE), j0 + 32 * WAVES, s.m);
-                v.load(mine + (here ^ 2 * F::SHARE) + F::SHARE, j0 + 32 * WAVES, s.m);
+        if constexpr (F::STAGES == 1) {
+            in_turn(k, mine, v, mine + F::TILE, j1, to, 32 * WAVES, s.m, [&](int j0, auto between) { run.template step<1>(g, own, own + F::TILE, place, j0, between); });
+        } else {
+            uint32_t here = 0;
+            for (int j0 = j1; j0 < to; j0 += 32 * WAVES, here ^= 2 * F::TILE) {
+                arrived_but<0>();
+                if (j0 + 32 * WAVES < to) {
+                    k.load(mine + (here ^ 2 * F::TILE), j0 + 32 * WAVES, s.m);
+                    v.load(mine + (here ^ 2 * F::TILE) + F::TILE, j0 + 32 * WAVES, s.m);
+                }
+                run.template step<1>(g, own + here, own + here + F::TILE, place, j0);
             }
-            run.template step<1>(g, lds + wave * 4 * F::SHARE + here, lds + wave * 4 * F::SHARE + here + F::SHARE, place, j0);
         }
         if constexpr (WAVES > 1) {
             // the waves' sums, each brought to the common maximum; wave 0 goes on with them
@@ -873,15 +917,23 @@ struct Backward {
         clear(dq);
     }
 
-    // 32 keys from j0 on, in LDS from row `at` on
-    __device__ __forceinline__ void step(const AttentionArgs &g, const char *k_lds, const char *v_lds, const typename R::Place &place, int j0, int at)
+    // 32 keys from j0 on, in LDS from row `at` on; `between`, if there is one, runs once the values have been read and before the keys are
+    template <class Between = Nothing>
+    __device__ __forceinline__ void step(const AttentionArgs &g, const char *k_lds, const char *v_lds, const typename R::Place &place, int j0, int at,
+                                         const Between &between = {})
     {
         const int h = threadIdx.x >> 5 & 1;
         f32x16 a, d;
 #pragma unroll
         for (int j = 0; j < 16; ++j) a[j] = d[j] = 0.0f;
-        along_product<R, T>(k_lds, place, at, q, a);
-        along_product<R, T>(v_lds, place, at, dy, d);
+        if constexpr (std::is_same<Between, Nothing>::value) {
+            along_product<R, T>(k_lds, place, at, q, a);
+            along_product<R, T>(v_lds, place, at, dy, d);
+        } else {
+            along_product<R, T>(v_lds, place, at, dy, d);
+            between();
+            along_product<R, T>(k_lds, place, at, q, a);
+        }
         const float by_log = EXTRA ? 1.0f : g.scale * LOG2E;
         if constexpr (EXTRA) {
             if (g.cap != 0.0f) {
@@ -982,7 +1034,7 @@ __global__ __launch_bounds__((FewShape<T, DB>::WAVES * 64)) void attention_dq_fe
     using F = FewShape<T, DB>;
     using R = Rows<T, DB>;
     constexpr int WAVES = F::WAVES;
-    __shared__ __align__(1024) char lds[WAVES * 4 * F::SHARE];
+    __shared__ __align__(1024) char lds[F::LDS];
     const int kv = (int)((blockIdx.x + g.before) % g.kv_heads), lane = threadIdx.x & 63;
     Span s = find_span<true>(g.offsets, g.seqs, g.rows, g.group, 32, (int)((blockIdx.x + g.before) / g.kv_heads));
     if (s.seq >= g.seqs) {
@@ -994,27 +1046,32 @@ __global__ __launch_bounds__((FewShape<T, DB>::WAVES * 64)) void attention_dq_fe
     const int index = g.splits - 1 - (int)blockIdx.y, from = index * part.chunk, to = min(from + part.chunk, part.most);
     if (index >= part.count) return;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = s.r0 + (lane & 31);
-    const KeyLoader<R, 32, 64> k(g.k.p + (int64_t)s.k_first * g.k.row + (int64_t)kv * g.k.head, g.k.row, g.bytes);
-    const KeyLoader<R, 32, 64> v(g.v.p + (int64_t)s.k_first * g.v.row + (int64_t)kv * g.v.head, g.v.row, g.bytes);
-    const uint32_t mine = lds_at(lds) + wave * 4 * F::SHARE;
-    uint32_t here = 0;
+    const typename F::Loader k(g.k.p + (int64_t)s.k_first * g.k.row + (int64_t)kv * g.k.head, g.k.row, g.bytes);
+    const typename F::Loader v(g.v.p + (int64_t)s.k_first * g.v.row + (int64_t)kv * g.v.head, g.v.row, g.bytes);
+    const char *const own = lds + wave * F::STAGES * 2 * F::TILE;
+    const uint32_t mine = lds_at(lds) + wave * F::STAGES * 2 * F::TILE;
     const bool wanted = g.out.p != nullptr;
-    if (wanted && from + wave * 32 < to) {
-        k.load(mine, from + wave * 32, s.m);
-        v.load(mine + F::SHARE, from + wave * 32, s.m);
+    const int j1 = from + wave * 32;
+    if (wanted && j1 < to) {
+        v.load(mine + F::TILE, j1, s.m);
+        k.load(mine, j1, s.m);
     }
     Backward<T, DB, EXTRA> run;
     run.begin(g, s, kv, r);
     if (!wanted) return;
     const typename R::Place place;
-    for (int j0 = from + wave * 32; j0 < to; j0 += 32 * WAVES, here ^= 2 * F::SHARE) {
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-        if (j0 + 32 * WAVES < to) {
-            k.load(mine + (here ^ 2 * F::SHARE), j0 + 32 * WAVES, s.m);
-            v.load(mine + (here ^ 2 * F::SHARE) + F::SHARE, j0 + 32 * WAVES, s.m);
+    if constexpr (F::STAGES == 1) {
+        in_turn(v, mine + F::TILE, k, mine, j1, to, 32 * WAVES, s.m, [&](int j0, auto between) { run.step(g, own, own + F::TILE, place, j0, 0, between); });
+    } else {
+        uint32_t here = 0;
+        for (int j0 = j1; j0 < to; j0 += 32 * WAVES, here ^= 2 * F::TILE) {
+            arrived_but<0>();
+            if (j0 + 32 * WAVES < to) {
+                k.load(mine + (here ^ 2 * F::TILE), j0 + 32 * WAVES, s.m);
+                v.load(mine + (here ^ 2 * F::TILE) + F::TILE, j0 + 32 * WAVES, s.m);
+            }
+            run.step(g, own + here, own + here + F::TILE, place, j0, 0);
         }
-        const char *const at = lds + wave * 4 * F::SHARE + here;
-        run.step(g, at, at + F::SHARE, place, j0, 0);
     }
     const float scale = g.scale / run.by;
     if constexpr (WAVES > 1) {
