@@ -123,7 +123,8 @@ struct Plan {
         g.causal = a.causal != 0;
         g.scale = a.scale;
         g.cap = a.cap;
-        g.twice = a.cap > 0.0f ? (float)(2.0 * a.scale * 1.4426950408889634 / a.cap) : 0.0f;
+        // (finite, so that a score of zero stays one)
+        g.twice = a.cap > 0.0f ? (float)std::min(std::max(2.0 * a.scale * 1.4426950408889634 / a.cap, -3.4e38), 3.4e38) : 0.0f;
         g.splits = 1;
         pack.len = a.dim;
         pack.to_len = (int)(g.bytes / es);

@@ -209,6 +209,8 @@ __device__ __forceinline__ int limit_of(const AttentionArgs &g, const Span &s, i
 
 // A capped score from the product of q and k, in units of the binary logarithm, and the slope of the cap.  1 - tanh(x) = 2 / (1 + exp(2 x)) = 2 u, and the
 // slope is 4 u^2 exp(2 x), which keeps its relative error where the cap is reached; tanh is off by a few units of 2^-24 absolute so, which float32 gets better.
+// The score itself takes the exponential as it is, infinite ones (u = 0) and no numbers among them: a minimum, which gives the other operand for a NaN, may
+// only stand in the slope.
 template <class T>
 __device__ __forceinline__ float capped(const AttentionArgs &g, float s, float &bent)
 {
@@ -217,8 +219,8 @@ __device__ __forceinline__ float capped(const AttentionArgs &g, float s, float &
         bent = 4.0f * u * (1.0f - u);
         return g.cap * tanhf(x) * LOG2E;
     } else {
-        const float e = __builtin_amdgcn_exp2f(fminf(s * g.twice, 60.0f)), u = __builtin_amdgcn_rcpf(1.0f + e);
-        bent = 4.0f * e * u * u;
+        const float e = __builtin_amdgcn_exp2f(s * g.twice), u = __builtin_amdgcn_rcpf(1.0f + e);
+        bent = 4.0f * fminf(e, 0x1p60f) * u * u;
         return fmaf(-2.0f * LOG2E * g.cap, u, LOG2E * g.cap);
     }
 }

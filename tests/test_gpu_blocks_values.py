@@ -1,0 +1,87 @@
+"""Attention where numbers end: scores that are no number under a cap, caps far above the scores, and weights below what float16 holds."""
+import math
+
+import pytest
+import torch
+
+from paper_2201_12023_amd import blocks as B
+from tests import block_cases as C
+from tests.layer_cases import D, gen, normal
+
+pytestmark = pytest.mark.gpu
+BF16, F16, F32 = torch.bfloat16, torch.float16, torch.float32
+TYPES = [BF16, F16, F32]
+
+
+def ints(*v):
+    return torch.tensor(v, dtype=torch.int32, device="cuda")
+
+
+def both(q, k, v, dy, **how):
+    y, lse = B.alpa_attention_forward(q, k, v, keep_lse=True, **how)
+    return y, lse, *B.alpa_attention_backward(dy, q, k, v, y, lse, **how)
+
+
+# (rows, keys, heads, kv heads, dim, offsets, key offsets): few rows and keys in tiles of 128; tiles of many rows and keys in tiles of 256; heads above 128
+SHAPES = [(130, 130, 4, 2, 64, (0, 40, 80, 120), (0, 40, 80, 120)), (1815, 2000, 20, 20, 64, (7, 607, 1807), (2, 777, 1990)), (90, 100, 4, 2, 200, (0, 90), (0, 100))]
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("shape", SHAPES, ids=lambda s: "-".join(map(str, s[:5])))
+@pytest.mark.parametrize("cap, slopes", [(30.0, False), (30.0, True), (1e5, False), (0.0, True)])
+def test_a_score_that_is_no_number_stays_none(dtype, shape, cap, slopes):
+    """A NaN in a row of q, or in a key, is one in y, lse and dq of the rows that see it, and in the gradients of what they see; other sequences and kv heads keep their bits."""
+    rows, k_rows, heads, kv, dim, off, k_off = shape
+    g, group = gen(41), heads // kv
+    q, k, v, dy = normal(g, dtype, rows, heads, dim), normal(g, dtype, k_rows, kv, dim), normal(g, dtype, k_rows, kv, dim), normal(g, dtype, rows, heads, dim)
+    how = dict(offsets=ints(*off), k_offsets=ints(*k_off), causal=True, cap=cap, slopes=torch.linspace(0.01, 0.5, heads, device="cuda") if slopes else None)
+    clean = both(q, k, v, dy, **how)
+    s = len(off) - 2                                       # the last sequence
+    a, b, c, e = off[s], off[s + 1], k_off[s], k_off[s + 1]
+    nan = lambda t: bool(torch.isnan(t).all())
+
+    def others(got):
+        for t, ref in zip(got, clean):
+            kept = torch.ones_like(ref, dtype=torch.bool)
+            first, last = (a, b) if ref.shape[0] == rows and ref.shape[1] == heads else (c, e)
+            kept[first:last, :group if ref.shape[1] == heads else 1] = False
+            assert torch.equal(t[kept], ref[kept])
+    # a row: it sees the keys up to its own place
+    i = b - 10
+    last = c + (i - a) + (e - c) - (b - a)
+    was = q[i, 0].clone()
+    q[i, 0, dim // 2] = math.nan
+    y, lse, dq, dk, dv = got = both(q, k, v, dy, **how)
+    q[i, 0] = was
+    assert nan(y[i, 0]) and nan(lse[i, 0]) and nan(dq[i, 0]) and nan(dk[c:last + 1, 0]) and nan(dv[c:last + 1, 0])
+    # the rows of this head and sequence beside it are what they were but for roundings (when sums are brought to a new reference is up to all rows of a tile)
+    rest = torch.arange(a, b, device="cuda") != i
+    near = lambda x, ref: float((x.float() - ref.float()).abs().max()) <= 2.0 ** -5
+    assert near(y[a:b, 0][rest], clean[0][a:b, 0][rest]) and near(lse[a:b, 0][rest], clean[1][a:b, 0][rest])
+    others(got)
+    # a key
+    j = e - 20
+    k[j, 0, 1] = math.nan
+    y, lse, dq, dk, dv = got = both(q, k, v, dy, **how)
+    first = b - 20                                         # (the last row meets the last key)
+    assert nan(y[first:b, :group]) and nan(lse[first:b, :group]) and nan(dq[first:b, :group]) and nan(dk[j, 0])
+    assert near(y[a:first, :group], clean[0][a:first, :group]) and near(lse[a:first, :group], clean[1][a:first, :group])
+    others(got)
+    # all keys: no score is a number
+    k[c:e, 0] = math.nan
+    y, lse, dq, dk, dv = got = both(q, k, v, dy, **how)
+    assert nan(y[a:b, :group]) and nan(lse[a:b, :group]) and nan(dq[a:b, :group]) and nan(dk[c:e, 0])
+    others(got)
+
+
+def test_a_cap_whose_inverse_overflows():
+    """2 scale / cap beyond 32 bits: a score of zero is zero, the others are at the cap, too small to count: all keys weigh the same."""
+    for dtype in TYPES:
+        q, k = torch.zeros(3, 1, 64, device="cuda", dtype=dtype), normal(gen(44), dtype, 50, 1, 64)
+        q[1, 0, 0] = 1.0
+        v = normal(gen(45), dtype, 50, 1, 64)
+        y, lse = B.alpa_attention_forward(q, k, v, cap=1e-39, scale=1.0, keep_lse=True)
+        mean = v[:, 0].to(D).mean(0)
+        # 50 values in 32 bits, one rounding
+        assert bool(((y[:, 0].to(D) - mean).abs() <= 60 * 2.0 ** -23 * v.to(D).abs().amax() + {BF16: 2.0 ** -8, F16: 2.0 ** -11, F32: 0.0}[dtype] * mean.abs()).all())
+        assert bool(((lse - math.log(50.0)).abs() <= 1e-5).all())
