@@ -208,13 +208,14 @@ __device__ __forceinline__ int limit_of(const AttentionArgs &g, const Span &s, i
 }
 
 // A capped score from the product of q and k, in units of the binary logarithm, and the slope of the cap.  1 - tanh(x) = 2 / (1 + exp(2 x)) = 2 u, and the
-// slope is 4 u^2 exp(2 x), which keeps its relative error where the cap is reached; tanh is off by a few units of 2^-24 absolute so, which float32 gets better.
+// slope is 4 u^2 exp(2 x), which keeps its relative error where the cap is reached; tanh is off by a few units of 2^-24 absolute so, and the score by as much of the cap.
+// EXACT, for float32 and for caps above 256 (where that would be more than 2^-15 of a weight): the score's error goes with the score.
 // The score itself takes the exponential as it is, infinite ones (u = 0) and no numbers among them: a minimum, which gives the other operand for a NaN, may
 // only stand in the slope.
-template <class T>
+template <bool EXACT>
 __device__ __forceinline__ float capped(const AttentionArgs &g, float s, float &bent)
 {
-    if constexpr (sizeof(T) == 4) {
+    if constexpr (EXACT) {
         const float x = s * g.scale / g.cap, u = 1.0f / (1.0f + expf(2.0f * fabsf(x)));
         bent = 4.0f * u * (1.0f - u);
         return g.cap * tanhf(x) * LOG2E;
@@ -402,9 +403,10 @@ struct Nothing {
 };
 
 // One row a lane, twice: what has been seen of the keys so far.
-template <class T, int DB, bool EXTRA>
+template <class T, int DB, bool EXTRA, bool FAR_CAP>
 struct Running {
     using R = Rows<T, DB>;
+    static constexpr bool EXACT = sizeof(T) == 4 || FAR_CAP;
     u32x4 q[R::STEPS];
     f32x16 y[DB];
     float top, sum;                 // in units of the binary logarithm; of this lane's half of the keys
@@ -480,7 +482,7 @@ struct Running {
             for (int b = 0; b < NB; ++b) {
                 if (g.cap != 0.0f) {
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) s[b][i] = capped<T>(g, s[b][i], bent);
+                    for (int i = 0; i < 16; ++i) s[b][i] = capped<EXACT>(g, s[b][i], bent);
                 } else {
 #pragma unroll
                     for (int i = 0; i < 16; ++i) s[b][i] *= g.scale * LOG2E;
@@ -614,7 +616,7 @@ struct KeyParts {
 };
 
 // Many rows: a wave has 32 packed rows, the waves share tiles of keys, of which one is worked on and the next one under way.
-template <class T, int DB, bool EXTRA, int WAVES>
+template <class T, int DB, bool EXTRA, int WAVES, bool FAR_CAP>
 __global__ __launch_bounds__(WAVES * 64, 2) void attention_kernel(const AttentionArgs g)
 {
     using R = Rows<T, DB>;
@@ -638,7 +640,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attention_kernel(const Attentio
         k.load(lds_at(lds), from, s.m);
         v.load(lds_at(lds) + HALF, from, s.m);
     }
-    Running<T, DB, EXTRA> run;
+    Running<T, DB, EXTRA, FAR_CAP> run;
     run.begin(g, s, kv, r);
     const typename R::Place place;
     const int mine = __builtin_amdgcn_readlane(run.limit, 31);
@@ -749,7 +751,7 @@ __device__ __forceinline__ void join_waves(char *lds, f32x16 (&acc)[DB], float b
     }
 }
 
-template <class T, int DB, bool EXTRA>
+template <class T, int DB, bool EXTRA, bool FAR_CAP>
 __global__ __launch_bounds__((FewShape<T, DB>::WAVES * 64)) void attention_few_kernel(const AttentionArgs g)
 {
     using F = FewShape<T, DB>;
@@ -785,7 +787,7 @@ __global__ __launch_bounds__((FewShape<T, DB>::WAVES * 64)) void attention_few_k
             k.load(mine, j1, s.m);
             v.load(mine + F::TILE, j1, s.m);
         }
-        Running<T, DB, EXTRA> run;
+        Running<T, DB, EXTRA, FAR_CAP> run;
         run.begin(g, s, kv, r);
         if constexpr (F::STAGES == 1) {
             in_turn(k, mine, v, mine + F::TILE, j1, to, 32 * WAVES, s.m, [&](int j0, auto between) { run.template step<1>(g, own, own + F::TILE, place, j0, between); });
@@ -878,9 +880,10 @@ template <class T>
 __device__ __forceinline__ float first_factor() { return std::is_same_v<T, f16> ? 0x1p60f : 1.0f; }
 
 // One row a lane, twice: what of its gradient the keys so far have given; the sum of dy y on the way.
-template <class T, int DB, bool EXTRA>
+template <class T, int DB, bool EXTRA, bool FAR_CAP>
 struct Backward {
     using R = Rows<T, DB>;
+    static constexpr bool EXACT = sizeof(T) == 4 || FAR_CAP;
     u32x4 q[R::STEPS], dy[R::STEPS];
     f32x16 dq[DB];
     float delta, lse, slope, by;
@@ -942,7 +945,7 @@ struct Backward {
 #pragma unroll
                 for (int j = 0; j < 16; ++j) {
                     float bent;
-                    a[j] = capped<T>(g, a[j], bent);
+                    a[j] = capped<EXACT>(g, a[j], bent);
                     d[j] = (d[j] - delta) * bent;
                 }
             } else {
@@ -986,7 +989,7 @@ struct Backward {
 };
 
 // dq of many rows: a wave has 32 packed rows, the waves share tiles of keys.
-template <class T, int DB, bool EXTRA, int WAVES>
+template <class T, int DB, bool EXTRA, int WAVES, bool FAR_CAP>
 __global__ __launch_bounds__(WAVES * 64, sizeof(T) == 2 && DB <= 4 ? 2 : 1) void attention_dq_kernel(const AttentionArgs g)
 {
     using R = Rows<T, DB>;
@@ -1011,7 +1014,7 @@ __global__ __launch_bounds__(WAVES * 64, sizeof(T) == 2 && DB <= 4 ? 2 : 1) void
         k.load(lds_at(lds), from, s.m);
         v.load(lds_at(lds) + HALF, from, s.m);
     }
-    Backward<T, DB, EXTRA> run;
+    Backward<T, DB, EXTRA, FAR_CAP> run;
     run.begin(g, s, kv, r);
     if (!wanted) return;
     const int mine = __builtin_amdgcn_readlane(run.limit, 31);
@@ -1030,7 +1033,7 @@ __global__ __launch_bounds__(WAVES * 64, sizeof(T) == 2 && DB <= 4 ? 2 : 1) void
 }
 
 // dq of few rows: as in attention_few_kernel, the waves have the same 32 packed rows and take tiles of 32 keys in turn.
-template <class T, int DB, bool EXTRA>
+template <class T, int DB, bool EXTRA, bool FAR_CAP>
 __global__ __launch_bounds__((FewShape<T, DB>::WAVES * 64)) void attention_dq_few_kernel(const AttentionArgs g)
 {
     using F = FewShape<T, DB>;
@@ -1058,7 +1061,7 @@ __global__ __launch_bounds__((FewShape<T, DB>::WAVES * 64)) void attention_dq_fe
         v.load(mine + F::TILE, j1, s.m);
         k.load(mine, j1, s.m);
     }
-    Backward<T, DB, EXTRA> run;
+    Backward<T, DB, EXTRA, FAR_CAP> run;
     run.begin(g, s, kv, r);
     if (!wanted) return;
     const typename R::Place place;
@@ -1087,11 +1090,12 @@ __global__ __launch_bounds__((FewShape<T, DB>::WAVES * 64)) void attention_dq_fe
 
 // dk and dv: a wave has 32 keys, the waves share tiles of 32 packed rows of the kv head.
 // DK, DV: which of the two; heads of 256 elements have no registers for both at once.
-template <class T, int DB, bool EXTRA, int WAVES, bool DK, bool DV>
+template <class T, int DB, bool EXTRA, int WAVES, bool DK, bool DV, bool FAR_CAP>
 __global__ __launch_bounds__(WAVES * 64, sizeof(T) == 2 && (DB <= 4 || !DK) ? 2 : 1) void attention_dkv_kernel(const AttentionArgs g)
 {
     using R = Rows<T, DB>;
     constexpr int TILE = WAVES == 8 ? 64 : 32, NT = WAVES * 64, HALF = TILE * R::ROWB;
+    constexpr bool EXACT = sizeof(T) == 4 || FAR_CAP;
     // (in registers the keys would leave room for one wave a SIMD)
     constexpr bool K_IN_LDS = sizeof(T) == 2 && DB == 4;
     struct RowsInfo { float lse[TILE], delta[TILE], slope[TILE]; int limit[TILE], place[TILE]; };
@@ -1194,7 +1198,7 @@ __global__ __launch_bounds__(WAVES * 64, sizeof(T) == 2 && (DB <= 4 || !DK) ? 2 
 #pragma unroll
                     for (int j = 0; j < 16; ++j) {
                         float bent;
-                        a[j] = capped<T>(g, a[j], bent);
+                        a[j] = capped<EXACT>(g, a[j], bent);
                         d[j] = (d[j] - info.delta[at + block_row(j, h)]) * bent;
                     }
                 } else {
@@ -1368,27 +1372,27 @@ AttentionArgs with_unit(int few, AttentionArgs g)
     g.unit = few ? 32 * FewShape<T, DB>::WAVES : 64;
     return g;
 }
-template <class T, int DB, bool EXTRA>
+template <class T, int DB, bool EXTRA, bool FAR_CAP>
 hipError_t launch_rows(hipStream_t st, int few, const AttentionArgs &args)
 {
     const AttentionArgs g = with_unit<T, DB>(few, args);
     const hipError_t e = in_launches(g, (g.tiles ? g.tiles : (int64_t)g.seqs + 1) * g.kv_heads, [&](const AttentionArgs &p, dim3 grid) {
-        if (few) attention_few_kernel<T, DB, EXTRA><<<grid, FewShape<T, DB>::WAVES * 64, 0, st>>>(p);
-        else attention_kernel<T, DB, EXTRA, 4><<<grid, 256, 0, st>>>(p);
+        if (few) attention_few_kernel<T, DB, EXTRA, FAR_CAP><<<grid, FewShape<T, DB>::WAVES * 64, 0, st>>>(p);
+        else attention_kernel<T, DB, EXTRA, 4, FAR_CAP><<<grid, 256, 0, st>>>(p);
     });
     return e != hipSuccess || g.splits == 1 ? e : launch_join<T, false>(st, few, g);
 }
-template <class T, int DB, bool EXTRA>
+template <class T, int DB, bool EXTRA, bool FAR_CAP>
 hipError_t launch_dq(hipStream_t st, int few, const AttentionArgs &args)
 {
     const AttentionArgs g = with_unit<T, DB>(few, args);
     const hipError_t e = in_launches(g, (int64_t)g.tiles * g.kv_heads, [&](const AttentionArgs &p, dim3 grid) {
-        if (few) attention_dq_few_kernel<T, DB, EXTRA><<<grid, FewShape<T, DB>::WAVES * 64, 0, st>>>(p);
-        else attention_dq_kernel<T, DB, EXTRA, 4><<<grid, 256, 0, st>>>(p);
+        if (few) attention_dq_few_kernel<T, DB, EXTRA, FAR_CAP><<<grid, FewShape<T, DB>::WAVES * 64, 0, st>>>(p);
+        else attention_dq_kernel<T, DB, EXTRA, 4, FAR_CAP><<<grid, 256, 0, st>>>(p);
     });
     return e != hipSuccess || g.splits == 1 || !g.out.p ? e : launch_join<T, true>(st, few, g);
 }
-template <class T, int DB, bool EXTRA>
+template <class T, int DB, bool EXTRA, bool FAR_CAP>
 hipError_t launch_dkv(hipStream_t st, const AttentionArgs &g)
 {
     const int64_t tiles = (int64_t)g.tiles * g.kv_heads;
@@ -1396,14 +1400,14 @@ hipError_t launch_dkv(hipStream_t st, const AttentionArgs &g)
         if constexpr (DB <= 4) {
             if constexpr (sizeof(T) == 2) {
                 if (p.key_tile == 256) {
-                    attention_dkv_kernel<T, DB, EXTRA, 8, true, true><<<grid, 512, 0, st>>>(p);
+                    attention_dkv_kernel<T, DB, EXTRA, 8, true, true, FAR_CAP><<<grid, 512, 0, st>>>(p);
                     return;
                 }
             }
-            attention_dkv_kernel<T, DB, EXTRA, 4, true, true><<<grid, 256, 0, st>>>(p);
+            attention_dkv_kernel<T, DB, EXTRA, 4, true, true, FAR_CAP><<<grid, 256, 0, st>>>(p);
         } else {
-            if (p.out.p) attention_dkv_kernel<T, DB, EXTRA, 4, true, false><<<grid, 256, 0, st>>>(p);
-            if (p.out2.p) attention_dkv_kernel<T, DB, EXTRA, 4, false, true><<<grid, 256, 0, st>>>(p);
+            if (p.out.p) attention_dkv_kernel<T, DB, EXTRA, 4, true, false, FAR_CAP><<<grid, 256, 0, st>>>(p);
+            if (p.out2.p) attention_dkv_kernel<T, DB, EXTRA, 4, false, true, FAR_CAP><<<grid, 256, 0, st>>>(p);
         }
     });
     if (e != hipSuccess || g.splits == 1) return e;
@@ -1413,12 +1417,16 @@ hipError_t launch_dkv(hipStream_t st, const AttentionArgs &g)
     });
 }
 
-#define ALPA_BY_DIM(call, T, g, ...)                                                                           \
-    switch (dim_blocks((g).dim)) {                                                                             \
-    case 2: return extra(g) ? call<T, 2, true>(__VA_ARGS__) : call<T, 2, false>(__VA_ARGS__);                  \
-    case 3: return extra(g) ? call<T, 3, true>(__VA_ARGS__) : call<T, 3, false>(__VA_ARGS__);                  \
-    case 4: return extra(g) ? call<T, 4, true>(__VA_ARGS__) : call<T, 4, false>(__VA_ARGS__);                  \
-    default: return extra(g) ? call<T, 8, true>(__VA_ARGS__) : call<T, 8, false>(__VA_ARGS__);                 \
+// (a cap far above the scores is compiled apart: in one kernel with the others it took 20 to 45 registers more, and a wave a SIMD of dq)
+inline bool far_cap(const AttentionArgs &g) { return g.cap > 256.0f; }
+#define ALPA_BY_CAP(call, T, DB, g, ...) \
+    (!extra(g) ? call<T, DB, false, false>(__VA_ARGS__) : far_cap(g) ? call<T, DB, true, sizeof(T) == 2>(__VA_ARGS__) : call<T, DB, true, false>(__VA_ARGS__))
+#define ALPA_BY_DIM(call, T, g, ...)                                   \
+    switch (dim_blocks((g).dim)) {                                     \
+    case 2: return ALPA_BY_CAP(call, T, 2, g, __VA_ARGS__);            \
+    case 3: return ALPA_BY_CAP(call, T, 3, g, __VA_ARGS__);            \
+    case 4: return ALPA_BY_CAP(call, T, 4, g, __VA_ARGS__);            \
+    default: return ALPA_BY_CAP(call, T, 8, g, __VA_ARGS__);           \
     }
 
 }  // namespace alpa

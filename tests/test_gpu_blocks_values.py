@@ -74,6 +74,35 @@ def test_a_score_that_is_no_number_stays_none(dtype, shape, cap, slopes):
     others(got)
 
 
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("rows, heads, kv", [(90, 4, 2), (2000, 20, 20)])
+@pytest.mark.parametrize("cap", [1e5, 1e8, 3e38])
+def test_caps_far_above_the_scores(dtype, rows, heads, kv, cap):
+    """Scores of up to 8 under a cap of 1e5 and more are what they are without one to 8^3 / (3 cap^2) = 2e-8, which the bounds without a cap leave room for (4 * 2^-23 a score).
+    The slope of the cap, 1 to 2e-8, is known to 6 units of 2^-23, a hundredth of the roundings to 16 bits that the bounds of the gradients count, and a sixtieth of the products'
+    of 64 terms in 32 bits."""
+    g = gen(42)
+    q, k, v, dy = normal(g, dtype, rows, heads, 64), normal(g, dtype, rows, kv, 64), normal(g, dtype, rows, kv, 64), normal(g, dtype, rows, heads, 64)
+    assert float(torch.matmul(q[:, :1].transpose(0, 1).float(), k[:, 0].float().t()).abs().max()) / 8.0 < 8.0
+    ref = C.attention(q, k, v, dy, causal=True)
+    for name, got in zip(("y", "lse", "dq", "dk", "dv"), both(q, k, v, dy, causal=True, cap=cap)):
+        value, bound = ref[name]
+        C.within(name, got, (value, bound * (1.02 if name in ("dq", "dk") else 1.0)))
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("cap", [1e-30, 1e-3, 0.5, 255.0, 257.0, 1000.0])
+@pytest.mark.parametrize("reach", [0.2, 3.0])
+def test_caps_of_all_sizes(dtype, cap, reach):
+    """Scores from far below the cap to several times it."""
+    g = gen(43)
+    q, k, v, dy = (normal(g, dtype, 70, n, 64) for n in (4, 2, 2, 4))
+    how = dict(causal=True, cap=cap, scale=cap * reach / 8.0)
+    ref = C.attention(q, k, v, dy, **how)
+    for name, got in zip(("y", "lse", "dq", "dk", "dv"), both(q, k, v, dy, **how)):
+        C.within(name, got, ref[name])
+
+
 def test_a_cap_whose_inverse_overflows():
     """2 scale / cap beyond 32 bits: a score of zero is zero, the others are at the cap, too small to count: all keys weigh the same."""
     for dtype in TYPES:
