@@ -63,8 +63,8 @@ int alpa_attention_forward(const alpa_attention_t *how, alpa_heads_t q, alpa_hea
  * Its gradients, any of dq, dk, dv NULL (p NULL).  Keys have to be packed (k_step 1).  Slopes are constants.
  *     P = exp(a - lse),  dA = P (dy . v - dy . y),  dR = dA (1 - tanh^2)
  *     dv_j = sum_i P_ij dy_i,   dq_i = scale sum_j dR_ij k_j,   dk_j = scale sum_i dR_ij q_i    (kv heads: over their query heads too)
- * P and dR are rounded to `dtype` as operands of the products (dR in float16 times powers of two that keep it from overflowing and small ones
- * from losing bits).  Rows and keys of no sequence get zeros.
+ * P and dR are rounded to `dtype` as operands of the products (in float16 P times 2^14, so that the weights of many keys keep their bits, dR times powers of two that keep it
+ * from overflowing and small ones from losing bits).  Rows and keys of no sequence get zeros.
  */
 int64_t alpa_attention_backward_work(const alpa_attention_t *how, alpa_heads_t dy, alpa_heads_t q, alpa_heads_t k,
                                      alpa_heads_t v, alpa_heads_t y);

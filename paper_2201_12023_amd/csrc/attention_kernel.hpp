@@ -1096,6 +1096,9 @@ __global__ __launch_bounds__(WAVES * 64, sizeof(T) == 2 && (DB <= 4 || !DK) ? 2 
     using R = Rows<T, DB>;
     constexpr int TILE = WAVES == 8 ? 64 : 32, NT = WAVES * 64, HALF = TILE * R::ROWB;
     constexpr bool EXACT = sizeof(T) == 4 || FAR_CAP;
+    // Weights are up to 1, and 1 / keys where rows weigh their keys alike, less than float16's smallest normal number from 2^14 keys on: there they, and dR with them,
+    // are kept times 2^14.
+    constexpr float WEIGHT_BITS = std::is_same_v<T, f16> ? 14.0f : 0.0f, WEIGHT_UNIT = std::is_same_v<T, f16> ? 0x1p-14f : 1.0f;
     // (in registers the keys would leave room for one wave a SIMD)
     constexpr bool K_IN_LDS = sizeof(T) == 2 && DB == 4;
     struct RowsInfo { float lse[TILE], delta[TILE], slope[TILE]; int limit[TILE], place[TILE]; };
@@ -1155,7 +1158,7 @@ __global__ __launch_bounds__(WAVES * 64, sizeof(T) == 2 && (DB <= 4 || !DK) ? 2 
         if (threadIdx.x >= TILE) return;
         const int t = threadIdx.x;
         const bool none = r0 + t >= to;
-        info.lse[t] = none || lse_next == -INFINITY ? INFINITY : lse_next * LOG2E;
+        info.lse[t] = none || lse_next == -INFINITY ? INFINITY : fmaf(lse_next, LOG2E, -WEIGHT_BITS);
         info.delta[t] = none ? 0.0f : delta_next;
         info.limit[t] = limit_of(g, s, row_next);
         info.place[t] = row_next + s.ahead;
@@ -1247,16 +1250,17 @@ __global__ __launch_bounds__(WAVES * 64, sizeof(T) == 2 && (DB <= 4 || !DK) ? 2 
         if (r0 > from) put(r0 - TILE, infos[here ^ 1]);
     }
     if (key >= s.m) return;
+    const float dk_unit = g.scale / by * WEIGHT_UNIT;
     const int64_t row = s.k_first + key;
     if (part.count > 1) {
         const int64_t at = ((int64_t)index * g.k_rows + row) * g.kv_heads + kv;
         const int wide = (g.dim & 3) == 0;
-        if constexpr (DK) if (g.out.p) store_head<float, DB>((char *)(g.part + at * g.dim), dk, g.scale / by, g.dim, wide);
-        if constexpr (DV) if (g.out2.p) store_head<float, DB>((char *)(g.part2 + at * g.dim), dv, 1.0f, g.dim, wide);
+        if constexpr (DK) if (g.out.p) store_head<float, DB>((char *)(g.part + at * g.dim), dk, dk_unit, g.dim, wide);
+        if constexpr (DV) if (g.out2.p) store_head<float, DB>((char *)(g.part2 + at * g.dim), dv, WEIGHT_UNIT, g.dim, wide);
         return;
     }
-    if constexpr (DK) if (g.out.p) store_head<T, DB>(g.out.p + row * g.out.row + kv * g.out.head, dk, g.scale / by, g.dim, g.wide);
-    if constexpr (DV) if (g.out2.p) store_head<T, DB>(g.out2.p + row * g.out2.row + kv * g.out2.head, dv, 1.0f, g.dim, g.wide);
+    if constexpr (DK) if (g.out.p) store_head<T, DB>(g.out.p + row * g.out.row + kv * g.out.head, dk, dk_unit, g.dim, g.wide);
+    if constexpr (DV) if (g.out2.p) store_head<T, DB>(g.out2.p + row * g.out2.row + kv * g.out2.head, dv, WEIGHT_UNIT, g.dim, g.wide);
 }
 
 // Rows of tiles whose keys went in several parts, eight a workgroup and a wave each: y and lse, each part brought to the common maximum, or (SUM) dq.  Four

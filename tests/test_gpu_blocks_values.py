@@ -114,3 +114,20 @@ def test_a_cap_whose_inverse_overflows():
         # 50 values in 32 bits, one rounding
         assert bool(((y[:, 0].to(D) - mean).abs() <= 60 * 2.0 ** -23 * v.to(D).abs().amax() + {BF16: 2.0 ** -8, F16: 2.0 ** -11, F32: 0.0}[dtype] * mean.abs()).all())
         assert bool(((lse - math.log(50.0)).abs() <= 1e-5).all())
+
+
+@pytest.mark.parametrize("keys, dim", [(100003, 64), ((1 << 25) + 3, 8)])
+def test_gradients_of_weights_that_float16_does_not_hold(keys, dim):
+    """Rows of zeros weigh all keys alike, by 1 / keys, which float16 has with 8 bits (1e-5) or not at all (2^-25).  dv = sum(dy) / keys for each key, of an ordinary size.
+    A weight's exponent, up to 26, is off by 4 units of 2^-23 of it: 1.3e-5; the weight is rounded once and dv once, 2^-11 each; 32 terms are summed in 32 bits."""
+    g, rows = gen(46), 32
+    k, v = normal(g, F16, keys, 1, dim), normal(g, F16, keys, 1, dim)
+    q = torch.zeros(rows, 1, dim, device="cuda", dtype=F16)
+    dy = ((1.0 + torch.rand(rows, 1, dim, device="cuda", generator=g)) * (keys / 4096.0)).clamp(max=30000.0).to(F16)
+    y, lse = B.alpa_attention_forward(q, k, v, keep_lse=True)
+    assert bool(((lse - math.log(keys)).abs() <= 1e-4).all())
+    dv = B.alpa_attention_backward(dy, q, k, v, y, lse, need=("v",))[2]
+    ref = dy[:, 0].to(D).sum(0) / keys
+    assert float(ref.min()) > 2.0 ** -9
+    off = ((dv[:, 0].to(D) - ref).abs() / ref).amax()
+    assert float(off) <= 2 * 2.0 ** -11 + 1e-4, float(off)
