@@ -435,6 +435,10 @@ struct Running {
         asm volatile("" ::"v"(slope));
     }
 
+    // Float16 has exponentials up to 2^15, and 2^-14 as its smallest normal number: with 2^12 for the largest one, weights of 2^-26 of it keep their bits (with 1, those
+    // below 2^-25 were zeros, however many).
+    static constexpr float LEAD = std::is_same_v<T, f16> ? 3.0f : 8.0f, ROOM = std::is_same_v<T, f16> ? 12.0f : 0.0f;
+
     // The fragments that products of 16-bit types read go through two sets of DB registers of four, in the order of their use: a set is read from LDS
     // while the products of the other one run (read as they were needed, a product waited for LDS three times as long as it takes).
     static constexpr bool AHEAD = sizeof(T) == 2 && DB <= 4;
@@ -505,9 +509,10 @@ struct Running {
 #pragma unroll
             for (int i = 0; i < 16; ++i) most = fmaxf(most, s[b][i]);
         most = max_halves(most) * by;
-        // Exponents are taken from a reference that follows the maximum once it is 8 ahead: exponentials up to 2^8 round to the type like those up to 1
-        if (__any(most > top + 8.0f)) {
-            const float next = fmaxf(top, most), down = exp2f(top - (next == -INFINITY ? 0.0f : next));
+        // Exponents are taken from a reference, ROOM below a maximum, that follows the maximum once that is LEAD ahead: exponentials up to 2^(LEAD + ROOM) round to the type like
+        // those up to 1
+        if (__any(most > top + (LEAD + ROOM))) {
+            const float next = fmaxf(top, most - ROOM), down = exp2f(top - (next == -INFINITY ? 0.0f : next));
 #pragma unroll
             for (int b = 0; b < DB; ++b)
 #pragma unroll

@@ -131,3 +131,20 @@ def test_gradients_of_weights_that_float16_does_not_hold(keys, dim):
     assert float(ref.min()) > 2.0 ** -9
     off = ((dv[:, 0].to(D) - ref).abs() / ref).amax()
     assert float(off) <= 2 * 2.0 ** -11 + 1e-4, float(off)
+
+
+@pytest.mark.parametrize("rows", [3, 76900])
+def test_many_small_weights_beside_a_large_one_in_float16(rows):
+    """One key has a score of 0, the others 17.5 less: each weighs 2^-25.2, 131071 of them 0.0033 together, which is y where the first key's value is 0 and theirs 1.
+    The weights are rounded once (2^-11), y once; their exponents, up to 26, are off by 4 units of 2^-23 of them; and what y is divided by, a sum in 32 bits, may lose the
+    small weights beside the large one, 0.0033 of it.  With few rows the weights are relative to each wave's own largest, with many rows to the first key's."""
+    keys = 1 << 17
+    q, k = torch.zeros(rows, 1, 8, device="cuda", dtype=F16), torch.zeros(keys, 1, 8, device="cuda", dtype=F16)
+    q[..., 0] = 1.0
+    k[1:, 0, 0] = -17.5
+    v = torch.ones(keys, 1, 8, device="cuda", dtype=F16)
+    v[0] = 0.0
+    y = B.alpa_attention_forward(q, k, v, scale=1.0)
+    total = (keys - 1) * math.exp(-17.5)
+    ref = total / (1.0 + total)
+    assert float((y.to(D) - ref).abs().max()) <= ref * (2 * 2.0 ** -11 + total + 2e-5)
