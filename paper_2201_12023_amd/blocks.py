@@ -121,6 +121,13 @@ def _new(t):
     return _NONE if t is None else alpa_heads_t(t.data_ptr(), t.shape[1] * t.shape[2], t.shape[2])
 
 
+def _written(*tensors):
+    """Tells torch's graph that given tensors were written to, so that it refuses a backward pass that needs what they held (1 us of the host's time each)."""
+    for t in tensors:
+        if t is not None:
+            torch.autograd.graph.increment_version(t)
+
+
 # ------------------------------------------------------------------ attention
 
 def _how(q, k, offsets, k_offsets, scale, cap, slopes, causal, prefix):
@@ -231,6 +238,8 @@ def _attention_backward_on(s, dy, q, k, v, y, lse, offsets, k_offsets, scale, ca
         results = [_NONE if t is None else _heads("d" + name, t, size, dtype, device) for t, (name, size) in zip(grads, sizes)]
     held, p, n = _l._work(L.alpa_attention_backward_work(a, *mats), device)
     binding._check(L.alpa_attention_backward(a, *mats, l, *results, p, n, s))
+    if out is not None:
+        _written(*grads)
     return grads
 
 
@@ -257,6 +266,8 @@ def _rotary_on(s, name, x, positions, frequencies, interleaved, scale, out):
     y = x.new_empty(shape) if out is None else out
     ym = _new(y) if out is None else _heads("out", out, shape, dtype, device)
     binding._check(getattr(L, name)(_l._type(x), *shape, 2 * half, interleaved, scale, p, f, xm, ym, s))
+    if out is not None:
+        _written(out)
     return y
 
 

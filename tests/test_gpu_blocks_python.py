@@ -1,0 +1,37 @@
+"""What torch is told by the calls of ``blocks``: tensors that were written to."""
+import pytest
+import torch
+
+from paper_2201_12023_amd import blocks as B
+from tests.layer_cases import gen, normal
+
+pytestmark = pytest.mark.gpu
+BF16 = torch.bfloat16
+
+
+def test_what_is_written_to_cannot_be_what_the_graph_has_saved():
+    """A tensor that a product has kept for its gradient is turned in place, or gets a gradient: torch refuses the product's backward pass, as after its own calls in place."""
+    g = gen(51)
+    f, pos = B.alpa_rotary_frequencies(16), torch.arange(20, device="cuda")
+    q, k, v, dy = (normal(g, BF16, 20, n, 16) for n in (4, 2, 2, 4))
+    y, lse = B.alpa_attention_forward(q, k, v, causal=True, keep_lse=True)
+    room = normal(g, BF16, 20, 8, 16)
+    parts = room[:, :4], room[:, 4:6], room[:, 6:]
+    for call in (lambda: B.alpa_rotary_forward(parts[0], pos, f, out=parts[0]), lambda: B.alpa_rotary_backward(q, pos, f, out=parts[0]),
+                 lambda: B.alpa_attention_backward(dy, q, k, v, y, lse, causal=True, out=parts),
+                 lambda: B.alpa_attention_backward(dy, q, k, v, y, lse, causal=True, need=("v",), out=(None, None, parts[2]))):
+        w = torch.ones_like(room, requires_grad=True)
+        loss = (room * w).sum()
+        call()
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            loss.backward()
+    # results of their own, and tensors that are only read, are not touched
+    w = torch.ones_like(room, requires_grad=True)
+    loss = (room * w).sum()
+    B.alpa_rotary_forward(room, pos, f)
+    B.alpa_attention_backward(dy, parts[0], parts[1], parts[2], y, lse, causal=True)
+    loss.backward()
+    assert torch.equal(w.grad, room)
+    with torch.inference_mode():
+        t = q.clone()
+        assert B.alpa_rotary_forward(t, pos, f, out=t) is t
