@@ -7,8 +7,8 @@ be any distance apart, so that queries, keys and values may be slices of one pro
 
 The forward calls can be differentiated: where an argument requires a gradient their results are part of torch's graph, and its backward pass makes
 the calls of this module.  What is kept for those (lse; mean and rstd) has no gradient: a loss that depends on it raises an error in the backward pass.
-The backward calls themselves record nothing.  All calls may be recorded into a HIP graph; a backward pass of torch's graph only if that graph was built in the
-same recording.
+The backward calls themselves record nothing.  There are no forward-mode derivatives: tensors that have one are refused.  All calls may be recorded into a
+HIP graph; a backward pass of torch's graph only if that graph was built in the same recording.
 """
 from __future__ import annotations
 
@@ -213,6 +213,7 @@ def alpa_attention_backward(dy, q, k, v, y, lse, offsets=None, k_offsets=None, s
                             need=("q", "k", "v"), out=None, stream=None):
     """(dq, dk, dv) of alpa_attention_forward, None for those not in ``need``; y and lse are its results.  ``out``: three tensors to put them in (None where
     one is not needed), such as the slices of one product's gradient."""
+    _l._no_tangents(dy, q, k, v, y, lse)
     if not set(need) <= {"q", "k", "v"}:
         raise ValueError(f"need is {need!r}: names out of 'q', 'k', 'v' expected")
     if k_offsets is not None and k_offsets.dim() == 2:
@@ -289,6 +290,7 @@ class _Rotary(torch.autograd.Function):
 def alpa_rotary_forward(x, positions, frequencies, interleaved=False, scale=1.0, out=None, stream=None):
     """x [rows, heads, dim] with the first 2 * len(frequencies) elements of each head turned by positions (int64 [rows]) times frequencies (float64, radians) and
     scaled: pairs (t, t + half), or (2 t, 2 t + 1) if ``interleaved``.  ``out``: where to put it, x itself to turn it in place."""
+    _l._no_tangents(frequencies)
     if _l._recorded(x, out):
         if out is not None:
             raise ValueError("a result that is given cannot be recorded")
@@ -298,6 +300,7 @@ def alpa_rotary_forward(x, positions, frequencies, interleaved=False, scale=1.0,
 
 def alpa_rotary_backward(dy, positions, frequencies, interleaved=False, scale=1.0, out=None, stream=None):
     """dx: the same turned the other way."""
+    _l._no_tangents(dy, frequencies)
     return _rotary("alpa_rotary_backward", dy, positions, frequencies, interleaved, scale, out, stream)
 
 
@@ -347,6 +350,7 @@ def alpa_norm_forward(x, weight=None, bias=None, eps=1e-5, keep=False, stream=No
 
 def alpa_norm_backward(dy, x, mean, rstd, weight=None, need=("x", "weight", "bias"), stream=None):
     """(dx, dweight, dbias) of alpa_norm_forward, None for those not in ``need``."""
+    _l._no_tangents(dy, x, mean, rstd, weight)
     if not set(need) <= {"x", "weight", "bias"}:
         raise ValueError(f"need is {need!r}: names out of 'x', 'weight', 'bias' expected")
     return _on(_norm_backward_on, x, stream, dy, x, mean, rstd, weight, need)

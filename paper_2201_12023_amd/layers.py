@@ -9,13 +9,14 @@ any distance apart.
 
 The forward calls can be differentiated: where an argument requires a gradient their results are part of torch's graph, and its backward
 pass makes the calls of this module.  What is kept for those, z and lse, can not be: a loss that depends on them raises an error in the
-backward pass.  The backward calls themselves record nothing.
+backward pass.  The backward calls themselves record nothing.  There are no forward-mode derivatives: tensors that have one are refused.
 """
 from __future__ import annotations
 
 import ctypes
 
 import torch
+from torch.autograd import forward_ad
 from torch.autograd.function import once_differentiable
 
 from . import binding
@@ -179,6 +180,7 @@ def _forward(x, w, offsets, bias, residual, act, keep_z, stream):
 
 
 def _backward(dy, x, w, offsets, z, act, need, stream):
+    _no_tangents(dy, x, w, z)
     L, d = load(), _type(dy)
     if not set(need) <= {"x", "w", "bias"}:
         raise ValueError(f"need is {need!r}: names out of 'x', 'w', 'bias' expected")
@@ -208,7 +210,15 @@ def _backward(dy, x, w, offsets, z, act, need, stream):
     return dx, dw, db
 
 
+def _no_tangents(*tensors):
+    """Refuses tensors of forward-mode differentiation: the library would take their values and drop the derivatives."""
+    if forward_ad._current_level >= 0 and any(t is not None and forward_ad.unpack_dual(t).tangent is not None for t in tensors):
+        raise RuntimeError("forward-mode derivatives are not computed: torch.autograd.forward_ad.unpack_dual gives the tensors without them")
+
+
 def _recorded(*tensors):
+    """Whether a forward call of these arguments is a node of torch's graph."""
+    _no_tangents(*tensors)
     return torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors)
 
 
@@ -323,6 +333,7 @@ def alpa_vocab_loss_forward(x, w, target, stream=None):
 
 def alpa_vocab_loss_backward(dloss, x, w, target, lse, need=("x", "w"), stream=None):
     """(dx, dw) for the rows' loss gradients (float32 [rows]), None for those not in ``need``."""
+    _no_tangents(dloss, x, w, lse)
     L, d = load(), _type(x)
     if not set(need) <= {"x", "w"}:
         raise ValueError(f"need is {need!r}: names out of 'x', 'w' expected")
