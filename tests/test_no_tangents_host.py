@@ -36,3 +36,11 @@ def test_derivatives_are_not_dropped(call, args, names, leaf):
             call(**args)
         with pytest.raises(ValueError, match="GPU"):
             call(**{name: forward_ad.unpack_dual(t).primal if name in names else t for name, t in args.items()})
+
+
+def test_frequencies_are_constants():
+    f = F.clone().requires_grad_()
+    with pytest.raises(ValueError, match="frequencies have no gradient"):
+        B.alpa_rotary_forward(H, POS, f)
+    with torch.no_grad(), pytest.raises(ValueError, match="GPU"):
+        B.alpa_rotary_forward(H, POS, f)
