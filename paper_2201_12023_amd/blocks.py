@@ -197,7 +197,8 @@ def alpa_attention_forward(q, k, v, offsets=None, k_offsets=None, scale=None, ca
     (y, lse), float32 [rows, heads].
 
     offsets: int32 [seqs + 1] on the GPU, sequence s being rows offsets[s] .. offsets[s + 1] - 1 (None: one sequence of all rows).
-    k_offsets: the same for keys (None: those of the rows, with one sequence all keys), or [seqs, 2], first key and end of each sequence in a cache with gaps.
+    k_offsets: the same for keys (None: ``offsets``, with one sequence too, so that rows of none have keys of none; if that is None as well, all keys), or [seqs, 2],
+    first key and end of each sequence in a cache with gaps.
     scale: of q k^T (None: dim ** -0.5).  cap: scores become cap * tanh(score / cap), 0 leaves them.  slopes: float32 [heads], the score's loss with each key of
     distance.  causal: a row sees keys up to its own place, the last row standing at the last key, and the first prefix[s] (int32 [seqs]) ones."""
     if _l._recorded(q, k, v, slopes):

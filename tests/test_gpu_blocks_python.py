@@ -1,4 +1,4 @@
-"""What torch is told by the calls of ``blocks``: tensors that were written to."""
+"""What torch is told by the calls of ``blocks``: tensors that were written to; and what arguments stand for that are left out."""
 import pytest
 import torch
 
@@ -35,3 +35,22 @@ def test_what_is_written_to_cannot_be_what_the_graph_has_saved():
     with torch.inference_mode():
         t = q.clone()
         assert B.alpa_rotary_forward(t, pos, f, out=t) is t
+
+
+def test_keys_without_offsets_of_their_own():
+    """They have those of the rows, one sequence or several; without any all rows see all keys."""
+    g = gen(52)
+    q, k, v, dy = (normal(g, BF16, 70, n, 64) for n in (4, 2, 2, 4))
+
+    def both(**how):
+        y, lse = B.alpa_attention_forward(q, k, v, keep_lse=True, **how)
+        return y, lse, *B.alpa_attention_backward(dy, q, k, v, y, lse, **how)
+    for off in ([5, 60], [5, 30, 60]):
+        off = torch.tensor(off, dtype=torch.int32, device="cuda")
+        got = both(offsets=off)
+        for a, b in zip(got, both(offsets=off, k_offsets=off)):
+            assert torch.equal(a, b)
+        assert bool((got[3][:5] == 0).all()) and bool((got[3][60:] == 0).all())              # (keys of no sequence)
+    every = torch.tensor([0, 70], dtype=torch.int32, device="cuda")
+    for a, b in zip(both(), both(offsets=every, k_offsets=every)):
+        assert torch.equal(a, b)
