@@ -46,7 +46,7 @@ hipError_t launch_head_pack(hipStream_t st, int dtype, const HeadPack &g)
 // ---------------------------------------------------------------- rotary positions
 
 // A workgroup takes `per` rows: their sines and cosines once, for all heads, then the heads.  The angle is counted in turns in 64 bits, where a position of
-// 2^40 still leaves 13 bits behind the point, and what is left of it after whole turns is exact enough in 32.
+// 2^40 still leaves 13 bits behind the point; what is left of it after whole turns is exact enough in 32 for results of 16 bits.
 template <class T, int V>
 __global__ __launch_bounds__(256) void rotary_kernel(const RotaryArgs g, int per)
 {
@@ -60,8 +60,16 @@ __global__ __launch_bounds__(256) void rotary_kernel(const RotaryArgs g, int per
         for (int c = threadIdx.x; c < rows * half; c += 256) {
             const int r = c / half;
             const double u = (double)g.positions[row0 + r] * g.frequencies[c - r * half] * 0.15915494309189533577;
+            const double part = u - rint(u);
+            const float near = (float)part;
             float sin, cos;
-            sincospif(2.0f * (float)(u - rint(u)), &sin, &cos);
+            sincospif(2.0f * near, &sin, &cos);
+            if constexpr (sizeof(T) == 4) {
+                // (what 32 bits of the turn leave out, up to 9e-8 of a radian: the rest of a sine of float32 is off by less)
+                const float rest = 6.2831853071795865f * (float)(part - near), c = cos;
+                cos = fmaf(-sin, rest, cos);
+                sin = fmaf(c, rest, sin);
+            }
             turns[c] = make_float2(cos * g.scale, sin * g.scale * g.sign);
         }
         __syncthreads();
