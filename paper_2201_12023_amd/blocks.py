@@ -291,9 +291,9 @@ class _Rotary(torch.autograd.Function):
 def alpa_rotary_forward(x, positions, frequencies, interleaved=False, scale=1.0, out=None, stream=None):
     """x [rows, heads, dim] with the first 2 * len(frequencies) elements of each head turned by positions (int64 [rows]) times frequencies (float64, radians) and
     scaled: pairs (t, t + half), or (2 t, 2 t + 1) if ``interleaved``.  ``out``: where to put it, x itself to turn it in place.  Frequencies are constants."""
-    if _l._recorded(frequencies):
-        raise ValueError("frequencies have no gradient")
-    if _l._recorded(x, out):
+    if _l._recorded(x, frequencies, out):
+        if frequencies.requires_grad:
+            raise ValueError("frequencies have no gradient")
         if out is not None:
             raise ValueError("a result that is given cannot be recorded")
         return _l._apply(_Rotary, stream, x, positions, frequencies, interleaved, scale)

@@ -218,8 +218,12 @@ def _no_tangents(*tensors):
 
 def _recorded(*tensors):
     """Whether a forward call of these arguments is a node of torch's graph."""
-    _no_tangents(*tensors)
-    return torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors)
+    if forward_ad._current_level >= 0:
+        _no_tangents(*tensors)
+    for t in tensors:
+        if t is not None and t.requires_grad:
+            return torch.is_grad_enabled()
+    return False
 
 
 def _apply(function, stream, *args):
