@@ -36,7 +36,7 @@ typedef struct { void *p; int64_t row, head; } alpa_heads_t;    /* first element
  * a row of no sequence, gets zeros and an lse of -infinity.
  * Query head h reads kv head h / (heads / kv_heads).
  * Offsets are taken as they come, cut to the tensors' rows, as in alpa_experts_forward; sequences must not overlap in queries.
- * exp(a - lse) is rounded to `dtype` as an operand of the product with v.  Values that are not finite in q, k, v or dy may reach all rows and keys of
+ * exp(a - lse) is rounded to `dtype` as an operand of the product with v (in float16 times 2^12 of the row's largest, about, so that small ones keep their bits).  Values that are not finite in q, k, v or dy may reach all rows and keys of
  * their sequence and kv head, also where the mask hides them (zero times infinity); keys and rows of no sequence are not read.
  */
 typedef struct {
@@ -64,7 +64,7 @@ int alpa_attention_forward(const alpa_attention_t *how, alpa_heads_t q, alpa_hea
  *     P = exp(a - lse),  dA = P (dy . v - dy . y),  dR = dA (1 - tanh^2)
  *     dv_j = sum_i P_ij dy_i,   dq_i = scale sum_j dR_ij k_j,   dk_j = scale sum_i dR_ij q_i    (kv heads: over their query heads too)
  * P and dR are rounded to `dtype` as operands of the products (in float16 P times 2^14, so that the weights of many keys keep their bits, dR times powers of two that keep it
- * from overflowing and small ones from losing bits).  Rows and keys of no sequence get zeros.
+ * from overflowing and small ones from losing bits); y is taken as it was rounded.  Rows and keys of no sequence get zeros.
  */
 int64_t alpa_attention_backward_work(const alpa_attention_t *how, alpa_heads_t dy, alpa_heads_t q, alpa_heads_t k,
                                      alpa_heads_t v, alpa_heads_t y);

@@ -3,7 +3,8 @@ between its products, which are in ``layers``: attention, rotary positions and l
 
 Same names as the C entry points, same manner as ``layers``: torch tensors on one GPU, results and work memory from torch's allocator, work queued on
 ``stream`` (a torch.cuda.Stream; the current one if None) and not waited for.  The last dimension of a tensor must be contiguous, rows and heads may
-be any distance apart, so that queries, keys and values may be slices of one product's result.
+be any distance apart, so that queries, keys and values may be slices of one product's result.  A result that is given must not overlap another tensor of
+the call, but for x where rotary positions turn it in place.
 
 The forward calls can be differentiated: where an argument requires a gradient their results are part of torch's graph, and its backward pass makes
 the calls of this module.  What is kept for those (lse; mean and rstd) has no gradient: a loss that depends on it raises an error in the backward pass.

@@ -322,8 +322,8 @@ __global__ __launch_bounds__(1024) void norm_long_kernel(const NormArgs g)
 constexpr int rows_at_once(int threads, int c) { return threads == 64 ? 4 : threads == 256 && c <= 2 ? 2 : 1; }
 
 // A workgroup's rows, some at once, the next ones under way: dx, and the sums for dweight and dbias in registers, as a thread has the same columns of all of
-// them.  The rows' sums are joined through LDS, so that few parts go to memory: bound by memory and by the sums of parts, 8192 rows of 4096 in 16 bits take
-// 40 us with the sums of parts, 65536 of 768 60 us (a part to memory for each of the rows at once: 57 and 105).
+// them.  The rows' sums are joined through LDS, so that few parts go to memory: bound by memory, 8192 rows of 4096 in 16 bits take 38 us and 65536 of 768 59, and the
+// sums of parts 5 (with a part to memory for each of the rows at once 57 and 105, those among them).
 template <class T, int THREADS, int C, bool WIDE>
 __global__ __launch_bounds__(THREADS * rows_at_once(THREADS, C)) void norm_backward_kernel(const NormArgs g)
 {
